@@ -331,6 +331,77 @@ oscars_status oscars_aggregate(float* global, float* replicas, const float* weig
 oscars_status oscars_broadcast(const float* global, float* replicas, int32_t K, int64_t n,
                                int64_t ld, void* hip_stream);
 
+/* Orthogonalisation of updates by Newton-Schulz products (the update rule of
+ * the Muon optimiser), for `count` matrices in one call:
+ *   X_0 = G / |G|_F;  for t = 0 .. steps - 1, with (a, b, c) = coeffs[t]:
+ *     A = X_t X_t',  X_{t+1} = a X_t + (b A + c A A) X_t;   out = X_steps.
+ * It brings every singular value of G near 1 and keeps the singular vectors.
+ *   mats     host [count], 1 <= count <= OSCARS_MAX_MATRICES: rows x cols each
+ *            in [1, OSCARS_MAX_WIDTH], row-major with row strides x_ld, out_ld
+ *            >= cols (elements), x and out aligned to their elements.  out may
+ *            be x (with the same stride) or overlap any input; outputs share no
+ *            element.  A matrix stored column-major is the transpose stored
+ *            row-major: pass it so, its result is the transpose's too;
+ *   dtype    OSCARS_FP32 or OSCARS_BF16, of every x and out.  fp32: products
+ *            of 22-bit operands summed in fp32; bf16: the last steps, whose
+ *            roundings are not amplified any more, on 11-bit operands;
+ *   coeffs   host [steps][3], 1 <= steps <= OSCARS_MAX_ORTH_STEPS; refused where
+ *            a step's polynomial a + b s^2 + c s^4 passes 400, or a singular
+ *            value 16, from singular values s in [0, 1] on;
+ *   workspace  device, 16-byte aligned, oscars_orthogonalize_workspace bytes,
+ *            no part of a matrix; the call's own until the stream has run it.
+ * A matrix of zeros gives zeros, one with a NaN or an infinity gives NaN; the
+ * others of the call are not touched by it.  Sums are in a fixed order: the
+ * same inputs give the same bits, and a matrix's result does not depend on
+ * the others of the call where the tiles are the same (their size goes by the
+ * whole call's work; sums differ between tile sizes only in how K is cut).
+ * Allocates nothing and may be captured into a graph. */
+#define OSCARS_MAX_MATRICES 32
+#define OSCARS_MAX_ORTH_STEPS 16
+typedef struct {
+  int32_t rows, cols;
+  const void* x;
+  int64_t x_ld;
+  void* out;
+  int64_t out_ld;
+} oscars_matrix;
+/* Device bytes (0 for an invalid argument; only rows and cols are read). */
+int64_t oscars_orthogonalize_workspace(const oscars_matrix* mats, int32_t count);
+oscars_status oscars_orthogonalize(const oscars_matrix* mats, int32_t count, int32_t dtype,
+                                   const float* coeffs, int32_t steps, void* workspace,
+                                   int64_t workspace_bytes, void* hip_stream);
+
+/* The server's step after the barrier of a round, with a momentum and
+ * orthogonalised updates in the place of the plain average of Eq. 4:
+ *   avg = the average of oscars_aggregate (same tree, same bits)
+ *   d = global - avg;  m = beta momentum + d;  u = nesterov ? d + beta m : m
+ *   weight matrix W_l [o][i] (conv layers: [o][9 in]):
+ *     W <- (1 - lr weight_decay) W - lr sqrt(max(1, o / i)) orth(u)
+ *   everything else (biases; matrices of plain_layers):  x <- x - plain_lr u
+ * With beta = 0, plain_lr = 1 and every layer plain it is Eq. 4's average.
+ *   global, momentum          device [oscars_num_params] fp32, read;
+ *   global_out, momentum_out  device, written; may be global and momentum;
+ *   replicas   device [K][oscars_num_params] fp32, read: the workers' models at
+ *              the barrier;  weights  host [K] fp32, finite;
+ *   all 16-byte aligned; outputs overlap nothing but their own input;
+ *   plain_layers  bit l - 1: layer l's matrix is updated plainly;
+ *   lr, beta, weight_decay, plain_lr finite; coeffs, steps as above;
+ *   workspace  device, 16-byte aligned, oscars_server_workspace bytes.
+ * On the context's stream; allocates nothing and may be captured into a graph
+ * (replays read the buffers as they are then). */
+typedef struct {
+  float lr, beta, weight_decay, plain_lr;
+  int32_t nesterov;
+  uint32_t plain_layers;
+  const float* coeffs;
+  int32_t steps;
+} oscars_server_options;
+int64_t oscars_server_workspace(const oscars_ctx* ctx);
+oscars_status oscars_server_step(oscars_ctx* ctx, const float* global, const float* replicas,
+                                 const float* weights, const float* momentum, float* global_out,
+                                 float* momentum_out, const oscars_server_options* options,
+                                 void* workspace, int64_t workspace_bytes);
+
 /* Resume support: per-worker count of local steps done so far. host [K]. */
 oscars_status oscars_get_cursors(const oscars_ctx* ctx, int64_t* steps_done);
 oscars_status oscars_set_cursors(oscars_ctx* ctx, const int64_t* steps_done);

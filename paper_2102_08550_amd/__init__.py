@@ -12,6 +12,7 @@ Build with ``python paper_2102_08550_amd/build.py`` (or
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import List, Optional, Sequence, Tuple
@@ -25,6 +26,10 @@ OK, E_INVALID, E_NOMEM, E_HIP, E_INFEASIBLE, E_STATE = 0, -1, -2, -3, -4, -5
 FP32, BF16 = 0, 1
 MAX_K = 64
 EVAL_NOALLOC_MAX_ROWS = 262144
+MAX_MATRICES = 32
+# Newton-Schulz steps (a, b, c) of ``orthogonalize``: the quintic whose slope at
+# zero is steep, five times (singular values end between about 0.7 and 1.2).
+NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 (KERNEL_CAST, KERNEL_FWD, KERNEL_SOFTMAX, KERNEL_DGRAD, KERNEL_WGRAD, KERNEL_AGGREGATE,
  KERNEL_BWD_FUSED) = range(7)
 KERNEL_NAMES = ("cast_bf16", "gemm_fwd", "softmax_ce", "gemm_dgrad", "gemm_wgrad_update",
@@ -51,6 +56,17 @@ class _CnnModel(ctypes.Structure):
     _fields_ = [("height", _i32), ("width", _i32), ("channels", _i32), ("n_conv", _i32),
                 ("conv_channels", _P(_i32)), ("conv_strides", _P(_i32)), ("classes", _i32),
                 ("conv_skip", _P(_i32))]
+
+
+class _Matrix(ctypes.Structure):
+    _fields_ = [("rows", _i32), ("cols", _i32), ("x", _vp), ("x_ld", _i64), ("out", _vp),
+                ("out_ld", _i64)]
+
+
+class _ServerOptions(ctypes.Structure):
+    _fields_ = [("lr", _f32), ("beta", _f32), ("weight_decay", _f32), ("plain_lr", _f32),
+                ("nesterov", _i32), ("plain_layers", _u32), ("coeffs", _P(_f32)),
+                ("steps", _i32)]
 
 
 class _Shards(ctypes.Structure):
@@ -88,6 +104,11 @@ _SIGS = {
     "oscars_evaluate": (_i32, [_vp, _vp, _vp, _vp, _i64, _P(ctypes.c_double), _P(_i64)]),
     "oscars_evaluate_noalloc": (_i32, [_vp, _vp, _vp, _vp, _i64, _P(ctypes.c_double),
                                        _P(_i64)]),
+    "oscars_orthogonalize_workspace": (_i64, [_P(_Matrix), _i32]),
+    "oscars_orthogonalize": (_i32, [_P(_Matrix), _i32, _i32, _P(_f32), _i32, _vp, _i64, _vp]),
+    "oscars_server_workspace": (_i64, [_vp]),
+    "oscars_server_step": (_i32, [_vp, _vp, _vp, _P(_f32), _vp, _vp, _vp, _P(_ServerOptions), _vp,
+                                  _i64]),
     "oscars_status_str": (ctypes.c_char_p, [_i32]),
     "oscars_last_hip_error": (_i32, []),
 }
@@ -255,6 +276,90 @@ def broadcast(global_, replicas, K: int, n: int, ld: int, stream=None):
            "oscars_broadcast")
 
 
+def _workspace(nbytes: int, device, stream=None):
+    """Device memory for one call on ``stream`` (None: the current one): torch's
+    allocator gives it to later work of that stream only."""
+    import torch
+    if stream is None or stream == torch.cuda.current_stream(device):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+@functools.lru_cache(maxsize=16)
+def _coeffs(coeffs):
+    """((a, b, c), ...) as a C array, kept with its number of steps."""
+    flat = [float(v) for step in coeffs for v in step]
+    if not coeffs or any(len(step) != 3 for step in coeffs):
+        raise ValueError("coeffs must be a sequence of (a, b, c)")
+    return (_f32 * len(flat))(*flat), len(coeffs)
+
+
+def _matrix_view(t, what):
+    """(rows, cols, row stride, turned) of a 2-D tensor stored by rows, or by
+    columns (then of its transpose).  A single row or column is a column of
+    rows of one element each, whatever its stride."""
+    if t.dim() != 2 or t.numel() == 0:
+        raise ValueError(f"{what} must be a matrix that is not empty")
+    (r, c), (sr, sc) = t.shape, t.stride()
+    if r == 1 or c == 1:
+        n, step = (r, sr) if c == 1 else (c, sc)
+        if step >= 1 or n == 1:
+            return n, 1, step if n > 1 else 1, False
+    elif sc == 1 and sr >= c:
+        return r, c, sr, False
+    elif sr == 1 and sc >= r:
+        return c, r, sc, True
+    raise ValueError(f"{what} must have one unit stride and rows that do not overlap")
+
+
+def orthogonalize(x, out=None, coeffs=NEWTON_SCHULZ, stream=None):
+    """Newton-Schulz orthogonalisation (oscars_orthogonalize) of the matrix ``x``
+    or of every matrix of a sequence, in one call: fp32 or bf16 device tensors
+    of one type, stored by rows or by columns, with any stride between them.
+    ``out``: where the results go (``x`` itself is allowed), stored the same
+    way; new tensors by default.  Returns ``out``."""
+    import torch
+    single = isinstance(x, torch.Tensor)
+    xs = [x] if single else list(x)
+    if not 1 <= len(xs) <= MAX_MATRICES:
+        raise ValueError(f"1 to {MAX_MATRICES} matrices per call")
+    dt, dev = xs[0].dtype, xs[0].device
+    if dt not in (torch.float32, torch.bfloat16):
+        raise TypeError("matrices must be fp32 or bf16")
+    views = [_matrix_view(t, "x") for t in xs]
+    if out is None:
+        # dense results stored as x is, for work on the call's stream
+        with torch.cuda.stream(stream):
+            outs = [torch.empty_like(t.mT).mT if v[3] else torch.empty_like(t)
+                    for t, v in zip(xs, views)]
+    else:
+        outs = [out] if single else list(out)
+    if len(outs) != len(xs):
+        raise ValueError("one output per matrix")
+    mats = (_Matrix * len(xs))()
+    for m, t, o, v in zip(mats, xs, outs, views):
+        if not (t.is_cuda and o.is_cuda) or t.device != dev or o.device != dev:
+            raise TypeError("matrices must be on one CUDA (HIP) device")
+        if t.dtype != dt or o.dtype != dt:
+            raise TypeError("matrices must have one type")
+        if t.shape != o.shape:
+            raise ValueError("an output must have its matrix's shape")
+        ov = _matrix_view(o, "out")
+        if v[3] != ov[3]:
+            raise ValueError("out must be stored as x is")
+        m.rows, m.cols, m.x, m.x_ld, m.out, m.out_ld = (v[0], v[1], t.data_ptr(), v[2],
+                                                        o.data_ptr(), ov[2])
+    ca, steps = _coeffs(tuple(map(tuple, coeffs)))
+    with torch.cuda.device(dev):
+        need = _lib().oscars_orthogonalize_workspace(mats, len(xs))
+        ws = _workspace(need, dev, stream)
+        _check(_lib().oscars_orthogonalize(mats, len(xs), FP32 if dt == torch.float32 else BF16,
+                                           ca, steps, ws.data_ptr(), need,
+                                           _stream_handle(stream)), "oscars_orthogonalize")
+    return outs[0] if single else outs
+
+
 class Context:
     """K replicas of a ReLU MLP (dims = (d, h_1, ..., C)) and their workspace;
     or, with ``cnn = (image, conv)``, of the convolutional model: image =
@@ -294,6 +399,7 @@ class Context:
                                             int(max_batch), _stream_handle(stream)),
                    "oscars_create_cnn")
         self._h = h
+        self._bind_stream(stream)
         self.n_pad = int(_lib().oscars_num_params(h))
 
     def close(self):
@@ -309,6 +415,11 @@ class Context:
 
     def set_stream(self, stream=None):
         _check(_lib().oscars_set_stream(self._h, _stream_handle(stream)), "oscars_set_stream")
+        self._bind_stream(stream)
+
+    def _bind_stream(self, stream):
+        import torch
+        self._stream = stream if stream is not None else torch.cuda.current_stream()
 
     def layer_offsets(self, l: int) -> Tuple[int, int]:
         w, b = _i64(0), _i64(0)
@@ -392,6 +503,43 @@ class Context:
                                      _dev_ptr(x, None, "x"), _dev_ptr(y, torch.int32, "y"), n,
                                      ctypes.byref(loss), ctypes.byref(hits)), name)
         return float(loss.value), int(hits.value)
+
+    def server_step(self, global_, replicas, weights: Sequence[float], momentum, lr: float,
+                    beta: float = 0.9, nesterov: bool = True, weight_decay: float = 0.0,
+                    plain_lr: float = 1.0, plain_layers: Sequence[int] = (),
+                    coeffs=NEWTON_SCHULZ, out=None):
+        """The server's step with a momentum and orthogonalised updates
+        (oscars_server_step) in the place of ``aggregate``: from the global model
+        before the round and the workers' models at its barrier.  ``out``:
+        (new global model, new momentum), by default in place.  Layers
+        ``plain_layers`` (1..L) and all biases take the momentum as it is,
+        times ``plain_lr``.  Returns ``out``."""
+        import torch
+        g_out, m_out = (global_, momentum) if out is None else out
+        n = self.n_pad
+        ptrs = []
+        for t, size, what in ((global_, n, "global"), (replicas, self.K * n, "replicas"),
+                              (momentum, n, "momentum"), (g_out, n, "global out"),
+                              (m_out, n, "momentum out")):
+            ptrs.append(_dev_ptr(t, torch.float32, what))
+            if t.numel() < size:
+                raise ValueError(f"{what} is smaller than the model needs")
+        w, wp = _arr(weights, np.float32)
+        if len(w) != self.K:
+            raise ValueError("one weight per worker")
+        mask = 0
+        for l in plain_layers:
+            if not 1 <= int(l) <= len(self.shapes):
+                raise ValueError("plain_layers are layers 1 .. L")
+            mask |= 1 << (int(l) - 1)
+        ca, steps = _coeffs(tuple(map(tuple, coeffs)))
+        o = _ServerOptions(lr, beta, weight_decay, plain_lr, int(bool(nesterov)), mask, ca, steps)
+        need = _lib().oscars_server_workspace(self._h)
+        ws = _workspace(need, global_.device, self._stream)
+        _check(_lib().oscars_server_step(self._h, ptrs[0], ptrs[1], wp, ptrs[2], ptrs[3], ptrs[4],
+                                         ctypes.byref(o), ws.data_ptr(), need),
+               "oscars_server_step")
+        return g_out, m_out
 
     def cursors(self) -> List[int]:
         out = np.zeros(self.K, np.int64)

@@ -1,0 +1,159 @@
+// Tile product C[r][c] = sum_k A[r][k] B[c][k] shared by the operators on the
+// global model (orthogonalize.hip, int8_kernels.hip).
+//
+// Both operands are stored K-contiguous as rows of whole 128-byte blocks; a
+// block is what one row takes of one K step, whatever the element type:
+//   NT_I8      128 int8;
+//   NT_F16     64 fp16;
+//   NT_SPLIT   32 values as two fp16 each, hi = fp16(v) in the first 64 bytes,
+//              lo = fp16(v - hi) in the last 64: 22 bits of mantissa.  A product
+//              is hi hi + hi lo + lo hi (lo lo is below the 22 bits).
+// The 16 bytes that a lane feeds a matrix instruction are 8 fp16 or 16 int8 and
+// sit at the same place for all of them (row = lane & 31, 16-byte chunk 2 s +
+// (lane >> 5) of K group s), so staging and LDS reads are the same code.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace oscars {
+
+typedef float nt_f32x4 __attribute__((ext_vector_type(4)));
+typedef float nt_f32x16 __attribute__((ext_vector_type(16)));
+typedef int32_t nt_i32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t nt_i32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t nt_u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t nt_u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 nt_f16x8 __attribute__((ext_vector_type(8)));
+
+enum NtFormat { NT_I8 = 0, NT_F16 = 1, NT_SPLIT = 2, NT_SPLIT_B0 = 3 };  // B0: B's lo are zero
+
+constexpr int NT_BLOCK = 128;  // bytes of a row per K step
+
+template <int F> struct NtAcc { typedef nt_f32x16 type; };
+template <> struct NtAcc<NT_I8> { typedef nt_i32x16 type; };
+
+template <int F>
+__device__ __forceinline__ typename NtAcc<F>::type nt_mfma(nt_u32x4 a, nt_u32x4 b,
+                                                           typename NtAcc<F>::type c) {
+  if constexpr (F == NT_I8)
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(nt_i32x4, a),
+                                                 __builtin_bit_cast(nt_i32x4, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(nt_f16x8, a),
+                                                  __builtin_bit_cast(nt_f16x8, b), c, 0, 0, 0);
+}
+
+// Workgroup tile: BM x BN outputs, WM x WN waves, ST stages in LDS.
+template <int BM_, int BN_, int WM_, int WN_, int ST_>
+struct NtShape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_;
+  static constexpr int NT = 64 * WM * WN, MI = BM / WM / 32, NJ = BN / WN / 32;
+  static constexpr int LDS_BYTES = ST * (BM + BN) * NT_BLOCK;
+  static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0, "whole matrix blocks per wave");
+};
+
+// One operand's rows as a buffer: the resource starts at the tile's first row.
+// A lane's 16 bytes of a stage: row r, chunk p at LDS byte 128 r + 16 p holds
+// chunk p ^ ((r ^ r >> 3) & 7) of the row, so that both the reads of 32
+// consecutive rows and the writes spread over the banks.  Rows past the last
+// one read the last one again (their outputs are not stored).
+template <int NTHR, int ROWS>
+struct NtRows {
+  static constexpr int P = ROWS * 8 / NTHR;
+  static_assert(ROWS * 8 % NTHR == 0, "whole wave instructions");
+  __amdgpu_buffer_rsrc_t rsrc;
+  int voff[P];
+  // base: row 0 of the operand; bytes: from base to the operand's end
+  __device__ __forceinline__ void init(const void* base, int64_t ld, int64_t bytes, int row0,
+                                       int rows, int tid) {
+    const int64_t at = row0 * ld, left = bytes - at;
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(static_cast<const char*>(base) + at), 0,
+        static_cast<int>(left < 0x7FFFFFFF ? left : 0x7FFFFFFF), 0x00020000u);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int idx = tid + NTHR * p, r = idx >> 3;
+      const int c = (idx & 7) ^ ((r ^ (r >> 3)) & 7);
+      const int rr = row0 + r < rows ? r : rows - 1 - row0;
+      voff[p] = static_cast<int>(rr * ld) + 16 * c;
+    }
+  }
+  // wave w's instruction p fills tile rows (64 w + NTHR p) / 8 .. + 7
+  __device__ __forceinline__ void issue(char* tile, int kbyte, int tid) const {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rsrc, (__attribute__((address_space(3))) void*)(tile + ((tid & ~63) + NTHR * p) * 16),
+          16, voff[p], kbyte, 0, 0);
+  }
+};
+
+template <int N>
+__device__ __forceinline__ void nt_wait_vm() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+__device__ __forceinline__ void nt_barrier() {
+  __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
+  asm volatile("s_barrier" ::: "memory");
+}
+
+__device__ __forceinline__ nt_u32x4 nt_read(const char* tile, int row, int chunk) {
+  return *reinterpret_cast<const nt_u32x4*>(tile + row * NT_BLOCK +
+                                            16 * (chunk ^ ((row ^ (row >> 3)) & 7)));
+}
+
+// acc[i][j] += the tile's products over `blocks` K blocks from block `first` on.
+// lds: S::LDS_BYTES.  Ends with nothing in flight; the caller puts a barrier
+// before it reuses the LDS.
+template <class S, int F, class RowsA, class RowsB, class Acc>
+__device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int first, int blocks,
+                                        char* lds, int tid, Acc (&acc)[S::MI][S::NJ]) {
+  constexpr int ABYTES = S::BM * NT_BLOCK, STAGE = (S::BM + S::BN) * NT_BLOCK;
+  constexpr int PER = RowsA::P + RowsB::P;
+  const int lane = tid & 63, wave = tid >> 6;
+  const int arow = (wave / S::WN) * 32 * S::MI + (lane & 31);
+  const int brow = (wave % S::WN) * 32 * S::NJ + (lane & 31), h = lane >> 5;
+  auto issue = [&](int s) {
+    // past the end the last block is loaded again: the number in flight stays the same
+    const int k = (first + (s < blocks ? s : blocks - 1)) * NT_BLOCK;
+    char* t = lds + (s % S::ST) * STAGE;
+    a.issue(t, k, tid);
+    b.issue(t + ABYTES, k, tid);
+  };
+  for (int s = 0; s < S::ST - 1; ++s) issue(s);
+  for (int s = 0; s < blocks; ++s) {
+    nt_wait_vm<(S::ST - 2) * PER>();
+    nt_barrier();
+    issue(s + S::ST - 1);
+    const char* ta = lds + (s % S::ST) * STAGE;
+    const char* tb = ta + ABYTES;
+    auto step = [&](int ca, int cb) {
+      nt_u32x4 fa[S::MI], fb[S::NJ];
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) fb[j] = nt_read(tb, brow + 32 * j, 2 * cb + h);
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i) fa[i] = nt_read(ta, arow + 32 * i, 2 * ca + h);
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) acc[i][j] = nt_mfma<F>(fa[i], fb[j], acc[i][j]);
+    };
+    if constexpr (F == NT_SPLIT || F == NT_SPLIT_B0) {
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        step(s2, s2);
+        if constexpr (F == NT_SPLIT) step(s2, 2 + s2);
+        step(2 + s2, s2);
+      }
+    } else {
+#pragma unroll
+      for (int s2 = 0; s2 < 4; ++s2) step(s2, s2);
+    }
+  }
+  nt_wait_vm<0>();
+}
+
+}  // namespace oscars

@@ -23,6 +23,7 @@
 #include "conv.h"
 #include "host_logic.h"
 #include "kernels.h"
+#include "orthogonalize.h"
 
 using namespace oscars;
 
@@ -1666,6 +1667,211 @@ oscars_status oscars_broadcast(const float* global, float* replicas, int32_t K, 
                   r1 = r0 + ((K - 1) * ld + n) * sizeof(float);
   if (g0 < r1 && r0 < g1) return OSCARS_E_INVALID;
   hipError_t e = launch_broadcast(global, replicas, K, n, ld, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+namespace {
+
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+  return a0 < b0 + static_cast<uintptr_t>(b_bytes) && b0 < a0 + static_cast<uintptr_t>(a_bytes);
+}
+
+// Coefficients of a call; false where the kernels' number ranges do not hold them.
+bool read_coeffs(const float* coeffs, int32_t steps, OrthCoeffs* c) {
+  if (!coeffs || steps < 1 || steps > ORTH_MAX_STEPS) return false;
+  c->steps = steps;
+  for (int t = 0; t < steps; ++t) {
+    c->a[t] = coeffs[3 * t];
+    c->b[t] = coeffs[3 * t + 1];
+    c->c[t] = coeffs[3 * t + 2];
+  }
+  return orth_coeffs_ok(*c);
+}
+
+static_assert(ORTH_MAX_MATS == OSCARS_MAX_MATRICES && ORTH_MAX_STEPS == OSCARS_MAX_ORTH_STEPS &&
+                  ORTH_MAX_DIM == OSCARS_MAX_WIDTH, "limits of oscars.h");
+
+bool matrix_dims_ok(const oscars_matrix* mats, int32_t count) {
+  if (!mats || count < 1 || count > ORTH_MAX_MATS) return false;
+  for (int i = 0; i < count; ++i)
+    if (mats[i].rows < 1 || mats[i].cols < 1 || mats[i].rows > ORTH_MAX_DIM ||
+        mats[i].cols > ORTH_MAX_DIM)
+      return false;
+  return true;
+}
+
+// Bytes from a matrix's first element to behind its last.
+int64_t matrix_span(int32_t rows, int32_t cols, int64_t ld, int64_t esize) {
+  return ((rows - 1) * ld + cols) * esize;
+}
+
+// Whether two outputs share an element.  Of equal strides, windows of columns
+// of one array may interleave.
+bool outputs_clash(const oscars_matrix& a, const oscars_matrix& b, int64_t esize) {
+  if (!overlap(a.out, matrix_span(a.rows, a.cols, a.out_ld, esize), b.out,
+               matrix_span(b.rows, b.cols, b.out_ld, esize)))
+    return false;
+  if (a.out_ld != b.out_ld) return true;
+  const int64_t ld = a.out_ld;
+  const int64_t off = (static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.out)) -
+                       static_cast<int64_t>(reinterpret_cast<uintptr_t>(a.out))) / esize;
+  const int64_t at = (off % ld + ld) % ld;
+  return at < a.cols || at + b.cols > ld;
+}
+
+// The matrices that a server's step orthogonalises: (layer, rows, cols).
+struct ServerMat {
+  int layer, rows, cols;
+};
+int server_mats(const oscars_ctx* c, uint32_t plain_layers, ServerMat* out) {
+  int n = 0;
+  for (int l = 1; l <= c->L; ++l) {
+    if (plain_layers >> (l - 1) & 1u) continue;
+    ServerMat m{l, 0, 0};
+    if (c->cnn) {
+      m.rows = l < c->L ? c->img_c[l] : c->dims[l];
+      m.cols = l < c->L ? 9 * c->img_c[l - 1] : c->img_c[l - 1];
+    } else {
+      m.rows = c->dims[l];
+      m.cols = c->dims[l - 1];
+    }
+    out[n++] = m;
+  }
+  return n;
+}
+
+// Workspace of a server's step: u [n_pad] fp32, then the orthogonalisation's.
+int64_t server_update_bytes(const oscars_ctx* c) { return round_up(c->n_pad * 4, 256); }
+
+}  // namespace
+
+int64_t oscars_orthogonalize_workspace(const oscars_matrix* mats, int32_t count) {
+  if (!matrix_dims_ok(mats, count)) return 0;
+  OrthMat m[ORTH_MAX_MATS] = {};
+  for (int i = 0; i < count; ++i) {
+    m[i].rows = mats[i].rows;
+    m[i].cols = mats[i].cols;
+  }
+  return orth_workspace(m, count);
+}
+
+oscars_status oscars_orthogonalize(const oscars_matrix* mats, int32_t count, int32_t dtype,
+                                   const float* coeffs, int32_t steps, void* workspace,
+                                   int64_t workspace_bytes, void* hip_stream) {
+  if (!matrix_dims_ok(mats, count)) return OSCARS_E_INVALID;
+  if (dtype != OSCARS_FP32 && dtype != OSCARS_BF16) return OSCARS_E_INVALID;
+  OrthCoeffs c;
+  if (!read_coeffs(coeffs, steps, &c)) return OSCARS_E_INVALID;
+  const int64_t es = dtype == OSCARS_FP32 ? 4 : 2;
+  OrthMat m[ORTH_MAX_MATS];
+  for (int i = 0; i < count; ++i) {
+    const oscars_matrix& u = mats[i];
+    if (!u.x || !u.out || u.x_ld < u.cols || u.out_ld < u.cols) return OSCARS_E_INVALID;
+    if (u.x_ld > (int64_t{1} << 40) || u.out_ld > (int64_t{1} << 40)) return OSCARS_E_INVALID;
+    if (reinterpret_cast<uintptr_t>(u.x) % es || reinterpret_cast<uintptr_t>(u.out) % es)
+      return OSCARS_E_INVALID;
+    m[i] = OrthMat{u.rows, u.cols, u.x, u.x_ld, u.out, u.out_ld, nullptr, 0.0f, 0.0f};
+  }
+  const int64_t need = orth_workspace(m, count);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < need) return OSCARS_E_INVALID;
+  for (int i = 0; i < count; ++i) {
+    const oscars_matrix& u = mats[i];
+    if (overlap(workspace, need, u.x, matrix_span(u.rows, u.cols, u.x_ld, es)) ||
+        overlap(workspace, need, u.out, matrix_span(u.rows, u.cols, u.out_ld, es)))
+      return OSCARS_E_INVALID;
+    for (int j = 0; j < i; ++j)
+      if (outputs_clash(u, mats[j], es)) return OSCARS_E_INVALID;
+  }
+  const hipError_t e = launch_orthogonalize(m, count, dtype == OSCARS_BF16, c, workspace,
+                                            static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+int64_t oscars_server_workspace(const oscars_ctx* c) {
+  if (!c) return 0;
+  ServerMat sm[OSCARS_MAX_LAYERS];
+  OrthMat m[OSCARS_MAX_LAYERS] = {};
+  const int count = server_mats(c, 0, sm);
+  for (int i = 0; i < count; ++i) {
+    m[i].rows = sm[i].rows;
+    m[i].cols = sm[i].cols;
+  }
+  return server_update_bytes(c) + orth_workspace(m, count);
+}
+
+oscars_status oscars_server_step(oscars_ctx* c, const float* global, const float* replicas,
+                                 const float* weights, const float* momentum, float* global_out,
+                                 float* momentum_out, const oscars_server_options* o,
+                                 void* workspace, int64_t workspace_bytes) {
+  if (!c || !global || !replicas || !weights || !momentum || !global_out || !momentum_out || !o)
+    return OSCARS_E_INVALID;
+  for (const void* p : {static_cast<const void*>(global), static_cast<const void*>(replicas),
+                        static_cast<const void*>(momentum), static_cast<const void*>(global_out),
+                        static_cast<const void*>(momentum_out),
+                        static_cast<const void*>(workspace)})
+    if (!p || !aligned16(p)) return OSCARS_E_INVALID;
+  for (float v : {o->lr, o->beta, o->weight_decay, o->plain_lr})
+    if (!std::isfinite(v)) return OSCARS_E_INVALID;
+  for (int k = 0; k < c->K; ++k)
+    if (!std::isfinite(weights[k])) return OSCARS_E_INVALID;
+  OrthCoeffs co;
+  if (!read_coeffs(o->coeffs, o->steps, &co)) return OSCARS_E_INVALID;
+  const int64_t need = oscars_server_workspace(c), one = c->n_pad * 4, all = one * c->K;
+  if (workspace_bytes < need) return OSCARS_E_INVALID;
+  if (overlap(global_out, one, momentum_out, one) || overlap(global_out, one, momentum, one) ||
+      overlap(momentum_out, one, global, one) || overlap(global_out, one, replicas, all) ||
+      overlap(momentum_out, one, replicas, all))
+    return OSCARS_E_INVALID;
+  if ((global_out != global && overlap(global_out, one, global, one)) ||
+      (momentum_out != momentum && overlap(momentum_out, one, momentum, one)))
+    return OSCARS_E_INVALID;
+  if (overlap(workspace, need, global, one) || overlap(workspace, need, momentum, one) ||
+      overlap(workspace, need, global_out, one) || overlap(workspace, need, momentum_out, one) ||
+      overlap(workspace, need, replicas, all))
+    return OSCARS_E_INVALID;
+
+  ServerMat sm[OSCARS_MAX_LAYERS];
+  const int count = server_mats(c, o->plain_layers, sm);
+  float* u = static_cast<float*>(workspace);
+  void* orth_ws = static_cast<char*>(workspace) + server_update_bytes(c);
+  ServerArgs a{};
+  a.global = global;
+  a.replicas = replicas;
+  a.momentum = momentum;
+  a.global_out = global_out;
+  a.momentum_out = momentum_out;
+  a.update = u;
+  a.K = c->K;
+  a.n = c->n_pad;
+  a.beta = o->beta;
+  a.plain_lr = o->plain_lr;
+  a.nesterov = o->nesterov != 0;
+  for (int k = 0; k < c->K; ++k) a.w[k] = weights[k];
+  OrthMat m[OSCARS_MAX_LAYERS] = {};
+  int64_t done = 0;  // segments: each matrix, and what lies between them
+  auto segment = [&](int64_t end, int mat, int64_t size) {
+    if (end == done) return;
+    a.start[a.n_segs] = done;
+    a.end[a.n_segs] = end;
+    a.mat[a.n_segs] = mat;
+    a.size[a.n_segs] = size;
+    ++a.n_segs;
+    done = end;
+  };
+  for (int i = 0; i < count; ++i) {
+    const int64_t at = c->w_off[sm[i].layer], size = static_cast<int64_t>(sm[i].rows) * sm[i].cols;
+    segment(at, -1, 0);
+    segment(round_up(at + size, 64), i, size);
+    const double ratio = static_cast<double>(sm[i].rows) / sm[i].cols;
+    m[i] = OrthMat{sm[i].rows, sm[i].cols, u + at, sm[i].cols, global_out + at, sm[i].cols,
+                   global + at, static_cast<float>(1.0 - static_cast<double>(o->lr) * o->weight_decay),
+                   static_cast<float>(o->lr * std::sqrt(std::max(1.0, ratio)))};
+  }
+  segment(c->n_pad, -1, 0);
+  hipError_t e = launch_server_pass(a, orth_ws, c->stream);
+  if (e == hipSuccess && count > 0)
+    e = launch_orthogonalize(m, count, false, co, orth_ws, c->stream, true);
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
 
