@@ -32,8 +32,8 @@ namespace oscars {
 namespace {
 
 typedef NtShape<256, 256, 2, 4, 2> OrthL;
-typedef NtShape<128, 128, 2, 2, 2> OrthM;
-typedef NtShape<64, 64, 2, 2, 3> OrthS;
+typedef NtShape<128, 128, 2, 2, 2, 1> OrthM;
+typedef NtShape<64, 64, 2, 2, 3, 2> OrthS;
 
 enum OrthKind { ORTH_GRAM = 0, ORTH_POLY = 1, ORTH_APPLY = 2, ORTH_LAST = 3 };
 
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(OrthArgs g) {
 // 8 q + 4 h + t: four consecutive rows, which are four consecutive entries of
 // the transposed result; the straight one goes through LDS.
 template <class S, int KIND, int F>
-__global__ __launch_bounds__(S::NT, 1) void orth_product_kernel(OrthArgs g) {
+__global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
   constexpr int TURN = 36;  // floats of an LDS row of the turned block
   constexpr bool SYM = KIND == ORTH_GRAM || KIND == ORTH_POLY;
