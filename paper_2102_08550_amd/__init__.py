@@ -109,6 +109,15 @@ _SIGS = {
     "oscars_server_workspace": (_i64, [_vp]),
     "oscars_server_step": (_i32, [_vp, _vp, _vp, _P(_f32), _vp, _vp, _vp, _P(_ServerOptions), _vp,
                                   _i64]),
+    "oscars_quantize_rows": (_i32, [_vp, _i64, _vp, _vp, _i64, _i32, _i64, _i32, _vp]),
+    "oscars_matmul_i8": (_i32, [_vp, _i64, _i32, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i32, _i64,
+                                _i32, _i32, _vp]),
+    "oscars_linear_i8_workspace": (_i64, [_i64, _i32]),
+    "oscars_linear_i8": (_i32, [_vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _i32, _i64,
+                                _i32, _i32, _vp, _i64, _vp]),
+    "oscars_i8_model_bytes": (_i64, [_vp]),
+    "oscars_quantize_model": (_i32, [_vp, _vp, _vp]),
+    "oscars_evaluate_i8": (_i32, [_vp, _vp, _vp, _vp, _i64, _P(ctypes.c_double), _P(_i64)]),
     "oscars_status_str": (ctypes.c_char_p, [_i32]),
     "oscars_last_hip_error": (_i32, []),
 }
@@ -360,6 +369,135 @@ def orthogonalize(x, out=None, coeffs=NEWTON_SCHULZ, stream=None):
     return outs[0] if single else outs
 
 
+def _float_type(dtype, what) -> int:
+    import torch
+    if dtype == torch.float32:
+        return FP32
+    if dtype == torch.bfloat16:
+        return BF16
+    raise TypeError(f"{what} must be fp32 or bf16, got {dtype}")
+
+
+def _rows(t, dtype, device, what):
+    """(pointer, rows, row stride, columns) of a 2-D device tensor stored by rows."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+        raise TypeError(f"{what} must be a tensor on the input's CUDA (HIP) device")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (
+            t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{what} must be a matrix stored by rows that do not overlap")
+    n, c = t.shape
+    return t.data_ptr(), n, max(t.stride(0), c), c
+
+
+def _vector(t, n, device, what):
+    import torch
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+        raise TypeError(f"{what} must be a tensor on the input's CUDA (HIP) device")
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be {n} contiguous fp32 values")
+    return t.data_ptr()
+
+
+def _new(shape, dtype, device, stream):
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def quantize_rows(x, out=None, stream=None):
+    """The rows of ``x`` (fp32 or bf16 matrix, any row stride) in 8 bits with a
+    scale each (oscars_quantize_rows): ``(q, scale)``, q int8 [rows][columns
+    rounded up to 128, zero behind the columns], scale fp32 [rows].  ``out``:
+    such a pair to write into (the row stride of q a multiple of 16)."""
+    import torch
+    dev = x.device
+    xp, n, ld, cols = _rows(x, x.dtype, dev, "x")
+    dt = _float_type(x.dtype, "x")
+    if out is None:
+        out = (_new((n, (cols + 127) // 128 * 128), torch.int8, dev, stream),
+               _new((n,), torch.float32, dev, stream))
+    q, scale = out
+    qp, qn, qld, qc = _rows(q, torch.int8, dev, "q")
+    if qn != n or qc < cols:
+        raise ValueError("q must have a row per row of x, as long or longer")
+    if n == 0:
+        return out
+    with torch.cuda.device(dev):
+        _check(_lib().oscars_quantize_rows(qp, qld, _vector(scale, n, dev, "scale"), xp, ld, dt, n,
+                                           cols, _stream_handle(stream)), "oscars_quantize_rows")
+    return out
+
+
+def matmul_i8(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool = False,
+              out_dtype=None, out=None, stream=None):
+    """xscale wscale (xq wq') + bias (oscars_matmul_i8) for quantised rows ``xq``
+    [rows][..] and weights ``wq`` [outputs][..] as quantize_rows gives them, of
+    ``in_features`` columns; fp32 by default.  Returns ``out``."""
+    import torch
+    dev = xq.device
+    xp, n, xld, xc = _rows(xq, torch.int8, dev, "xq")
+    wp, outs, wld, wc = _rows(wq, torch.int8, dev, "wq")
+    if xc < (in_features + 127) // 128 * 128 or wc < in_features:
+        raise ValueError("xq must hold in_features columns rounded up to 128, wq in_features")
+    if out is None:
+        out = _new((n, outs), out_dtype or torch.float32, dev, stream)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError("out has another dtype than out_dtype")
+    op, on, old, oc = _rows(out, out.dtype, dev, "out")
+    if (on, oc) != (n, outs):
+        raise ValueError("out must be [rows][outputs]")
+    if n == 0:
+        return out
+    with torch.cuda.device(dev):
+        _check(_lib().oscars_matmul_i8(op, old, _float_type(out.dtype, "out"), xp, xld,
+                                       _vector(xscale, n, dev, "xscale"), wp, wld,
+                                       _vector(wscale, outs, dev, "wscale"),
+                                       _vector(bias, outs, dev, "bias"), int(bool(relu)), n,
+                                       int(in_features), outs, _stream_handle(stream)),
+               "oscars_matmul_i8")
+    return out
+
+
+def linear_i8(x, wq, wscale, bias=None, relu: bool = False, out_dtype=None, out=None, stream=None):
+    """A linear layer in 8 bits (oscars_linear_i8): the rows of ``x`` (fp32 or
+    bf16) are quantised with a scale each, ``wq`` [outputs][inputs or more, the
+    row stride a multiple of 16] and ``wscale`` are a weight matrix's
+    quantize_rows.  The result has ``x``'s type by default.  Returns ``out``."""
+    import torch
+    dev = x.device
+    xp, n, xld, cols = _rows(x, x.dtype, dev, "x")
+    dt = _float_type(x.dtype, "x")
+    wp, outs, wld, wc = _rows(wq, torch.int8, dev, "wq")
+    if wc < cols:
+        raise ValueError("wq must have as many columns as x, or more")
+    if out is None:
+        out = _new((n, outs), out_dtype or x.dtype, dev, stream)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError("out has another dtype than out_dtype")
+    op, on, old, oc = _rows(out, out.dtype, dev, "out")
+    if (on, oc) != (n, outs):
+        raise ValueError("out must be [rows][outputs]")
+    if n == 0:
+        return out
+    lib = _lib()
+    need = lib.oscars_linear_i8_workspace(n, cols)
+    ws = _workspace(need, dev, stream) if need else None
+    with torch.cuda.device(dev):
+        _check(lib.oscars_linear_i8(op, old, _float_type(out.dtype, "out"), xp, xld, dt, wp, wld,
+                                    _vector(wscale, outs, dev, "wscale"),
+                                    _vector(bias, outs, dev, "bias"), int(bool(relu)), n, cols,
+                                    outs, ws.data_ptr() if need else None, need,
+                                    _stream_handle(stream)), "oscars_linear_i8")
+    return out
+
+
 class Context:
     """K replicas of a ReLU MLP (dims = (d, h_1, ..., C)) and their workspace;
     or, with ``cnn = (image, conv)``, of the convolutional model: image =
@@ -502,6 +640,44 @@ class Context:
         _check(getattr(_lib(), name)(self._h, _dev_ptr(params, torch.float32, "params"),
                                      _dev_ptr(x, None, "x"), _dev_ptr(y, torch.int32, "y"), n,
                                      ctypes.byref(loss), ctypes.byref(hits)), name)
+        return float(loss.value), int(hits.value)
+
+    def quantize_model(self, params, out=None):
+        """The flat model ``params`` (device tensor [n_pad] fp32) in 8-bit integers,
+        a scale per output channel (oscars_quantize_model): one device tensor
+        for evaluate_i8.  Fully connected models only."""
+        import torch
+        need = int(_lib().oscars_i8_model_bytes(self._h))
+        pp = _dev_ptr(params, torch.float32, "params")
+        if params.numel() < self.n_pad:
+            raise ValueError("params must hold n_pad floats")
+        if out is None:
+            out = _workspace(max(need, 1), params.device, self._stream)
+        op = _dev_ptr(out, torch.uint8, "out")
+        if out.numel() < need:
+            raise ValueError(f"a quantised model takes {need} bytes")
+        _check(_lib().oscars_quantize_model(self._h, pp, op), "oscars_quantize_model")
+        return out
+
+    def evaluate_i8(self, model, x, y, n_rows: Optional[int] = None):
+        """``evaluate`` with the products of the quantised ``model``
+        (oscars_evaluate_i8)."""
+        import torch
+        n = int(x.shape[0] if n_rows is None else n_rows)
+        if n > x.shape[0] or n > y.shape[0]:
+            raise ValueError("n_rows exceeds the rows of x or y")
+        mp = _dev_ptr(model, torch.uint8, "model")
+        if model.numel() < int(_lib().oscars_i8_model_bytes(self._h)):
+            raise ValueError("model is not a quantised model of this context")
+        xdt = x.dtype if self.dtype == BF16 and x.dtype in (torch.int16, torch.uint16) else (
+            torch.bfloat16 if self.dtype == BF16 else torch.float32)
+        if x.dim() != 2 or x.shape[1] != self.dims[0]:
+            raise ValueError("x must be [n_rows][d]")
+        loss = ctypes.c_double(0.0)
+        hits = _i64(0)
+        _check(_lib().oscars_evaluate_i8(self._h, mp, _dev_ptr(x, xdt, "x"),
+                                         _dev_ptr(y, torch.int32, "y"), n, ctypes.byref(loss),
+                                         ctypes.byref(hits)), "oscars_evaluate_i8")
         return float(loss.value), int(hits.value)
 
     def server_step(self, global_, replicas, weights: Sequence[float], momentum, lr: float,

@@ -45,7 +45,7 @@ def build(verbose: bool = False) -> str:
     os.makedirs(objdir, exist_ok=True)
     objs = []
     for src in ("kernels.hip", "f32_kernels.hip", "conv_direct.hip", "conv_kernels.hip",
-                "orthogonalize.hip", "runtime.hip"):
+                "orthogonalize.hip", "int8_kernels.hip", "runtime.hip"):
         obj = os.path.join(objdir, src + ".o")
         _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)

@@ -22,6 +22,7 @@
 #include "../../include/oscars.h"
 #include "conv.h"
 #include "host_logic.h"
+#include "int8.h"
 #include "kernels.h"
 #include "orthogonalize.h"
 
@@ -1872,6 +1873,265 @@ oscars_status oscars_server_step(oscars_ctx* c, const float* global, const float
   hipError_t e = launch_server_pass(a, orth_ws, c->stream);
   if (e == hipSuccess && count > 0)
     e = launch_orthogonalize(m, count, false, co, orth_ws, c->stream, true);
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+namespace {
+
+bool is_dtype(int32_t t) { return t == OSCARS_FP32 || t == OSCARS_BF16; }
+int64_t dtype_bytes(int32_t t) { return t == OSCARS_FP32 ? 4 : 2; }
+bool aligned_to(const void* p, int64_t bytes) {
+  return reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(bytes) == 0;
+}
+constexpr int64_t kMaxLd = int64_t{1} << 40;
+// Rows of `width` elements, `ld` apart.
+bool rows_ok(const void* p, int64_t ld, int64_t width, int64_t esize) {
+  return p && ld >= width && ld <= kMaxLd && aligned_to(p, esize);
+}
+bool i8_rows_ok(const int8_t* p, int64_t ld, int64_t width) {
+  return p && aligned16(p) && ld % 16 == 0 && ld >= width && ld <= kMaxLd;
+}
+int64_t rows_span(int64_t rows, int64_t ld, int64_t width, int64_t esize) {
+  return rows > 0 ? ((rows - 1) * ld + width) * esize : 0;
+}
+bool i8_sizes_ok(int64_t rows, int32_t in, int32_t outs) {
+  return rows >= 0 && rows < (int64_t{1} << 31) && in >= 1 && in <= OSCARS_MAX_WIDTH &&
+         outs >= 1 && outs <= OSCARS_MAX_WIDTH;
+}
+// What the product and the fused layer have in common.
+bool i8_product_ok(const MatmulI8Args& a) {
+  const int64_t es = a.out_bf16 ? 2 : 4;
+  if (!i8_sizes_ok(a.rows, a.in, a.outs) || !i8_rows_ok(a.wq, a.w_ld, a.in)) return false;
+  if (!a.wscale || !aligned_to(a.wscale, 4) || !aligned_to(a.bias, 4)) return false;
+  if (!rows_ok(a.out, a.out_ld, a.outs, es)) return false;
+  const int64_t n = rows_span(a.rows, a.out_ld, a.outs, es);
+  return !overlap(a.out, n, a.wq, rows_span(a.outs, a.w_ld, a.in, 1)) &&
+         !overlap(a.out, n, a.wscale, a.outs * int64_t{4}) &&
+         !(a.bias && overlap(a.out, n, a.bias, a.outs * int64_t{4}));
+}
+
+// A quantised model: byte offsets of layer l's integers, scales and biases.
+struct I8Layout {
+  int64_t w[OSCARS_MAX_LAYERS + 1], s[OSCARS_MAX_LAYERS + 1], b[OSCARS_MAX_LAYERS + 1], end;
+  static int64_t ld(int32_t in) { return (int64_t{in} + 127) / 128 * 128; }
+  explicit I8Layout(const oscars_ctx* c) {
+    end = 0;
+    for (int l = 1; l <= c->L; ++l) {
+      w[l] = end;
+      s[l] = w[l] + round_up(c->dims[l] * ld(c->dims[l - 1]), 256);
+      b[l] = s[l] + round_up(c->dims[l] * int64_t{4}, 256);
+      end = b[l] + round_up(c->dims[l] * int64_t{4}, 256);
+    }
+  }
+};
+
+constexpr int64_t kI8EvalRows = 8192;  // rows of an evaluation's pass
+
+// oscars_evaluate_i8's temporaries behind EvalLayout's: quantised rows and their
+// scales, two activations, logits.
+struct I8EvalLayout {
+  int64_t rows, xq, scale, act[2], logits, end;
+  I8EvalLayout(const oscars_ctx* c, int64_t n_rows) {
+    const int64_t passes = (n_rows + kI8EvalRows - 1) / kI8EvalRows;
+    rows = (n_rows + passes - 1) / passes;
+    int64_t in = 0, hidden = 0;
+    for (int l = 0; l < c->L; ++l) {
+      in = std::max(in, I8Layout::ld(c->dims[l]));
+      if (l > 0) hidden = std::max<int64_t>(hidden, c->ld[l]);
+    }
+    xq = EvalLayout(n_rows).end;
+    scale = xq + round_up(rows * in, 256);
+    act[0] = scale + round_up(rows * 4, 256);
+    act[1] = act[0] + round_up(rows * hidden * static_cast<int64_t>(c->esize), 256);
+    logits = act[1] + round_up(rows * hidden * static_cast<int64_t>(c->esize), 256);
+    end = logits + round_up(rows * c->ld[c->L] * 4, 256);
+  }
+};
+
+hipError_t run_evaluate_i8(oscars_ctx* c, const void* model, const void* x, const int32_t* y,
+                           int64_t n_rows, void* buf, double* loss_sum, int64_t* correct) {
+  const EvalLayout lay(n_rows);
+  const I8EvalLayout tmp(c, n_rows);
+  const I8Layout m(c);
+  char* base = static_cast<char*>(buf);
+  const char* mod = static_cast<const char*>(model);
+  struct Results {
+    double loss;
+    int64_t hits;
+  };
+  Results* d_res = reinterpret_cast<Results*>(base);
+  float* d_loss = reinterpret_cast<float*>(base + lay.loss);
+  int32_t* d_hit = reinterpret_cast<int32_t*>(base + lay.hit);
+  int8_t* xq = reinterpret_cast<int8_t*>(base + tmp.xq);
+  float* scale = reinterpret_cast<float*>(base + tmp.scale);
+  float* logits = reinterpret_cast<float*>(base + tmp.logits);
+  const int L = c->L;
+  hipError_t e = hipSuccess;
+  for (int64_t i0 = 0; i0 < n_rows && e == hipSuccess; i0 += tmp.rows) {
+    const int64_t n = std::min(tmp.rows, n_rows - i0);
+    const void* in = static_cast<const char*>(x) + i0 * c->dims[0] * static_cast<int64_t>(c->esize);
+    int64_t in_ld = c->dims[0];
+    for (int l = 1; l <= L && e == hipSuccess; ++l) {
+      const int64_t q_ld = I8Layout::ld(c->dims[l - 1]);
+      e = launch_quantize_rows(QuantArgs{in, in_ld, c->bf16, n, c->dims[l - 1], xq, q_ld, scale},
+                               c->stream);
+      if (e != hipSuccess) break;
+      void* out = l < L ? static_cast<void*>(base + tmp.act[l & 1]) : static_cast<void*>(logits);
+      e = launch_matmul_i8(
+          MatmulI8Args{xq, q_ld, scale, reinterpret_cast<const int8_t*>(mod + m.w[l]), q_ld,
+                       reinterpret_cast<const float*>(mod + m.s[l]),
+                       reinterpret_cast<const float*>(mod + m.b[l]), l < L, n, c->dims[l - 1],
+                       c->dims[l], out, c->ld[l], l < L && c->bf16},
+          c->stream);
+      in = out;
+      in_ld = c->ld[l];
+    }
+    if (e == hipSuccess)
+      e = launch_softmax_ce(logits, c->ld[L], 0, c->dims[L], static_cast<int>(n), y + i0, nullptr,
+                            0, nullptr, c->bf16, d_loss + i0, 0, 1, c->stream, d_hit + i0);
+  }
+  if (e == hipSuccess)
+    e = launch_eval_reduce(d_loss, d_hit, n_rows, &d_res->loss, &d_res->hits, c->stream);
+  Results h{};
+  if (e == hipSuccess)
+    e = hipMemcpyAsync(&h, d_res, sizeof(Results), hipMemcpyDeviceToHost, c->stream);
+  // also behind a failure: what was enqueued reads buffers that the caller frees
+  const hipError_t f = hipStreamSynchronize(c->stream);
+  if (e == hipSuccess) e = f;
+  if (e != hipSuccess) return e;
+  *loss_sum = h.loss;
+  *correct = h.hits;
+  return hipSuccess;
+}
+
+}  // namespace
+
+oscars_status oscars_quantize_rows(int8_t* q, int64_t q_ld, float* scale, const void* x,
+                                   int64_t x_ld, int32_t dtype, int64_t rows, int32_t cols,
+                                   void* hip_stream) {
+  if (!is_dtype(dtype) || !i8_sizes_ok(rows, cols, 1)) return OSCARS_E_INVALID;
+  const int64_t es = dtype_bytes(dtype);
+  if (!rows_ok(x, x_ld, cols, es) || !i8_rows_ok(q, q_ld, cols)) return OSCARS_E_INVALID;
+  if (!scale || !aligned_to(scale, 4)) return OSCARS_E_INVALID;
+  const int64_t xn = rows_span(rows, x_ld, cols, es),
+                qn = rows_span(rows, q_ld, std::min(q_ld, round_up(cols, 128)), 1);
+  if (overlap(q, qn, x, xn) || overlap(scale, rows * 4, x, xn) || overlap(q, qn, scale, rows * 4))
+    return OSCARS_E_INVALID;
+  if (rows == 0) return OSCARS_OK;
+  const hipError_t e =
+      launch_quantize_rows(QuantArgs{x, x_ld, dtype == OSCARS_BF16, rows, cols, q, q_ld, scale},
+                           static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+oscars_status oscars_matmul_i8(void* out, int64_t out_ld, int32_t out_dtype, const int8_t* xq,
+                               int64_t x_ld, const float* xscale, const int8_t* wq, int64_t w_ld,
+                               const float* wscale, const float* bias, int32_t relu, int64_t rows,
+                               int32_t in, int32_t outs, void* hip_stream) {
+  if (!is_dtype(out_dtype)) return OSCARS_E_INVALID;
+  const MatmulI8Args a{xq,   x_ld,      xscale, wq,   w_ld, wscale, bias,
+                       relu != 0, rows, in,     outs, out,  out_ld, out_dtype == OSCARS_BF16};
+  if (!i8_product_ok(a) || !i8_rows_ok(xq, x_ld, round_up(in, 128))) return OSCARS_E_INVALID;
+  if (!xscale || !aligned_to(xscale, 4)) return OSCARS_E_INVALID;
+  const int64_t n = rows_span(rows, out_ld, outs, dtype_bytes(out_dtype));
+  if (overlap(out, n, xq, rows_span(rows, x_ld, round_up(in, 128), 1)) ||
+      overlap(out, n, xscale, rows * 4))
+    return OSCARS_E_INVALID;
+  if (rows == 0) return OSCARS_OK;
+  const hipError_t e = launch_matmul_i8(a, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+int64_t oscars_linear_i8_workspace(int64_t rows, int32_t in) {
+  if (!i8_sizes_ok(rows, in, 1) || linear_i8_one_launch(rows, in)) return 0;
+  return round_up(rows * round_up(in, 128), 256) + rows * 4;
+}
+
+oscars_status oscars_linear_i8(void* out, int64_t out_ld, int32_t out_dtype, const void* x,
+                               int64_t x_ld, int32_t dtype, const int8_t* wq, int64_t w_ld,
+                               const float* wscale, const float* bias, int32_t relu, int64_t rows,
+                               int32_t in, int32_t outs, void* workspace, int64_t workspace_bytes,
+                               void* hip_stream) {
+  if (!is_dtype(dtype) || !is_dtype(out_dtype)) return OSCARS_E_INVALID;
+  MatmulI8Args a{nullptr,   0,    nullptr, wq,   w_ld, wscale, bias,
+                 relu != 0, rows, in,      outs, out,  out_ld, out_dtype == OSCARS_BF16};
+  const int64_t es = dtype_bytes(dtype);
+  if (!i8_product_ok(a) || !rows_ok(x, x_ld, in, es)) return OSCARS_E_INVALID;
+  const int64_t n = rows_span(rows, out_ld, outs, dtype_bytes(out_dtype)),
+                xn = rows_span(rows, x_ld, in, es);
+  if (overlap(out, n, x, xn)) return OSCARS_E_INVALID;
+  const int64_t need = oscars_linear_i8_workspace(rows, in);
+  if (need > 0) {
+    if (!workspace || !aligned16(workspace) || workspace_bytes < need) return OSCARS_E_INVALID;
+    if (overlap(workspace, need, out, n) || overlap(workspace, need, x, xn) ||
+        overlap(workspace, need, wq, rows_span(outs, w_ld, in, 1)) ||
+        overlap(workspace, need, wscale, outs * int64_t{4}) ||
+        (bias && overlap(workspace, need, bias, outs * int64_t{4})))
+      return OSCARS_E_INVALID;
+  }
+  if (rows == 0) return OSCARS_OK;
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  hipError_t e;
+  if (need == 0) {
+    e = launch_linear_i8_few(a, x, x_ld, dtype == OSCARS_BF16, s);
+  } else {
+    int8_t* q = static_cast<int8_t*>(workspace);
+    const int64_t q_ld = round_up(in, 128);
+    float* scale = reinterpret_cast<float*>(q + round_up(rows * q_ld, 256));
+    e = launch_quantize_rows(QuantArgs{x, x_ld, dtype == OSCARS_BF16, rows, in, q, q_ld, scale}, s);
+    a.xq = q;
+    a.x_ld = q_ld;
+    a.xscale = scale;
+    if (e == hipSuccess) e = launch_matmul_i8(a, s);
+  }
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+int64_t oscars_i8_model_bytes(const oscars_ctx* c) {
+  return !c || c->cnn ? 0 : I8Layout(c).end;
+}
+
+oscars_status oscars_quantize_model(oscars_ctx* c, const float* params, void* model) {
+  if (!c || c->cnn || !params || !model || !aligned16(params) || !aligned16(model))
+    return OSCARS_E_INVALID;
+  const I8Layout m(c);
+  if (overlap(model, m.end, params, c->n_pad * 4)) return OSCARS_E_INVALID;
+  char* base = static_cast<char*>(model);
+  hipError_t e = hipSuccess;
+  for (int l = 1; l <= c->L && e == hipSuccess; ++l) {
+    const int in = c->dims[l - 1], outs = c->dims[l];
+    e = launch_quantize_rows(
+        QuantArgs{params + c->w_off[l], in, false, outs, in,
+                  reinterpret_cast<int8_t*>(base + m.w[l]), I8Layout::ld(in),
+                  reinterpret_cast<float*>(base + m.s[l])},
+        c->stream);
+    if (e == hipSuccess)
+      e = launch_broadcast(params + c->b_off[l], reinterpret_cast<float*>(base + m.b[l]), 1, outs,
+                           round_up(outs, 4), c->stream);
+  }
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+oscars_status oscars_evaluate_i8(oscars_ctx* c, const void* model, const void* x, const int32_t* y,
+                                 int64_t n_rows, double* loss_sum, int64_t* correct) {
+  const oscars_status st =
+      check_evaluate(c, static_cast<const float*>(model), x, y, n_rows, loss_sum, correct);
+  if (st != OSCARS_OK) return st;
+  if (c->cnn) return OSCARS_E_INVALID;
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  hipError_t e = hipStreamIsCapturing(c->stream, &cap);
+  if (e != hipSuccess) return hip_fail(e);
+  if (cap != hipStreamCaptureStatusNone) return OSCARS_E_STATE;
+  void* buf = nullptr;
+  e = hipMalloc(&buf, static_cast<size_t>(I8EvalLayout(c, n_rows).end));
+  if (e != hipSuccess) {
+    if (e != hipErrorOutOfMemory) return hip_fail(e);
+    (void)hipGetLastError();
+    return OSCARS_E_NOMEM;
+  }
+  e = run_evaluate_i8(c, model, x, y, n_rows, buf, loss_sum, correct);
+  const hipError_t f = hipFree(buf);  // waits for the device
+  if (e == hipSuccess) e = f;
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
 

@@ -112,3 +112,79 @@ def test_python_checks_come_first():
 
 def test_numbers_of_the_default_steps():
     assert np.allclose(P.NEWTON_SCHULZ, ((3.4445, -4.7750, 2.0315),) * 5)
+
+
+# ------------------------------------------------------------------ 8 bits
+
+Q, X, W, S, OUT = (BASE + k * 0x1000000 for k in range(2, 7))
+
+
+def _quantize(**kw):
+    a = dict(q=Q, q_ld=128, scale=S, x=X, x_ld=100, dtype=P.FP32, rows=4, cols=100)
+    a.update(kw)
+    return lib.oscars_quantize_rows(a["q"], a["q_ld"], a["scale"], a["x"], a["x_ld"], a["dtype"],
+                                    a["rows"], a["cols"], None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(x=None), dict(scale=None), dict(q=Q + 8), dict(q_ld=120), dict(q_ld=96),
+    dict(x_ld=99), dict(x=X + 2), dict(scale=S + 2), dict(dtype=2), dict(rows=-1), dict(cols=0),
+    dict(cols=65537, x_ld=65537, q_ld=1 << 17), dict(rows=1 << 31), dict(x=Q), dict(scale=X),
+    dict(scale=Q), dict(x=X + 1, dtype=P.BF16)])
+def test_quantize_rows_refuses(bad):
+    assert _quantize(**bad) == P.E_INVALID
+
+
+def _linear(matmul=False, **kw):
+    a = dict(out=OUT, out_ld=50, out_dtype=P.FP32, x=X, x_ld=128, dtype=P.FP32, xscale=S + 0x1000,
+             wq=W, w_ld=112, wscale=S, bias=S + 0x8000, relu=1, rows=40, inf=100, outs=50, ws=Q,
+             nbytes=None)
+    a.update(kw)
+    if matmul:
+        return lib.oscars_matmul_i8(a["out"], a["out_ld"], a["out_dtype"], a["x"], a["x_ld"],
+                                    a["xscale"], a["wq"], a["w_ld"], a["wscale"], a["bias"],
+                                    a["relu"], a["rows"], a["inf"], a["outs"], None)
+    need = lib.oscars_linear_i8_workspace(a["rows"], a["inf"])
+    return lib.oscars_linear_i8(a["out"], a["out_ld"], a["out_dtype"], a["x"], a["x_ld"],
+                                a["dtype"], a["wq"], a["w_ld"], a["wscale"], a["bias"], a["relu"],
+                                a["rows"], a["inf"], a["outs"], a["ws"],
+                                need if a["nbytes"] is None else a["nbytes"], None)
+
+
+@pytest.mark.parametrize("matmul", [False, True])
+@pytest.mark.parametrize("bad", [
+    dict(out=None), dict(x=None), dict(wq=None), dict(wscale=None), dict(out=OUT + 2),
+    dict(out_ld=49), dict(out_dtype=7), dict(x_ld=99), dict(wq=W + 4), dict(w_ld=104),
+    dict(w_ld=96), dict(wscale=S + 1), dict(bias=S + 3), dict(rows=-1), dict(rows=1 << 31),
+    dict(inf=0), dict(inf=65537), dict(outs=0), dict(outs=65537), dict(out=X), dict(out=W),
+    dict(out=S), dict(out=S + 0x8000), dict(out=OUT + 1, out_dtype=P.BF16)])
+def test_linear_i8_refuses(bad, matmul):
+    assert _linear(matmul, **bad) == P.E_INVALID
+
+
+def test_linear_i8_refuses_workspace():
+    need = lib.oscars_linear_i8_workspace(40, 100)
+    assert need >= 40 * 128 + 40 * 4 and lib.oscars_linear_i8_workspace(16, 100) == 0
+    assert lib.oscars_linear_i8_workspace(-1, 100) == 0
+    for bad in (dict(ws=None), dict(ws=Q + 8), dict(nbytes=need - 1), dict(ws=OUT), dict(ws=X),
+                dict(ws=W), dict(ws=S), dict(dtype=3)):
+        assert _linear(**bad) == P.E_INVALID, bad
+
+
+def test_matmul_i8_refuses():
+    for bad in (dict(xscale=None), dict(x=X + 8), dict(x_ld=112), dict(x_ld=136), dict(out=S + 0x1000)):
+        assert _linear(True, **bad) == P.E_INVALID, bad
+
+
+def test_no_rows_is_no_work():
+    assert _quantize(rows=0) == P.OK
+    assert _linear(rows=0, ws=None) == P.OK
+    assert _linear(True, rows=0) == P.OK
+
+
+def test_int8_model_refuses_null():
+    loss, hits = ctypes.c_double(0.0), ctypes.c_int64(0)
+    assert lib.oscars_i8_model_bytes(None) == 0
+    assert lib.oscars_quantize_model(None, BASE, BASE) == P.E_INVALID
+    assert lib.oscars_evaluate_i8(None, BASE, BASE, BASE, 1, ctypes.byref(loss),
+                                  ctypes.byref(hits)) == P.E_INVALID
