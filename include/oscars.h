@@ -352,9 +352,9 @@ oscars_status oscars_broadcast(const float* global, float* replicas, int32_t K, 
  *            no part of a matrix; the call's own until the stream has run it.
  * A matrix of zeros gives zeros, one with a NaN or an infinity gives NaN; the
  * others of the call are not touched by it.  Sums are in a fixed order: the
- * same inputs give the same bits, and a matrix's result does not depend on
- * the others of the call where the tiles are the same (their size goes by the
- * whole call's work; sums differ between tile sizes only in how K is cut).
+ * same call gives the same bits.  (The tiles' size goes by the whole call's
+ * work, and with it where a sum of K is rounded: a matrix's last bits may differ
+ * between calls with other matrices beside it.)
  * Allocates nothing and may be captured into a graph. */
 #define OSCARS_MAX_MATRICES 32
 #define OSCARS_MAX_ORTH_STEPS 16

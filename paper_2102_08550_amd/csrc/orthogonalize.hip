@@ -33,7 +33,6 @@ namespace {
 
 typedef NtShape<256, 256, 2, 4, 2> OrthL;
 typedef NtShape<128, 128, 2, 2, 2, 1> OrthM;
-typedef NtShape<64, 64, 2, 2, 3, 2> OrthS;
 
 enum OrthKind { ORTH_GRAM = 0, ORTH_POLY = 1, ORTH_APPLY = 2, ORTH_LAST = 3 };
 
@@ -49,8 +48,13 @@ struct MatDesc {
 
 struct OrthArgs {
   MatDesc mat[ORTH_MAX_MATS];
-  int first[ORTH_MAX_MATS + 1];  // first workgroup of each matrix (multiples of 8)
   int count;
+  // A launch's workgroups go matrix after matrix: position i is matrix order[i],
+  // its first workgroup first[i], a multiple of 8.  (Whole words: beside an array
+  // of bytes with the same index the compiler addressed first[i] as (base + i) +
+  // 3 i, and scalar loads drop the low bits of each summand.)
+  int first[ORTH_MAX_MATS + 1];
+  int order[ORTH_MAX_MATS];
   char* ws;
   float a, b, c;
   int in_scaled;       // 1: the planes hold X times orth_scale; 0: X_0 (factor in the workspace)
@@ -81,7 +85,7 @@ struct Planes {
   char *x, *xt[2], *a, *p;
 };
 __host__ __device__ __forceinline__ int64_t plane_bytes(int rows, int k) {
-  return (static_cast<int64_t>(rows) * pad64(k) * 4 + 255) / 256 * 256;
+  return (static_cast<int64_t>(rows) * (pad64(k) / 32 + 1) * NT_BLOCK + 255) / 256 * 256;
 }
 __host__ __device__ __forceinline__ Planes mat_planes(char* ws, const MatDesc& d) {
   const int m = mat_m(d.u), n = mat_n(d.u);
@@ -97,9 +101,15 @@ __host__ __device__ int64_t mat_bytes(const OrthMat& u) {
   const int m = mat_m(u), n = mat_n(u);
   return plane_bytes(m, n) + 2 * plane_bytes(n, m) + 2 * plane_bytes(m, m);
 }
-// Bytes of a row of k values (k padded to 64 with zeros).
+// K blocks of a row of k values (k padded to 64 with zeros), and the bytes from one
+// row to the next: an odd number of blocks.  Every tile reads and writes the same
+// columns of many rows at a time; rows a power of two apart would put them all
+// on a few memory channels.
+__host__ __device__ __forceinline__ int row_blocks(int k, int fmt) {
+  return pad64(k) / (fmt == NT_F16 ? 64 : 32);
+}
 __host__ __device__ __forceinline__ int64_t row_bytes(int k, int fmt) {
-  return static_cast<int64_t>(pad64(k)) * (fmt == NT_F16 ? 2 : 4);
+  return static_cast<int64_t>(row_blocks(k, fmt) | 1) * NT_BLOCK;
 }
 
 // Power of two on the iterates in their planes.  The rms of an m x n matrix
@@ -111,15 +121,14 @@ __host__ __device__ __forceinline__ float orth_scale(int n) {
   return static_cast<float>(1 << e);
 }
 
-// Which matrix a workgroup works for, and its index among the matrix's
-// workgroups such that those on one XCD (index mod 8) take neighbouring tiles.
-__device__ __forceinline__ int find_mat(const OrthArgs& g, int block, int tiles_of_all,
-                                        int* local) {
-  int i = 0;
-  while (i + 1 < g.count && block >= g.first[i + 1]) ++i;
-  *local = block - g.first[i];
-  return i;
+// The position of entry `at` of a launch's list: how many positions end at or
+// before it.  A lane looks at each (ORTH_MAX_MATS <= 64), one load in all.
+__device__ __forceinline__ int find_position(const int* first, int count, int at) {
+  const int lane = threadIdx.x & 63;
+  const bool past = lane < count - 1 && at >= first[lane + 1];
+  return __builtin_popcountll(__ballot(past));
 }
+// Workgroups or tiles of one XCD (index mod 8) take neighbouring work.
 __device__ __forceinline__ int xcd_index(int id, int total) {
   const int per = total >> 3, rem = total & 7, x = id & 7, q = id >> 3;
   return x * per + (x < rem ? x : rem) + q;
@@ -146,39 +155,57 @@ __device__ __forceinline__ void put4(char* row, int k, int fmt, const float* v) 
     *reinterpret_cast<nt_u32x2*>(p + 64) = lo;
   }
 }
-// Sixteen values from k (a multiple of 16).
-__device__ __forceinline__ void put16(char* row, int k, int fmt, const float* v) {
-  const nt_u32x4 h0 = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
-  const nt_u32x4 h1 = {pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]),
-                       pack2(v[14], v[15])};
-  if (fmt == NT_F16) {
-    nt_u32x4* p = reinterpret_cast<nt_u32x4*>(row + 2 * static_cast<int64_t>(k));
-    p[0] = h0;
-    p[1] = h1;
-  } else {
-    nt_u32x4* p =
-        reinterpret_cast<nt_u32x4*>(row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31));
-    p[0] = h0;
-    p[1] = h1;
-    float l[16];
+// One 16-byte piece of a plane row: eight values from k (a multiple of 8), as hi
+// or as lo.  The pieces of a 128-byte line are stored by neighbouring lanes in
+// one instruction (store_lines): the L2 takes one request a line instead of one
+// a piece, which had made the stores of 4096 x 4096 planes 70 us of 380.
+__device__ __forceinline__ void put8(char* row, int k, int fmt, bool lo, const float* v) {
+  nt_u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) l[i] = lo_of(v[i]);
-    p[4] = nt_u32x4{pack2(l[0], l[1]), pack2(l[2], l[3]), pack2(l[4], l[5]), pack2(l[6], l[7])};
-    p[5] = nt_u32x4{pack2(l[8], l[9]), pack2(l[10], l[11]), pack2(l[12], l[13]),
-                    pack2(l[14], l[15])};
+  for (int i = 0; i < 4; ++i) {
+    const float a = lo ? lo_of(v[2 * i]) : v[2 * i], b = lo ? lo_of(v[2 * i + 1]) : v[2 * i + 1];
+    w[i] = pack2(a, b);
+  }
+  char* p = fmt == NT_F16 ? row + 2 * static_cast<int64_t>(k)
+                          : row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31) + (lo ? 64 : 0);
+  *reinterpret_cast<nt_u32x4*>(p) = w;
+}
+// Rows first .. first + 31 below `rows` of planes at `base`, entries k0 .. k0 + 31:
+// value(i, k, v) gives eight values of row first + i from entry k0 + k on.  A wave.
+template <typename Value>
+__device__ __forceinline__ void store_lines(char* base, int64_t ld, int first, int rows, int k0,
+                                            int fmt, int lane, Value&& value) {
+  const bool f16 = fmt == NT_F16;
+  // SPLIT: 8 rows of 4 hi and 4 lo pieces; F16: 16 rows of 4 pieces
+  const int per = f16 ? 16 : 8, mine = f16 ? lane >> 2 : lane >> 3, k = 8 * (lane & 3);
+  const bool lo = !f16 && (lane & 4);
+  for (int i = mine; i < 32; i += per) {
+    float v[8];
+    value(i, k, v);
+    if (first + i < rows) put8(base + (first + i) * ld, k0 + k, fmt, lo, v);
   }
 }
-__device__ __forceinline__ void get4(const char* row, int k, int fmt, float* v) {
+
+// N values from k (both multiples of 4, within 16).
+template <int N>
+__device__ __forceinline__ void get(const char* row, int k, int fmt, float* v) {
   typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-  if (fmt == NT_F16) {
-    const h4 h = *reinterpret_cast<const h4*>(row + 2 * static_cast<int64_t>(k));
+  const h4* p = reinterpret_cast<const h4*>(
+      fmt == NT_F16 ? row + 2 * static_cast<int64_t>(k)
+                    : row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31));
 #pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = static_cast<float>(h[t]);
-  } else {
-    const char* p = row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31);
-    const h4 h = *reinterpret_cast<const h4*>(p), l = *reinterpret_cast<const h4*>(p + 64);
+  for (int i = 0; i < N / 4; ++i) {
+    const h4 h = p[i];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = static_cast<float>(h[t]) + static_cast<float>(l[t]);
+    for (int t = 0; t < 4; ++t) v[4 * i + t] = static_cast<float>(h[t]);
+  }
+  if (fmt != NT_F16) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const h4 l = p[8 + i];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[4 * i + t] += static_cast<float>(l[t]);
+    }
   }
 }
 
@@ -217,8 +244,7 @@ __device__ __forceinline__ float load_elem(const void* p, int64_t i) {
 template <bool BF16>
 __global__ __launch_bounds__(256) void orth_norm_kernel(OrthArgs g) {
   __shared__ double lds4[4];
-  int local;
-  const int i = find_mat(g, blockIdx.x, 0, &local);
+  const int i = find_position(g.first, g.count, blockIdx.x), local = blockIdx.x - g.first[i];
   const OrthMat& u = g.mat[i].u;
   const int64_t size = static_cast<int64_t>(u.rows) * u.cols;
   const int parts = norm_parts(size);
@@ -251,11 +277,10 @@ template <bool BF16>
 __global__ __launch_bounds__(256) void orth_convert_kernel(OrthArgs g) {
   __shared__ double lds4[4];
   __shared__ float tile[64][65];
-  int local;
-  const int i = find_mat(g, blockIdx.x, 0, &local);
+  const int i = find_position(g.first, g.count, blockIdx.x), local = blockIdx.x - g.first[i];
   const OrthMat& u = g.mat[i].u;
-  const int gc = (u.cols + 63) / 64, gr = (u.rows + 63) / 64;
-  if (local >= gc * gr) return;
+  const int gc = (u.cols + 63) / 64;
+  if (local >= gc * ((u.rows + 63) / 64)) return;
   const int64_t size = static_cast<int64_t>(u.rows) * u.cols;
   const int parts = norm_parts(size);
   const double* part = ws_parts(g.ws, i);
@@ -281,21 +306,20 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(OrthArgs g) {
   __syncthreads();
   const bool tall = mat_tall(u);
   const Planes q = mat_planes(g.ws, g.mat[i]);
-  // "straight": rows of G; "turned": rows of G'.  X is the one with m rows.
-  const int row = threadIdx.x >> 2, k = (threadIdx.x & 3) * 16;
-  float v[16];
-  if (r0 + row < u.rows) {
+  // G's rows and those of G': X is the one with m rows.  Wave w: quarter w of the tile.
+  const int lane = threadIdx.x & 63, i0 = (threadIdx.x >> 7) * 32;
+  const int j0 = (threadIdx.x >> 6 & 1) * 32;
+  const int fmt1 = tall ? g.xt_fmt : g.x_fmt, fmt2 = tall ? g.x_fmt : g.xt_fmt;
+  store_lines(tall ? q.xt[0] : q.x, row_bytes(u.cols, fmt1), r0 + i0, u.rows, c0 + j0, fmt1, lane,
+              [&](int i, int k, float* v) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t) v[t] = tile[row][k + t];
-    const int fmt = tall ? g.xt_fmt : g.x_fmt;
-    put16((tall ? q.xt[0] : q.x) + (r0 + row) * row_bytes(u.cols, fmt), c0 + k, fmt, v);
-  }
-  if (c0 + row < u.cols) {
+                for (int e = 0; e < 8; ++e) v[e] = tile[i0 + i][j0 + k + e];
+              });
+  store_lines(tall ? q.x : q.xt[0], row_bytes(u.rows, fmt2), c0 + i0, u.cols, r0 + j0, fmt2, lane,
+              [&](int i, int k, float* v) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t) v[t] = tile[k + t][row];
-    const int fmt = tall ? g.x_fmt : g.xt_fmt;
-    put16((tall ? q.x : q.xt[0]) + (c0 + row) * row_bytes(u.rows, fmt), r0 + k, fmt, v);
-  }
+                for (int e = 0; e < 8; ++e) v[e] = tile[j0 + k + e][i0 + i];
+              });
 }
 
 // One product for every matrix of the call.
@@ -303,56 +327,175 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(OrthArgs g) {
 //   POLY   P = a I + b A + c A A (same)
 //   APPLY  X <- P X, into X and the other X' buffer
 //   LAST   the same into the caller's matrix
-// A 32 x 32 block of the accumulator has, in lane (h, l), column l and rows
-// 8 q + 4 h + t: four consecutive rows, which are four consecutive entries of
-// the transposed result; the straight one goes through LDS.
+
+// A product's operands, and where a matrix's tile `local` lies.
+template <int KIND>
+struct Product {
+  static constexpr bool SYM = KIND == ORTH_GRAM || KIND == ORTH_POLY;
+  char *x, *a, *p;           // planes
+  char *xt, *xt_next;        // X' that is read, and the other one
+  const char *left, *right;  // operands
+  int im, m, n, R, C, K;     // R x C results, K summed over
+  void* dst;
+  const float* base;
+  int64_t dst_ld;
+  float keep, rate;
+  __device__ __forceinline__ Product(const OrthArgs& g, int mat) {
+    const OrthMat& u = g.mat[mat].u;
+    dst = u.dst;
+    base = u.base;
+    dst_ld = u.dst_ld;
+    keep = u.keep;
+    rate = u.rate;
+    im = mat;
+    m = mat_m(u);
+    n = mat_n(u);
+    const Planes q = mat_planes(g.ws, g.mat[mat]);
+    x = q.x;
+    a = q.a;
+    p = q.p;
+    // (arithmetic, not a choice between two members: that would put this in memory)
+    const int64_t apart = q.xt[1] - q.xt[0];
+    xt = q.xt[0] + (g.parity ? apart : 0);
+    xt_next = q.xt[0] + (g.parity ? 0 : apart);
+    const bool swap = KIND == ORTH_LAST && !mat_tall(u);  // a wide matrix's rows are columns here
+    R = SYM ? m : (swap ? n : m);
+    C = SYM ? m : (swap ? m : n);
+    K = KIND == ORTH_GRAM ? n : m;
+    left = KIND == ORTH_GRAM ? x : KIND == ORTH_POLY ? a : swap ? xt : p;
+    right = KIND == ORTH_GRAM ? x : KIND == ORTH_POLY ? a : swap ? p : xt;
+  }
+  template <int B>
+  __device__ __forceinline__ int tiles() const {
+    const int tr = (R + B - 1) / B, tc = (C + B - 1) / B;
+    return SYM ? tr * (tr + 1) / 2 : tr * tc;
+  }
+  // `id`: of the matrix's tiles of B x B
+  template <int B>
+  __device__ __forceinline__ void tile(int id, int* ti, int* tj) const {
+    const int tr = (R + B - 1) / B, tc = (C + B - 1) / B;
+    if (SYM) {
+      int i = static_cast<int>((sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
+      while (i * (i + 1) / 2 > id) --i;
+      while ((i + 1) * (i + 2) / 2 <= id) ++i;
+      *ti = i;
+      *tj = id - i * (i + 1) / 2;
+    } else {
+      // bands of four tile rows, column by column: a band's operands stay in L2
+      constexpr int BAND = 4;
+      const int band = id / (BAND * tc), rows = tr - band * BAND < BAND ? tr - band * BAND : BAND;
+      const int at = id - band * BAND * tc;
+      *ti = band * BAND + at % rows;
+      *tj = at / rows;
+    }
+  }
+  // What a sum is multiplied with: the planes' scales, and POLY's c.
+  __device__ __forceinline__ float factor(const OrthArgs& g) const {
+    const float in = g.in_scaled ? 1.0f / orth_scale(n) : ws_scale(g.ws)[im];  // on one X
+    return KIND == ORTH_GRAM    ? in * in * kScaleA
+           : KIND == ORTH_POLY  ? g.c / kScaleA
+           : KIND == ORTH_APPLY ? in / kScaleA * orth_scale(n)
+                                : in / kScaleA;
+  }
+  // Planes that a result goes to: rows C with entries R, and rows R with entries C.
+  __device__ __forceinline__ char* turned() const {
+    return KIND == ORTH_GRAM ? a : KIND == ORTH_POLY ? p : xt_next;
+  }
+  __device__ __forceinline__ char* straight() const {
+    return KIND == ORTH_GRAM ? a : KIND == ORTH_POLY ? p : x;
+  }
+  // Rows r .. r + N - 1 of column c: POLY's other terms, zeros in the planes'
+  // padding.  `fmt`: POLY, of A.
+  template <int N>
+  __device__ __forceinline__ void finish(const OrthArgs& g, int r, int c, int fmt, float* v) const {
+    if constexpr (KIND == ORTH_POLY) {
+      if (c < C) {
+        // A(r, c) = A(c, r), consecutive
+        float t[N];
+        get<N>(a + c * row_bytes(m, fmt), r, fmt, t);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          v[e] += g.b * t[e] + (r + e == c ? g.a * kScaleA : 0.0f);
+      }
+    }
+    if constexpr (KIND != ORTH_LAST) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (r + e >= R || c >= C) v[e] = 0.0f;
+    }
+  }
+  // LAST: N consecutive entries from `r` of the caller's row `c`.
+  template <int N>
+  __device__ __forceinline__ void out(const OrthArgs& g, int r, int c, const float* v) const {
+    if (c >= C || r >= R) return;
+    const int64_t at = c * dst_ld + r;
+    const bool whole = r + N <= R;
+    if (g.bf16) {
+      uint16_t* p = static_cast<uint16_t*>(dst) + at;
+      if (whole && (reinterpret_cast<uintptr_t>(p) & 7) == 0) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+          *reinterpret_cast<nt_u32x2*>(p + e) =
+              nt_u32x2{f32_to_bf16(v[e]) | static_cast<uint32_t>(f32_to_bf16(v[e + 1])) << 16,
+                       f32_to_bf16(v[e + 2]) | static_cast<uint32_t>(f32_to_bf16(v[e + 3])) << 16};
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (r + e < R) p[e] = f32_to_bf16(v[e]);
+      }
+      return;
+    }
+    float* p = static_cast<float*>(dst) + at;
+    const float* from = base + at;  // where there is one
+    const uintptr_t low =
+        reinterpret_cast<uintptr_t>(p) | (base ? reinterpret_cast<uintptr_t>(from) : 0);
+    if (whole && (low & 15) == 0) {
+      nt_f32x4 b[N / 4];
+      if (base) {
+#pragma unroll
+        for (int e = 0; e < N / 4; ++e) b[e] = reinterpret_cast<const nt_f32x4*>(from)[e];
+      }
+#pragma unroll
+      for (int e = 0; e < N / 4; ++e) {
+        nt_f32x4 o = {v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+        if (base) o = keep * b[e] - rate * o;
+        reinterpret_cast<nt_f32x4*>(p)[e] = o;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (r + e < R) p[e] = base ? keep * from[e] - rate * v[e] : v[e];
+    }
+  }
+};
+
+// One tile a workgroup.  A 32 x 32 block of the accumulator has, in lane (h, l),
+// column l and rows 8 q + 4 h + t: four consecutive rows, which are four
+// consecutive entries of the turned result.
+// (LDS of exactly S::LDS_BYTES: one more variable beside the 128 KB of the 256 x
+// 256 tile cost it 45 us of 335.)
 template <class S, int KIND, int F>
 __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
   constexpr int TURN = 36;  // floats of an LDS row of the turned block
-  constexpr bool SYM = KIND == ORTH_GRAM || KIND == ORTH_POLY;
+  typedef Product<KIND> Prod;
   static_assert(S::BM == S::BN, "symmetric tiles");
   static_assert(S::LDS_BYTES >= S::WM * S::WN * 32 * TURN * 4, "room to turn blocks");
+  constexpr int PF = F == NT_SPLIT_B0 ? static_cast<int>(NT_SPLIT) : F;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS_BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
-  int local;
-  const int im = find_mat(g, blockIdx.x, 0, &local);
-  const MatDesc& d = g.mat[im];
-  const int m = mat_m(d.u), n = mat_n(d.u);
-  const bool tall = mat_tall(d.u);
-  const Planes q = mat_planes(g.ws, d);
-  // rows of the left (R) and right (C) operand
-  const bool swap = KIND == ORTH_LAST && !tall;
-  const int R = SYM ? m : (swap ? n : m), C = SYM ? m : (swap ? m : n);
-  const int tr = (R + S::BM - 1) / S::BM, tc = (C + S::BN - 1) / S::BN;
-  const int total = SYM ? tr * (tr + 1) / 2 : tr * tc;
-  if (local >= total) return;
-  const int id = xcd_index(local, total);
+  const int pos = find_position(g.first, g.count, blockIdx.x);
+  const Prod p(g, g.order[pos]);
+  const int local = blockIdx.x - g.first[pos], tiles = p.template tiles<S::BM>();
+  if (local >= tiles) return;
   int ti, tj;
-  if (SYM) {
-    ti = static_cast<int>((sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
-    while (ti * (ti + 1) / 2 > id) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= id) ++ti;
-    tj = id - ti * (ti + 1) / 2;
-  } else {
-    // bands of four tile rows, column by column: a band's operands stay in L2
-    constexpr int BAND = 4;
-    const int band = id / (BAND * tc), rows = tr - band * BAND < BAND ? tr - band * BAND : BAND;
-    const int at = id - band * BAND * tc;
-    ti = band * BAND + at % rows;
-    tj = at / rows;
-  }
+  p.template tile<S::BM>(xcd_index(local, tiles), &ti, &tj);
   const int r0 = ti * S::BM, c0 = tj * S::BN;
-
-  const int K = KIND == ORTH_GRAM ? n : m;
-  const int64_t ld = row_bytes(K, F == NT_SPLIT_B0 ? NT_SPLIT : F);
-  const char* xt = g.parity ? q.xt[1] : q.xt[0];
-  const char* left = KIND == ORTH_GRAM ? q.x : KIND == ORTH_POLY ? q.a : (swap ? xt : q.p);
-  const char* right = KIND == ORTH_GRAM ? q.x : KIND == ORTH_POLY ? q.a : (swap ? q.p : xt);
+  const int64_t ld = row_bytes(p.K, PF);
   NtRows<S::NT, S::BM> ra;
   NtRows<S::NT, S::BN> rb;
-  ra.init(left, ld, ld * R, r0, R, tid);
-  rb.init(right, ld, ld * C, c0, C, tid);
+  ra.init(p.left, ld, ld * p.R, r0, p.R, tid);
+  rb.init(p.right, ld, ld * p.C, c0, p.C, tid);
   typename NtAcc<F>::type acc[S::MI][S::NJ];
 #pragma unroll
   for (int i = 0; i < S::MI; ++i)
@@ -360,100 +503,201 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
     for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  nt_tile<S, F>(ra, rb, 0, static_cast<int>(ld / NT_BLOCK), lds, tid, acc);
+  nt_tile<S, F>(ra, rb, 0, row_blocks(p.K, PF), lds, tid, acc);
 
-  const float x_scale = orth_scale(n);
-  const float in = g.in_scaled ? 1.0f / x_scale : ws_scale(g.ws)[im];  // on one X of a product
-  const float f_acc = KIND == ORTH_GRAM   ? in * in * kScaleA
-                      : KIND == ORTH_POLY ? g.c / kScaleA
-                      : KIND == ORTH_APPLY ? in / kScaleA * x_scale
-                                           : in / kScaleA;
+  // Block by block through LDS of the wave's own, turned[column][row]: a lane's
+  // four consecutive rows lie together, and both the columns (the turned
+  // result) and the rows (the straight one) are read 16 entries a lane.  One
+  // copy of this code for all blocks (unrolled over the accumulators it is 30 KB).
+  const float f = p.factor(g);
   const int rw = r0 + (wave / S::WN) * 32 * S::MI, cw = c0 + (wave % S::WN) * 32 * S::NJ;
   float* turn = reinterpret_cast<float*>(lds) + wave * 32 * TURN;
-  constexpr int PF = F == NT_SPLIT_B0 ? static_cast<int>(NT_SPLIT) : F;  // POLY: planes of A and P
+  const int fmt1 = KIND == ORTH_GRAM ? g.p_fmt : KIND == ORTH_POLY ? PF : g.xt_fmt;
+  const int fmt2 = KIND == ORTH_APPLY ? g.x_fmt : fmt1;
+  const int64_t ld1 = row_bytes(p.R, fmt1), ld2 = row_bytes(p.C, fmt2);
+  const int line = lane >> 1, k16 = 16 * (lane & 1);
   nt_barrier();  // the stages are read: LDS is free
+#pragma nounroll
+  for (int block = 0; block < S::MI * S::NJ; ++block) {
+    const int rb0 = rw + 32 * (block / S::NJ), cb0 = cw + 32 * (block % S::NJ);
+    if (rb0 >= pad64(p.R) || cb0 >= pad64(p.C)) continue;  // uniform over the wave
 #pragma unroll
-  for (int i = 0; i < S::MI; ++i)
+    for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-    for (int j = 0; j < S::NJ; ++j) {
-      const int rb0 = rw + 32 * i, cb0 = cw + 32 * j, c = cb0 + (lane & 31);
-      if (rb0 >= pad64(R) || cb0 >= pad64(C)) continue;  // uniform over the wave
-      float v[16];
+      for (int j = 0; j < S::NJ; ++j)
+        if (block == i * S::NJ + j) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e] * f_acc;
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<nt_f32x4*>(turn + (lane & 31) * TURN + 8 * e + 4 * h) =
+                nt_f32x4{acc[i][j][4 * e] * f, acc[i][j][4 * e + 1] * f,
+                         acc[i][j][4 * e + 2] * f, acc[i][j][4 * e + 3] * f};
+        }
+    __builtin_amdgcn_wave_barrier();
+    if constexpr (KIND == ORTH_LAST) {
+      // eight lanes store the 32 entries of a caller's row
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = 8 * e + (lane >> 3), k = 4 * (lane & 7);
+        const nt_f32x4 t = *reinterpret_cast<const nt_f32x4*>(turn + row * TURN + k);
+        const float v[4] = {t[0], t[1], t[2], t[3]};
+        p.template out<4>(g, rb0 + k, cb0 + row, v);
+      }
+    } else {
       if constexpr (KIND == ORTH_POLY) {
-        if (c < C) {
+        float v[16];
+        float* mine = turn + line * TURN + k16;
 #pragma unroll
-          for (int s4 = 0; s4 < 4; ++s4) {
-            // A(r, c) = A(c, r), four consecutive
-            const int r = rb0 + 8 * s4 + 4 * h;
-            float t[4];
-            get4(q.a + c * row_bytes(m, PF), r, PF, t);
+        for (int e = 0; e < 4; ++e) {
+          const nt_f32x4 t = *reinterpret_cast<const nt_f32x4*>(mine + 4 * e);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              v[4 * s4 + e] += g.b * t[e] + (r + e == c ? g.a * kScaleA : 0.0f);
-          }
+          for (int o = 0; o < 4; ++o) v[4 * e + o] = t[o];
         }
+        p.template finish<16>(g, rb0 + k16, cb0 + line, PF, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<nt_f32x4*>(mine + 4 * e) =
+              nt_f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+        __builtin_amdgcn_wave_barrier();
       }
-      if constexpr (KIND == ORTH_LAST) {
-        if (c < C) {
+      // turned: rows c, entries r (zeros in the padding)
+      store_lines(p.turned(), ld1, cb0, p.C, rb0, fmt1, lane, [&](int i, int k, float* v) {
 #pragma unroll
-          for (int s4 = 0; s4 < 4; ++s4) {
-            const int r = rb0 + 8 * s4 + 4 * h;
-            const int64_t at = c * d.u.dst_ld + r;
-            if (g.bf16) {
-              uint16_t* p = static_cast<uint16_t*>(d.u.dst) + at;
+        for (int e = 0; e < 2; ++e) {
+          const nt_f32x4 t = *reinterpret_cast<const nt_f32x4*>(turn + i * TURN + k + 4 * e);
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (r + e < R) p[e] = f32_to_bf16(v[4 * s4 + e]);
-            } else {
-              float* p = static_cast<float*>(d.u.dst) + at;
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (r + e < R) {
-                  float o = v[4 * s4 + e];
-                  if (d.u.base) o = d.u.keep * d.u.base[at + e] - d.u.rate * o;
-                  p[e] = o;
-                }
-            }
-          }
+          for (int o = 0; o < 4; ++o) v[4 * e + o] = rb0 + k + 4 * e + o < p.R ? t[o] : 0.0f;
         }
-      } else {
+      });
+      // straight: rows r, entries c (a diagonal tile holds both already)
+      if (!Prod::SYM || ti != tj)
+        store_lines(p.straight(), ld2, rb0, p.R, cb0, fmt2, lane, [&](int i, int k, float* v) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int r = rb0 + 8 * (e >> 2) + 4 * h + (e & 3);
-          if (r >= R || c >= C) v[e] = 0.0f;  // the planes are padded with zeros
-        }
-        const int fmt1 = KIND == ORTH_GRAM ? g.p_fmt : KIND == ORTH_POLY ? PF : g.xt_fmt;
-        const int fmt2 = KIND == ORTH_APPLY ? g.x_fmt : fmt1;
-        char* d1 = KIND == ORTH_GRAM ? q.a : KIND == ORTH_POLY ? q.p : g.parity ? q.xt[0] : q.xt[1];
-        char* d2 = KIND == ORTH_APPLY ? q.x : d1;
-        // transposed: rows c, entries r
-        if (c < C) {
-#pragma unroll
-          for (int s4 = 0; s4 < 4; ++s4)
-            put4(d1 + c * row_bytes(R, fmt1), rb0 + 8 * s4 + 4 * h, fmt1, v + 4 * s4);
-        }
-        // straight: rows r, entries c (a diagonal tile holds both already)
-        if (!SYM || ti != tj) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            turn[(8 * (e >> 2) + 4 * h + (e & 3)) * TURN + (lane & 31)] = v[e];
-          __builtin_amdgcn_wave_barrier();
-          const int r = rb0 + (lane >> 1), k = 16 * (lane & 1);
-          float w[16];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const nt_f32x4 t =
-                *reinterpret_cast<const nt_f32x4*>(turn + (lane >> 1) * TURN + k + 4 * e);
-#pragma unroll
-            for (int o = 0; o < 4; ++o) w[4 * e + o] = t[o];
-          }
-          __builtin_amdgcn_wave_barrier();
-          if (r < R) put16(d2 + r * row_bytes(C, fmt2), cb0 + k, fmt2, w);
-        }
-      }
+          for (int e = 0; e < 8; ++e)
+            v[e] = cb0 + k + e < p.C ? turn[(k + e) * TURN + i] : 0.0f;
+        });
     }
+    __builtin_amdgcn_wave_barrier();
+  }
+#endif
+}
+
+// Small products, where a launch's latency is all there is: 32 x 32 results a
+// workgroup, K dealt to its four waves block by block.  A wave streams its blocks
+// through LDS of its own, all of them in flight at once up to RING, and waits for
+// no other wave until the four sums meet.  The small planes' products have
+// accumulators of their own and lo lo is kept (see NtShape::EXACT).
+constexpr int SMALL_RING = 2;
+constexpr int SMALL_WAVES = 4;
+
+template <int KIND, int F>
+__global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g) {
+#if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
+  constexpr int STAGE = 64 * NT_BLOCK, TURN = 33;
+  constexpr int PF = F == NT_SPLIT_B0 ? static_cast<int>(NT_SPLIT) : F;
+  typedef Product<KIND> Prod;
+  __shared__ __attribute__((aligned(16))) char lds[SMALL_WAVES * SMALL_RING * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // scalar addresses below
+  const int pos = find_position(g.first, g.count, blockIdx.x);
+  const Prod p(g, g.order[pos]);
+  const int local = blockIdx.x - g.first[pos], tiles = p.template tiles<32>();
+  if (local >= tiles) return;
+  int ti, tj;
+  p.template tile<32>(xcd_index(local, tiles), &ti, &tj);
+  const int r0 = ti * 32, c0 = tj * 32;
+  const int64_t ld = row_bytes(p.K, PF);
+  const int blocks = row_blocks(p.K, PF);
+  NtRows<64, 32> ra, rb;
+  ra.init(p.left, ld, ld * p.R, r0, p.R, lane);
+  rb.init(p.right, ld, ld * p.C, c0, p.C, lane);
+  char* ring = lds + wave * SMALL_RING * STAGE;
+  auto issue = [&](int i) {  // the wave's block i
+    const int k = wave + SMALL_WAVES * i;
+    char* t = ring + (i % SMALL_RING) * STAGE;
+    const int at = (k < blocks ? k : blocks - 1) * NT_BLOCK;
+    ra.issue(t, at, lane);
+    rb.issue(t + STAGE / 2, at, lane);
+  };
+  nt_f32x16 acc, cross;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = cross[e] = 0.0f;
+  constexpr int PER = NtRows<64, 32>::P * 2;
+  for (int i = 0; i < SMALL_RING; ++i) issue(i);
+  for (int i = 0; wave + SMALL_WAVES * i < blocks; ++i) {
+    nt_wait_vm<(SMALL_RING - 1) * PER>();
+    const char* ta = ring + (i % SMALL_RING) * STAGE;
+    const char* tb = ta + STAGE / 2;
+    nt_u32x4 fa[4], fb[4];
+    const int row = lane & 31;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      fa[c] = nt_read(ta, row, 2 * c + h);
+      fb[c] = nt_read(tb, row, 2 * c + h);
+    }
+    // the stage is in registers: refill it
+    __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    issue(i + SMALL_RING);
+    if constexpr (PF == NT_SPLIT) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        acc = nt_mfma<F>(fa[k], fb[k], acc);
+        cross = nt_mfma<F>(fa[2 + k], fb[k], cross);
+        if constexpr (F == NT_SPLIT) {
+          cross = nt_mfma<F>(fa[k], fb[2 + k], cross);
+          cross = nt_mfma<F>(fa[2 + k], fb[2 + k], cross);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc = nt_mfma<F>(fa[k], fb[k], acc);
+    }
+  }
+  nt_wait_vm<0>();
+  __syncthreads();  // every wave is through with LDS: now the four sums
+  float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) sums[(wave * 16 + e) * 64 + lane] = acc[e] + cross[e];
+  __syncthreads();
+  // wave w finishes rows 8 w + 4 h .. + 3 of column (lane & 31)
+  const float f = p.factor(g);
+  const int r = r0 + 8 * wave + 4 * h, c = c0 + (lane & 31);
+  float v[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < SMALL_WAVES; ++w) s += sums[(w * 16 + 4 * wave + t) * 64 + lane];
+    v[t] = s * f;
+  }
+  p.template finish<4>(g, r, c, PF, v);
+  if constexpr (KIND == ORTH_LAST) {
+    p.template out<4>(g, r, c, v);
+  } else {
+    const int fmt1 = KIND == ORTH_GRAM ? g.p_fmt : KIND == ORTH_POLY ? PF : g.xt_fmt;
+    const int fmt2 = KIND == ORTH_APPLY ? g.x_fmt : fmt1;
+    // rows are padded to 64 entries: the last tile zeros what no tile covers
+    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < p.C) {
+      char* row = p.turned() + c * row_bytes(p.R, fmt1);
+      put4(row, r, fmt1, v);
+      if (r0 + 32 >= p.R && r + 32 < pad64(p.R)) put4(row, r + 32, fmt1, none);
+    }
+    if (Prod::SYM && ti == tj) return;  // uniform over the workgroup
+    float* turn = sums + SMALL_WAVES * 16 * 64;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) turn[(8 * wave + 4 * h + t) * TURN + (lane & 31)] = v[t];
+    __syncthreads();
+    const int row = tid >> 3, k = 4 * (tid & 7);
+    float w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) w[t] = turn[row * TURN + k + t];
+    if (r0 + row < p.R) {
+      char* to = p.straight() + (r0 + row) * row_bytes(p.C, fmt2);
+      put4(to, c0 + k, fmt2, w);
+      if (c0 + 32 >= p.C && c0 + k + 32 < pad64(p.C)) put4(to, c0 + k + 32, fmt2, none);
+    }
+  }
 #endif
 }
 
@@ -463,18 +707,25 @@ int tiles_of(const OrthMat& u, int kind, int bt) {
   const int tm = (mat_m(u) + bt - 1) / bt, tn = (mat_n(u) + bt - 1) / bt;
   return kind == ORTH_GRAM || kind == ORTH_POLY ? tm * (tm + 1) / 2 : tm * tn;
 }
+int blocks_of(const OrthMat& u, int kind, int fmt) {
+  return row_blocks(kind == ORTH_GRAM ? mat_n(u) : mat_m(u), fmt);
+}
 
-// first[] for `work(i)` workgroups per matrix; returns the grid.
+// first[] for `work(i)` workgroups per matrix, matrices in order[]; the grid, or
+// -1 where there is none of that size.
 template <typename Work>
 int layout_grid(OrthArgs* g, Work&& work) {
   int64_t at = 0;
   for (int i = 0; i < g->count; ++i) {
     g->first[i] = static_cast<int>(at);
-    at += (work(i) + 7) / 8 * 8;
+    at += (static_cast<int64_t>(work(g->order[i])) + 7) / 8 * 8;
     if (at > 0x7FFFFFF0) return -1;
   }
   g->first[g->count] = static_cast<int>(at);
   return static_cast<int>(at);
+}
+void matrices_in_order(OrthArgs* g) {
+  for (int i = 0; i < g->count; ++i) g->order[i] = i;
 }
 
 template <class S, int KIND, int F>
@@ -485,17 +736,66 @@ hipError_t launch_product_shape(OrthArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 
+// A product's time in us with tiles of 32, 128 or 256, from what the kernels take
+// on this card (NT_SPLIT; a K block of 32 values):
+//   32    4 us, and 1870 blocks a us over all CUs
+//   128   9 us, and a block 0.75 us while no CU has two tiles, else 1.45 us for
+//         512 at a time
+//   256   20 us, and a block 2.1 us while half of the CUs have a tile, else 2.45 us
+//         for 256 at a time
+// and, with more tiles than fit at once, some of a tile for the CUs that run dry.
+// Whole calls, fp32 (32 / 128 / 256, us): 512: 112 / 352 / 783, 1280: 401 / 602 /
+// 1390, 2048: 1331 / 862 / 1999, 4096: 10214 / 4402 / 4100; three 4096 x 4096 and
+// 1000 x 4096: 31327 / 12011 / 11216.  (Tiles cut along K, their sums joined by
+// the last workgroup to arrive, were slower everywhere but there by 3%: the sums'
+// way through memory and the caches' write-back.)
+int best_tile(const OrthArgs& g, int kind, int fmt) {
+  int best = 0;
+  double best_t = 0.0;
+  for (int bt : {32, 128, 256}) {
+    double tiles = 0.0, blocks = 0.0, longest = 0.0;
+    for (int i = 0; i < g.count; ++i) {
+      const double t = tiles_of(g.mat[i].u, kind, bt), k = blocks_of(g.mat[i].u, kind, fmt);
+      tiles += t;
+      blocks += t * k;
+      longest = std::fmax(longest, k);
+    }
+    double us;
+    if (bt == 32)
+      us = 4.0 + blocks / 1870.0;
+    else if (bt == 128)
+      us = 9.0 + (tiles <= 256.0 ? 0.75 * longest : 1.45 * (blocks / 512.0 + 0.3 * longest));
+    else
+      us = 20.0 + (tiles <= 144.0   ? 2.1 * longest
+                   : tiles <= 256.0 ? 2.45 * longest
+                                    : 2.45 * (blocks / 256.0 + 0.3 * longest));
+    if (best == 0 || us < best_t) {
+      best = bt;
+      best_t = us;
+    }
+  }
+  return best;
+}
+
 template <int KIND, int F>
 hipError_t launch_product(OrthArgs& g, hipStream_t s) {
-  int64_t big = 0, mid = 0;
-  for (int i = 0; i < g.count; ++i) {
-    big += tiles_of(g.mat[i].u, KIND, OrthL::BM);
-    mid += tiles_of(g.mat[i].u, KIND, OrthM::BM);
-  }
-  // the largest tile that still gives most of the 256 CUs a workgroup
-  if (big >= 192) return launch_product_shape<OrthL, KIND, F>(g, s);
-  if (mid >= 192) return launch_product_shape<OrthM, KIND, F>(g, s);
-  return launch_product_shape<OrthS, KIND, F>(g, s);
+  constexpr int PF = F == NT_SPLIT_B0 ? static_cast<int>(NT_SPLIT) : F;
+  // longest K first: the short tiles fill the gaps at the end
+  matrices_in_order(&g);
+  for (int i = 1; i < g.count; ++i)
+    for (int j = i; j > 0 && blocks_of(g.mat[g.order[j]].u, KIND, PF) >
+                                 blocks_of(g.mat[g.order[j - 1]].u, KIND, PF); --j) {
+      const int t = g.order[j];
+      g.order[j] = g.order[j - 1];
+      g.order[j - 1] = t;
+    }
+  const int tile = best_tile(g, KIND, PF);
+  if (tile == 256) return launch_product_shape<OrthL, KIND, F>(g, s);
+  if (tile == 128) return launch_product_shape<OrthM, KIND, F>(g, s);
+  const int grid = layout_grid(&g, [&](int i) { return tiles_of(g.mat[i].u, KIND, 32); });
+  if (grid < 0) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((orth_small_kernel<KIND, F>), dim3(grid), dim3(64 * SMALL_WAVES), 0, s, g);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -548,6 +848,7 @@ hipError_t launch_orthogonalize(const OrthMat* mats, int count, bool bf16, const
   }
   auto fmt = [&](int t) { return plain[t] ? static_cast<int>(NT_F16) : static_cast<int>(NT_SPLIT); };
   hipError_t e = hipSuccess;
+  matrices_in_order(&g);
   if (!norms_done) {
     const int grid = layout_grid(&g, [&](int i) {
       return norm_parts(static_cast<int64_t>(mats[i].rows) * mats[i].cols);
