@@ -11,6 +11,7 @@ Build with ``python paper_2102_08550_amd/build.py`` (or
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import math
@@ -74,6 +75,7 @@ class _Shards(ctypes.Structure):
 
 
 _LIB = None
+_SAME_DEVICE = contextlib.nullcontext()
 
 # name -> (restype, argtypes)
 _SIGS = {
@@ -166,8 +168,13 @@ def _arr(a, dtype):
 
 def _stream_handle(stream=None) -> Optional[int]:
     import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    # the handle alone where torch gives it (0.5 us, by way of a Stream object 4)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is not None:
+        return raw(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _dev_ptr(t, dtype=None, what="tensor") -> int:
@@ -285,6 +292,12 @@ def broadcast(global_, replicas, K: int, n: int, ld: int, stream=None):
            "oscars_broadcast")
 
 
+def _on_device(device):
+    """The context in which a call's kernels go to ``device``."""
+    import torch
+    return _SAME_DEVICE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
 def _workspace(nbytes: int, device, stream=None):
     """Device memory for one call on ``stream`` (None: the current one): torch's
     allocator gives it to later work of that stream only."""
@@ -360,7 +373,7 @@ def orthogonalize(x, out=None, coeffs=NEWTON_SCHULZ, stream=None):
         m.rows, m.cols, m.x, m.x_ld, m.out, m.out_ld = (v[0], v[1], t.data_ptr(), v[2],
                                                         o.data_ptr(), ov[2])
     ca, steps = _coeffs(tuple(map(tuple, coeffs)))
-    with torch.cuda.device(dev):
+    with _on_device(dev):
         need = _lib().oscars_orthogonalize_workspace(mats, len(xs))
         ws = _workspace(need, dev, stream)
         _check(_lib().oscars_orthogonalize(mats, len(xs), FP32 if dt == torch.float32 else BF16,
@@ -385,11 +398,12 @@ def _rows(t, dtype, device, what):
         raise TypeError(f"{what} must be a tensor on the input's CUDA (HIP) device")
     if t.dtype != dtype:
         raise TypeError(f"{what} must have dtype {dtype}, got {t.dtype}")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (
-            t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or (shape[1] > 1 and strides[1] != 1) or (
+            shape[0] > 1 and strides[0] < shape[1]):
         raise ValueError(f"{what} must be a matrix stored by rows that do not overlap")
-    n, c = t.shape
-    return t.data_ptr(), n, max(t.stride(0), c), c
+    n, c = shape
+    return t.data_ptr(), n, max(strides[0], c), c
 
 
 def _vector(t, n, device, what):
@@ -429,7 +443,7 @@ def quantize_rows(x, out=None, stream=None):
         raise ValueError("q must have a row per row of x, as long or longer")
     if n == 0:
         return out
-    with torch.cuda.device(dev):
+    with _on_device(dev):
         _check(_lib().oscars_quantize_rows(qp, qld, _vector(scale, n, dev, "scale"), xp, ld, dt, n,
                                            cols, _stream_handle(stream)), "oscars_quantize_rows")
     return out
@@ -455,7 +469,7 @@ def matmul_i8(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool = 
         raise ValueError("out must be [rows][outputs]")
     if n == 0:
         return out
-    with torch.cuda.device(dev):
+    with _on_device(dev):
         _check(_lib().oscars_matmul_i8(op, old, _float_type(out.dtype, "out"), xp, xld,
                                        _vector(xscale, n, dev, "xscale"), wp, wld,
                                        _vector(wscale, outs, dev, "wscale"),
@@ -489,7 +503,7 @@ def linear_i8(x, wq, wscale, bias=None, relu: bool = False, out_dtype=None, out=
     lib = _lib()
     need = lib.oscars_linear_i8_workspace(n, cols)
     ws = _workspace(need, dev, stream) if need else None
-    with torch.cuda.device(dev):
+    with _on_device(dev):
         _check(lib.oscars_linear_i8(op, old, _float_type(out.dtype, "out"), xp, xld, dt, wp, wld,
                                     _vector(wscale, outs, dev, "wscale"),
                                     _vector(bias, outs, dev, "bias"), int(bool(relu)), n, cols,

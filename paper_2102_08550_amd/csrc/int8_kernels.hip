@@ -11,6 +11,8 @@
 //                   quantisation in front of it in every workgroup.
 #include "int8.h"
 
+#include <cmath>
+
 #include "nt_mma.h"
 
 namespace oscars {
@@ -202,7 +204,6 @@ bool aligned_rows(const void* p, int64_t row_bytes, int to) {
 
 typedef NtShape<256, 256, 2, 4, 2> I8L;
 typedef NtShape<128, 128, 2, 2, 2> I8M;
-typedef NtShape<64, 64, 2, 2, 3> I8S;
 
 __device__ __forceinline__ float i8_finish(int32_t acc, float sx, float sw, float b, bool relu) {
   float y = static_cast<float>(acc) * (sx * sw) + b;
@@ -210,14 +211,49 @@ __device__ __forceinline__ float i8_finish(int32_t acc, float sx, float sw, floa
   return y;
 }
 
+// N channels from o on of an output row.
+template <int N, bool OUT_BF16, bool VEC>
+__device__ __forceinline__ void store_outs(const MatmulI8Args& a, int64_t row, int o,
+                                           const float* v) {
+  if constexpr (OUT_BF16) {
+    uint16_t* p = static_cast<uint16_t*>(a.out) + row * a.out_ld + o;
+    if (VEC && o + N <= a.outs) {
+      uint32_t w[N / 2];
+#pragma unroll
+      for (int e = 0; e < N / 2; ++e)
+        w[e] = i8_to_bf16(v[2 * e]) | static_cast<uint32_t>(i8_to_bf16(v[2 * e + 1])) << 16;
+      if constexpr (N == 8)
+        *reinterpret_cast<nt_u32x4*>(p) = nt_u32x4{w[0], w[1], w[2], w[3]};
+      else
+        *reinterpret_cast<nt_u32x2*>(p) = nt_u32x2{w[0], w[1]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (o + e < a.outs) p[e] = i8_to_bf16(v[e]);
+    }
+  } else {
+    float* p = static_cast<float*>(a.out) + row * a.out_ld + o;
+    if (VEC && o + N <= a.outs) {
+#pragma unroll
+      for (int e = 0; e < N; e += 4)
+        *reinterpret_cast<nt_f32x4*>(p + e) = nt_f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (o + e < a.outs) p[e] = v[e];
+    }
+  }
+}
+
 // Output rows are input rows; the tile's own rows (R) are output channels, four
-// consecutive ones a lane.  A block of 32 x 32 goes through LDS so that a row's
-// 32 outputs are stored together.  VEC: 16-byte stores.
+// consecutive ones a lane.  Two blocks of 32 channels go through LDS so that
+// neighbouring lanes store whole 128-byte lines of an output row.  VEC: 16-byte
+// stores.
 template <class S, bool OUT_BF16, bool VEC>
 __global__ __launch_bounds__(S::NT, 2) void matmul_i8_kernel(MatmulI8Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
-  constexpr int TURN = 36;
-  static_assert(S::LDS_BYTES >= S::WM * S::WN * 32 * TURN * 4, "room to turn blocks");
+  constexpr int TURN = 68;  // 64 channels of a row
+  static_assert(S::LDS_BYTES >= S::WM * S::WN * 32 * TURN * 4 && S::MI % 2 == 0, "turned blocks");
   __shared__ __attribute__((aligned(16))) char lds[S::LDS_BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
   const int tr = (a.outs + S::BM - 1) / S::BM;
@@ -255,92 +291,145 @@ __global__ __launch_bounds__(S::NT, 2) void matmul_i8_kernel(MatmulI8Args a) {
 
   const int rw = r0 + (wave / S::WN) * 32 * S::MI;
   const int64_t cw = c0 + (wave % S::WN) * 32 * S::NJ;
-  float* turn = reinterpret_cast<float*>(lds) + wave * 32 * TURN;
+  int* turn = reinterpret_cast<int*>(lds) + wave * 32 * TURN;
+  constexpr int PER = OUT_BF16 ? 8 : 4, LANES = 64 / PER;  // 16 bytes a lane
+  const int k = PER * (lane % LANES);
   nt_barrier();  // the stages are read: LDS is free
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i) {
+#pragma nounroll
+  for (int i = 0; i < S::MI; i += 2) {
+    const int o = rw + 32 * i + k;  // the lane's channels
     if (rw + 32 * i >= a.outs) continue;
-    float sw[16], bias[16];
+    float sw[PER], bias[PER];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int o = rw + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
-      const int oc = o < a.outs ? o : a.outs - 1;
+    for (int e = 0; e < PER; ++e) {
+      const int oc = o + e < a.outs ? o + e : a.outs - 1;
       sw[e] = a.wscale[oc];
       bias[e] = a.bias ? a.bias[oc] : 0.0f;
     }
-#pragma unroll
+#pragma nounroll
     for (int j = 0; j < S::NJ; ++j) {
-      const int64_t c = cw + 32 * j + (lane & 31);
-      if (cw + 32 * j >= a.rows) continue;  // uniform over the wave
-      const float sx = a.xscale[c < a.rows ? c : a.rows - 1];
+      const int64_t row0 = cw + 32 * j;
+      if (row0 >= a.rows) continue;  // uniform over the wave
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        nt_f32x4 t;
+      for (int ii = 0; ii < S::MI; ++ii)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          t[e] = i8_finish(acc[i][j][4 * q + e], sx, sw[4 * q + e], bias[4 * q + e], a.relu);
-        *reinterpret_cast<nt_f32x4*>(turn + (lane & 31) * TURN + 8 * q + 4 * h) = t;
+        for (int jj = 0; jj < S::NJ; ++jj)
+          if ((ii & ~1) == i && jj == j) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<nt_i32x4*>(turn + (lane & 31) * TURN + 32 * (ii & 1) + 8 * q +
+                                           4 * h) =
+                  nt_i32x4{acc[ii][jj][4 * q], acc[ii][jj][4 * q + 1], acc[ii][jj][4 * q + 2],
+                           acc[ii][jj][4 * q + 3]};
+          }
+      __builtin_amdgcn_wave_barrier();
+      for (int r = lane / LANES; r < 32; r += 64 / LANES) {
+        const int64_t row = row0 + r;
+        const float sx = a.xscale[row < a.rows ? row : a.rows - 1];
+        float v[PER];
+#pragma unroll
+        for (int e = 0; e < PER; e += 4) {
+          const nt_i32x4 t = *reinterpret_cast<const nt_i32x4*>(turn + r * TURN + k + e);
+#pragma unroll
+          for (int f = 0; f < 4; ++f)
+            v[e + f] = i8_finish(t[f], sx, sw[e + f], bias[e + f], a.relu);
+        }
+        if (row < a.rows && o < a.outs) store_outs<PER, OUT_BF16, VEC>(a, row, o, v);
       }
       __builtin_amdgcn_wave_barrier();
-      const int64_t row = cw + 32 * j + (lane >> 1);
-      const int k = 16 * (lane & 1), o = rw + 32 * i + k;
-      float v[16];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const nt_f32x4 t =
-            *reinterpret_cast<const nt_f32x4*>(turn + (lane >> 1) * TURN + k + 4 * e);
-#pragma unroll
-        for (int f = 0; f < 4; ++f) v[4 * e + f] = t[f];
-      }
-      __builtin_amdgcn_wave_barrier();
-      if (row >= a.rows || o >= a.outs) continue;
-      const int n = a.outs - o < 16 ? a.outs - o : 16;
-      if constexpr (OUT_BF16) {
-        uint16_t* p = static_cast<uint16_t*>(a.out) + row * a.out_ld + o;
-        if (VEC && n == 16) {
-          nt_u32x4 w[2];
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            w[e >> 2][e & 3] = i8_to_bf16(v[2 * e]) |
-                               static_cast<uint32_t>(i8_to_bf16(v[2 * e + 1])) << 16;
-          reinterpret_cast<nt_u32x4*>(p)[0] = w[0];
-          reinterpret_cast<nt_u32x4*>(p)[1] = w[1];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (e < n) p[e] = i8_to_bf16(v[e]);
-        }
-      } else {
-        float* p = static_cast<float*>(a.out) + row * a.out_ld + o;
-        if (VEC && n == 16) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            reinterpret_cast<nt_f32x4*>(p)[e] =
-                nt_f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (e < n) p[e] = v[e];
-        }
-      }
     }
   }
 #endif
 }
 
-template <class S>
-hipError_t matmul_launch(const MatmulI8Args& a, hipStream_t s) {
-  const int64_t tiles = ((a.outs + S::BM - 1) / S::BM) * ((a.rows + S::BN - 1) / S::BN);
+// Few tiles: 32 x 32 outputs a workgroup, K dealt to its four waves block by block.
+// A wave streams its blocks through LDS of its own (RING of them), into registers,
+// and waits for no other wave until the four sums meet.
+constexpr int I8_SMALL_RING = 2;
+
+template <bool OUT_BF16, bool VEC>
+__global__ __launch_bounds__(256) void matmul_i8_small_kernel(MatmulI8Args a) {
+#if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
+  constexpr int STAGE = 64 * NT_BLOCK, RING = I8_SMALL_RING;
+  __shared__ __attribute__((aligned(16))) char lds[4 * RING * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // scalar addresses below
+  const int tr = (a.outs + 31) / 32;
+  const int r0 = static_cast<int>(blockIdx.x % tr) * 32;
+  const int64_t c0 = static_cast<int64_t>(blockIdx.x / tr) * 32;
+  const int blocks = (a.in + NT_BLOCK - 1) / NT_BLOCK;
+  NtRows<64, 32> ra, rb;
+  // as in matmul_i8_kernel
+  ra.init(a.wq, a.w_ld, (a.outs - 1) * a.w_ld + (a.in + 15) / 16 * 16, r0, a.outs, lane);
+  const int64_t left = a.rows - c0;
+  rb.init(a.xq + c0 * a.x_ld, a.x_ld, left * a.x_ld, 0, static_cast<int>(left < 32 ? left : 32),
+          lane);
+  char* ring = lds + wave * RING * STAGE;
+  auto issue = [&](int i) {  // the wave's block i
+    const int k = wave + 4 * i;
+    char* t = ring + (i % RING) * STAGE;
+    const int at = (k < blocks ? k : blocks - 1) * NT_BLOCK;
+    ra.issue(t, at, lane);
+    rb.issue(t + STAGE / 2, at, lane);
+  };
+  nt_i32x16 acc;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0;
+  constexpr int PER = NtRows<64, 32>::P * 2;
+  for (int i = 0; i < RING; ++i) issue(i);
+  for (int i = 0; wave + 4 * i < blocks; ++i) {
+    nt_wait_vm<(RING - 1) * PER>();
+    const char* ta = ring + (i % RING) * STAGE;
+    const char* tb = ta + STAGE / 2;
+    nt_u32x4 fa[4], fb[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      fa[c] = nt_read(ta, lane & 31, 2 * c + h);
+      fb[c] = nt_read(tb, lane & 31, 2 * c + h);
+    }
+    // the stage is in registers: refill it
+    __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    issue(i + RING);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc = nt_mfma<NT_I8>(fa[c], fb[c], acc);
+  }
+  nt_wait_vm<0>();
+  __syncthreads();  // every wave is through with LDS: now the four sums
+  int* sums = reinterpret_cast<int*>(lds);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) sums[(wave * 16 + e) * 64 + lane] = acc[e];
+  __syncthreads();
+  // wave w finishes channels 8 w + 4 h .. + 3 of row (lane & 31)
+  const int o = r0 + 8 * wave + 4 * h;
+  const int64_t row = c0 + (lane & 31);
+  if (row >= a.rows || o >= a.outs) return;
+  const float sx = a.xscale[row];
+  float v[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    int s = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s += sums[(w * 16 + 4 * wave + t) * 64 + lane];
+    const int oc = o + t < a.outs ? o + t : a.outs - 1;
+    v[t] = i8_finish(s, sx, a.wscale[oc], a.bias ? a.bias[oc] : 0.0f, a.relu);
+  }
+  store_outs<4, OUT_BF16, VEC>(a, row, o, v);
+#endif
+}
+
+template <bool OUT_BF16, bool VEC>
+hipError_t matmul_launch(const MatmulI8Args& a, int tile, hipStream_t s) {
+  const int64_t tiles =
+      static_cast<int64_t>((a.outs + tile - 1) / tile) * ((a.rows + tile - 1) / tile);
   if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(tiles));
-  const bool vec = aligned_rows(a.out, a.out_ld * (a.out_bf16 ? 2 : 4), 16);
-  if (a.out_bf16) {
-    if (vec) hipLaunchKernelGGL((matmul_i8_kernel<S, true, true>), grid, dim3(S::NT), 0, s, a);
-    else hipLaunchKernelGGL((matmul_i8_kernel<S, true, false>), grid, dim3(S::NT), 0, s, a);
-  } else {
-    if (vec) hipLaunchKernelGGL((matmul_i8_kernel<S, false, true>), grid, dim3(S::NT), 0, s, a);
-    else hipLaunchKernelGGL((matmul_i8_kernel<S, false, false>), grid, dim3(S::NT), 0, s, a);
-  }
+  if (tile == I8L::BM)
+    hipLaunchKernelGGL((matmul_i8_kernel<I8L, OUT_BF16, VEC>), grid, dim3(I8L::NT), 0, s, a);
+  else if (tile == I8M::BM)
+    hipLaunchKernelGGL((matmul_i8_kernel<I8M, OUT_BF16, VEC>), grid, dim3(I8M::NT), 0, s, a);
+  else
+    hipLaunchKernelGGL((matmul_i8_small_kernel<OUT_BF16, VEC>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -348,15 +437,19 @@ hipError_t matmul_launch(const MatmulI8Args& a, hipStream_t s) {
 
 // Up to 16 rows.  A workgroup takes 16 output channels, its eight waves K slices
 // of 64 in turn (16x16x64: lane l has channel or row l & 15, bytes 16 (l >> 4)).
-// The weights' loads are in flight before anything else; meanwhile every
-// workgroup quantises all rows into LDS for itself (they come from the L2).
+// While the weights are on their way every workgroup quantises all rows into LDS
+// for itself (they come from the L2).
 // The eight partial sums meet in LDS: integers, in any order the same.
 constexpr int FEW_ROWS = 16;
 constexpr int FEW_WAVES = 8;
 constexpr int FEW_AHEAD = 8;           // K slices of a wave loaded ahead
-// Bytes of quantised rows: the smaller one where it holds them, so that more than
-// one workgroup fits a CU.
-constexpr int FEW_LDS_S = 32 << 10, FEW_LDS_L = 136 << 10;
+// Every workgroup quantises all rows: up to so many entries that is less than a
+// launch of its own takes (4 x 4096 x 4096: 11.4 us, in two launches 12; 16 x
+// 4096: 24.7 and 12).  One row is taken at any length.
+constexpr int FEW_ENTRIES = 16384;
+// Bytes of quantised rows: the smaller one where it holds them, so that more
+// workgroups fit a CU.
+constexpr int FEW_LDS_S = 18 << 10, FEW_LDS_L = 65 << 10;
 
 __host__ __device__ __forceinline__ int few_row_bytes(int in) {
   return (in + 63) / 64 * 64 + 16;  // 16 more: consecutive rows start in other banks
@@ -368,6 +461,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void linear_i8_few_kernel(MatmulI8A
   __shared__ __attribute__((aligned(16))) char few_lds[LDS];  // quantised rows
   __shared__ int part[FEW_WAVES][64][4];
   __shared__ float scales[FEW_ROWS];
+  __shared__ uint32_t tops[2 * FEW_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rows = static_cast<int>(a.rows), in = a.in, ld = few_row_bytes(in);
   const int slices = (in + 63) / 64;
@@ -379,33 +473,53 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void linear_i8_few_kernel(MatmulI8A
     // past the row's end: its first bytes, against zeros of the quantised rows
     return *reinterpret_cast<const nt_i32x4*>(w + (k < end ? k : 0));
   };
+  // All threads on the rows: 512 / R of them a row, R the power of two that holds
+  // the rows (one row: all 512).  Loads come back in order, so the rows' first
+  // ones go out in front of the weights'.
+  int shift = 9;
+  while (shift > 5 && (512 >> shift) < rows) --shift;
+  const int per = 1 << shift, r = tid >> shift, at = tid & (per - 1);
+  const char* row = static_cast<const char*>(x) + (r < rows ? r : 0) * x_ld * (X_BF16 ? 2 : 4);
+  const bool once = in <= 8 * per;  // the row stays in registers
+  float v[8] = {};
+  uint32_t top = 0;
+  if (once) {
+    load8<X_BF16, VEC>(row, 8 * at, in, v);
+  } else {
+    for (int c = 8 * at; c < in; c += 8 * per) {
+      load8<X_BF16, VEC>(row, c, in, v);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) top = max(top, abs_bits(v[t]));
+    }
+  }
   nt_i32x4 ahead[FEW_AHEAD];
 #pragma unroll
   for (int i = 0; i < FEW_AHEAD; ++i) {
     const int sl = wave + FEW_WAVES * i;
     ahead[i] = load_w(sl < slices ? sl : 0);
   }
-  // rows wave, wave + 8: a wave quantises a row
-  for (int r = wave; r < rows; r += FEW_WAVES) {
-    const char* row = static_cast<const char*>(x) + r * x_ld * (X_BF16 ? 2 : 4);
-    uint32_t top = 0;
-    float v[8];
-    for (int c = 8 * lane; c < in; c += 512) {
-      load8<X_BF16, VEC>(row, c, in, v);
+  if (once) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t) top = max(top, abs_bits(v[t]));
-    }
-    const float scale = row_scale(wave_max(top));
-    const Divisor d = divisor(scale);
-    const bool drop = !(scale > 0.0f);
-    if (lane == 0) scales[r] = scale;
-    for (int c = 8 * lane; c < slices * 64; c += 512) {
-      load8<X_BF16, VEC>(row, c, in, v);
+    for (int t = 0; t < 8; ++t) top = max(top, abs_bits(v[t]));
+  }
+  for (int d = 1; d < (per < 64 ? per : 64); d *= 2) {
+    const uint32_t o = __shfl_xor(top, d);
+    top = o > top ? o : top;
+  }
+  if ((lane & 31) == 0) tops[tid >> 5] = top;  // by halves of a wave
+  __syncthreads();
+  for (int h = (r << shift) >> 5; h < ((r + 1) << shift) >> 5; ++h) top = max(top, tops[h]);
+  const float scale = row_scale(top);
+  const Divisor d = divisor(scale);
+  const bool drop = !(scale > 0.0f);
+  if (at == 0) scales[r] = scale;
+  if (r < rows)
+    for (int c = 8 * at; c < slices * 64; c += 8 * per) {
+      if (!once) load8<X_BF16, VEC>(row, c, in, v);
       drop_if(drop, v);
       *reinterpret_cast<nt_u32x2*>(few_lds + r * ld + c) =
           nt_u32x2{quant4(v, d.s, d.inv), quant4(v + 4, d.s, d.inv)};
     }
-  }
   __syncthreads();
   nt_i32x4 acc = {0, 0, 0, 0};
   // lanes of rows that are not there read the last one; their sums are not used
@@ -430,11 +544,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void linear_i8_few_kernel(MatmulI8A
     int sum = 0;
 #pragma unroll
     for (int i = 0; i < FEW_WAVES; ++i) sum += part[i][l][e];
-    const int r = l & 15, o = blockIdx.x * 16 + 4 * (l >> 4) + e;
-    if (r < rows && o < a.outs) {
-      const float y = i8_finish(sum, scales[r], a.wscale[o], a.bias ? a.bias[o] : 0.0f, a.relu);
-      if constexpr (OUT_BF16) static_cast<uint16_t*>(a.out)[r * a.out_ld + o] = i8_to_bf16(y);
-      else static_cast<float*>(a.out)[r * a.out_ld + o] = y;
+    const int q = l & 15, o = blockIdx.x * 16 + 4 * (l >> 4) + e;
+    if (q < rows && o < a.outs) {
+      const float y = i8_finish(sum, scales[q], a.wscale[o], a.bias ? a.bias[o] : 0.0f, a.relu);
+      if constexpr (OUT_BF16) static_cast<uint16_t*>(a.out)[q * a.out_ld + o] = i8_to_bf16(y);
+      else static_cast<float*>(a.out)[q * a.out_ld + o] = y;
     }
   }
 }
@@ -464,16 +578,47 @@ hipError_t launch_quantize_rows(const QuantArgs& a, hipStream_t s) {
   return vec ? quantize_launch<false, true>(a, s) : quantize_launch<false, false>(a, s);
 }
 
+// The tile with the least time by what the kernels take on this card, in us (a K
+// block: 128 inputs):
+//   32    3.5, and 2100 blocks a us over all CUs
+//   128   8, and a block 0.55 while no CU has two tiles, else 1.2 for 512 at a time
+//   256   12, and a block 1.5 while half of the CUs have a tile, 1.95 up to all
+//         of them, else 2.05 for 256 at a time
+// Rows x inputs x outputs, measured with 32 / 128 / 256: 256 x 4096 x 1000: 7.0 /
+// 24.4 / 53, 1024 x 2048 x 2048: 19.9 / 17.9 / 34.5, 10000 x 2048 x 2048: 155 / 65 /
+// 76, 4096 x 4096 x 4096: 235 / 86 / 74.
+int i8_best_tile(const MatmulI8Args& a) {
+  const double k = (a.in + NT_BLOCK - 1) / NT_BLOCK;
+  int best = 0;
+  double best_us = 0.0;
+  for (int t : {32, 128, 256}) {
+    const double n =
+        static_cast<double>((a.outs + t - 1) / t) * static_cast<double>((a.rows + t - 1) / t);
+    const double us = t == 32    ? 3.5 + n * k / 2100.0
+                      : t == 128 ? 8.0 + k * (n <= 256.0 ? 0.55 : 1.2 * std::ceil(n / 512.0))
+                                 : 12.0 + k * (n <= 144.0   ? 1.5
+                                               : n <= 256.0 ? 1.95
+                                                            : 2.05 * std::ceil(n / 256.0));
+    if (best == 0 || us < best_us) {
+      best = t;
+      best_us = us;
+    }
+  }
+  return best;
+}
+
 hipError_t launch_matmul_i8(const MatmulI8Args& a, hipStream_t s) {
-  auto tiles = [&](int t) { return ((a.outs + t - 1) / t) * ((a.rows + t - 1) / t); };
-  // the largest tile that still gives most of the 256 CUs a workgroup
-  if (tiles(I8L::BM) >= 192) return matmul_launch<I8L>(a, s);
-  if (tiles(I8M::BM) >= 192) return matmul_launch<I8M>(a, s);
-  return matmul_launch<I8S>(a, s);
+  const int tile = i8_best_tile(a);
+  const bool vec = aligned_rows(a.out, a.out_ld * (a.out_bf16 ? 2 : 4), 16);
+  if (a.out_bf16)
+    return vec ? matmul_launch<true, true>(a, tile, s) : matmul_launch<true, false>(a, tile, s);
+  return vec ? matmul_launch<false, true>(a, tile, s) : matmul_launch<false, false>(a, tile, s);
 }
 
 bool linear_i8_one_launch(int64_t rows, int in) {
-  return rows <= FEW_ROWS && rows * few_row_bytes(in) <= FEW_LDS_L;
+  static_assert(FEW_LDS_S >= FEW_ENTRIES + FEW_ROWS * (63 + 16) && FEW_LDS_L >= 65536 + 63 + 16,
+                "room for the rows");
+  return rows == 1 || (rows <= FEW_ROWS && rows * in <= FEW_ENTRIES);
 }
 
 hipError_t launch_linear_i8_few(const MatmulI8Args& a, const void* x, int64_t x_ld, bool x_bf16,

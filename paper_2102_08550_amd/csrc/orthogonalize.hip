@@ -227,9 +227,9 @@ __device__ __forceinline__ double block_sum(double v, double* lds4) {
   return (lds4[0] + lds4[1]) + (lds4[2] + lds4[3]);
 }
 
-// Workgroups (= partial sums) that a matrix's sum of squares takes.
+// Workgroups (= partial sums) that a matrix's sum of squares takes: runs of 1024.
 __host__ __device__ __forceinline__ int norm_parts(int64_t size) {
-  const int64_t p = (size + 4095) / 4096;
+  const int64_t p = (size + 1023) / 1024;
   return static_cast<int>(p < kNormParts ? p : kNormParts);
 }
 
@@ -238,9 +238,36 @@ __device__ __forceinline__ float load_elem(const void* p, int64_t i) {
   if constexpr (BF16) return bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
   else return static_cast<const float*>(p)[i];
 }
+// Four elements from i; zeros from `end` on.  vec: i a multiple of 4 behind an
+// address of whole vectors.
+template <bool BF16>
+__device__ __forceinline__ void load4(const void* p, int64_t i, int64_t end, bool vec, float* v) {
+  if (vec && i + 4 <= end) {
+    if constexpr (BF16) {
+      const nt_u32x2 w = *reinterpret_cast<const nt_u32x2*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        v[2 * t] = bf16_to_f32(static_cast<uint16_t>(w[t]));
+        v[2 * t + 1] = bf16_to_f32(static_cast<uint16_t>(w[t] >> 16));
+      }
+    } else {
+      const nt_f32x4 w = *reinterpret_cast<const nt_f32x4*>(static_cast<const float*>(p) + i);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[t] = w[t];
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = i + t < end ? load_elem<BF16>(p, i + t) : 0.0f;
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ bool whole_vectors(const OrthMat& u) {
+  return ((reinterpret_cast<uintptr_t>(u.src) | static_cast<uintptr_t>(u.src_ld * (BF16 ? 2 : 4))) &
+          (BF16 ? 7 : 15)) == 0;
+}
 
 // Partial sums of squares: workgroup p of a matrix takes its rows p, p + parts, ...
-// (of a contiguous matrix, chunks of 1024 elements).
+// (of a contiguous matrix, runs of 1024 elements, four at a time).
 template <bool BF16>
 __global__ __launch_bounds__(256) void orth_norm_kernel(OrthArgs g) {
   __shared__ double lds4[4];
@@ -249,22 +276,27 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(OrthArgs g) {
   const int64_t size = static_cast<int64_t>(u.rows) * u.cols;
   const int parts = norm_parts(size);
   if (local >= parts) return;
+  const bool vec = whole_vectors<BF16>(u);
   double acc = 0.0;
   if (u.src_ld == u.cols) {
-    for (int64_t base = static_cast<int64_t>(local) * 1024; base < size;
-         base += static_cast<int64_t>(parts) * 1024) {
+    const int64_t step = static_cast<int64_t>(parts) * 1024;
+    for (int64_t base = static_cast<int64_t>(local) * 1024; base < size; base += 4 * step) {
+      float v[4][4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int64_t e = base + t * 256 + threadIdx.x;
-        const double v = e < size ? load_elem<BF16>(u.src, e) : 0.0f;
-        acc += v * v;
-      }
+      for (int t = 0; t < 4; ++t)
+        load4<BF16>(u.src, base + t * step + threadIdx.x * 4, size, vec, v[t]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc += static_cast<double>(v[t][e]) * v[t][e];
     }
   } else {
     for (int r = local; r < u.rows; r += parts)
-      for (int c = threadIdx.x; c < u.cols; c += 256) {
-        const double v = load_elem<BF16>(u.src, r * u.src_ld + c);
-        acc += v * v;
+      for (int c = 4 * threadIdx.x; c < u.cols; c += 1024) {
+        float v[4];
+        load4<BF16>(u.src, r * u.src_ld + c, r * u.src_ld + u.cols, vec, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc += static_cast<double>(v[e]) * v[e];
       }
   }
   acc = block_sum(acc, lds4);
@@ -281,6 +313,16 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(OrthArgs g) {
   const OrthMat& u = g.mat[i].u;
   const int gc = (u.cols + 63) / 64;
   if (local >= gc * ((u.rows + 63) / 64)) return;
+  // the tile's loads are on their way while the norm is added up
+  const int r0 = (local / gc) * 64, c0 = (local % gc) * 64;
+  const bool vec = whole_vectors<BF16>(u);
+  float v[4][4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int r = r0 + 16 * t + (threadIdx.x >> 4), c = c0 + 4 * (threadIdx.x & 15);
+    const int64_t row = (r < u.rows ? r : u.rows - 1) * u.src_ld;
+    load4<BF16>(u.src, row + c, r < u.rows ? row + u.cols : row, vec, v[t]);
+  }
   const int64_t size = static_cast<int64_t>(u.rows) * u.cols;
   const int parts = norm_parts(size);
   const double* part = ws_parts(g.ws, i);
@@ -291,18 +333,15 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(OrthArgs g) {
   int e = 0;
   const double f = frexp(norm, &e);  // norm = f 2^e
   const bool usable = norm > 0.0 && norm <= 1.7976931348623157e308;
-  const double mul = usable ? ldexp(1.0, 14 - e) : 0.0;
   if (local == 0 && threadIdx.x == 0)
     ws_scale(g.ws)[i] = usable ? static_cast<float>(1.0 / (f * 16384.0))
                                : (norm == 0.0 ? 0.0f : __builtin_nanf(""));
-  const int r0 = (local / gc) * 64, c0 = (local % gc) * 64;
-  for (int t = threadIdx.x; t < 4096; t += 256) {
-    const int r = t >> 6, c = t & 63;
-    float v = 0.0f;
-    if (usable && r0 + r < u.rows && c0 + c < u.cols)
-      v = static_cast<float>(load_elem<BF16>(u.src, (r0 + r) * u.src_ld + c0 + c) * mul);
-    tile[r][c] = v;
-  }
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      tile[16 * t + (threadIdx.x >> 4)][4 * (threadIdx.x & 15) + k] =
+          usable ? __builtin_ldexpf(v[t][k], 14 - e) : 0.0f;
   __syncthreads();
   const bool tall = mat_tall(u);
   const Planes q = mat_planes(g.ws, g.mat[i]);
@@ -582,20 +621,23 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
 }
 
 // Small products, where a launch's latency is all there is: 32 x 32 results a
-// workgroup, K dealt to its four waves block by block.  A wave streams its blocks
-// through LDS of its own, all of them in flight at once up to RING, and waits for
-// no other wave until the four sums meet.  The small planes' products have
-// accumulators of their own and lo lo is kept (see NtShape::EXACT).
-constexpr int SMALL_RING = 2;
+// workgroup, K dealt to its waves block by block.  A wave streams its blocks
+// through LDS of its own (RING of them), into registers, and waits for no other
+// wave until the sums meet.  The small planes' products have accumulators of
+// their own and lo lo is kept (see NtShape::EXACT).
+//   RING 2 (64 KB): up to two workgroups a CU, all there at once;
+//   RING 1 (32 KB): more of them, five a CU cover for each other.
+// (Calls of 17 launches: 512 x 512 106 us with RING 2, 113 with 1; 16 of 256 x 256
+// 183 and 161.  Eight waves, K in eight: 8 us more a call at 64 x 64, 14 less
+// at 256 x 8192.)
 constexpr int SMALL_WAVES = 4;
-
-template <int KIND, int F>
+template <int KIND, int F, int RING>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
   constexpr int STAGE = 64 * NT_BLOCK, TURN = 33;
   constexpr int PF = F == NT_SPLIT_B0 ? static_cast<int>(NT_SPLIT) : F;
   typedef Product<KIND> Prod;
-  __shared__ __attribute__((aligned(16))) char lds[SMALL_WAVES * SMALL_RING * STAGE];
+  __shared__ __attribute__((aligned(16))) char lds[SMALL_WAVES * RING * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // scalar addresses below
   const int pos = find_position(g.first, g.count, blockIdx.x);
@@ -610,10 +652,10 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
   NtRows<64, 32> ra, rb;
   ra.init(p.left, ld, ld * p.R, r0, p.R, lane);
   rb.init(p.right, ld, ld * p.C, c0, p.C, lane);
-  char* ring = lds + wave * SMALL_RING * STAGE;
+  char* ring = lds + wave * RING * STAGE;
   auto issue = [&](int i) {  // the wave's block i
     const int k = wave + SMALL_WAVES * i;
-    char* t = ring + (i % SMALL_RING) * STAGE;
+    char* t = ring + (i % RING) * STAGE;
     const int at = (k < blocks ? k : blocks - 1) * NT_BLOCK;
     ra.issue(t, at, lane);
     rb.issue(t + STAGE / 2, at, lane);
@@ -622,10 +664,10 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = cross[e] = 0.0f;
   constexpr int PER = NtRows<64, 32>::P * 2;
-  for (int i = 0; i < SMALL_RING; ++i) issue(i);
+  for (int i = 0; i < RING; ++i) issue(i);
   for (int i = 0; wave + SMALL_WAVES * i < blocks; ++i) {
-    nt_wait_vm<(SMALL_RING - 1) * PER>();
-    const char* ta = ring + (i % SMALL_RING) * STAGE;
+    nt_wait_vm<(RING - 1) * PER>();
+    const char* ta = ring + (i % RING) * STAGE;
     const char* tb = ta + STAGE / 2;
     nt_u32x4 fa[4], fb[4];
     const int row = lane & 31;
@@ -637,7 +679,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
     // the stage is in registers: refill it
     __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
     asm volatile("" ::: "memory");
-    issue(i + SMALL_RING);
+    issue(i + RING);
     if constexpr (PF == NT_SPLIT) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -728,6 +770,8 @@ void matrices_in_order(OrthArgs* g) {
   for (int i = 0; i < g->count; ++i) g->order[i] = i;
 }
 
+constexpr int kCus = 256;
+
 template <class S, int KIND, int F>
 hipError_t launch_product_shape(OrthArgs& g, hipStream_t s) {
   const int grid = layout_grid(&g, [&](int i) { return tiles_of(g.mat[i].u, KIND, S::BM); });
@@ -794,7 +838,11 @@ hipError_t launch_product(OrthArgs& g, hipStream_t s) {
   if (tile == 128) return launch_product_shape<OrthM, KIND, F>(g, s);
   const int grid = layout_grid(&g, [&](int i) { return tiles_of(g.mat[i].u, KIND, 32); });
   if (grid < 0) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((orth_small_kernel<KIND, F>), dim3(grid), dim3(64 * SMALL_WAVES), 0, s, g);
+  const dim3 wg(64 * SMALL_WAVES);
+  if (grid <= 2 * kCus)
+    hipLaunchKernelGGL((orth_small_kernel<KIND, F, 2>), dim3(grid), wg, 0, s, g);
+  else
+    hipLaunchKernelGGL((orth_small_kernel<KIND, F, 1>), dim3(grid), wg, 0, s, g);
   return hipGetLastError();
 }
 
