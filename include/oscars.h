@@ -419,7 +419,7 @@ oscars_status oscars_server_step(oscars_ctx* ctx, const float* global, const flo
  *   q      device [rows][q_ld] int8, 16-byte aligned, q_ld % 16 == 0, q_ld >= cols;
  *          columns from cols to the next multiple of 128 (or q_ld) are set to 0;
  *   scale  device [rows] fp32.
- * oscars_matmul_i8: the product of quantised rows and weights.
+ * oscars_matmul_quantized: the product of quantised rows and weights.
  *   xq     device [rows][x_ld], 16-byte aligned, x_ld % 16 == 0, zero in the
  *          columns from `in` to the next multiple of 128, which x_ld holds (as
  *          oscars_quantize_rows leaves them);  xscale  device [rows];
@@ -428,42 +428,43 @@ oscars_status oscars_server_step(oscars_ctx* ctx, const float* global, const flo
  *          lies behind a row's `in` columns does not count);  wscale  device [outs];
  *   bias   device [outs] fp32 or NULL;  out  device [rows][out_ld] of out_dtype,
  *          out_ld >= outs, aligned to its elements; 1 <= in, outs <= OSCARS_MAX_WIDTH.
- * oscars_linear_i8: both, x [rows][x_ld] of `dtype` as for oscars_quantize_rows;
+ * oscars_linear_quantized: both, x [rows][x_ld] of `dtype` as for oscars_quantize_rows;
  *   up to 16 rows in one launch.  workspace: device, 16-byte aligned,
- *   oscars_linear_i8_workspace bytes (NULL where those are 0), the call's own
+ *   oscars_linear_quantized_workspace bytes (NULL where those are 0), the call's own
  *   until the stream has run it. */
 oscars_status oscars_quantize_rows(int8_t* q, int64_t q_ld, float* scale, const void* x,
                                    int64_t x_ld, int32_t dtype, int64_t rows, int32_t cols,
                                    void* hip_stream);
-oscars_status oscars_matmul_i8(void* out, int64_t out_ld, int32_t out_dtype, const int8_t* xq,
-                               int64_t x_ld, const float* xscale, const int8_t* wq, int64_t w_ld,
-                               const float* wscale, const float* bias, int32_t relu, int64_t rows,
-                               int32_t in, int32_t outs, void* hip_stream);
-int64_t oscars_linear_i8_workspace(int64_t rows, int32_t in);
-oscars_status oscars_linear_i8(void* out, int64_t out_ld, int32_t out_dtype, const void* x,
-                               int64_t x_ld, int32_t dtype, const int8_t* wq, int64_t w_ld,
-                               const float* wscale, const float* bias, int32_t relu, int64_t rows,
-                               int32_t in, int32_t outs, void* workspace, int64_t workspace_bytes,
-                               void* hip_stream);
+oscars_status oscars_matmul_quantized(void* out, int64_t out_ld, int32_t out_dtype,
+                                      const int8_t* xq, int64_t x_ld, const float* xscale,
+                                      const int8_t* wq, int64_t w_ld, const float* wscale,
+                                      const float* bias, int32_t relu, int64_t rows, int32_t in,
+                                      int32_t outs, void* hip_stream);
+int64_t oscars_linear_quantized_workspace(int64_t rows, int32_t in);
+oscars_status oscars_linear_quantized(void* out, int64_t out_ld, int32_t out_dtype, const void* x,
+                                      int64_t x_ld, int32_t dtype, const int8_t* wq, int64_t w_ld,
+                                      const float* wscale, const float* bias, int32_t relu,
+                                      int64_t rows, int32_t in, int32_t outs, void* workspace,
+                                      int64_t workspace_bytes, void* hip_stream);
 
 /* A fully connected model in 8-bit integers: weights quantised by output
  * channel, activations by sample as they come.  OSCARS_E_INVALID for a
  * convolutional context.
- *   oscars_i8_model_bytes  device bytes of a quantised model (0 for an invalid
+ *   oscars_quantized_model_bytes  device bytes of a quantised model (0 for an invalid
  *          context): per layer wq [out][in rounded up to 128], its scales and
  *          its biases, each from a multiple of 256 bytes on;
  *   oscars_quantize_model  params (flat layout, as oscars_evaluate) -> model,
  *          16-byte aligned, not overlapping params; on the context's stream;
- *   oscars_evaluate_i8     as oscars_evaluate, with every layer's product from
+ *   oscars_evaluate_quantized     as oscars_evaluate, with every layer's product from
  *          the quantised model: hidden activations in the model's dtype, logits
  *          in fp32.  Allocates and frees temporary device buffers and waits for
  *          the stream; not for a stream being captured into a graph
  *          (OSCARS_E_STATE). */
-int64_t oscars_i8_model_bytes(const oscars_ctx* ctx);
+int64_t oscars_quantized_model_bytes(const oscars_ctx* ctx);
 oscars_status oscars_quantize_model(oscars_ctx* ctx, const float* params, void* model);
-oscars_status oscars_evaluate_i8(oscars_ctx* ctx, const void* model, const void* x,
-                                 const int32_t* y, int64_t n_rows, double* loss_sum,
-                                 int64_t* correct);
+oscars_status oscars_evaluate_quantized(oscars_ctx* ctx, const void* model, const void* x,
+                                        const int32_t* y, int64_t n_rows, double* loss_sum,
+                                        int64_t* correct);
 
 /* Resume support: per-worker count of local steps done so far. host [K]. */
 oscars_status oscars_get_cursors(const oscars_ctx* ctx, int64_t* steps_done);

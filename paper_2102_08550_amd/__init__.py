@@ -112,14 +112,14 @@ _SIGS = {
     "oscars_server_step": (_i32, [_vp, _vp, _vp, _P(_f32), _vp, _vp, _vp, _P(_ServerOptions), _vp,
                                   _i64]),
     "oscars_quantize_rows": (_i32, [_vp, _i64, _vp, _vp, _i64, _i32, _i64, _i32, _vp]),
-    "oscars_matmul_i8": (_i32, [_vp, _i64, _i32, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i32, _i64,
-                                _i32, _i32, _vp]),
-    "oscars_linear_i8_workspace": (_i64, [_i64, _i32]),
-    "oscars_linear_i8": (_i32, [_vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _i32, _i64,
-                                _i32, _i32, _vp, _i64, _vp]),
-    "oscars_i8_model_bytes": (_i64, [_vp]),
+    "oscars_matmul_quantized": (_i32, [_vp, _i64, _i32, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i32,
+                                       _i64, _i32, _i32, _vp]),
+    "oscars_linear_quantized_workspace": (_i64, [_i64, _i32]),
+    "oscars_linear_quantized": (_i32, [_vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _i32,
+                                       _i64, _i32, _i32, _vp, _i64, _vp]),
+    "oscars_quantized_model_bytes": (_i64, [_vp]),
     "oscars_quantize_model": (_i32, [_vp, _vp, _vp]),
-    "oscars_evaluate_i8": (_i32, [_vp, _vp, _vp, _vp, _i64, _P(ctypes.c_double), _P(_i64)]),
+    "oscars_evaluate_quantized": (_i32, [_vp, _vp, _vp, _vp, _i64, _P(ctypes.c_double), _P(_i64)]),
     "oscars_status_str": (ctypes.c_char_p, [_i32]),
     "oscars_last_hip_error": (_i32, []),
 }
@@ -295,7 +295,9 @@ def broadcast(global_, replicas, K: int, n: int, ld: int, stream=None):
 def _on_device(device):
     """The context in which a call's kernels go to ``device``."""
     import torch
-    return _SAME_DEVICE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    if torch.cuda.current_device() == device.index:
+        return _SAME_DEVICE
+    return torch.cuda.device(device)
 
 
 def _workspace(nbytes: int, device, stream=None):
@@ -451,7 +453,7 @@ def quantize_rows(x, out=None, stream=None):
 
 def matmul_i8(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool = False,
               out_dtype=None, out=None, stream=None):
-    """xscale wscale (xq wq') + bias (oscars_matmul_i8) for quantised rows ``xq``
+    """xscale wscale (xq wq') + bias (oscars_matmul_quantized) for quantised rows ``xq``
     [rows][..] and weights ``wq`` [outputs][..] as quantize_rows gives them, of
     ``in_features`` columns; fp32 by default.  Returns ``out``."""
     import torch
@@ -470,17 +472,16 @@ def matmul_i8(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool = 
     if n == 0:
         return out
     with _on_device(dev):
-        _check(_lib().oscars_matmul_i8(op, old, _float_type(out.dtype, "out"), xp, xld,
-                                       _vector(xscale, n, dev, "xscale"), wp, wld,
-                                       _vector(wscale, outs, dev, "wscale"),
-                                       _vector(bias, outs, dev, "bias"), int(bool(relu)), n,
-                                       int(in_features), outs, _stream_handle(stream)),
-               "oscars_matmul_i8")
+        _check(_lib().oscars_matmul_quantized(
+            op, old, _float_type(out.dtype, "out"), xp, xld, _vector(xscale, n, dev, "xscale"), wp,
+            wld, _vector(wscale, outs, dev, "wscale"), _vector(bias, outs, dev, "bias"),
+            int(bool(relu)), n, int(in_features), outs, _stream_handle(stream)),
+            "oscars_matmul_quantized")
     return out
 
 
 def linear_i8(x, wq, wscale, bias=None, relu: bool = False, out_dtype=None, out=None, stream=None):
-    """A linear layer in 8 bits (oscars_linear_i8): the rows of ``x`` (fp32 or
+    """A linear layer in 8 bits (oscars_linear_quantized): the rows of ``x`` (fp32 or
     bf16) are quantised with a scale each, ``wq`` [outputs][inputs or more, the
     row stride a multiple of 16] and ``wscale`` are a weight matrix's
     quantize_rows.  The result has ``x``'s type by default.  Returns ``out``."""
@@ -501,14 +502,14 @@ def linear_i8(x, wq, wscale, bias=None, relu: bool = False, out_dtype=None, out=
     if n == 0:
         return out
     lib = _lib()
-    need = lib.oscars_linear_i8_workspace(n, cols)
+    need = lib.oscars_linear_quantized_workspace(n, cols)
     ws = _workspace(need, dev, stream) if need else None
     with _on_device(dev):
-        _check(lib.oscars_linear_i8(op, old, _float_type(out.dtype, "out"), xp, xld, dt, wp, wld,
-                                    _vector(wscale, outs, dev, "wscale"),
-                                    _vector(bias, outs, dev, "bias"), int(bool(relu)), n, cols,
-                                    outs, ws.data_ptr() if need else None, need,
-                                    _stream_handle(stream)), "oscars_linear_i8")
+        _check(lib.oscars_linear_quantized(
+            op, old, _float_type(out.dtype, "out"), xp, xld, dt, wp, wld,
+            _vector(wscale, outs, dev, "wscale"), _vector(bias, outs, dev, "bias"),
+            int(bool(relu)), n, cols, outs, ws.data_ptr() if need else None, need,
+            _stream_handle(stream)), "oscars_linear_quantized")
     return out
 
 
@@ -661,7 +662,7 @@ class Context:
         a scale per output channel (oscars_quantize_model): one device tensor
         for evaluate_i8.  Fully connected models only."""
         import torch
-        need = int(_lib().oscars_i8_model_bytes(self._h))
+        need = int(_lib().oscars_quantized_model_bytes(self._h))
         pp = _dev_ptr(params, torch.float32, "params")
         if params.numel() < self.n_pad:
             raise ValueError("params must hold n_pad floats")
@@ -675,13 +676,13 @@ class Context:
 
     def evaluate_i8(self, model, x, y, n_rows: Optional[int] = None):
         """``evaluate`` with the products of the quantised ``model``
-        (oscars_evaluate_i8)."""
+        (oscars_evaluate_quantized)."""
         import torch
         n = int(x.shape[0] if n_rows is None else n_rows)
         if n > x.shape[0] or n > y.shape[0]:
             raise ValueError("n_rows exceeds the rows of x or y")
         mp = _dev_ptr(model, torch.uint8, "model")
-        if model.numel() < int(_lib().oscars_i8_model_bytes(self._h)):
+        if model.numel() < int(_lib().oscars_quantized_model_bytes(self._h)):
             raise ValueError("model is not a quantised model of this context")
         xdt = x.dtype if self.dtype == BF16 and x.dtype in (torch.int16, torch.uint16) else (
             torch.bfloat16 if self.dtype == BF16 else torch.float32)
@@ -689,9 +690,9 @@ class Context:
             raise ValueError("x must be [n_rows][d]")
         loss = ctypes.c_double(0.0)
         hits = _i64(0)
-        _check(_lib().oscars_evaluate_i8(self._h, mp, _dev_ptr(x, xdt, "x"),
+        _check(_lib().oscars_evaluate_quantized(self._h, mp, _dev_ptr(x, xdt, "x"),
                                          _dev_ptr(y, torch.int32, "y"), n, ctypes.byref(loss),
-                                         ctypes.byref(hits)), "oscars_evaluate_i8")
+                                         ctypes.byref(hits)), "oscars_evaluate_quantized")
         return float(loss.value), int(hits.value)
 
     def server_step(self, global_, replicas, weights: Sequence[float], momentum, lr: float,

@@ -177,10 +177,14 @@ def measure_step_ms(cfg, dataset, init, reps: int = 5) -> float:
 def run_paradigm(cfg, dataset, init, eval_set, paradigm: str, schedule: SpeedSchedule,
                  base: float, time_budget: float, local_steps: int = 4, resolution: int = 8,
                  max_rounds: int = 100000, eval_every: int = 1,
-                 return_model: bool = False) -> Dict:
+                 return_model: bool = False, server: Optional[Dict] = None,
+                 int8_eval: bool = False) -> Dict:
     """Train with one paradigm until the emulated cluster clock reaches
     ``time_budget`` (same unit as ``base``).  Returns per-round records (and
-    the final global model as layers when ``return_model``)."""
+    the final global model as layers when ``return_model``).  ``server``: the
+    arguments of OscarsRun.round_server, which then ends every round in the
+    place of the average.  ``int8_eval``: every evaluation also with the model
+    in 8-bit integers (eval_loss_i8, eval_acc_i8)."""
     import torch
 
     from .rounds import OscarsRun
@@ -198,10 +202,16 @@ def run_paradigm(cfg, dataset, init, eval_set, paradigm: str, schedule: SpeedSch
     clock = 0.0
     samples = 0
     gpu_ms = 0.0
+
+    def measure(rec):
+        for kind, int8 in (("", False), ("_i8", True))[:1 + int(int8_eval)]:
+            loss, hit = run.evaluate(x_eval, y_eval, int8)
+            rec["eval_loss" + kind] = loss / n_eval
+            rec["eval_acc" + kind] = hit / n_eval
+        return rec
+
     try:
-        loss0, hit0 = run.ctx.evaluate(run.g, x_eval, y_eval)
-        records.append({"round": -1, "clock": 0.0, "samples": 0, "eval_loss": loss0 / n_eval,
-                        "eval_acc": hit0 / n_eval})
+        records.append(measure({"round": -1, "clock": 0.0, "samples": 0}))
         r = 0
         observed = schedule.iteration_times(-1, 0.0, base)
         while clock < time_budget and r < max_rounds:
@@ -211,7 +221,10 @@ def run_paradigm(cfg, dataset, init, eval_set, paradigm: str, schedule: SpeedSch
             a = torch.cuda.Event(enable_timing=True)
             b = torch.cuda.Event(enable_timing=True)
             a.record()
-            run.round(tau)
+            if server is None:
+                run.round(tau)
+            else:
+                run.round_server(tau, **server)
             b.record()
             torch.cuda.synchronize()
             gpu_ms += a.elapsed_time(b)
@@ -223,9 +236,7 @@ def run_paradigm(cfg, dataset, init, eval_set, paradigm: str, schedule: SpeedSch
                 rec["T_star"] = balancer.T_star
                 rec["ticks"] = list(balancer.ticks)
             if (r + 1) % eval_every == 0:
-                loss, hit = run.ctx.evaluate(run.g, x_eval, y_eval)
-                rec["eval_loss"] = loss / n_eval
-                rec["eval_acc"] = hit / n_eval
+                measure(rec)
             records.append(rec)
             r += 1
         model = run.global_layers() if return_model else None
@@ -336,9 +347,10 @@ def time_to_loss(result: Dict, target: float) -> Optional[float]:
 
 def compare(cfg, schedule: SpeedSchedule, time_budget_steps: float, local_steps: int = 4,
             resolution: int = 8, n_eval: int = 10000, base: Optional[float] = None,
-            eval_every: int = 1) -> Dict:
+            eval_every: int = 1, server: Optional[Dict] = None, int8_eval: bool = False) -> Dict:
     """The three paradigms on one workload and one emulated cluster.  The
-    budget is in units of the speed-1 step time."""
+    budget is in units of the speed-1 step time; ``server`` and ``int8_eval`` as
+    for run_paradigm."""
     import workload
     dataset = workload.gen_dataset(cfg)
     init = workload.gen_init(cfg)
@@ -348,13 +360,14 @@ def compare(cfg, schedule: SpeedSchedule, time_budget_steps: float, local_steps:
     out = {"workload": cfg.name, "K": cfg.K, "batch": cfg.batch, "lr": cfg.lr,
            "speeds": schedule.speeds, "changes": {str(k): v for k, v in schedule.changes.items()},
            "jitter": schedule.jitter, "step_ms_speed1": base_ms, "time_budget_ms": budget,
-           "local_steps": local_steps, "resolution": resolution, "M": cfg.M, "paradigms": {}}
+           "local_steps": local_steps, "resolution": resolution, "M": cfg.M, "server": server,
+           "paradigms": {}}
     results = {}
     for p in PARADIGMS:
         t0 = time.perf_counter()
         res = run_paradigm(cfg, dataset, init, eval_set, p, schedule, base_ms, budget,
                            local_steps=local_steps, resolution=resolution,
-                           eval_every=eval_every)
+                           eval_every=eval_every, server=server, int8_eval=int8_eval)
         res["wall_s"] = time.perf_counter() - t0
         results[p] = res
     # target: the best loss BSP reached within the budget
@@ -376,6 +389,9 @@ def compare(cfg, schedule: SpeedSchedule, time_budget_steps: float, local_steps:
             "curve": [(round(rec["clock"], 4), rec.get("eval_loss"), rec.get("eval_acc"))
                       for rec in recs if "eval_loss" in rec],
         }
+        if int8_eval:
+            out["paradigms"][p]["final_eval_loss_i8"] = last_eval["eval_loss_i8"]
+            out["paradigms"][p]["final_eval_acc_i8"] = last_eval["eval_acc_i8"]
     out["bsp_best_loss"] = target
     return out
 
@@ -402,6 +418,12 @@ def main(argv=None):
     ap.add_argument("--jitter", type=float, default=0.02)
     ap.add_argument("--mean-scale", type=float, default=0.1)
     ap.add_argument("--eval-every", type=int, default=1)
+    ap.add_argument("--server-lr", type=float, default=None, metavar="LR",
+                    help="end every round with the server's step: a momentum and orthogonalised "
+                         "updates of this learning rate in the place of the average")
+    ap.add_argument("--server-beta", type=float, default=0.9, help="its momentum")
+    ap.add_argument("--int8-eval", action="store_true",
+                    help="evaluate the global model in 8-bit integers too")
     ap.add_argument("--out", default=None, help="also write the JSON here")
     ap.add_argument("--measured", type=int, default=0, metavar="ROUNDS",
                     help="instead: this many rounds with the plan from measured times on the "
@@ -425,7 +447,10 @@ def main(argv=None):
     schedule = SpeedSchedule(cfg.speeds, changes={args.budget / 2: tuple(reversed(cfg.speeds))},
                              jitter=args.jitter, seed=cfg.seed)
     res = compare(cfg, schedule, args.budget, local_steps=args.local_steps,
-                  resolution=args.resolution, eval_every=args.eval_every)
+                  resolution=args.resolution, eval_every=args.eval_every,
+                  server=None if args.server_lr is None else {"lr": args.server_lr,
+                                                              "beta": args.server_beta},
+                  int8_eval=args.int8_eval)
     line = json.dumps(res)
     print(line)
     if args.out:

@@ -1927,7 +1927,7 @@ struct I8Layout {
 
 constexpr int64_t kI8EvalRows = 8192;  // rows of an evaluation's pass
 
-// oscars_evaluate_i8's temporaries behind EvalLayout's: quantised rows and their
+// oscars_evaluate_quantized's temporaries behind EvalLayout's: quantised rows and their
 // scales, two activations, logits.
 struct I8EvalLayout {
   int64_t rows, xq, scale, act[2], logits, end;
@@ -2024,10 +2024,11 @@ oscars_status oscars_quantize_rows(int8_t* q, int64_t q_ld, float* scale, const 
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
 
-oscars_status oscars_matmul_i8(void* out, int64_t out_ld, int32_t out_dtype, const int8_t* xq,
-                               int64_t x_ld, const float* xscale, const int8_t* wq, int64_t w_ld,
-                               const float* wscale, const float* bias, int32_t relu, int64_t rows,
-                               int32_t in, int32_t outs, void* hip_stream) {
+oscars_status oscars_matmul_quantized(void* out, int64_t out_ld, int32_t out_dtype,
+                                      const int8_t* xq, int64_t x_ld, const float* xscale,
+                                      const int8_t* wq, int64_t w_ld, const float* wscale,
+                                      const float* bias, int32_t relu, int64_t rows, int32_t in,
+                                      int32_t outs, void* hip_stream) {
   if (!is_dtype(out_dtype)) return OSCARS_E_INVALID;
   const MatmulI8Args a{xq,   x_ld,      xscale, wq,   w_ld, wscale, bias,
                        relu != 0, rows, in,     outs, out,  out_ld, out_dtype == OSCARS_BF16};
@@ -2042,16 +2043,16 @@ oscars_status oscars_matmul_i8(void* out, int64_t out_ld, int32_t out_dtype, con
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
 
-int64_t oscars_linear_i8_workspace(int64_t rows, int32_t in) {
+int64_t oscars_linear_quantized_workspace(int64_t rows, int32_t in) {
   if (!i8_sizes_ok(rows, in, 1) || linear_i8_one_launch(rows, in)) return 0;
   return round_up(rows * round_up(in, 128), 256) + rows * 4;
 }
 
-oscars_status oscars_linear_i8(void* out, int64_t out_ld, int32_t out_dtype, const void* x,
-                               int64_t x_ld, int32_t dtype, const int8_t* wq, int64_t w_ld,
-                               const float* wscale, const float* bias, int32_t relu, int64_t rows,
-                               int32_t in, int32_t outs, void* workspace, int64_t workspace_bytes,
-                               void* hip_stream) {
+oscars_status oscars_linear_quantized(void* out, int64_t out_ld, int32_t out_dtype, const void* x,
+                                      int64_t x_ld, int32_t dtype, const int8_t* wq, int64_t w_ld,
+                                      const float* wscale, const float* bias, int32_t relu,
+                                      int64_t rows, int32_t in, int32_t outs, void* workspace,
+                                      int64_t workspace_bytes, void* hip_stream) {
   if (!is_dtype(dtype) || !is_dtype(out_dtype)) return OSCARS_E_INVALID;
   MatmulI8Args a{nullptr,   0,    nullptr, wq,   w_ld, wscale, bias,
                  relu != 0, rows, in,      outs, out,  out_ld, out_dtype == OSCARS_BF16};
@@ -2060,7 +2061,7 @@ oscars_status oscars_linear_i8(void* out, int64_t out_ld, int32_t out_dtype, con
   const int64_t n = rows_span(rows, out_ld, outs, dtype_bytes(out_dtype)),
                 xn = rows_span(rows, x_ld, in, es);
   if (overlap(out, n, x, xn)) return OSCARS_E_INVALID;
-  const int64_t need = oscars_linear_i8_workspace(rows, in);
+  const int64_t need = oscars_linear_quantized_workspace(rows, in);
   if (need > 0) {
     if (!workspace || !aligned16(workspace) || workspace_bytes < need) return OSCARS_E_INVALID;
     if (overlap(workspace, need, out, n) || overlap(workspace, need, x, xn) ||
@@ -2087,7 +2088,7 @@ oscars_status oscars_linear_i8(void* out, int64_t out_ld, int32_t out_dtype, con
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
 
-int64_t oscars_i8_model_bytes(const oscars_ctx* c) {
+int64_t oscars_quantized_model_bytes(const oscars_ctx* c) {
   return !c || c->cnn ? 0 : I8Layout(c).end;
 }
 
@@ -2112,8 +2113,9 @@ oscars_status oscars_quantize_model(oscars_ctx* c, const float* params, void* mo
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
 
-oscars_status oscars_evaluate_i8(oscars_ctx* c, const void* model, const void* x, const int32_t* y,
-                                 int64_t n_rows, double* loss_sum, int64_t* correct) {
+oscars_status oscars_evaluate_quantized(oscars_ctx* c, const void* model, const void* x,
+                                        const int32_t* y, int64_t n_rows, double* loss_sum,
+                                        int64_t* correct) {
   const oscars_status st =
       check_evaluate(c, static_cast<const float*>(model), x, y, n_rows, loss_sum, correct);
   if (st != OSCARS_OK) return st;

@@ -2,8 +2,10 @@
 ``oscars_round`` (every worker starts from the global model, runs its tau_k
 local SGD steps, and the 1/K average becomes the new global model), or the
 two separate calls ``oscars_local_steps`` then ``oscars_aggregate`` with
-broadcast (the average written back to every replica).  This module only
-moves data into device memory and sequences calls; all arithmetic runs in
+broadcast (the average written back to every replica).  ``round_server`` puts
+the server's step with a momentum and orthogonalised updates in the place of
+the average, ``evaluate`` measures the global model, in its own arithmetic or
+in 8-bit integers.  This module only moves data into device memory and sequences calls; all arithmetic runs in
 the HIP library."""
 from __future__ import annotations
 
@@ -11,7 +13,8 @@ from typing import Optional, Sequence
 
 import numpy as np
 
-from . import BF16, FP32, Context, aggregate, load_balance, paper_weights, shard_offsets
+from . import (BF16, FP32, Context, aggregate, broadcast, load_balance, paper_weights,
+               shard_offsets)
 
 
 def tau_schedule(cfg, rounds: Optional[int] = None) -> np.ndarray:
@@ -52,6 +55,8 @@ class OscarsRun:
         self.g = flat.clone()
         self.replicas = flat.repeat(cfg.K).contiguous()
         self.weights = paper_weights(cfg.K)
+        self.momentum = None   # of round_server
+        self.quantized = None  # of evaluate(int8=True)
 
     def local_steps(self, tau: Sequence[int]):
         self.ctx.local_steps(self.replicas, self.x, self.y, self.offsets, self.seed, tau,
@@ -70,6 +75,30 @@ class OscarsRun:
         """The same round as local steps plus aggregation with broadcast."""
         self.local_steps(tau)
         self.aggregate(True)
+
+    def round_server(self, tau: Sequence[int], lr: float, beta: float = 0.9,
+                     nesterov: bool = True, weight_decay: float = 0.0, plain_lr: float = 1.0,
+                     plain_layers: Sequence[int] = ()):
+        """A round whose end is the server's step (``Context.server_step``): every
+        worker starts from the global model, runs its local steps, and the
+        server moves ``g`` by the orthogonalised momentum of their average's
+        difference.  The momentum (``momentum``) starts at zero."""
+        import torch
+        if self.momentum is None:
+            self.momentum = torch.zeros_like(self.g)
+        broadcast(self.g, self.replicas, self.cfg.K, self.n, self.n)
+        self.local_steps(tau)
+        self.ctx.server_step(self.g, self.replicas, self.weights, self.momentum, lr, beta=beta,
+                             nesterov=nesterov, weight_decay=weight_decay, plain_lr=plain_lr,
+                             plain_layers=plain_layers)
+
+    def evaluate(self, x, y, int8: bool = False):
+        """Held-out (summed loss, correct count) of the global model; ``int8``:
+        with its weights and activations in 8-bit integers."""
+        if not int8:
+            return self.ctx.evaluate(self.g, x, y)
+        self.quantized = self.ctx.quantize_model(self.g, out=self.quantized)
+        return self.ctx.evaluate_i8(self.quantized, x, y)
 
     def global_layers(self):
         return self.ctx.unpack(self.g.cpu().numpy())

@@ -87,3 +87,14 @@ def test_batch_schedule(C):
         C.BatchSchedule([64, 0])
     with pytest.raises(ValueError):
         C.BatchSchedule([64, 32], {1: [8]})
+
+
+def test_command_line_takes_the_servers_step_and_int8(C, monkeypatch, capsys):
+    """The options reach the comparison; without them it is called as before."""
+    seen = []
+    monkeypatch.setattr(C, "compare", lambda cfg, schedule, budget, **kw: seen.append(kw) or {})
+    assert C.main(["--budget", "10"]) == 0
+    assert C.main(["--server-lr", "0.02", "--server-beta", "0.5", "--int8-eval"]) == 0
+    capsys.readouterr()
+    assert seen[0]["server"] is None and seen[0]["int8_eval"] is False
+    assert seen[1]["server"] == {"lr": 0.02, "beta": 0.5} and seen[1]["int8_eval"] is True

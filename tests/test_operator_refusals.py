@@ -141,11 +141,11 @@ def _linear(matmul=False, **kw):
              nbytes=None)
     a.update(kw)
     if matmul:
-        return lib.oscars_matmul_i8(a["out"], a["out_ld"], a["out_dtype"], a["x"], a["x_ld"],
+        return lib.oscars_matmul_quantized(a["out"], a["out_ld"], a["out_dtype"], a["x"], a["x_ld"],
                                     a["xscale"], a["wq"], a["w_ld"], a["wscale"], a["bias"],
                                     a["relu"], a["rows"], a["inf"], a["outs"], None)
-    need = lib.oscars_linear_i8_workspace(a["rows"], a["inf"])
-    return lib.oscars_linear_i8(a["out"], a["out_ld"], a["out_dtype"], a["x"], a["x_ld"],
+    need = lib.oscars_linear_quantized_workspace(a["rows"], a["inf"])
+    return lib.oscars_linear_quantized(a["out"], a["out_ld"], a["out_dtype"], a["x"], a["x_ld"],
                                 a["dtype"], a["wq"], a["w_ld"], a["wscale"], a["bias"], a["relu"],
                                 a["rows"], a["inf"], a["outs"], a["ws"],
                                 need if a["nbytes"] is None else a["nbytes"], None)
@@ -163,9 +163,9 @@ def test_linear_i8_refuses(bad, matmul):
 
 
 def test_linear_i8_refuses_workspace():
-    need = lib.oscars_linear_i8_workspace(40, 100)
-    assert need >= 40 * 128 + 40 * 4 and lib.oscars_linear_i8_workspace(16, 100) == 0
-    assert lib.oscars_linear_i8_workspace(-1, 100) == 0
+    need = lib.oscars_linear_quantized_workspace(40, 100)
+    assert need >= 40 * 128 + 40 * 4 and lib.oscars_linear_quantized_workspace(16, 100) == 0
+    assert lib.oscars_linear_quantized_workspace(-1, 100) == 0
     for bad in (dict(ws=None), dict(ws=Q + 8), dict(nbytes=need - 1), dict(ws=OUT), dict(ws=X),
                 dict(ws=W), dict(ws=S), dict(dtype=3)):
         assert _linear(**bad) == P.E_INVALID, bad
@@ -184,7 +184,7 @@ def test_no_rows_is_no_work():
 
 def test_int8_model_refuses_null():
     loss, hits = ctypes.c_double(0.0), ctypes.c_int64(0)
-    assert lib.oscars_i8_model_bytes(None) == 0
+    assert lib.oscars_quantized_model_bytes(None) == 0
     assert lib.oscars_quantize_model(None, BASE, BASE) == P.E_INVALID
-    assert lib.oscars_evaluate_i8(None, BASE, BASE, BASE, 1, ctypes.byref(loss),
+    assert lib.oscars_evaluate_quantized(None, BASE, BASE, BASE, 1, ctypes.byref(loss),
                                   ctypes.byref(hits)) == P.E_INVALID
