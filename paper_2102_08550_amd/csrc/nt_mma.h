@@ -45,18 +45,16 @@ __device__ __forceinline__ typename NtAcc<F>::type nt_mfma(nt_u32x4 a, nt_u32x4 
                                                   __builtin_bit_cast(nt_f16x8, b), c, 0, 0, 0);
 }
 
-// Workgroup tile: BM x BN outputs, WM x WN waves, ST stages in LDS.  EXACT: what
-// NT_SPLIT adds for the last bits, where there are registers and time for it.
-//   1: the hi lo and lo hi products have accumulators of their own, added at the
-//      end: every product rounds the sum it goes into, and the small ones would
-//      round the large sum two more times;
-//   2: the lo lo products too, in the small accumulators.
-// Five Newton-Schulz steps of 10 x 256 matrices, error in 2-norm, median and
-// worst of 24: 0: 1.2e-6 and 1.5e-6; 1: 7.3e-7 and 1.3e-6; in fp32 6.1e-7 and
-// 7.7e-7.
-template <int BM_, int BN_, int WM_, int WN_, int ST_, int EXACT_ = 0>
+// Workgroup tile: BM x BN outputs, WM x WN waves, ST stages in LDS.  EXACT, where
+// there are registers for it: NT_SPLIT's products with a lo plane have accumulators
+// of their own, added at the end.  Every product rounds the sum it goes into, and
+// the small ones would round the large sum two more times.  Five Newton-Schulz
+// steps of 10 x 256 matrices, error in 2-norm, median and worst of 24: 1.2e-6 and
+// 1.5e-6 without, 7.3e-7 and 1.3e-6 with; in fp32 6.1e-7 and 7.7e-7.
+template <int BM_, int BN_, int WM_, int WN_, int ST_, bool EXACT_ = false>
 struct NtShape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_, EXACT = EXACT_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_;
+  static constexpr bool EXACT = EXACT_;
   static constexpr int NT = 64 * WM * WN, MI = BM / WM / 32, NJ = BN / WN / 32;
   static constexpr int LDS_BYTES = ST * (BM + BN) * NT_BLOCK;
   static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0, "whole matrix blocks per wave");
@@ -130,7 +128,7 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int firs
                                         char* lds, int tid, Acc (&acc)[S::MI][S::NJ]) {
   constexpr int ABYTES = S::BM * NT_BLOCK, STAGE = (S::BM + S::BN) * NT_BLOCK;
   constexpr int PER = RowsA::P + RowsB::P;
-  constexpr bool SPLIT = F == NT_SPLIT || F == NT_SPLIT_B0, CROSS = S::EXACT > 0 && SPLIT;
+  constexpr bool SPLIT = F == NT_SPLIT || F == NT_SPLIT_B0, CROSS = S::EXACT && SPLIT;
   const int lane = tid & 63, wave = tid >> 6;
   const int arow = (wave / S::WN) * 32 * S::MI + (lane & 31);
   const int brow = (wave % S::WN) * 32 * S::NJ + (lane & 31), h = lane >> 5;
@@ -253,7 +251,6 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int firs
           step(k, k);
           if constexpr (F == NT_SPLIT) step(k, 2 + k);
           step(2 + k, k);
-          if constexpr (F == NT_SPLIT && S::EXACT > 1) step(2 + k, 2 + k);
         }
       } else {
 #pragma unroll

@@ -32,7 +32,7 @@ namespace oscars {
 namespace {
 
 typedef NtShape<256, 256, 2, 4, 2> OrthL;
-typedef NtShape<128, 128, 2, 2, 2, 1> OrthM;
+typedef NtShape<128, 128, 2, 2, 2, true> OrthM;
 
 enum OrthKind { ORTH_GRAM = 0, ORTH_POLY = 1, ORTH_APPLY = 2, ORTH_LAST = 3 };
 
@@ -55,6 +55,10 @@ struct OrthArgs {
   // 3 i, and scalar loads drop the low bits of each summand.)
   int first[ORTH_MAX_MATS + 1];
   int order[ORTH_MAX_MATS];
+  // Products in tiles of 128 or 256: position i's before cut[i] are done as such, the
+  // others (of 128) as tiles of 32, in a launch with `rest` set.
+  int cut[ORTH_MAX_MATS];
+  int rest;
   char* ws;
   float a, b, c;
   int in_scaled;       // 1: the planes hold X times orth_scale; 0: X_0 (factor in the workspace)
@@ -525,7 +529,7 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
   const int pos = find_position(g.first, g.count, blockIdx.x);
   const Prod p(g, g.order[pos]);
-  const int local = blockIdx.x - g.first[pos], tiles = p.template tiles<S::BM>();
+  const int local = blockIdx.x - g.first[pos], tiles = g.cut[pos];
   if (local >= tiles) return;
   int ti, tj;
   p.template tile<S::BM>(xcd_index(local, tiles), &ti, &tj);
@@ -642,10 +646,21 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // scalar addresses below
   const int pos = find_position(g.first, g.count, blockIdx.x);
   const Prod p(g, g.order[pos]);
-  const int local = blockIdx.x - g.first[pos], tiles = p.template tiles<32>();
-  if (local >= tiles) return;
+  const int local = blockIdx.x - g.first[pos];
   int ti, tj;
-  p.template tile<32>(xcd_index(local, tiles), &ti, &tj);
+  if (g.rest) {  // sixteenths of the tiles of 128 from cut[pos] on
+    const int from = g.cut[pos], parts = (p.template tiles<128>() - from) * 16;
+    if (local >= parts) return;
+    const int id = xcd_index(local, parts);
+    p.template tile<128>(from + id / 16, &ti, &tj);
+    ti = 4 * ti + (id & 3);
+    tj = 4 * tj + (id >> 2 & 3);
+    if (ti * 32 >= p.R || tj * 32 >= p.C || (Prod::SYM && ti < tj)) return;
+  } else {
+    const int tiles = p.template tiles<32>();
+    if (local >= tiles) return;
+    p.template tile<32>(xcd_index(local, tiles), &ti, &tj);
+  }
   const int r0 = ti * 32, c0 = tj * 32;
   const int64_t ld = row_bytes(p.K, PF);
   const int blocks = row_blocks(p.K, PF);
@@ -773,10 +788,33 @@ void matrices_in_order(OrthArgs* g) {
 constexpr int kCus = 256;
 
 template <class S, int KIND, int F>
-hipError_t launch_product_shape(OrthArgs& g, hipStream_t s) {
-  const int grid = layout_grid(&g, [&](int i) { return tiles_of(g.mat[i].u, KIND, S::BM); });
+hipError_t launch_product_shape(OrthArgs& g, hipStream_t s, int64_t most) {
+  int at = 0;
+  const int grid = layout_grid(&g, [&](int i) {
+    const int64_t tiles = tiles_of(g.mat[i].u, KIND, S::BM);
+    g.cut[at] = static_cast<int>(tiles < most ? tiles : most);
+    most -= g.cut[at];
+    return g.cut[at++];
+  });
   if (grid < 0) return hipErrorInvalidValue;
   hipLaunchKernelGGL((orth_product_kernel<S, KIND, F>), dim3(grid), dim3(S::NT), 0, s, g);
+  return hipGetLastError();
+}
+
+template <int KIND, int F>
+hipError_t launch_product_small(OrthArgs& g, hipStream_t s, int rest) {
+  int at = 0;
+  g.rest = rest;
+  const int grid = layout_grid(&g, [&](int i) {
+    if (!rest) return tiles_of(g.mat[i].u, KIND, 32);
+    return (tiles_of(g.mat[i].u, KIND, 128) - g.cut[at++]) * 16;
+  });
+  if (grid < 0) return hipErrorInvalidValue;
+  const dim3 wg(64 * SMALL_WAVES);
+  if (grid <= 2 * kCus)
+    hipLaunchKernelGGL((orth_small_kernel<KIND, F, 2>), dim3(grid), wg, 0, s, g);
+  else
+    hipLaunchKernelGGL((orth_small_kernel<KIND, F, 1>), dim3(grid), wg, 0, s, g);
   return hipGetLastError();
 }
 
@@ -788,12 +826,18 @@ hipError_t launch_product_shape(OrthArgs& g, hipStream_t s) {
 //   256   20 us, and a block 2.1 us while half of the CUs have a tile, else 2.45 us
 //         for 256 at a time
 // and, with more tiles than fit at once, some of a tile for the CUs that run dry.
+// Where a few tiles of 128 are left after full turns of one or two to a CU, they
+// are done in tiles of 32 by a second launch, 9 us and their blocks: one matrix of
+// 4096 (two turns of 256 and 16 left) went from 4329 to 3883 us (bf16 3121 to 2774),
+// 2900 from 2170 to 1919, two of 2048 from 1432 to 1338; eight of 1024 (32 blocks of
+// K, 32 tiles left) would have gone from 886 to 1000.
 // Whole calls, fp32 (32 / 128 / 256, us): 512: 112 / 352 / 783, 1280: 401 / 602 /
 // 1390, 2048: 1331 / 862 / 1999, 4096: 10214 / 4402 / 4100; three 4096 x 4096 and
 // 1000 x 4096: 31327 / 12011 / 11216.  (Tiles cut along K, their sums joined by
 // the last workgroup to arrive, were slower everywhere but there by 3%: the sums'
 // way through memory and the caches' write-back.)
-int best_tile(const OrthArgs& g, int kind, int fmt) {
+// `most`: of the tiles of 128, those done as such; the others are done in tiles of 32.
+int best_tile(const OrthArgs& g, int kind, int fmt, int64_t* most) {
   int best = 0;
   double best_t = 0.0;
   for (int bt : {32, 128, 256}) {
@@ -816,6 +860,25 @@ int best_tile(const OrthArgs& g, int kind, int fmt) {
     if (best == 0 || us < best_t) {
       best = bt;
       best_t = us;
+      *most = INT64_MAX;
+    }
+    if (bt == 128 && tiles > 256.0) {
+      const double turns = std::floor(tiles / 256.0), rest = tiles - 256.0 * turns;
+      double left = rest, over = 0.0;  // blocks of the last tiles
+      for (int i = g.count - 1; i >= 0 && left > 0.0; --i) {
+        const int at = g.order[i];
+        const double n = std::fmin(left, tiles_of(g.mat[at].u, kind, bt));
+        left -= n;
+        over += n * blocks_of(g.mat[at].u, kind, fmt);
+      }
+      us = 9.0 + 0.725 * (blocks - over) / 256.0;
+      if (rest > 0.0) us += 9.0 + 16.0 * over / 1870.0;
+      if (std::fmod(turns, 2.0) != 0.0) us += 0.025 * longest;
+      if (us < best_t) {
+        best = bt;
+        best_t = us;
+        *most = rest > 0.0 ? static_cast<int64_t>(256.0 * turns) : INT64_MAX;
+      }
     }
   }
   return best;
@@ -833,17 +896,12 @@ hipError_t launch_product(OrthArgs& g, hipStream_t s) {
       g.order[j] = g.order[j - 1];
       g.order[j - 1] = t;
     }
-  const int tile = best_tile(g, KIND, PF);
-  if (tile == 256) return launch_product_shape<OrthL, KIND, F>(g, s);
-  if (tile == 128) return launch_product_shape<OrthM, KIND, F>(g, s);
-  const int grid = layout_grid(&g, [&](int i) { return tiles_of(g.mat[i].u, KIND, 32); });
-  if (grid < 0) return hipErrorInvalidValue;
-  const dim3 wg(64 * SMALL_WAVES);
-  if (grid <= 2 * kCus)
-    hipLaunchKernelGGL((orth_small_kernel<KIND, F, 2>), dim3(grid), wg, 0, s, g);
-  else
-    hipLaunchKernelGGL((orth_small_kernel<KIND, F, 1>), dim3(grid), wg, 0, s, g);
-  return hipGetLastError();
+  int64_t most;
+  const int tile = best_tile(g, KIND, PF, &most);
+  if (tile == 32) return launch_product_small<KIND, F>(g, s, 0);
+  if (tile == 256) return launch_product_shape<OrthL, KIND, F>(g, s, most);
+  const hipError_t e = launch_product_shape<OrthM, KIND, F>(g, s, most);
+  return e != hipSuccess || most == INT64_MAX ? e : launch_product_small<KIND, F>(g, s, 1);
 }
 
 }  // namespace

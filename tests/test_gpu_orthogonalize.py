@@ -121,7 +121,8 @@ def test_orthogonalize(P, r, c, dtype):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("shapes", [[(512, 784), (256, 512), (10, 256)],
                                     [(300, 40), (40, 300), (1, 9), (64, 64), (1500, 700)],
-                                    [(3600, 3700), (33, 900)]])
+                                    [(3600, 3700), (33, 900)],
+                                    [(2900, 2950)], [(2048, 2060), (2100, 2040)]])
 def test_orthogonalize_group(P, shapes, dtype):
     import torch
     dt = torch.float32 if dtype == "fp32" else torch.bfloat16
