@@ -7,8 +7,8 @@
 //
 //   quantize_rows   one pass over the rows, a wave or a workgroup a row;
 //   matmul_i8       tiles on 32x32x32 matrix instructions (nt_mma.h);
-//   linear_i8_few   up to 16 rows: a stream of the weights, with the rows'
-//                   quantisation in front of it in every workgroup.
+//   linear_i8_few   one row, or up to 16 short ones: a stream of the weights, with
+//                   the rows' quantisation in front of it in every workgroup.
 #include "int8.h"
 
 #include <cmath>
@@ -578,41 +578,79 @@ hipError_t launch_quantize_rows(const QuantArgs& a, hipStream_t s) {
   return vec ? quantize_launch<false, true>(a, s) : quantize_launch<false, false>(a, s);
 }
 
-// The tile with the least time by what the kernels take on this card, in us (a K
-// block: 128 inputs):
+// The first `rows` rows of a product in tiles of `tile`, and its time by what the
+// kernels take on this card, in us (a K block: 128 inputs):
 //   32    3.5, and 2100 blocks a us over all CUs
-//   128   8, and a block 0.55 while no CU has two tiles, else 1.2 for 512 at a time
+//   128   8, and a block 0.55 while no CU has two tiles, else 1.2 for 512 at a time,
+//         of which the last up to 256 take 0.75
 //   256   12, and a block 1.5 while half of the CUs have a tile, 1.95 up to all
 //         of them, else 2.05 for 256 at a time
 // Rows x inputs x outputs, measured with 32 / 128 / 256: 256 x 4096 x 1000: 7.0 /
 // 24.4 / 53, 1024 x 2048 x 2048: 19.9 / 17.9 / 34.5, 10000 x 2048 x 2048: 155 / 65 /
 // 76, 4096 x 4096 x 4096: 235 / 86 / 74.
-int i8_best_tile(const MatmulI8Args& a) {
+struct I8Plan {
+  int tile;
+  int64_t rows;
+  double us;
+};
+I8Plan i8_plan(const MatmulI8Args& a, int64_t rows) {
   const double k = (a.in + NT_BLOCK - 1) / NT_BLOCK;
-  int best = 0;
-  double best_us = 0.0;
+  I8Plan best{0, rows, 0.0};
   for (int t : {32, 128, 256}) {
     const double n =
-        static_cast<double>((a.outs + t - 1) / t) * static_cast<double>((a.rows + t - 1) / t);
-    const double us = t == 32    ? 3.5 + n * k / 2100.0
-                      : t == 128 ? 8.0 + k * (n <= 256.0 ? 0.55 : 1.2 * std::ceil(n / 512.0))
-                                 : 12.0 + k * (n <= 144.0   ? 1.5
-                                               : n <= 256.0 ? 1.95
-                                                            : 2.05 * std::ceil(n / 256.0));
-    if (best == 0 || us < best_us) {
-      best = t;
-      best_us = us;
+        static_cast<double>((a.outs + t - 1) / t) * static_cast<double>((rows + t - 1) / t);
+    const double turns = std::floor(n / 512.0), last = n - 512.0 * turns;
+    double us;
+    if (t == 32)
+      us = 3.5 + n * k / 2100.0;
+    else if (t == 128)
+      us = 8.0 + k * (n <= 256.0 ? 0.55
+                                 : 1.2 * turns + (last > 256.0 ? 1.2 : last > 0.0 ? 0.75 : 0.0));
+    else
+      us = 12.0 + k * (n <= 144.0 ? 1.5 : n <= 256.0 ? 1.95 : 2.05 * std::ceil(n / 256.0));
+    if (best.tile == 0 || us < best.us) {
+      best.tile = t;
+      best.us = us;
     }
   }
   return best;
 }
 
-hipError_t launch_matmul_i8(const MatmulI8Args& a, hipStream_t s) {
-  const int tile = i8_best_tile(a);
-  const bool vec = aligned_rows(a.out, a.out_ld * (a.out_bf16 ? 2 : 4), 16);
-  if (a.out_bf16)
-    return vec ? matmul_launch<true, true>(a, tile, s) : matmul_launch<true, false>(a, tile, s);
-  return vec ? matmul_launch<false, true>(a, tile, s) : matmul_launch<false, false>(a, tile, s);
+// Rows that fill the CUs with tiles of 128 or 256 a whole number of times, where
+// the others and a second launch (1 us) then take less than one more turn would:
+// 4352 x 2048 x 2048 went from 38.3 to 32.0 us, 9000 x 4096 x 4096 from 171 to 160;
+// 9216 x 2048 x 2048, which stays as it is at 57.8, would take 59.8.
+I8Plan i8_first_rows(const MatmulI8Args& a) {
+  I8Plan best = i8_plan(a, a.rows);
+  for (int t : {128, 256}) {
+    const int64_t across = (a.outs + t - 1) / t, slots = t == 128 ? 512 : 256;
+    const int64_t turns = across * ((a.rows + t - 1) / t) / slots;
+    const int64_t rows = turns * slots / across * t;
+    if (rows == 0 || rows >= a.rows) continue;
+    const I8Plan first = i8_plan(a, rows);
+    const double us = first.us + 1.0 + i8_plan(a, a.rows - rows).us;
+    if (us < best.us) best = {first.tile, rows, us};
+  }
+  return best;
+}
+
+hipError_t launch_matmul_i8(const MatmulI8Args& args, hipStream_t s) {
+  const bool vec = aligned_rows(args.out, args.out_ld * (args.out_bf16 ? 2 : 4), 16);
+  auto launch = [&](const MatmulI8Args& a, int tile) {
+    if (a.out_bf16)
+      return vec ? matmul_launch<true, true>(a, tile, s) : matmul_launch<true, false>(a, tile, s);
+    return vec ? matmul_launch<false, true>(a, tile, s) : matmul_launch<false, false>(a, tile, s);
+  };
+  const I8Plan plan = i8_first_rows(args);
+  MatmulI8Args a = args;
+  a.rows = plan.rows;
+  const hipError_t e = launch(a, plan.tile);
+  if (e != hipSuccess || plan.rows == args.rows) return e;
+  a.rows = args.rows - plan.rows;
+  a.xq += plan.rows * a.x_ld;
+  a.xscale += plan.rows;
+  a.out = static_cast<char*>(a.out) + plan.rows * a.out_ld * (a.out_bf16 ? 2 : 4);
+  return launch(a, i8_plan(args, a.rows).tile);
 }
 
 bool linear_i8_one_launch(int64_t rows, int in) {

@@ -179,7 +179,8 @@ def test_linear_i8_strides_and_padding(P, n, dtype):
     assert (edge == -5.0).all()
 
 
-@pytest.mark.parametrize("n,i,o", [(6200, 300, 2050), (4000, 130, 900)])
+@pytest.mark.parametrize("n,i,o", [(6200, 300, 2050), (4000, 130, 900), (4161, 3010, 2043),
+                                   (4301, 4100, 4095)])
 def test_linear_i8_large_tiles(P, n, i, o):
     import torch
     gen = torch.Generator("cuda")
