@@ -407,7 +407,8 @@ oscars_status oscars_server_step(oscars_ctx* ctx, const float* global, const flo
  *   y[r][o] = xscale[r] wscale[o] sum_k xq[r][k] wq[o][k] + bias[o]
  * The sum is exact; then fl(fl(sum) fl(xscale wscale)) + bias in fp32, ReLU
  * (which keeps a NaN) and the rounding to the output's type.  No call allocates,
- * all may be captured into a graph; an output overlaps no other argument.
+ * all may be captured into a graph; an output overlaps no other argument.  Rows of
+ * integers are at most 2^23 bytes apart.
  *
  * oscars_quantize_rows: the integers and scales of the rows of x,
  *   scale[r] = max |x[r]| / 127 in fp32;  q[r][c] = x[r][c] / scale[r], rounded
@@ -429,7 +430,7 @@ oscars_status oscars_server_step(oscars_ctx* ctx, const float* global, const flo
  *   bias   device [outs] fp32 or NULL;  out  device [rows][out_ld] of out_dtype,
  *          out_ld >= outs, aligned to its elements; 1 <= in, outs <= OSCARS_MAX_WIDTH.
  * oscars_linear_quantized: both, x [rows][x_ld] of `dtype` as for oscars_quantize_rows;
- *   up to 16 rows in one launch.  workspace: device, 16-byte aligned,
+ *   one row, or up to 16 of together 16384 entries, in one launch.  workspace: device, 16-byte aligned,
  *   oscars_linear_quantized_workspace bytes (NULL where those are 0), the call's own
  *   until the stream has run it. */
 oscars_status oscars_quantize_rows(int8_t* q, int64_t q_ld, float* scale, const void* x,

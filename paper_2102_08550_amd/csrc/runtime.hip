@@ -1888,8 +1888,10 @@ constexpr int64_t kMaxLd = int64_t{1} << 40;
 bool rows_ok(const void* p, int64_t ld, int64_t width, int64_t esize) {
   return p && ld >= width && ld <= kMaxLd && aligned_to(p, esize);
 }
+// A product's tile addresses its up to 256 rows from the first one by 32 bits.
+constexpr int64_t kMaxI8Ld = int64_t{1} << 23;
 bool i8_rows_ok(const int8_t* p, int64_t ld, int64_t width) {
-  return p && aligned16(p) && ld % 16 == 0 && ld >= width && ld <= kMaxLd;
+  return p && aligned16(p) && ld % 16 == 0 && ld >= width && ld <= kMaxI8Ld;
 }
 int64_t rows_span(int64_t rows, int64_t ld, int64_t width, int64_t esize) {
   return rows > 0 ? ((rows - 1) * ld + width) * esize : 0;

@@ -176,6 +176,15 @@ def test_matmul_i8_refuses():
         assert _linear(True, **bad) == P.E_INVALID, bad
 
 
+def test_int8_rows_too_far_apart():
+    """A tile's 256 rows are addressed by 32 bits: 255 times the stride has to fit."""
+    far, ld = OUT + (1 << 44), (1 << 23) + 16
+    assert _linear(out=far, w_ld=ld) == P.E_INVALID
+    assert _linear(True, out=far, w_ld=ld) == P.E_INVALID
+    assert _linear(True, out=far, x_ld=ld) == P.E_INVALID
+    assert _quantize(q=far & ~0xF, q_ld=ld) == P.E_INVALID
+
+
 def test_no_rows_is_no_work():
     assert _quantize(rows=0) == P.OK
     assert _linear(rows=0, ws=None) == P.OK
