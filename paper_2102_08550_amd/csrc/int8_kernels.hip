@@ -173,26 +173,20 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
 
 template <bool BF16, bool VEC>
 hipError_t quantize_launch(const QuantArgs& a, hipStream_t s) {
-  if (a.cols <= 1024) {  // a wave a row
-    const int64_t blocks = (a.rows + 3) / 4;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(blocks));
-    if (a.cols <= 512)
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 64, 1>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 64, 2>), grid, dim3(256), 0, s, a);
-  } else {
-    if (a.rows > 0x7FFFFFFF) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(a.rows));
-    if (a.cols <= 2048)
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 256, 1>), grid, dim3(256), 0, s, a);
-    else if (a.cols <= 4096)
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 256, 2>), grid, dim3(256), 0, s, a);
-    else if (a.cols <= 8192)
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 256, 4>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 256, 0>), grid, dim3(256), 0, s, a);
-  }
+  const bool waves = a.cols <= 1024;  // a wave a row
+  const dim3 grid(static_cast<unsigned>(waves ? (a.rows + 3) / 4 : a.rows));
+  if (a.cols <= 512)
+    hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 64, 1>), grid, dim3(256), 0, s, a);
+  else if (waves)
+    hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 64, 2>), grid, dim3(256), 0, s, a);
+  else if (a.cols <= 2048)
+    hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 256, 1>), grid, dim3(256), 0, s, a);
+  else if (a.cols <= 4096)
+    hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 256, 2>), grid, dim3(256), 0, s, a);
+  else if (a.cols <= 8192)
+    hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 256, 4>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 256, 0>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -456,7 +450,8 @@ __host__ __device__ __forceinline__ int few_row_bytes(int in) {
 }
 
 template <int LDS, bool X_BF16, bool VEC, bool OUT_BF16>
-__global__ __launch_bounds__(64 * FEW_WAVES) void linear_i8_few_kernel(MatmulI8Args a, const void* x,
+__global__ __launch_bounds__(64 * FEW_WAVES) void linear_i8_few_kernel(MatmulI8Args a,
+                                                                       const void* x,
                                                                        int64_t x_ld) {
   __shared__ __attribute__((aligned(16))) char few_lds[LDS];  // quantised rows
   __shared__ int part[FEW_WAVES][64][4];
@@ -572,10 +567,22 @@ hipError_t few_launch(const MatmulI8Args& a, const void* x, int64_t x_ld, hipStr
 
 }  // namespace
 
-hipError_t launch_quantize_rows(const QuantArgs& a, hipStream_t s) {
-  const bool vec = aligned_rows(a.x, a.x_ld * (a.bf16 ? 2 : 4), 16);
-  if (a.bf16) return vec ? quantize_launch<true, true>(a, s) : quantize_launch<true, false>(a, s);
-  return vec ? quantize_launch<false, true>(a, s) : quantize_launch<false, false>(a, s);
+hipError_t launch_quantize_rows(const QuantArgs& args, hipStream_t s) {
+  const int64_t es = args.bf16 ? 2 : 4;
+  const bool vec = aligned_rows(args.x, args.x_ld * es, 16);
+  constexpr int64_t MOST = int64_t{1} << 23;  // rows a launch: a grid has less than 2^32 threads
+  for (int64_t r = 0; r < args.rows; r += MOST) {
+    QuantArgs a = args;
+    a.x = static_cast<const char*>(args.x) + r * args.x_ld * es;
+    a.q += r * a.q_ld;
+    a.scale += r;
+    a.rows = args.rows - r < MOST ? args.rows - r : MOST;
+    hipError_t e;
+    if (a.bf16) e = vec ? quantize_launch<true, true>(a, s) : quantize_launch<true, false>(a, s);
+    else e = vec ? quantize_launch<false, true>(a, s) : quantize_launch<false, false>(a, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // The first `rows` rows of a product in tiles of `tile`, and its time by what the

@@ -952,7 +952,7 @@ hipError_t launch_orthogonalize(const OrthMat* mats, int count, bool bf16, const
     amp *= std::fmax(1.0, std::fabs(static_cast<double>(c.a[t])));
     plain[t] = bf16 && amp <= 16.0;
   }
-  auto fmt = [&](int t) { return plain[t] ? static_cast<int>(NT_F16) : static_cast<int>(NT_SPLIT); };
+  auto fmt = [&](int t) -> int { return plain[t] ? NT_F16 : NT_SPLIT; };
   hipError_t e = hipSuccess;
   matrices_in_order(&g);
   if (!norms_done) {

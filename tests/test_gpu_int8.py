@@ -208,6 +208,51 @@ def test_linear_i8_longest_sums(P, n):
     assert (y[0] == float(want)).all() and (y[1] == -float(want)).all()
 
 
+def test_more_rows_than_threads_of_a_launch(P):
+    """2^26 + 5 rows: four a workgroup of 256 threads would be 2^32 threads and more.
+    Powers of two times 127: scales and integers are exact, whatever the division."""
+    import torch
+    n = (1 << 26) + 5
+    at = torch.arange(n, device="cuda")
+    k = torch.exp2((at % 11).float())
+    sign = torch.where(at % 3 == 0, -1.0, 1.0)
+    x = (127 * k * sign)[:, None]
+    q, scale = P.quantize_rows(x, out=(torch.full((n, 16), 5, dtype=torch.int8, device="cuda"),
+                                       torch.zeros(n, device="cuda")))
+    assert torch.equal(scale, k)
+    assert torch.equal(q[:, 0], (127 * sign).to(torch.int8))
+    assert not q[:, 1:].any()
+
+
+def test_outputs_past_32_bits(P):
+    """4.5e9 outputs (9 GB): the last rows are those of a call of their own."""
+    import torch
+    n, i, o = 1_100_003, 100, 4096
+    gen = torch.Generator("cuda")
+    gen.manual_seed(5)
+    x = torch.randn(n, i, generator=gen, device="cuda").bfloat16()
+    w, ws = P.quantize_rows(torch.randn(o, i, generator=gen, device="cuda"))
+    y = P.linear_i8(x, w, ws)
+    for rows in (slice(0, 300), slice(524200, 524400), slice(n - 700, n)):
+        assert torch.equal(y[rows], P.linear_i8(x[rows], w, ws))
+
+
+def test_two_streams_at_once(P):
+    import torch
+    w, ws = P.quantize_rows(torch.randn(1000, 500, device="cuda"))
+    xs = [torch.randn(n, 500, device="cuda") for n in (700, 3)]
+    want = [P.linear_i8(x, w, ws) for x in xs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[] for _ in streams]
+    for _ in range(10):
+        for s, x, g in zip(streams, xs, got):
+            with torch.cuda.stream(s):
+                g.append(P.linear_i8(x, w, ws))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, v) for g, v in zip(got, want) for y in g)
+
+
 @pytest.mark.parametrize("n", [4, 50])
 def test_linear_i8_rows_not_finite_or_zero(P, n):
     import torch

@@ -235,6 +235,57 @@ def test_orthogonalize_on_a_stream_and_in_a_graph(P):
         assert all(torch.equal(a, b) for a, b in zip(want, outs)), f"replay {k}"
 
 
+def test_orthogonalize_planes_past_32_bits(P):
+    """8192 x 65536: planes of more than 2^31 bytes, at offsets past 2^32.  All but
+    300 columns near the end are zero, and those are what they are beside fewer
+    zeros: a rounding of 2^-21 is amplified by at most the product of the |a|, and
+    each of the two results has its own."""
+    import torch
+    gen = torch.Generator("cuda")
+    gen.manual_seed(4)
+    cols = torch.randint(-9, 10, (8192, 300), generator=gen, device="cuda").float()
+    wide = torch.zeros(8192, 65536, device="cuda")
+    wide[:, 65216:65516] = cols
+    narrow = torch.zeros(8192, 8200, device="cuda")
+    narrow[:, :300] = cols
+    got, want = P.orthogonalize(wide), P.orthogonalize(narrow)
+    assert not got[:, :65216].any() and not got[:, 65516:].any() and not want[:, 300:].any()
+    got, want = got[:, 65216:65516].double(), want[:, :300].double()
+    amplified = np.prod([abs(a) for a, _, _ in COEFFS])
+    assert float((got - want).norm() / want.norm()) <= 2 * 2.0 ** -21 * amplified
+
+
+def test_two_streams_at_once(P):
+    """Calls on two streams have workspaces of their own."""
+    import torch
+    gs = [_gradient(300, 410, 1), _gradient(64, 64, 2)]
+    want = [P.orthogonalize(g) for g in gs]
+    streams = [torch.cuda.Stream() for _ in gs]
+    torch.cuda.synchronize()
+    got = [[] for _ in gs]
+    for k in range(8):
+        for s, g, res in zip(streams, gs, got):
+            if k % 2:
+                res.append(P.orthogonalize(g, stream=s))
+            else:
+                with torch.cuda.stream(s):
+                    res.append(P.orthogonalize(g))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for res, w in zip(got, want) for o in res)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -140, 2.0 ** -132, 2.0 ** 125])
+def test_orthogonalize_at_the_ends_of_fp32(P, scale):
+    """Entries below the normal numbers, and near the largest: the power of two
+    changes nothing that the entries still hold (in bf16, whose smallest number is
+    2^-133, 7 x 2^-140 is zero)."""
+    import torch
+    g = torch.randint(-7, 8, (40, 70), device="cuda").float()
+    for v in (g, g.bfloat16()):
+        held = ((v * scale).double() / scale).to(v.dtype)
+        assert torch.equal(P.orthogonalize(v * scale), P.orthogonalize(held))
+
+
 def test_orthogonalize_rejects(P):
     import torch
     g = torch.randn(8, 12, device="cuda")
@@ -271,6 +322,7 @@ def test_orthogonalize_rejects(P):
 
 MLP = ((264, 136, 72, 37), None)
 REG = ((24, 10), None)
+DEEP = ((40,) + (24, 32) * 7 + (16, 5), None)  # 16 layers, the most
 CNN = ((8 * 8 * 3, 10), ((8, 8, 3), ((16, 1), (16, 1), (16, 1, 1), (24, 2))))
 
 
@@ -301,7 +353,8 @@ def _matrices(ctx, flat):
             for w, b in ctx.unpack(flat.cpu().numpy())]
 
 
-@pytest.mark.parametrize("model,K", [(MLP, 8), (MLP, 3), (REG, 1), (CNN, 5), (REG, 33), (REG, 64)])
+@pytest.mark.parametrize("model,K", [(MLP, 8), (MLP, 3), (REG, 1), (CNN, 5), (REG, 33), (REG, 64),
+                                     (DEEP, 2)])
 @pytest.mark.parametrize("nesterov,decay", [(True, 0.0), (False, 0.1)])
 def test_server_step(P, model, K, nesterov, decay):
     import torch
