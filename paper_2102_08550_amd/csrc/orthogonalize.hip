@@ -147,18 +147,6 @@ __device__ __forceinline__ float lo_of(float v) {
   return v - static_cast<float>(static_cast<_Float16>(v));
 }
 
-// Four values k .. k + 3 (k a multiple of 4) of a plane row.
-__device__ __forceinline__ void put4(char* row, int k, int fmt, const float* v) {
-  const nt_u32x2 hi = {pack2(v[0], v[1]), pack2(v[2], v[3])};
-  if (fmt == NT_F16) {
-    *reinterpret_cast<nt_u32x2*>(row + 2 * static_cast<int64_t>(k)) = hi;
-  } else {
-    char* p = row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31);
-    *reinterpret_cast<nt_u32x2*>(p) = hi;
-    const nt_u32x2 lo = {pack2(lo_of(v[0]), lo_of(v[1])), pack2(lo_of(v[2]), lo_of(v[3]))};
-    *reinterpret_cast<nt_u32x2*>(p + 64) = lo;
-  }
-}
 // One 16-byte piece of a plane row: eight values from k (a multiple of 8), as hi
 // or as lo.  The pieces of a 128-byte line are stored by neighbouring lanes in
 // one instruction (store_lines): the L2 takes one request a line instead of one
@@ -190,28 +178,27 @@ __device__ __forceinline__ void store_lines(char* base, int64_t ld, int first, i
   }
 }
 
-// N values from k (both multiples of 4, within 16).
+// N values from k (both multiples of 4, within 16) of a plane row, as they are
+// stored: read by get, added up by value where they are used.
 template <int N>
-__device__ __forceinline__ void get(const char* row, int k, int fmt, float* v) {
+struct Stored {
   typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-  const h4* p = reinterpret_cast<const h4*>(
-      fmt == NT_F16 ? row + 2 * static_cast<int64_t>(k)
-                    : row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31));
-#pragma unroll
-  for (int i = 0; i < N / 4; ++i) {
-    const h4 h = p[i];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) v[4 * i + t] = static_cast<float>(h[t]);
-  }
-  if (fmt != NT_F16) {
+  h4 hi[N / 4], lo[N / 4];
+  __device__ __forceinline__ void get(const char* row, int k, int fmt) {
+    const h4* p = reinterpret_cast<const h4*>(
+        fmt == NT_F16 ? row + 2 * static_cast<int64_t>(k)
+                      : row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31));
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-      const h4 l = p[8 + i];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) v[4 * i + t] += static_cast<float>(l[t]);
+      hi[i] = p[i];
+      if (fmt != NT_F16) lo[i] = p[8 + i];
     }
   }
-}
+  __device__ __forceinline__ float value(int e, int fmt) const {
+    const float v = static_cast<float>(hi[e / 4][e & 3]);
+    return fmt == NT_F16 ? v : v + static_cast<float>(lo[e / 4][e & 3]);
+  }
+};
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t v) {
   return __builtin_bit_cast(float, static_cast<uint32_t>(v) << 16);
@@ -447,19 +434,20 @@ struct Product {
   __device__ __forceinline__ char* straight() const {
     return KIND == ORTH_GRAM ? a : KIND == ORTH_POLY ? p : x;
   }
-  // Rows r .. r + N - 1 of column c: POLY's other terms, zeros in the planes'
-  // padding.  `fmt`: POLY, of A.
+  // POLY: rows r .. r + N - 1 of column c of A, in `fmt`.
   template <int N>
-  __device__ __forceinline__ void finish(const OrthArgs& g, int r, int c, int fmt, float* v) const {
+  __device__ __forceinline__ void load_a(int r, int c, int fmt, Stored<N>* t) const {
+    // A(r, c) = A(c, r), consecutive
+    if (KIND == ORTH_POLY) t->get(a + (c < C ? c : C - 1) * row_bytes(m, fmt), r, fmt);
+  }
+  // Rows r .. r + N - 1 of column c: POLY's other terms (t of load_a), zeros in
+  // the planes' padding.
+  template <int N>
+  __device__ __forceinline__ void finish(const OrthArgs& g, int r, int c, int fmt,
+                                         const Stored<N>& t, float* v) const {
     if constexpr (KIND == ORTH_POLY) {
-      if (c < C) {
-        // A(r, c) = A(c, r), consecutive
-        float t[N];
-        get<N>(a + c * row_bytes(m, fmt), r, fmt, t);
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          v[e] += g.b * t[e] + (r + e == c ? g.a * kScaleA : 0.0f);
-      }
+      for (int e = 0; e < N; ++e) v[e] += g.b * t.value(e, fmt) + (r + e == c ? g.a * kScaleA : 0.0f);
     }
     if constexpr (KIND != ORTH_LAST) {
 #pragma unroll
@@ -595,7 +583,9 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
 #pragma unroll
           for (int o = 0; o < 4; ++o) v[4 * e + o] = t[o];
         }
-        p.template finish<16>(g, rb0 + k16, cb0 + line, PF, v);
+        Stored<16> t;
+        p.load_a(rb0 + k16, cb0 + line, PF, &t);
+        p.finish(g, rb0 + k16, cb0 + line, PF, t, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *reinterpret_cast<nt_f32x4*>(mine + 4 * e) =
@@ -632,7 +622,8 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
 //   RING 2 (64 KB): up to two workgroups a CU, all there at once;
 //   RING 1 (32 KB): more of them, five a CU cover for each other.
 // (Calls of 17 launches: 512 x 512 106 us with RING 2, 113 with 1; 16 of 256 x 256
-// 183 and 161.  Eight waves, K in eight: 8 us more a call at 64 x 64, 14 less
+// 183 and 161.  RING 4: 6 us more a call at 64 x 64, 4 more at 256 x 8192, where
+// what a CU can take from the L2 is the bound.  Eight waves, K in eight: 8 us more a call at 64 x 64, 14 less
 // at 256 x 8192.)
 constexpr int SMALL_WAVES = 4;
 template <int KIND, int F, int RING>
@@ -675,6 +666,11 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
     ra.issue(t, at, lane);
     rb.issue(t + STAGE / 2, at, lane);
   };
+  // the wave finishes rows 8 w + 4 h .. + 3 of column (lane & 31)
+  const int r = r0 + 8 * wave + 4 * h, c = c0 + (lane & 31);
+  Stored<4> terms;
+  p.load_a(r, c, PF, &terms);     // on its way during the products
+  asm volatile("" ::: "memory");  // ahead of the blocks, whose waits count what follows
   nt_f32x16 acc, cross;
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = cross[e] = 0.0f;
@@ -716,9 +712,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
 #pragma unroll
   for (int e = 0; e < 16; ++e) sums[(wave * 16 + e) * 64 + lane] = acc[e] + cross[e];
   __syncthreads();
-  // wave w finishes rows 8 w + 4 h .. + 3 of column (lane & 31)
   const float f = p.factor(g);
-  const int r = r0 + 8 * wave + 4 * h, c = c0 + (lane & 31);
   float v[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
@@ -727,32 +721,41 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
     for (int w = 0; w < SMALL_WAVES; ++w) s += sums[(w * 16 + 4 * wave + t) * 64 + lane];
     v[t] = s * f;
   }
-  p.template finish<4>(g, r, c, PF, v);
+  p.finish(g, r, c, PF, terms, v);
+  // Through LDS, turned[column][row], so that eight lanes store a whole line: of
+  // the caller's row, or 32 entries of a plane's.
+  float* turn = sums + SMALL_WAVES * 16 * 64;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) turn[(lane & 31) * TURN + 8 * wave + 4 * h + t] = v[t];
+  __syncthreads();
+  const int i = 8 * wave + (lane >> 3);
   if constexpr (KIND == ORTH_LAST) {
-    p.template out<4>(g, r, c, v);
+    const int k = 4 * (lane & 7);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = turn[i * TURN + k + t];
+    p.template out<4>(g, r0 + k, c0 + i, v);
   } else {
     const int fmt1 = KIND == ORTH_GRAM ? g.p_fmt : KIND == ORTH_POLY ? PF : g.xt_fmt;
     const int fmt2 = KIND == ORTH_APPLY ? g.x_fmt : fmt1;
+    const int k = 8 * (lane & 3);
+    const bool lo = lane & 4;
     // rows are padded to 64 entries: the last tile zeros what no tile covers
-    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (c < p.C) {
-      char* row = p.turned() + c * row_bytes(p.R, fmt1);
-      put4(row, r, fmt1, v);
-      if (r0 + 32 >= p.R && r + 32 < pad64(p.R)) put4(row, r + 32, fmt1, none);
+    const float none[8] = {};
+    float w[8];
+    if (c0 + i < p.C && (fmt1 != NT_F16 || !lo)) {
+      char* row = p.turned() + (c0 + i) * row_bytes(p.R, fmt1);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) w[t] = turn[i * TURN + k + t];
+      put8(row, r0 + k, fmt1, lo, w);
+      if (r0 + 32 >= p.R && r0 + 32 < pad64(p.R)) put8(row, r0 + 32 + k, fmt1, lo, none);
     }
-    if (Prod::SYM && ti == tj) return;  // uniform over the workgroup
-    float* turn = sums + SMALL_WAVES * 16 * 64;
+    if (Prod::SYM && ti == tj) return;
+    if (r0 + i < p.R && (fmt2 != NT_F16 || !lo)) {
+      char* row = p.straight() + (r0 + i) * row_bytes(p.C, fmt2);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) turn[(8 * wave + 4 * h + t) * TURN + (lane & 31)] = v[t];
-    __syncthreads();
-    const int row = tid >> 3, k = 4 * (tid & 7);
-    float w[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) w[t] = turn[row * TURN + k + t];
-    if (r0 + row < p.R) {
-      char* to = p.straight() + (r0 + row) * row_bytes(p.C, fmt2);
-      put4(to, c0 + k, fmt2, w);
-      if (c0 + 32 >= p.C && c0 + k + 32 < pad64(p.C)) put4(to, c0 + k + 32, fmt2, none);
+      for (int t = 0; t < 8; ++t) w[t] = turn[(k + t) * TURN + i];
+      put8(row, c0 + k, fmt2, lo, w);
+      if (c0 + 32 >= p.C && c0 + 32 < pad64(p.C)) put8(row, c0 + 32 + k, fmt2, lo, none);
     }
   }
 #endif
