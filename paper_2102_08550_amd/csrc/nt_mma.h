@@ -148,122 +148,88 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int firs
     for (int j = 0; j < S::NJ; ++j) fb[j] = nt_read(t + ABYTES, brow + 32 * j, 2 * c + h);
   };
 
-  if constexpr (S::NT == 512) {
-    static_assert(S::ST == 2 && !CROSS, "two stages, one set of accumulators");
-    // the scheduler keeps loads and products in the order written
-    auto mul = [&](nt_u32x4(&fa)[S::MI], nt_u32x4(&fb)[S::NJ]) {
-      __builtin_amdgcn_sched_barrier(0);
+  static_assert(S::ST == 2, "two stages");
+  // NT_SPLIT's products with a lo plane
+  Acc cross[CROSS ? S::MI : 1][CROSS ? S::NJ : 1];
+  if constexpr (CROSS) {
 #pragma unroll
-      for (int i = 0; i < S::MI; ++i)
+    for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-        for (int j = 0; j < S::NJ; ++j) acc[i][j] = nt_mfma<F>(fa[i], fb[j], acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    nt_u32x4 a0[S::MI], a1[S::MI], b0[S::NJ], b1[S::NJ], b2[S::NJ];
-    issue(0);
-    nt_wait_vm<0>();
-    nt_barrier();
-    issue(1);
-    load_a(lds, 0, a0);
-    load_b(lds, 0, b0);
-    for (int s = 0; s < blocks; ++s) {
-      const char* t = lds + (s & 1) * STAGE;
-      const char* next = lds + ((s + 1) & 1) * STAGE;
-      // what the last group multiplies is a1 and, of b, b2 (SPLIT) or b1
-      if constexpr (SPLIT) {
-        if constexpr (F == NT_SPLIT) {
-          load_b(t, 2, b1);
-          mul(a0, b0);  // hi hi, the first 16 of K
-          load_a(t, 2, a1);
-          mul(a0, b1);  // hi lo
-        } else {
-          load_a(t, 2, a1);
-          mul(a0, b0);
-        }
-        load_a(t, 1, a0);
-        load_b(t, 1, b2);
-        mul(a1, b0);  // lo hi
-        if constexpr (F == NT_SPLIT) {
-          load_b(t, 3, b1);
-          mul(a0, b2);  // the second 16
-          load_a(t, 3, a1);
-          mul(a0, b1);
-        } else {
-          load_a(t, 3, a1);
-          mul(a0, b2);
-        }
+      for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) cross[i][j][e] = 0;
+  }
+  auto& low = [&]() -> Acc(&)[S::MI][S::NJ] {
+    if constexpr (CROSS) return cross;
+    else return acc;
+  }();
+  // the scheduler keeps loads and products in the order written
+  auto mul = [&](nt_u32x4(&fa)[S::MI], nt_u32x4(&fb)[S::NJ], Acc(&to)[S::MI][S::NJ]) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) to[i][j] = nt_mfma<F>(fa[i], fb[j], to[i][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  nt_u32x4 a0[S::MI], a1[S::MI], b0[S::NJ], b1[S::NJ], b2[S::NJ];
+  issue(0);
+  nt_wait_vm<0>();
+  nt_barrier();
+  issue(1);
+  load_a(lds, 0, a0);
+  load_b(lds, 0, b0);
+  for (int s = 0; s < blocks; ++s) {
+    const char* t = lds + (s & 1) * STAGE;
+    const char* next = lds + ((s + 1) & 1) * STAGE;
+    // what the last group multiplies is a1 and, of b, b2 (SPLIT) or b1
+    if constexpr (SPLIT) {
+      if constexpr (F == NT_SPLIT) {
+        load_b(t, 2, b1);
+        mul(a0, b0, acc);  // hi hi, the first 16 of K
+        load_a(t, 2, a1);
+        mul(a0, b1, low);  // hi lo
       } else {
-        load_a(t, 1, a1);
-        load_b(t, 1, b1);
-        mul(a0, b0);
-        load_a(t, 2, a0);
-        load_b(t, 2, b0);
-        mul(a1, b1);
-        load_a(t, 3, a1);
+        load_a(t, 2, a1);
+        mul(a0, b0, acc);
+      }
+      load_a(t, 1, a0);
+      load_b(t, 1, b2);
+      mul(a1, b0, low);  // lo hi
+      if constexpr (F == NT_SPLIT) {
         load_b(t, 3, b1);
-        mul(a0, b0);
-      }
-      nt_wait_vm<0>();  // the next stage is there,
-      nt_barrier();     // and this one read by every wave
-      if (s + 2 < blocks) issue(s + 2);
-      load_a(next, 0, a0);
-      load_b(next, 0, b0);
-      if constexpr (SPLIT) mul(a1, b2);
-      else mul(a1, b1);
-    }
-    nt_wait_vm<0>();
-  } else {
-    Acc cross[CROSS ? S::MI : 1][CROSS ? S::NJ : 1];
-    if constexpr (CROSS) {
-#pragma unroll
-      for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-        for (int j = 0; j < S::NJ; ++j)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) cross[i][j][e] = 0;
-    }
-    for (int s = 0; s < S::ST - 1; ++s) issue(s);
-    for (int s = 0; s < blocks; ++s) {
-      nt_wait_vm<(S::ST - 2) * PER>();
-      nt_barrier();
-      issue(s + S::ST - 1);
-      const char* t = lds + (s % S::ST) * STAGE;
-      auto step = [&](int ca, int cb) {
-        nt_u32x4 fa[S::MI], fb[S::NJ];
-        load_b(t, cb, fb);
-        load_a(t, ca, fa);
-#pragma unroll
-        for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-          for (int j = 0; j < S::NJ; ++j) {
-            if constexpr (CROSS) {
-              if (ca != cb || ca > 1) {  // known at compile time: a lo plane
-                cross[i][j] = nt_mfma<F>(fa[i], fb[j], cross[i][j]);
-                continue;
-              }
-            }
-            acc[i][j] = nt_mfma<F>(fa[i], fb[j], acc[i][j]);
-          }
-      };
-      if constexpr (SPLIT) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          step(k, k);
-          if constexpr (F == NT_SPLIT) step(k, 2 + k);
-          step(2 + k, k);
-        }
+        mul(a0, b2, acc);  // the second 16
+        load_a(t, 3, a1);
+        mul(a0, b1, low);
       } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) step(k, k);
+        load_a(t, 3, a1);
+        mul(a0, b2, acc);
       }
+    } else {
+      load_a(t, 1, a1);
+      load_b(t, 1, b1);
+      mul(a0, b0, acc);
+      load_a(t, 2, a0);
+      load_b(t, 2, b0);
+      mul(a1, b1, acc);
+      load_a(t, 3, a1);
+      load_b(t, 3, b1);
+      mul(a0, b0, acc);
     }
-    nt_wait_vm<0>();
-    if constexpr (CROSS) {
+    nt_wait_vm<0>();  // the next stage is there,
+    nt_barrier();     // and this one read by every wave
+    if (s + 2 < blocks) issue(s + 2);
+    load_a(next, 0, a0);
+    load_b(next, 0, b0);
+    if constexpr (SPLIT) mul(a1, b2, low);
+    else mul(a1, b1, acc);
+  }
+  nt_wait_vm<0>();
+  if constexpr (CROSS) {
 #pragma unroll
-      for (int i = 0; i < S::MI; ++i)
+    for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-        for (int j = 0; j < S::NJ; ++j) acc[i][j] += cross[i][j];
-    }
+      for (int j = 0; j < S::NJ; ++j) acc[i][j] += cross[i][j];
   }
 }
 
