@@ -196,8 +196,8 @@ bool aligned_rows(const void* p, int64_t row_bytes, int to) {
 
 // ------------------------------------------------------------------ tiles
 
-typedef NtShape<256, 256, 2, 4, 2> I8L;
-typedef NtShape<128, 128, 2, 2, 2> I8M;
+typedef NtShape<256, 256, 2, 4> I8L;
+typedef NtShape<128, 128, 2, 2> I8M;
 
 __device__ __forceinline__ float i8_finish(int32_t acc, float sx, float sw, float b, bool relu) {
   float y = static_cast<float>(acc) * (sx * sw) + b;
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(S::NT, 2) void matmul_i8_kernel(MatmulI8Args a) {
     for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-  nt_tile<S, NT_I8>(ra, rb, 0, blocks, lds, tid, acc);
+  nt_tile<S, NT_I8>(ra, rb, blocks, lds, tid, acc);
 
   const int rw = r0 + (wave / S::WN) * 32 * S::MI;
   const int64_t cw = c0 + (wave % S::WN) * 32 * S::NJ;

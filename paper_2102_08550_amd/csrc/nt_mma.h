@@ -45,18 +45,18 @@ __device__ __forceinline__ typename NtAcc<F>::type nt_mfma(nt_u32x4 a, nt_u32x4 
                                                   __builtin_bit_cast(nt_f16x8, b), c, 0, 0, 0);
 }
 
-// Workgroup tile: BM x BN outputs, WM x WN waves, ST stages in LDS.  EXACT, where
+// Workgroup tile: BM x BN outputs, WM x WN waves, two stages in LDS.  EXACT, where
 // there are registers for it: NT_SPLIT's products with a lo plane have accumulators
 // of their own, added at the end.  Every product rounds the sum it goes into, and
 // the small ones would round the large sum two more times.  Five Newton-Schulz
 // steps of 10 x 256 matrices, error in 2-norm, median and worst of 24: 1.2e-6 and
 // 1.5e-6 without, 7.3e-7 and 1.3e-6 with; in fp32 6.1e-7 and 7.7e-7.
-template <int BM_, int BN_, int WM_, int WN_, int ST_, bool EXACT_ = false>
+template <int BM_, int BN_, int WM_, int WN_, bool EXACT_ = false>
 struct NtShape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr bool EXACT = EXACT_;
   static constexpr int NT = 64 * WM * WN, MI = BM / WM / 32, NJ = BN / WN / 32;
-  static constexpr int LDS_BYTES = ST * (BM + BN) * NT_BLOCK;
+  static constexpr int LDS_BYTES = 2 * (BM + BN) * NT_BLOCK;
   static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0, "whole matrix blocks per wave");
 };
 
@@ -87,12 +87,14 @@ struct NtRows {
     }
   }
   // wave w's instruction p fills tile rows (64 w + NTHR p) / 8 .. + 7
+  __device__ __forceinline__ void issue(char* tile, int kbyte, int tid, int p) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void*)(tile + ((tid & ~63) + NTHR * p) * 16), 16,
+        voff[p], kbyte, 0, 0);
+  }
   __device__ __forceinline__ void issue(char* tile, int kbyte, int tid) const {
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc, (__attribute__((address_space(3))) void*)(tile + ((tid & ~63) + NTHR * p) * 16),
-          16, voff[p], kbyte, 0, 0);
+    for (int p = 0; p < P; ++p) issue(tile, kbyte, tid, p);
   }
 };
 
@@ -111,33 +113,46 @@ __device__ __forceinline__ nt_u32x4 nt_read(const char* tile, int row, int chunk
                                             16 * (chunk ^ ((row ^ (row >> 3)) & 7)));
 }
 
-// acc[i][j] += the tile's products over `blocks` K blocks from block `first` on.
-// lds: S::LDS_BYTES, free (the caller puts a barrier between two calls).  Ends
-// with nothing in flight.
+// acc[i][j] += the tile's products over `blocks` K blocks.  lds: S::LDS_BYTES,
+// free.  Ends with nothing in flight.
 //
-// Eight waves of a 256 x 256 tile (two a SIMD) run in step, so what every stage
-// begins with, a barrier and the first operands' way from LDS, would leave the
-// matrix units idle.  There the stage's last products are issued behind the
-// barrier that ends it, with the next stage's first operands on their way, and
-// each group of products has the next group's operands loaded in front of it.
-// 4096 x 4096 with K = 4096: NT_SPLIT 1266 -> 1330 TFLOP/s of matrix work, int8
-// 2022 -> 2139, fp16 at 8192 996 -> 1188 (torch's product of 8192: 1393, int8
-// 2122).  Tiles of 128 x 128 overlap two workgroups instead: no difference.
+// A stage begins with a barrier and the first operands' way from LDS, and its loads
+// (eight a wave, 16 bytes a lane) hold the wave up while they are issued: the
+// L2 gives a CU 64 bytes a cycle, 512 cycles for the stage of a 128 x 128 tile.
+// So the stage's last products are issued behind the barrier that ends it, with
+// the next stage's first operands on their way, each group of products has the
+// next group's operands loaded in front of it, and the loads go out in four parts
+// between the groups.  4096 x 4096, K = 4096: NT_SPLIT 1266 TFLOP/s of matrix work
+// without all that, 1330 with, int8 2022 and 2139, fp16 at 8192 996 and 1188
+// (torch's product of 8192: 1393, int8 2122); the loads in parts are 7% of 8191 x
+// 4096 x 4096 in int8, 3% of 4096 x 4096 in NT_SPLIT.  A 128 x 128 tile's stage is too short
+// for that: its later parts would come too late (2048 x 2048 11% slower); three stages,
+// one workgroup a CU, lose more with 512 tiles than they gain with 256.  Two such
+// workgroups overlap; one alone (a 128 x 128 tile a CU, four waves) takes 0.71 us a block,
+// 0.38 without its loads and LDS reads, 0.50 without the loads, 0.59 without the reads.
 template <class S, int F, class RowsA, class RowsB, class Acc>
-__device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int first, int blocks,
-                                        char* lds, int tid, Acc (&acc)[S::MI][S::NJ]) {
+__device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int blocks, char* lds,
+                                        int tid, Acc (&acc)[S::MI][S::NJ]) {
   constexpr int ABYTES = S::BM * NT_BLOCK, STAGE = (S::BM + S::BN) * NT_BLOCK;
-  constexpr int PER = RowsA::P + RowsB::P;
   constexpr bool SPLIT = F == NT_SPLIT || F == NT_SPLIT_B0, CROSS = S::EXACT && SPLIT;
   const int lane = tid & 63, wave = tid >> 6;
   const int arow = (wave / S::WN) * 32 * S::MI + (lane & 31);
   const int brow = (wave % S::WN) * 32 * S::NJ + (lane & 31), h = lane >> 5;
-  auto issue = [&](int s) {
-    // past the end the last block is loaded again: the number in flight stays the same
-    const int k = (first + (s < blocks ? s : blocks - 1)) * NT_BLOCK;
-    char* t = lds + (s % S::ST) * STAGE;
-    a.issue(t, k, tid);
-    b.issue(t + ABYTES, k, tid);
+  static_assert(RowsA::P == 4 && RowsB::P == 4, "stages in four parts");
+  constexpr bool SPREAD = S::NT == 512;
+  auto issue = [&](int s, int part) {
+    if (s >= blocks) return;
+    const int k = s * NT_BLOCK;
+    char* t = lds + (s & 1) * STAGE;
+    a.issue(t, k, tid, part);
+    b.issue(t + ABYTES, k, tid, part);
+  };
+  auto issue_rest = [&](int s) {
+#pragma unroll
+    for (int part = 1; part < 4; ++part) issue(s, part);
+  };
+  auto later = [&](int s, int part) {
+    if constexpr (SPREAD) issue(s, part);
   };
   auto load_a = [&](const char* t, int c, nt_u32x4(&fa)[S::MI]) {
 #pragma unroll
@@ -148,7 +163,6 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int firs
     for (int j = 0; j < S::NJ; ++j) fb[j] = nt_read(t + ABYTES, brow + 32 * j, 2 * c + h);
   };
 
-  static_assert(S::ST == 2, "two stages");
   // NT_SPLIT's products with a lo plane
   Acc cross[CROSS ? S::MI : 1][CROSS ? S::NJ : 1];
   if constexpr (CROSS) {
@@ -173,10 +187,12 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int firs
     __builtin_amdgcn_sched_barrier(0);
   };
   nt_u32x4 a0[S::MI], a1[S::MI], b0[S::NJ], b1[S::NJ], b2[S::NJ];
-  issue(0);
+  issue(0, 0);
+  issue_rest(0);
   nt_wait_vm<0>();
   nt_barrier();
-  issue(1);
+  issue(1, 0);
+  if constexpr (!SPREAD) issue_rest(1);
   load_a(lds, 0, a0);
   load_b(lds, 0, b0);
   for (int s = 0; s < blocks; ++s) {
@@ -184,15 +200,19 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int firs
     const char* next = lds + ((s + 1) & 1) * STAGE;
     // what the last group multiplies is a1 and, of b, b2 (SPLIT) or b1
     if constexpr (SPLIT) {
+      later(s + 1, 1);
       if constexpr (F == NT_SPLIT) {
         load_b(t, 2, b1);
         mul(a0, b0, acc);  // hi hi, the first 16 of K
+        later(s + 1, 2);
         load_a(t, 2, a1);
         mul(a0, b1, low);  // hi lo
       } else {
+        later(s + 1, 2);
         load_a(t, 2, a1);
         mul(a0, b0, acc);
       }
+      later(s + 1, 3);
       load_a(t, 1, a0);
       load_b(t, 1, b2);
       mul(a1, b0, low);  // lo hi
@@ -206,9 +226,12 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int firs
         mul(a0, b2, acc);
       }
     } else {
+      later(s + 1, 1);
       load_a(t, 1, a1);
       load_b(t, 1, b1);
       mul(a0, b0, acc);
+      later(s + 1, 2);
+      later(s + 1, 3);
       load_a(t, 2, a0);
       load_b(t, 2, b0);
       mul(a1, b1, acc);
@@ -218,7 +241,8 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int firs
     }
     nt_wait_vm<0>();  // the next stage is there,
     nt_barrier();     // and this one read by every wave
-    if (s + 2 < blocks) issue(s + 2);
+    issue(s + 2, 0);
+    if constexpr (!SPREAD) issue_rest(s + 2);
     load_a(next, 0, a0);
     load_b(next, 0, b0);
     if constexpr (SPLIT) mul(a1, b2, low);

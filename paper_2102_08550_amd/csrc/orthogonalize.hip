@@ -31,8 +31,8 @@
 namespace oscars {
 namespace {
 
-typedef NtShape<256, 256, 2, 4, 2> OrthL;
-typedef NtShape<128, 128, 2, 2, 2, true> OrthM;
+typedef NtShape<256, 256, 2, 4> OrthL;
+typedef NtShape<128, 128, 2, 2, true> OrthM;
 
 enum OrthKind { ORTH_GRAM = 0, ORTH_POLY = 1, ORTH_APPLY = 2, ORTH_LAST = 3 };
 
@@ -403,16 +403,26 @@ struct Product {
   // `id`: of the matrix's tiles of B x B
   template <int B>
   __device__ __forceinline__ void tile(int id, int* ti, int* tj) const {
+    // bands of four tile rows, column by column: a band's operands stay in L2
+    constexpr int BAND = 4;
     const int tr = (R + B - 1) / B, tc = (C + B - 1) / B;
     if (SYM) {
+      // a band has the columns left of its first row, then a triangle
       int i = static_cast<int>((sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
       while (i * (i + 1) / 2 > id) --i;
       while ((i + 1) * (i + 2) / 2 <= id) ++i;
-      *ti = i;
-      *tj = id - i * (i + 1) / 2;
+      const int top = i / BAND * BAND, rows = tr - top < BAND ? tr - top : BAND;
+      int at = id - top * (top + 1) / 2;
+      if (at < rows * top) {
+        *ti = top + at % rows;
+        *tj = at / rows;
+      } else {
+        at -= rows * top;
+        const int r = at < 1 ? 0 : at < 3 ? 1 : at < 6 ? 2 : 3;
+        *ti = top + r;
+        *tj = top + at - r * (r + 1) / 2;
+      }
     } else {
-      // bands of four tile rows, column by column: a band's operands stay in L2
-      constexpr int BAND = 4;
       const int band = id / (BAND * tc), rows = tr - band * BAND < BAND ? tr - band * BAND : BAND;
       const int at = id - band * BAND * tc;
       *ti = band * BAND + at % rows;
@@ -447,7 +457,8 @@ struct Product {
                                          const Stored<N>& t, float* v) const {
     if constexpr (KIND == ORTH_POLY) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] += g.b * t.value(e, fmt) + (r + e == c ? g.a * kScaleA : 0.0f);
+      for (int e = 0; e < N; ++e)
+        v[e] += g.b * t.value(e, fmt) + (r + e == c ? g.a * kScaleA : 0.0f);
     }
     if constexpr (KIND != ORTH_LAST) {
 #pragma unroll
@@ -534,7 +545,7 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
     for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  nt_tile<S, F>(ra, rb, 0, row_blocks(p.K, PF), lds, tid, acc);
+  nt_tile<S, F>(ra, rb, row_blocks(p.K, PF), lds, tid, acc);
 
   // Block by block through LDS of the wave's own, turned[column][row]: a lane's
   // four consecutive rows lie together, and both the columns (the turned
@@ -623,8 +634,8 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
 //   RING 1 (32 KB): more of them, five a CU cover for each other.
 // (Calls of 17 launches: 512 x 512 106 us with RING 2, 113 with 1; 16 of 256 x 256
 // 183 and 161.  RING 4: 6 us more a call at 64 x 64, 4 more at 256 x 8192, where
-// what a CU can take from the L2 is the bound.  Eight waves, K in eight: 8 us more a call at 64 x 64, 14 less
-// at 256 x 8192.)
+// what a CU can take from the L2 is the bound.  Eight waves, K in eight: 8 us more
+// at 64 x 64, 14 less at 256 x 8192.)
 constexpr int SMALL_WAVES = 4;
 template <int KIND, int F, int RING>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g) {
