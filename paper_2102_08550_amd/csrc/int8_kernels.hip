@@ -590,8 +590,8 @@ hipError_t launch_quantize_rows(const QuantArgs& args, hipStream_t s) {
 //   32    3.5, and 2100 blocks a us over all CUs
 //   128   8, and a block 0.55 while no CU has two tiles, else 1.2 for 512 at a time,
 //         of which the last up to 256 take 0.75
-//   256   12, and a block 1.5 while half of the CUs have a tile, 1.95 up to all
-//         of them, else 2.05 for 256 at a time
+//   256   20, and a block 1.15 while half of the CUs have a tile, 1.55 up to all
+//         of them, else 1.75 for 256 at a time
 // Rows x inputs x outputs, measured with 32 / 128 / 256: 256 x 4096 x 1000: 7.0 /
 // 24.4 / 53, 1024 x 2048 x 2048: 19.9 / 17.9 / 34.5, 10000 x 2048 x 2048: 155 / 65 /
 // 76, 4096 x 4096 x 4096: 235 / 86 / 74.
@@ -614,7 +614,7 @@ I8Plan i8_plan(const MatmulI8Args& a, int64_t rows) {
       us = 8.0 + k * (n <= 256.0 ? 0.55
                                  : 1.2 * turns + (last > 256.0 ? 1.2 : last > 0.0 ? 0.75 : 0.0));
     else
-      us = 12.0 + k * (n <= 144.0 ? 1.5 : n <= 256.0 ? 1.95 : 2.05 * std::ceil(n / 256.0));
+      us = 20.0 + k * (n <= 144.0 ? 1.15 : n <= 256.0 ? 1.55 : 1.75 * std::ceil(n / 256.0));
     if (best.tile == 0 || us < best.us) {
       best.tile = t;
       best.us = us;
