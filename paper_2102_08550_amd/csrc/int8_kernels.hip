@@ -592,9 +592,9 @@ hipError_t launch_quantize_rows(const QuantArgs& args, hipStream_t s) {
 //         of which the last up to 256 take 0.75
 //   256   20, and a block 1.15 while half of the CUs have a tile, 1.55 up to all
 //         of them, else 1.75 for 256 at a time
-// Rows x inputs x outputs, measured with 32 / 128 / 256: 256 x 4096 x 1000: 7.0 /
-// 24.4 / 53, 1024 x 2048 x 2048: 19.9 / 17.9 / 34.5, 10000 x 2048 x 2048: 155 / 65 /
-// 76, 4096 x 4096 x 4096: 235 / 86 / 74.
+// Rows x inputs x outputs, measured with 32 / 128 / 256: 256 x 4096 x 1000: 7.1 /
+// 24.3 / 47.1, 1024 x 2048 x 2048: 20.4 / 17.9 / 31.7, 3000 x 3000 x 3000: 108 / 52 /
+// 45.5, 10000 x 2048 x 2048: 168 / 64.5 / 72, 4096 x 4096 x 4096: 229 / 82.5 / 69.2.
 struct I8Plan {
   int tile;
   int64_t rows;

@@ -834,22 +834,22 @@ hipError_t launch_product_small(OrthArgs& g, hipStream_t s, int rest) {
 
 // A product's time in us with tiles of 32, 128 or 256, from what the kernels take
 // on this card (NT_SPLIT; a K block of 32 values):
-//   32    4 us, and 1870 blocks a us over all CUs
+//   32    4 us, and 2400 blocks a us over all CUs
 //   128   9 us, and a block 0.75 us while no CU has two tiles, else 1.45 us for
 //         512 at a time
 //   256   20 us, and a block 2.1 us while half of the CUs have a tile, else 2.45 us
 //         for 256 at a time
 // and, with more tiles than fit at once, some of a tile for the CUs that run dry.
 // Where a few tiles of 128 are left after full turns of one or two to a CU, they
-// are done in tiles of 32 by a second launch, 9 us and their blocks: one matrix of
-// 4096 (two turns of 256 and 16 left) went from 4329 to 3883 us (bf16 3121 to 2774),
+// are done in tiles of 32 by a second launch, 9 us and 1870 blocks a us: one matrix
+// of 4096 (two turns of 256 and 16 left) went from 4329 to 3883 us (bf16 3121 to 2774),
 // 2900 from 2170 to 1919, two of 2048 from 1432 to 1338; eight of 1024 (32 blocks of
 // K, 32 tiles left) would have gone from 886 to 1000.
-// Whole calls, fp32 (32 / 128 / 256, us): 512: 112 / 352 / 783, 1280: 401 / 602 /
-// 1390, 2048: 1331 / 862 / 1999, 4096: 10214 / 4402 / 4100; three 4096 x 4096 and
-// 1000 x 4096: 31327 / 12011 / 11216.  (Tiles cut along K, their sums joined by
-// the last workgroup to arrive, were slower everywhere but there by 3%: the sums'
-// way through memory and the caches' write-back.)
+// Whole calls, fp32 (32 / 128 / 256, us): 512: 107 / 344 / 753, 1280: 357 / 583 /
+// 1329, 2048: 1087 / 847 / 1908, 3328: 4245 / 2445 / 2932, 4096: 7895 / 4422 / 3984;
+// three 4096 x 4096 and 1000 x 4096: 24179 / 11673 / 10962.  (Tiles cut along K,
+// their sums joined by the last workgroup to arrive, were slower everywhere but
+// there by 3%: the sums' way through memory and the caches' write-back.)
 // `most`: of the tiles of 128, those done as such; the others are done in tiles of 32.
 int best_tile(const OrthArgs& g, int kind, int fmt, int64_t* most) {
   int best = 0;
@@ -864,7 +864,7 @@ int best_tile(const OrthArgs& g, int kind, int fmt, int64_t* most) {
     }
     double us;
     if (bt == 32)
-      us = 4.0 + blocks / 1870.0;
+      us = 4.0 + blocks / 2400.0;
     else if (bt == 128)
       us = 9.0 + (tiles <= 256.0 ? 0.75 * longest : 1.45 * (blocks / 512.0 + 0.3 * longest));
     else
