@@ -117,19 +117,21 @@ __device__ __forceinline__ nt_u32x4 nt_read(const char* tile, int row, int chunk
 // free.  Ends with nothing in flight.
 //
 // A stage begins with a barrier and the first operands' way from LDS, and its loads
-// (eight a wave, 16 bytes a lane) hold the wave up while they are issued: the
-// L2 gives a CU 64 bytes a cycle, 512 cycles for the stage of a 128 x 128 tile.
-// So the stage's last products are issued behind the barrier that ends it, with
-// the next stage's first operands on their way, each group of products has the
-// next group's operands loaded in front of it, and the loads go out in four parts
-// between the groups.  4096 x 4096, K = 4096: NT_SPLIT 1266 TFLOP/s of matrix work
-// without all that, 1330 with, int8 2022 and 2139, fp16 at 8192 996 and 1188
-// (torch's product of 8192: 1393, int8 2122); the loads in parts are 7% of 8191 x
-// 4096 x 4096 in int8, 3% of 4096 x 4096 in NT_SPLIT.  A 128 x 128 tile's stage is too short
-// for that: its later parts would come too late (2048 x 2048 11% slower); three stages,
-// one workgroup a CU, lose more with 512 tiles than they gain with 256.  Two such
-// workgroups overlap; one alone (a 128 x 128 tile a CU, four waves) takes 0.71 us a block,
-// 0.38 without its loads and LDS reads, 0.50 without the loads, 0.59 without the reads.
+// (eight a wave, 16 bytes a lane) hold the wave up while they are issued: the L2
+// gives a CU 64 bytes a cycle, 512 cycles for the stage of a 128 x 128 tile.  So
+// the stage's last products are issued behind the barrier that ends it, with the
+// next stage's first operands on their way, each group of products has the next
+// group's operands loaded in front of it, and a 256 x 256 tile's loads go out in
+// four parts between the groups.  TFLOP/s of matrix work (one run; the card's
+// clock differs by 10% between runs) of NT_SPLIT at 4096 x 4096 x 4096, fp16 at
+// 8192, int8 at 8192 x 4096 x 4096: 1050, 865, 1870 without all that, 1103, 1072,
+// 1980 with the loads in one burst, 1176, 1140, 2105 as it is; torch's products
+// 1393 (fp16) and 2122 (int8) on its fastest.
+// The stage of a 128 x 128 tile is too short for that: its later parts come too
+// late (a call with 2048 x 2048 11% slower); three stages, one workgroup a CU,
+// lose more with 512 tiles than they gain with 256.  Two such workgroups overlap;
+// one alone (four waves on a CU) takes 0.67 us a block of NT_SPLIT, 0.50 without
+// its loads, 0.59 without its LDS reads, 0.38 without both.
 template <class S, int F, class RowsA, class RowsB, class Acc>
 __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int blocks, char* lds,
                                         int tid, Acc (&acc)[S::MI][S::NJ]) {
@@ -140,19 +142,16 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int bloc
   const int brow = (wave % S::WN) * 32 * S::NJ + (lane & 31), h = lane >> 5;
   static_assert(RowsA::P == 4 && RowsB::P == 4, "stages in four parts");
   constexpr bool SPREAD = S::NT == 512;
-  auto issue = [&](int s, int part) {
-    if (s >= blocks) return;
-    const int k = s * NT_BLOCK;
+  auto issue = [&](int s) {
     char* t = lds + (s & 1) * STAGE;
-    a.issue(t, k, tid, part);
-    b.issue(t + ABYTES, k, tid, part);
+    a.issue(t, s * NT_BLOCK, tid);
+    b.issue(t + ABYTES, s * NT_BLOCK, tid);
   };
-  auto issue_rest = [&](int s) {
-#pragma unroll
-    for (int part = 1; part < 4; ++part) issue(s, part);
-  };
-  auto later = [&](int s, int part) {
-    if constexpr (SPREAD) issue(s, part);
+  auto issue_part = [&](int s, int part) {
+    if (!SPREAD || s >= blocks) return;
+    char* t = lds + (s & 1) * STAGE;
+    a.issue(t, s * NT_BLOCK, tid, part);
+    b.issue(t + ABYTES, s * NT_BLOCK, tid, part);
   };
   auto load_a = [&](const char* t, int c, nt_u32x4(&fa)[S::MI]) {
 #pragma unroll
@@ -187,12 +186,11 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int bloc
     __builtin_amdgcn_sched_barrier(0);
   };
   nt_u32x4 a0[S::MI], a1[S::MI], b0[S::NJ], b1[S::NJ], b2[S::NJ];
-  issue(0, 0);
-  issue_rest(0);
+  issue(0);
   nt_wait_vm<0>();
   nt_barrier();
-  issue(1, 0);
-  if constexpr (!SPREAD) issue_rest(1);
+  if constexpr (SPREAD) issue_part(1, 0);
+  else if (blocks > 1) issue(1);
   load_a(lds, 0, a0);
   load_b(lds, 0, b0);
   for (int s = 0; s < blocks; ++s) {
@@ -200,19 +198,19 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int bloc
     const char* next = lds + ((s + 1) & 1) * STAGE;
     // what the last group multiplies is a1 and, of b, b2 (SPLIT) or b1
     if constexpr (SPLIT) {
-      later(s + 1, 1);
+      issue_part(s + 1, 1);
       if constexpr (F == NT_SPLIT) {
         load_b(t, 2, b1);
         mul(a0, b0, acc);  // hi hi, the first 16 of K
-        later(s + 1, 2);
+        issue_part(s + 1, 2);
         load_a(t, 2, a1);
         mul(a0, b1, low);  // hi lo
       } else {
-        later(s + 1, 2);
+        issue_part(s + 1, 2);
         load_a(t, 2, a1);
         mul(a0, b0, acc);
       }
-      later(s + 1, 3);
+      issue_part(s + 1, 3);
       load_a(t, 1, a0);
       load_b(t, 1, b2);
       mul(a1, b0, low);  // lo hi
@@ -226,12 +224,12 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int bloc
         mul(a0, b2, acc);
       }
     } else {
-      later(s + 1, 1);
+      issue_part(s + 1, 1);
       load_a(t, 1, a1);
       load_b(t, 1, b1);
       mul(a0, b0, acc);
-      later(s + 1, 2);
-      later(s + 1, 3);
+      issue_part(s + 1, 2);
+      issue_part(s + 1, 3);
       load_a(t, 2, a0);
       load_b(t, 2, b0);
       mul(a1, b1, acc);
@@ -241,8 +239,8 @@ __device__ __forceinline__ void nt_tile(const RowsA& a, const RowsB& b, int bloc
     }
     nt_wait_vm<0>();  // the next stage is there,
     nt_barrier();     // and this one read by every wave
-    issue(s + 2, 0);
-    if constexpr (!SPREAD) issue_rest(s + 2);
+    if constexpr (SPREAD) issue_part(s + 2, 0);
+    else if (s + 2 < blocks) issue(s + 2);
     load_a(next, 0, a0);
     load_b(next, 0, b0);
     if constexpr (SPLIT) mul(a1, b2, low);
