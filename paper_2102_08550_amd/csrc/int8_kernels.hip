@@ -49,11 +49,32 @@ __device__ __forceinline__ int quant(float x, float s, float inv) {
   if (t > s || (t == s && odd)) q += __builtin_copysignf(1.0f, r);
   return static_cast<int>(q);
 }
-__device__ __forceinline__ uint32_t quant4(const float* v, float s, float inv) {
-  uint32_t w = 0;
+// Eight of them, a byte each.  Added to 1.5 2^23 the quotient is rounded to an
+// integer, whose low byte is the result's; remainders below the half say that it
+// is right.  Where one of the eight is not (next to a half: about one in 10^6 of
+// ordinary entries) they are done again, one by one.  (8191 x 4096 in bf16: 23.3 us
+// with all one by one, mostly their instructions; 19.2 us, 5.3 TB/s, like this.)
+__device__ __forceinline__ nt_u32x2 quant8(const float* v, float s, float inv) {
+  constexpr float BIG = 12582912.0f;
+  uint32_t f[8];
+  float worst = 0.0f;
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-    w |= (static_cast<uint32_t>(quant(v[t], s, inv)) & 0xFFu) << (8 * t);
+  for (int t = 0; t < 8; ++t) {
+    const float y = __builtin_fmaf(v[t], inv, BIG);
+    worst = __builtin_fmaxf(worst, __builtin_fabsf(__builtin_fmaf(BIG - y, s, v[t])));
+    f[t] = __builtin_bit_cast(uint32_t, y);
+  }
+  if (2.0f * worst >= s) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) f[t] = static_cast<uint32_t>(quant(v[t], s, inv));
+  }
+  nt_u32x2 w;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint32_t lo = __builtin_amdgcn_perm(f[4 * t + 1], f[4 * t], 0x0C0C0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(f[4 * t + 3], f[4 * t + 2], 0x0C0C0400u);
+    w[t] = lo | hi << 16;
+  }
   return w;
 }
 // For scale 0 or NaN every integer is 0: 1 / s is replaced by 0 and s by 1.
@@ -157,8 +178,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
   auto put = [&](int c, float* x) {
     if (c >= end) return;
     drop_if(drop, x);
-    *reinterpret_cast<nt_u32x2*>(q + c) =
-        nt_u32x2{quant4(x, d.s, d.inv), quant4(x + 4, d.s, d.inv)};
+    *reinterpret_cast<nt_u32x2*>(q + c) = quant8(x, d.s, d.inv);
   };
   if constexpr (KEEP > 0) {
 #pragma unroll
@@ -512,8 +532,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void linear_i8_few_kernel(MatmulI8A
     for (int c = 8 * at; c < slices * 64; c += 8 * per) {
       if (!once) load8<X_BF16, VEC>(row, c, in, v);
       drop_if(drop, v);
-      *reinterpret_cast<nt_u32x2*>(few_lds + r * ld + c) =
-          nt_u32x2{quant4(v, d.s, d.inv), quant4(v + 4, d.s, d.inv)};
+      *reinterpret_cast<nt_u32x2*>(few_lds + r * ld + c) = quant8(v, d.s, d.inv);
     }
   __syncthreads();
   nt_i32x4 acc = {0, 0, 0, 0};

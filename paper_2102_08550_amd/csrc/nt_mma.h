@@ -122,11 +122,11 @@ __device__ __forceinline__ nt_u32x4 nt_read(const char* tile, int row, int chunk
 // the stage's last products are issued behind the barrier that ends it, with the
 // next stage's first operands on their way, each group of products has the next
 // group's operands loaded in front of it, and a 256 x 256 tile's loads go out in
-// four parts between the groups.  TFLOP/s of matrix work (one run; the card's
-// clock differs by 10% between runs) of NT_SPLIT at 4096 x 4096 x 4096, fp16 at
-// 8192, int8 at 8192 x 4096 x 4096: 1050, 865, 1870 without all that, 1103, 1072,
-// 1980 with the loads in one burst, 1176, 1140, 2105 as it is; torch's products
-// 1393 (fp16) and 2122 (int8) on its fastest.
+// four parts between the groups.  TFLOP/s of matrix work of NT_SPLIT at 4096 x 4096
+// x 4096, fp16 at 8192, int8 at 8192 x 4096 x 4096: in one run 1266, 996, 2022
+// without all that and 1330, 1188, 2139 with the loads in one burst (torch's
+// products: fp16 1393, int8 2122); in another, the card's clock 10% lower, 1103,
+// 1072, 1980 in one burst and 1176, 1140, 2105 in parts.
 // The stage of a 128 x 128 tile is too short for that: its later parts come too
 // late (a call with 2048 x 2048 11% slower); three stages, one workgroup a CU,
 // lose more with 512 tiles than they gain with 256.  Two such workgroups overlap;

@@ -5,8 +5,8 @@ two separate calls ``oscars_local_steps`` then ``oscars_aggregate`` with
 broadcast (the average written back to every replica).  ``round_server`` puts
 the server's step with a momentum and orthogonalised updates in the place of
 the average, ``evaluate`` measures the global model, in its own arithmetic or
-in 8-bit integers.  This module only moves data into device memory and sequences calls; all arithmetic runs in
-the HIP library."""
+in 8-bit integers.  This module only moves data into device memory and
+sequences calls; all arithmetic runs in the HIP library."""
 from __future__ import annotations
 
 from typing import Optional, Sequence
