@@ -331,8 +331,8 @@ oscars_status oscars_aggregate(float* global, float* replicas, const float* weig
 oscars_status oscars_broadcast(const float* global, float* replicas, int32_t K, int64_t n,
                                int64_t ld, void* hip_stream);
 
-/* Orthogonalisation of updates by Newton-Schulz products (the update rule of
- * the Muon optimiser), for `count` matrices in one call:
+/* Orthogonalisation of updates by Newton-Schulz products, for `count` matrices in
+ * one call:
  *   X_0 = G / |G|_F;  for t = 0 .. steps - 1, with (a, b, c) = coeffs[t]:
  *     A = X_t X_t',  X_{t+1} = a X_t + (b A + c A A) X_t;   out = X_steps.
  * It brings every singular value of G near 1 and keeps the singular vectors.

@@ -84,9 +84,11 @@ class OscarsRun:
         server moves ``g`` by the orthogonalised momentum of their average's
         difference.  The momentum (``momentum``) starts at zero."""
         import torch
+        stream = self.ctx._stream  # of the steps that follow
         if self.momentum is None:
-            self.momentum = torch.zeros_like(self.g)
-        broadcast(self.g, self.replicas, self.cfg.K, self.n, self.n)
+            with torch.cuda.stream(stream):
+                self.momentum = torch.zeros_like(self.g)
+        broadcast(self.g, self.replicas, self.cfg.K, self.n, self.n, stream=stream)
         self.local_steps(tau)
         self.ctx.server_step(self.g, self.replicas, self.weights, self.momentum, lr, beta=beta,
                              nesterov=nesterov, weight_decay=weight_decay, plain_lr=plain_lr,

@@ -186,3 +186,30 @@ def test_a_captured_round_end(R):
         torch.cuda.synchronize()
         run.close()
         eager.close()
+
+
+def test_rounds_on_the_contexts_own_stream(R):
+    """A context on a stream of its own, rounds called under the default one, with
+    other work on it: the rounds' copies follow the context's stream."""
+    import torch
+    cfg = MLP32
+    ds, init = workload.gen_dataset(cfg), workload.gen_init(cfg)
+    run, want = R.OscarsRun(cfg, ds, init), R.OscarsRun(cfg, ds, init)
+    side = torch.cuda.Stream()
+    other = torch.randn(2048, 2048, device="cuda")
+    torch.cuda.synchronize()
+    run.ctx.set_stream(side)
+    try:
+        for _ in range(4):
+            want.round_server(cfg.tau_given, **OPTS)
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for _ in range(5):
+                other = (other @ other).clamp(-1, 1)  # the default stream is behind
+            run.round_server(cfg.tau_given, **OPTS)
+        torch.cuda.synchronize()
+        assert torch.equal(run.g, want.g) and torch.equal(run.momentum, want.momentum)
+    finally:
+        torch.cuda.synchronize()
+        run.close()
+        want.close()
