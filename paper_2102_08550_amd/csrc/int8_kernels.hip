@@ -458,8 +458,9 @@ constexpr int FEW_ROWS = 16;
 constexpr int FEW_WAVES = 8;
 constexpr int FEW_AHEAD = 8;           // K slices of a wave loaded ahead
 // Every workgroup quantises all rows: up to so many entries that is less than a
-// launch of its own takes (4 x 4096 x 4096: 11.4 us, in two launches 12; 16 x
-// 4096: 24.7 and 12).  One row is taken at any length.
+// launch of its own takes (bf16, 4096 x 4096: 4 rows 10.5 us, 8 rows 13.6 and in two
+// launches 12.3, 16 rows 18.9 and 12.8; 16 rows of 1024 x 1024 8.5, of 2048 x 2048
+// 11.3 and 7.9).  One row is taken at any length.
 constexpr int FEW_ENTRIES = 16384;
 // Bytes of quantised rows: the smaller one where it holds them, so that more
 // workgroups fit a CU.
