@@ -640,9 +640,9 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
 //   RING 2 (64 KB): up to two workgroups a CU, all there at once;
 //   RING 1 (32 KB): more of them, five a CU cover for each other.
 // (Calls of 17 launches: 512 x 512 106 us with RING 2, 113 with 1; 16 of 256 x 256
-// 183 and 161; 536 workgroups, two turns of RING 2, 147 and 138.  RING 4: 6 us more a call at 64 x 64, 4 more at 256 x 8192, where
-// what a CU can take from the L2 is the bound.  Eight waves, K in eight: 8 us more
-// at 64 x 64, 14 less at 256 x 8192.)
+// 183 and 161; 536 workgroups, two turns of RING 2, 147 and 138.  RING 4: 6 us more
+// a call at 64 x 64, 4 more at 256 x 8192, where what a CU can take from the L2 is
+// the bound.  Eight waves, K in eight: 8 us more at 64 x 64, 14 less at 256 x 8192.)
 constexpr int SMALL_WAVES = 4;
 template <int KIND, int F, int RING>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g) {
