@@ -342,9 +342,9 @@ oscars_status oscars_broadcast(const float* global, float* replicas, int32_t K, 
  *            be x (with the same stride) or overlap any input; outputs share no
  *            element.  A matrix stored column-major is the transpose stored
  *            row-major: pass it so, its result is the transpose's too;
- *   dtype    OSCARS_FP32 or OSCARS_BF16, of every x and out.  fp32: products
- *            of 22-bit operands summed in fp32; bf16: the last steps, whose
- *            roundings are not amplified any more, on 11-bit operands;
+ *   dtype    OSCARS_FP32 or OSCARS_BF16, of every x and out.  Either way the
+ *            products are of 22-bit operands, summed in fp32, and a bf16 result
+ *            is rounded once, at the end;
  *   coeffs   host [steps][3], 1 <= steps <= OSCARS_MAX_ORTH_STEPS; refused where
  *            a step's polynomial a + b s^2 + c s^4 passes 400, or a singular
  *            value 16, from singular values s in [0, 1] on;

@@ -14,13 +14,14 @@
 //
 // Number format.  The iterates live in the workspace as fp16 planes, scaled by
 // powers of two so that neither end of fp16's range matters: NT_SPLIT (hi and
-// lo, 22 bits, three matrix instructions a product) for fp32 matrices, and for
-// bf16 matrices where a rounding would still be amplified by later steps: a
-// step multiplies the small singular directions by up to |a|, so a rounding
-// error of 2^-12 before a steps' product of 40 ends at 1e-2 of an entry, many
-// bf16 roundings; the last steps run in plain fp16 (one instruction a product).
-// X_0 is G times a power of two, exact for bf16; the rest of 1 / |G|_F is a
-// factor on the first products, so nothing is rounded before the first step.
+// lo, 22 bits, three matrix instructions a product) for fp32 and for bf16
+// matrices, because a rounding is amplified by later steps: one multiplies the
+// small singular directions by up to |a|.  With 11 bits in the last two steps of
+// five a bf16 result had 16 to 28% of its entries one step or more off what the
+// products in 32 bits give, with 22 bits it has 0.3% (4096 x 4096: 2607 us then, 3442
+// so).  X_0 is G times a power of two, exact and one plane for bf16 (one instruction
+// a product); the rest of 1 / |G|_F is a factor on the first products, so nothing is
+// rounded before the first step.
 // Products sum in fp32 in a fixed order; norms in double.
 #include "orthogonalize.h"
 
@@ -63,8 +64,6 @@ struct OrthArgs {
   float a, b, c;
   int in_scaled;       // 1: the planes hold X times orth_scale; 0: X_0 (factor in the workspace)
   int parity;          // which of the two X' buffers is read
-  int x_fmt, xt_fmt;   // APPLY, convert: formats written
-  int p_fmt;           // GRAM: format of A
   int bf16;            // convert / LAST: the caller's type
 };
 
@@ -178,25 +177,23 @@ __device__ __forceinline__ void store_lines(char* base, int64_t ld, int first, i
   }
 }
 
-// N values from k (both multiples of 4, within 16) of a plane row, as they are
-// stored: read by get, added up by value where they are used.
+// N values from k (both multiples of 4, within 16) of an NT_SPLIT plane row, as they
+// are stored: read by get, added up by value where they are used.
 template <int N>
 struct Stored {
   typedef _Float16 h4 __attribute__((ext_vector_type(4)));
   h4 hi[N / 4], lo[N / 4];
-  __device__ __forceinline__ void get(const char* row, int k, int fmt) {
-    const h4* p = reinterpret_cast<const h4*>(
-        fmt == NT_F16 ? row + 2 * static_cast<int64_t>(k)
-                      : row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31));
+  __device__ __forceinline__ void get(const char* row, int k) {
+    const h4* p =
+        reinterpret_cast<const h4*>(row + 4 * static_cast<int64_t>(k & ~31) + 2 * (k & 31));
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
       hi[i] = p[i];
-      if (fmt != NT_F16) lo[i] = p[8 + i];
+      lo[i] = p[8 + i];
     }
   }
-  __device__ __forceinline__ float value(int e, int fmt) const {
-    const float v = static_cast<float>(hi[e / 4][e & 3]);
-    return fmt == NT_F16 ? v : v + static_cast<float>(lo[e / 4][e & 3]);
+  __device__ __forceinline__ float value(int e) const {
+    return static_cast<float>(hi[e / 4][e & 3]) + static_cast<float>(lo[e / 4][e & 3]);
   }
 };
 
@@ -342,7 +339,8 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(OrthArgs g) {
   // G's rows and those of G': X is the one with m rows.  Wave w: quarter w of the tile.
   const int lane = threadIdx.x & 63, i0 = (threadIdx.x >> 7) * 32;
   const int j0 = (threadIdx.x >> 6 & 1) * 32;
-  const int fmt1 = tall ? g.xt_fmt : g.x_fmt, fmt2 = tall ? g.x_fmt : g.xt_fmt;
+  const int x_fmt = BF16 ? NT_F16 : NT_SPLIT;  // exact in one plane
+  const int fmt1 = tall ? NT_SPLIT : x_fmt, fmt2 = tall ? x_fmt : NT_SPLIT;
   store_lines(tall ? q.xt[0] : q.x, row_bytes(u.cols, fmt1), r0 + i0, u.rows, c0 + j0, fmt1, lane,
               [&](int i, int k, float* v) {
 #pragma unroll
@@ -447,21 +445,21 @@ struct Product {
   __device__ __forceinline__ char* straight() const {
     return KIND == ORTH_GRAM ? a : KIND == ORTH_POLY ? p : x;
   }
-  // POLY: rows r .. r + N - 1 of column c of A, in `fmt`.
+  // POLY: rows r .. r + N - 1 of column c of A.
   template <int N>
-  __device__ __forceinline__ void load_a(int r, int c, int fmt, Stored<N>* t) const {
+  __device__ __forceinline__ void load_a(int r, int c, Stored<N>* t) const {
     // A(r, c) = A(c, r), consecutive
-    if (KIND == ORTH_POLY) t->get(a + (c < C ? c : C - 1) * row_bytes(m, fmt), r, fmt);
+    if (KIND == ORTH_POLY) t->get(a + (c < C ? c : C - 1) * row_bytes(m, NT_SPLIT), r);
   }
   // Rows r .. r + N - 1 of column c: POLY's other terms (t of load_a), zeros in
   // the planes' padding.
   template <int N>
-  __device__ __forceinline__ void finish(const OrthArgs& g, int r, int c, int fmt,
-                                         const Stored<N>& t, float* v) const {
+  __device__ __forceinline__ void finish(const OrthArgs& g, int r, int c, const Stored<N>& t,
+                                         float* v) const {
     if constexpr (KIND == ORTH_POLY) {
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        v[e] += g.b * t.value(e, fmt) + (r + e == c ? g.a * kScaleA : 0.0f);
+        v[e] += g.b * t.value(e) + (r + e == c ? g.a * kScaleA : 0.0f);
     }
     if constexpr (KIND != ORTH_LAST) {
 #pragma unroll
@@ -561,9 +559,7 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
   const float f = p.factor(g);
   const int rw = r0 + (wave / S::WN) * 32 * S::MI, cw = c0 + (wave % S::WN) * 32 * S::NJ;
   float* turn = reinterpret_cast<float*>(lds) + wave * 32 * TURN;
-  const int fmt1 = KIND == ORTH_GRAM ? g.p_fmt : KIND == ORTH_POLY ? PF : g.xt_fmt;
-  const int fmt2 = KIND == ORTH_APPLY ? g.x_fmt : fmt1;
-  const int64_t ld1 = row_bytes(p.R, fmt1), ld2 = row_bytes(p.C, fmt2);
+  const int64_t ld1 = row_bytes(p.R, NT_SPLIT), ld2 = row_bytes(p.C, NT_SPLIT);
   const int line = lane >> 1, k16 = 16 * (lane & 1);
   nt_barrier();  // the stages are read: LDS is free
 #pragma nounroll
@@ -602,8 +598,8 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
           for (int o = 0; o < 4; ++o) v[4 * e + o] = t[o];
         }
         Stored<16> t;
-        p.load_a(rb0 + k16, cb0 + line, PF, &t);
-        p.finish(g, rb0 + k16, cb0 + line, PF, t, v);
+        p.load_a(rb0 + k16, cb0 + line, &t);
+        p.finish(g, rb0 + k16, cb0 + line, t, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *reinterpret_cast<nt_f32x4*>(mine + 4 * e) =
@@ -611,7 +607,7 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
         __builtin_amdgcn_wave_barrier();
       }
       // turned: rows c, entries r (zeros in the padding)
-      store_lines(p.turned(), ld1, cb0, p.C, rb0, fmt1, lane, [&](int i, int k, float* v) {
+      store_lines(p.turned(), ld1, cb0, p.C, rb0, NT_SPLIT, lane, [&](int i, int k, float* v) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const nt_f32x4 t = *reinterpret_cast<const nt_f32x4*>(turn + i * TURN + k + 4 * e);
@@ -621,7 +617,7 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
       });
       // straight: rows r, entries c (a diagonal tile holds both already)
       if (!Prod::SYM || ti != tj)
-        store_lines(p.straight(), ld2, rb0, p.R, cb0, fmt2, lane, [&](int i, int k, float* v) {
+        store_lines(p.straight(), ld2, rb0, p.R, cb0, NT_SPLIT, lane, [&](int i, int k, float* v) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             v[e] = cb0 + k + e < p.C ? turn[(k + e) * TURN + i] : 0.0f;
@@ -687,7 +683,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
   // the wave finishes rows 8 w + 4 h .. + 3 of column (lane & 31)
   const int r = r0 + 8 * wave + 4 * h, c = c0 + (lane & 31);
   Stored<4> terms;
-  p.load_a(r, c, PF, &terms);     // on its way during the products
+  p.load_a(r, c, &terms);         // on its way during the products
   asm volatile("" ::: "memory");  // ahead of the blocks, whose waits count what follows
   nt_f32x16 acc, cross;
 #pragma unroll
@@ -739,7 +735,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
     for (int w = 0; w < SMALL_WAVES; ++w) s += sums[(w * 16 + 4 * wave + t) * 64 + lane];
     v[t] = s * f;
   }
-  p.finish(g, r, c, PF, terms, v);
+  p.finish(g, r, c, terms, v);
   // Through LDS, turned[column][row], so that eight lanes store a whole line: of
   // the caller's row, or 32 entries of a plane's.
   float* turn = sums + SMALL_WAVES * 16 * 64;
@@ -753,27 +749,25 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void orth_small_kernel(OrthArgs g
     for (int t = 0; t < 4; ++t) v[t] = turn[i * TURN + k + t];
     p.template out<4>(g, r0 + k, c0 + i, v);
   } else {
-    const int fmt1 = KIND == ORTH_GRAM ? g.p_fmt : KIND == ORTH_POLY ? PF : g.xt_fmt;
-    const int fmt2 = KIND == ORTH_APPLY ? g.x_fmt : fmt1;
     const int k = 8 * (lane & 3);
     const bool lo = lane & 4;
     // rows are padded to 64 entries: the last tile zeros what no tile covers
     const float none[8] = {};
     float w[8];
-    if (c0 + i < p.C && (fmt1 != NT_F16 || !lo)) {
-      char* row = p.turned() + (c0 + i) * row_bytes(p.R, fmt1);
+    if (c0 + i < p.C) {
+      char* row = p.turned() + (c0 + i) * row_bytes(p.R, NT_SPLIT);
 #pragma unroll
       for (int t = 0; t < 8; ++t) w[t] = turn[i * TURN + k + t];
-      put8(row, r0 + k, fmt1, lo, w);
-      if (r0 + 32 >= p.R && r0 + 32 < pad64(p.R)) put8(row, r0 + 32 + k, fmt1, lo, none);
+      put8(row, r0 + k, NT_SPLIT, lo, w);
+      if (r0 + 32 >= p.R && r0 + 32 < pad64(p.R)) put8(row, r0 + 32 + k, NT_SPLIT, lo, none);
     }
     if (Prod::SYM && ti == tj) return;
-    if (r0 + i < p.R && (fmt2 != NT_F16 || !lo)) {
-      char* row = p.straight() + (r0 + i) * row_bytes(p.C, fmt2);
+    if (r0 + i < p.R) {
+      char* row = p.straight() + (r0 + i) * row_bytes(p.C, NT_SPLIT);
 #pragma unroll
       for (int t = 0; t < 8; ++t) w[t] = turn[(k + t) * TURN + i];
-      put8(row, c0 + k, fmt2, lo, w);
-      if (c0 + 32 >= p.C && c0 + 32 < pad64(p.C)) put8(row, c0 + 32 + k, fmt2, lo, none);
+      put8(row, c0 + k, NT_SPLIT, lo, w);
+      if (c0 + 32 >= p.C && c0 + 32 < pad64(p.C)) put8(row, c0 + 32 + k, NT_SPLIT, lo, none);
     }
   }
 #endif
@@ -849,9 +843,9 @@ hipError_t launch_product_small(OrthArgs& g, hipStream_t s, int rest) {
 // and, with more tiles than fit at once, some of a tile for the CUs that run dry.
 // Where a few tiles of 128 are left after full turns of one or two to a CU, they
 // are done in tiles of 32 by a second launch, 9 us and 1870 blocks a us: one matrix
-// of 4096 (two turns of 256 and 16 left) went from 4329 to 3883 us (bf16 3121 to 2774),
-// 2900 from 2170 to 1919, two of 2048 from 1432 to 1338; eight of 1024 (32 blocks of
-// K, 32 tiles left) would have gone from 886 to 1000.
+// of 4096 (two turns of 256 and 16 left) went from 4329 to 3883 us, 2900 from 2170 to
+// 1919, two of 2048 from 1432 to 1338; eight of 1024 (32 blocks of K, 32 tiles left)
+// would have gone from 886 to 1000.
 // Whole calls, fp32 (32 / 128 / 256, us): 512: 107 / 344 / 753, 1280: 357 / 583 /
 // 1329, 2048: 1087 / 847 / 1908, 3328: 4245 / 2445 / 2932, 4096: 7895 / 4422 / 3984;
 // three 4096 x 4096 and 1000 x 4096: 24179 / 11673 / 10962.  (Tiles cut along K,
@@ -964,16 +958,6 @@ hipError_t launch_orthogonalize(const OrthMat* mats, int count, bool bf16, const
     g.mat[i].at = at;
     at += mat_bytes(mats[i]);
   }
-  // Step t in plain fp16 (bf16 matrices): where a rounding in it is amplified
-  // by no more than 16 by the end.
-  bool plain[ORTH_MAX_STEPS + 1];
-  double amp = 1.0;
-  plain[c.steps] = bf16;
-  for (int t = c.steps - 1; t >= 0; --t) {
-    amp *= std::fmax(1.0, std::fabs(static_cast<double>(c.a[t])));
-    plain[t] = bf16 && amp <= 16.0;
-  }
-  auto fmt = [&](int t) -> int { return plain[t] ? NT_F16 : NT_SPLIT; };
   hipError_t e = hipSuccess;
   matrices_in_order(&g);
   if (!norms_done) {
@@ -985,10 +969,6 @@ hipError_t launch_orthogonalize(const OrthMat* mats, int count, bool bf16, const
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  // X_0 of a bf16 matrix is exact in one plane: its Gram product takes one
-  // instruction, its product with P (hi, lo) two.
-  g.x_fmt = bf16 ? static_cast<int>(NT_F16) : static_cast<int>(NT_SPLIT);
-  g.xt_fmt = fmt(0);
   {
     const int grid = layout_grid(&g, [&](int i) {
       return ((mats[i].rows + 63) / 64) * ((mats[i].cols + 63) / 64);
@@ -1004,22 +984,19 @@ hipError_t launch_orthogonalize(const OrthMat* mats, int count, bool bf16, const
     g.c = c.c[t];
     g.in_scaled = t > 0;
     g.parity = t & 1;
-    g.p_fmt = fmt(t);
-    const bool gram1 = t == 0 ? bf16 : plain[t];  // X in one plane
-    e = gram1 ? launch_product<ORTH_GRAM, NT_F16>(g, s) : launch_product<ORTH_GRAM, NT_SPLIT>(g, s);
+    // X_0 of a bf16 matrix is exact in one plane: its Gram product takes one
+    // instruction, its product with P (hi, lo) two.
+    const bool one_plane = t == 0 && bf16;
+    e = one_plane ? launch_product<ORTH_GRAM, NT_F16>(g, s)
+                  : launch_product<ORTH_GRAM, NT_SPLIT>(g, s);
     if (e != hipSuccess) break;
-    e = plain[t] ? launch_product<ORTH_POLY, NT_F16>(g, s)
-                 : launch_product<ORTH_POLY, NT_SPLIT>(g, s);
+    e = launch_product<ORTH_POLY, NT_SPLIT>(g, s);
     if (e != hipSuccess) break;
-    if (t + 1 < c.steps) {
-      g.x_fmt = g.xt_fmt = fmt(t + 1);
-      if (plain[t]) e = launch_product<ORTH_APPLY, NT_F16>(g, s);
-      else if (t == 0 && bf16) e = launch_product<ORTH_APPLY, NT_SPLIT_B0>(g, s);
-      else e = launch_product<ORTH_APPLY, NT_SPLIT>(g, s);
-    } else {
-      e = plain[t] ? launch_product<ORTH_LAST, NT_F16>(g, s)
-                   : launch_product<ORTH_LAST, NT_SPLIT>(g, s);
-    }
+    if (t + 1 == c.steps)
+      e = launch_product<ORTH_LAST, NT_SPLIT>(g, s);
+    else
+      e = one_plane ? launch_product<ORTH_APPLY, NT_SPLIT_B0>(g, s)
+                    : launch_product<ORTH_APPLY, NT_SPLIT>(g, s);
   }
   return e;
 }

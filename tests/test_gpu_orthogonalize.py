@@ -1,9 +1,10 @@
 """Orthogonalisation by Newton-Schulz products and the server's step, against
 the oracle in float64.
 
-Tolerances.  What the kernels round is known: fp32 matrices keep X, A and P in
-22 bits and drop lo lo, bf16 matrices keep those of the steps whose errors grow
-no more than 16 times in 11 bits; sums are fp32.  A step multiplies an error in
+Tolerances.  What the kernels round is known: X, A and P are kept in 22 bits,
+without lo lo; sums are fp32.  (Of bf16 matrices the model has the steps whose
+errors grow no more than 16 times in 11 bits, more than the kernels need;
+test_bf16_is_rounded_once has the closer bound.)  A step multiplies an error in
 X by at most about 4 (the largest divided difference of its polynomial), so the
 end error depends on the matrix.  It is modelled in float64: every stored value
 moved by a uniform relative error of that many bits, every sum by a normal one
@@ -116,6 +117,27 @@ def test_orthogonalize(P, r, c, dtype):
     out = P.orthogonalize(g)
     _check(out, g, where="one")
     assert torch.equal(g, keep) and out.dtype == g.dtype
+
+
+@pytest.mark.parametrize("shapes", [[(1, 5)], [(64, 64)], [(300, 40), (37, 2050)],
+                                    [(512, 784), (256, 512), (10, 256)], [(1030, 1100)],
+                                    [(2048, 2060)], [(3600, 3700)]])
+@pytest.mark.parametrize("steps", [5, 1])
+def test_bf16_is_rounded_once(P, shapes, steps):
+    """A bf16 result is the 22-bit products' own, rounded at the end: off by half a
+    step of bf16 beside what the fp32 matrix of the same values may be off by."""
+    import torch
+    gs = [_gradient(r, c, i + 40).bfloat16() for i, (r, c) in enumerate(shapes)]
+    coeffs = COEFFS[:steps]
+    for g, y in zip(gs, P.orthogonalize(gs, coeffs=coeffs)):
+        want = server.newton_schulz(g.double(), coeffs)
+        entry = 8 * _may(g.float(), torch.float32, coeffs)[1]
+        # a value that close may lie in the next binade, with its larger steps
+        exponent = torch.frexp(want.abs() + entry)[1]
+        half = torch.ldexp(torch.ones_like(want), exponent - 9)
+        over = float(((y.double() - want).abs() - half).max())
+        say(f"  {tuple(g.shape)}: {over / entry:.2f} of what it may be beside half a step")
+        assert over <= entry
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
