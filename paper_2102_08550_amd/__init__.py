@@ -431,7 +431,9 @@ def quantize_rows(x, out=None, stream=None):
     """The rows of ``x`` (fp32 or bf16 matrix, any row stride) in 8 bits with a
     scale each (oscars_quantize_rows): ``(q, scale)``, q int8 [rows][columns
     rounded up to 128, zero behind the columns], scale fp32 [rows].  ``out``:
-    such a pair to write into (the row stride of q a multiple of 16)."""
+    such a pair to write into: the row stride of q a multiple of 16, and q as
+    wide as the padding goes, to the next multiple of 128 columns or, where rows
+    are shorter than that, to their end (a window of wider rows holds all of it)."""
     import torch
     dev = x.device
     xp, n, ld, cols = _rows(x, x.dtype, dev, "x")
@@ -441,8 +443,8 @@ def quantize_rows(x, out=None, stream=None):
                _new((n,), torch.float32, dev, stream))
     q, scale = out
     qp, qn, qld, qc = _rows(q, torch.int8, dev, "q")
-    if qn != n or qc < cols:
-        raise ValueError("q must have a row per row of x, as long or longer")
+    if qn != n or qc < max(cols, min(qld, (cols + 127) // 128 * 128)):
+        raise ValueError("q must have a row per row of x, of its columns and the zeros behind them")
     if n == 0:
         return out
     with _on_device(dev):

@@ -90,6 +90,30 @@ def test_quantize_rows(P, n, c, dtype):
     assert torch.equal(out[1], s)
 
 
+@pytest.mark.parametrize("cols", [10, 40, 130])
+def test_quantize_rows_into_a_window(P, cols):
+    """A window of wider rows: its padding is inside it and what lies around it
+    stays; one that ends before its padding is refused."""
+    import torch
+    x = _rows(np.random.default_rng(cols), 5, cols, "fp32")
+    wide = -(-cols // 128) * 128
+    buf = torch.full((7, 16 + wide + 48), 99, dtype=torch.int8, device="cuda")
+    scale = torch.full((7,), -1.0, device="cuda")
+    q = buf[1:6, 16:16 + wide]
+    P.quantize_rows(_dev(x, "fp32"), out=(q, scale[1:6]))
+    want, s = int8.quantize_rows(x)
+    assert np.array_equal(q[:, :cols].cpu().numpy(), want) and not q[:, cols:].any()
+    assert np.array_equal(scale[1:6].cpu().numpy(), s.astype(np.float32))
+    edge = buf.clone()
+    edge[1:6, 16:16 + wide] = 99
+    assert (edge == 99).all() and (scale[[0, 6]] == -1).all()
+    keep = buf.clone()
+    for narrow in (buf[1:6, 16:16 + wide - 1], buf[1:6, 32:16 + wide], buf[6:, 32:16 + wide]):
+        with pytest.raises(ValueError):
+            P.quantize_rows(_dev(x[:len(narrow)], "fp32"), out=(narrow, scale[1:1 + len(narrow)]))
+    assert torch.equal(buf, keep)
+
+
 def test_quantize_rows_next_to_a_half(P):
     """Quotients on and beside every half: the nearest fp32 values to (k + 1/2) s
     and their neighbours, for scales of every kind."""

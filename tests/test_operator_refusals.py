@@ -197,3 +197,50 @@ def test_int8_model_refuses_null():
     assert lib.oscars_quantize_model(None, BASE, BASE) == P.E_INVALID
     assert lib.oscars_evaluate_quantized(None, BASE, BASE, BASE, 1, ctypes.byref(loss),
                                   ctypes.byref(hits)) == P.E_INVALID
+
+
+def _pretend(t):
+    """A CPU tensor that says it is on a GPU: refusals come before its use."""
+    import torch
+
+    class OnGpu(torch.Tensor):
+        is_cuda = property(lambda self: True)
+
+    return t.as_subclass(OnGpu)
+
+
+def test_quantize_rows_window_holds_its_padding(monkeypatch):
+    """The zeros go to the next multiple of 128 columns, or to the row's end: a window
+    of wider rows that ends before them is refused, and nothing is called."""
+    import contextlib
+
+    import torch
+    calls = []
+
+    class Lib:
+        def oscars_quantize_rows(self, *a):
+            calls.append(a)
+            return P.OK
+
+    monkeypatch.setattr(P, "_lib", Lib)
+    monkeypatch.setattr(P, "_on_device", lambda device: contextlib.nullcontext())
+    monkeypatch.setattr(P, "_stream_handle", lambda stream: None)
+    buf = _pretend(torch.zeros(6, 384, dtype=torch.int8))
+    scale = _pretend(torch.zeros(4))
+
+    def quantize(cols, q, rows=4):
+        return P.quantize_rows(_pretend(torch.zeros(rows, cols)), out=(q, scale[:rows]))
+
+    for cols, q in ((40, buf[:4, 208:256]), (10, buf[:4, 240:256]), (40, buf[:4, 256:383]),
+                    (129, buf[:4, :255]), (300, buf[:4, :320]), (40, buf[:4, 368:])):
+        with pytest.raises(ValueError):
+            quantize(cols, q)
+    with pytest.raises(ValueError):  # one row of a wider tensor
+        quantize(40, buf[5:, 208:256], rows=1)
+    assert not calls
+    whole = _pretend(torch.zeros(4, 48, dtype=torch.int8))
+    for cols, q in ((40, buf[:4, 256:]), (40, buf[:4, 16:144]), (129, buf[:4, :256]),
+                    (300, buf[:4]), (40, whole), (10, whole)):
+        quantize(cols, q)
+        assert calls[-1][1] == q.stride(0)
+    assert len(calls) == 6
