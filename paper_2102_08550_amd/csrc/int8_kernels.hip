@@ -11,8 +11,7 @@
 //                   the rows' quantisation in front of it in every workgroup.
 #include "int8.h"
 
-#include <cmath>
-
+#include "int8_plan.h"
 #include "nt_mma.h"
 
 namespace oscars {
@@ -218,6 +217,7 @@ bool aligned_rows(const void* p, int64_t row_bytes, int to) {
 
 typedef NtShape<256, 256, 2, 4> I8L;
 typedef NtShape<128, 128, 2, 2> I8M;
+static_assert(i8_threads(I8L::BM) == I8L::NT && i8_threads(I8M::BM) == I8M::NT, "int8_plan.h");
 
 __device__ __forceinline__ float i8_finish(int32_t acc, float sx, float sw, float b, bool relu) {
   float y = static_cast<float>(acc) * (sx * sw) + b;
@@ -434,10 +434,7 @@ __global__ __launch_bounds__(256) void matmul_i8_small_kernel(MatmulI8Args a) {
 
 template <bool OUT_BF16, bool VEC>
 hipError_t matmul_launch(const MatmulI8Args& a, int tile, hipStream_t s) {
-  const int64_t tiles =
-      static_cast<int64_t>((a.outs + tile - 1) / tile) * ((a.rows + tile - 1) / tile);
-  if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
-  const dim3 grid(static_cast<unsigned>(tiles));
+  const dim3 grid(static_cast<unsigned>((a.outs + tile - 1) / tile * ((a.rows + tile - 1) / tile)));
   if (tile == I8L::BM)
     hipLaunchKernelGGL((matmul_i8_kernel<I8L, OUT_BF16, VEC>), grid, dim3(I8L::NT), 0, s, a);
   else if (tile == I8M::BM)
@@ -605,62 +602,6 @@ hipError_t launch_quantize_rows(const QuantArgs& args, hipStream_t s) {
   return hipSuccess;
 }
 
-// The first `rows` rows of a product in tiles of `tile`, and its time by what the
-// kernels take on this card, in us (a K block: 128 inputs):
-//   32    3.5, and 2100 blocks a us over all CUs
-//   128   8, and a block 0.55 while no CU has two tiles, else 1.2 for 512 at a time,
-//         of which the last up to 256 take 0.75
-//   256   20, and a block 1.15 while half of the CUs have a tile, 1.55 up to all
-//         of them, else 1.75 for 256 at a time
-// Rows x inputs x outputs, measured with 32 / 128 / 256: 256 x 4096 x 1000: 7.1 /
-// 24.3 / 47.1, 1024 x 2048 x 2048: 20.4 / 17.9 / 31.7, 3000 x 3000 x 3000: 108 / 52 /
-// 45.5, 10000 x 2048 x 2048: 168 / 64.5 / 72, 4096 x 4096 x 4096: 229 / 82.5 / 69.2.
-struct I8Plan {
-  int tile;
-  int64_t rows;
-  double us;
-};
-I8Plan i8_plan(const MatmulI8Args& a, int64_t rows) {
-  const double k = (a.in + NT_BLOCK - 1) / NT_BLOCK;
-  I8Plan best{0, rows, 0.0};
-  for (int t : {32, 128, 256}) {
-    const double n =
-        static_cast<double>((a.outs + t - 1) / t) * static_cast<double>((rows + t - 1) / t);
-    const double turns = std::floor(n / 512.0), last = n - 512.0 * turns;
-    double us;
-    if (t == 32)
-      us = 3.5 + n * k / 2100.0;
-    else if (t == 128)
-      us = 8.0 + k * (n <= 256.0 ? 0.55
-                                 : 1.2 * turns + (last > 256.0 ? 1.2 : last > 0.0 ? 0.75 : 0.0));
-    else
-      us = 20.0 + k * (n <= 144.0 ? 1.15 : n <= 256.0 ? 1.55 : 1.75 * std::ceil(n / 256.0));
-    if (best.tile == 0 || us < best.us) {
-      best.tile = t;
-      best.us = us;
-    }
-  }
-  return best;
-}
-
-// Rows that fill the CUs with tiles of 128 or 256 a whole number of times, where
-// the others and a second launch (1 us) then take less than one more turn would:
-// 4352 x 2048 x 2048 went from 38.3 to 32.0 us, 9000 x 4096 x 4096 from 171 to 160;
-// 9216 x 2048 x 2048, which stays as it is at 57.8, would take 59.8.
-I8Plan i8_first_rows(const MatmulI8Args& a) {
-  I8Plan best = i8_plan(a, a.rows);
-  for (int t : {128, 256}) {
-    const int64_t across = (a.outs + t - 1) / t, slots = t == 128 ? 512 : 256;
-    const int64_t turns = across * ((a.rows + t - 1) / t) / slots;
-    const int64_t rows = turns * slots / across * t;
-    if (rows == 0 || rows >= a.rows) continue;
-    const I8Plan first = i8_plan(a, rows);
-    const double us = first.us + 1.0 + i8_plan(a, a.rows - rows).us;
-    if (us < best.us) best = {first.tile, rows, us};
-  }
-  return best;
-}
-
 hipError_t launch_matmul_i8(const MatmulI8Args& args, hipStream_t s) {
   const bool vec = aligned_rows(args.out, args.out_ld * (args.out_bf16 ? 2 : 4), 16);
   auto launch = [&](const MatmulI8Args& a, int tile) {
@@ -668,16 +609,17 @@ hipError_t launch_matmul_i8(const MatmulI8Args& args, hipStream_t s) {
       return vec ? matmul_launch<true, true>(a, tile, s) : matmul_launch<true, false>(a, tile, s);
     return vec ? matmul_launch<false, true>(a, tile, s) : matmul_launch<false, false>(a, tile, s);
   };
-  const I8Plan plan = i8_first_rows(args);
-  MatmulI8Args a = args;
-  a.rows = plan.rows;
-  const hipError_t e = launch(a, plan.tile);
-  if (e != hipSuccess || plan.rows == args.rows) return e;
-  a.rows = args.rows - plan.rows;
-  a.xq += plan.rows * a.x_ld;
-  a.xscale += plan.rows;
-  a.out = static_cast<char*>(a.out) + plan.rows * a.out_ld * (a.out_bf16 ? 2 : 4);
-  return launch(a, i8_plan(args, a.rows).tile);
+  hipError_t e = hipSuccess;
+  i8_launches(args.rows, args.in, args.outs, [&](int tile, int64_t at, int64_t rows) {
+    MatmulI8Args a = args;
+    a.rows = rows;
+    a.xq += at * a.x_ld;
+    a.xscale += at;
+    a.out = static_cast<char*>(a.out) + at * a.out_ld * (a.out_bf16 ? 2 : 4);
+    e = launch(a, tile);
+    return e == hipSuccess;
+  });
+  return e;
 }
 
 bool linear_i8_one_launch(int64_t rows, int in) {
