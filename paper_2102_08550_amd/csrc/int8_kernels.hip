@@ -336,7 +336,7 @@ __global__ __launch_bounds__(S::NT, 2) void matmul_i8_kernel(MatmulI8Args a) {
                   nt_i32x4{acc[ii][jj][4 * q], acc[ii][jj][4 * q + 1], acc[ii][jj][4 * q + 2],
                            acc[ii][jj][4 * q + 3]};
           }
-      __builtin_amdgcn_wave_barrier();
+      nt_wave_sync();
       for (int r = lane / LANES; r < 32; r += 64 / LANES) {
         const int64_t row = row0 + r;
         const float sx = a.xscale[row < a.rows ? row : a.rows - 1];
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(S::NT, 2) void matmul_i8_kernel(MatmulI8Args a) {
         }
         if (row < a.rows && o < a.outs) store_outs<PER, OUT_BF16, VEC>(a, row, o, v);
       }
-      __builtin_amdgcn_wave_barrier();
+      nt_wave_sync();
     }
   }
 #endif

@@ -108,6 +108,15 @@ __device__ __forceinline__ void nt_barrier() {
   asm volatile("s_barrier" ::: "memory");
 }
 
+// Between a wave's stores to LDS and other lanes' loads of them, or the next stores:
+// LDS operations of one wave execute in order, so it is the compiler alone that has
+// to keep it (no instruction comes of the fences).
+__device__ __forceinline__ void nt_wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __device__ __forceinline__ nt_u32x4 nt_read(const char* tile, int row, int chunk) {
   return *reinterpret_cast<const nt_u32x4*>(tile + row * NT_BLOCK +
                                             16 * (chunk ^ ((row ^ (row >> 3)) & 7)));

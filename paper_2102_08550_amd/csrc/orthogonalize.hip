@@ -577,7 +577,7 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
                 nt_f32x4{acc[i][j][4 * e] * f, acc[i][j][4 * e + 1] * f,
                          acc[i][j][4 * e + 2] * f, acc[i][j][4 * e + 3] * f};
         }
-    __builtin_amdgcn_wave_barrier();
+    nt_wave_sync();
     if constexpr (KIND == ORTH_LAST) {
       // eight lanes store the 32 entries of a caller's row
 #pragma unroll
@@ -604,7 +604,7 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
         for (int e = 0; e < 4; ++e)
           *reinterpret_cast<nt_f32x4*>(mine + 4 * e) =
               nt_f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
-        __builtin_amdgcn_wave_barrier();
+        nt_wave_sync();
       }
       // turned: rows c, entries r (zeros in the padding)
       store_lines(p.turned(), ld1, cb0, p.C, rb0, NT_SPLIT, lane, [&](int i, int k, float* v) {
@@ -623,7 +623,7 @@ __global__ __launch_bounds__(S::NT, 2) void orth_product_kernel(OrthArgs g) {
             v[e] = cb0 + k + e < p.C ? turn[(k + e) * TURN + i] : 0.0f;
         });
     }
-    __builtin_amdgcn_wave_barrier();
+    nt_wave_sync();
   }
 #endif
 }
