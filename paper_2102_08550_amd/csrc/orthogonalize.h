@@ -30,8 +30,8 @@ struct OrthCoeffs {
   float a[ORTH_MAX_STEPS], b[ORTH_MAX_STEPS], c[ORTH_MAX_STEPS];
 };
 
-// Whether the polynomials keep singular values in [0, 1] and every
-// intermediate within the range of the fp16 planes.
+// Whether the polynomials keep every intermediate, from singular values in [0, 1]
+// on, within the range of the fp16 planes, at both of its ends.
 bool orth_coeffs_ok(const OrthCoeffs& c);
 // Device bytes of a call's temporaries (256-byte aligned base).
 int64_t orth_workspace(const OrthMat* mats, int count);

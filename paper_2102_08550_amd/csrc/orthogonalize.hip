@@ -40,6 +40,10 @@ enum OrthKind { ORTH_GRAM = 0, ORTH_POLY = 1, ORTH_APPLY = 2, ORTH_LAST = 3 };
 constexpr float kScaleA = 128.0f;  // of A and P in their planes
 constexpr float kMaxSigma = 16.0f;
 constexpr float kMaxPoly = 400.0f;
+// Least Frobenius norm of an iterate in its planes.  They hold 2^-25 / orth_scale of
+// an entry, whatever its size: fp32 results stay where roundings to 22 bits put
+// them down to 0.01 (two steps; 3e-6), at 1e-4 they are 2e-4 to 4e-4 off.
+constexpr double kMinNorm = 1.0 / 16.0;
 constexpr int kNormParts = 512;  // partial sums of squares per matrix
 
 struct MatDesc {
@@ -925,17 +929,41 @@ bool orth_coeffs_ok(const OrthCoeffs& c) {
   if (c.steps < 1 || c.steps > ORTH_MAX_STEPS) return false;
   double top = 1.0;  // singular values lie in [0, top]
   for (int t = 0; t < c.steps; ++t) {
-    const double a = c.a[t], b = c.b[t], d = c.c[t];
+    const double a = c.a[t], b = c.b[t], d = c.c[t], u = top * top;
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(d)) return false;
-    double next = 0.0;
-    for (int i = 0; i <= 4096; ++i) {
-      const double x = top * i / 4096.0, s = x * x;
-      const double p = a + b * s + d * s * s;
-      if (!(std::fabs(p) <= kMaxPoly)) return false;
-      next = std::fmax(next, std::fabs(x * p));
+    // of v = s^2 in [0, u]: p(v) = a + b v + d v^2, and s p whose derivative is
+    // a + 3 b v + 5 d v^2; the largest are at an end or where a derivative is zero
+    auto p = [&](double v) { return std::fabs(a + (b + d * v) * v); };
+    double most = std::fmax(p(0.0), p(u)), next = top * p(u);
+    auto inside = [&](double v) { return v > 0.0 && v < u; };
+    const double flat = -b / (2.0 * d);
+    if (inside(flat)) most = std::fmax(most, p(flat));
+    const double disc = 9.0 * b * b - 20.0 * a * d;
+    if (disc >= 0.0) {
+      const double q = -0.5 * (3.0 * b + std::copysign(std::sqrt(disc), b));
+      for (double v : {q / (5.0 * d), a / q})
+        if (inside(v)) next = std::fmax(next, std::sqrt(v) * p(v));
     }
-    if (!(next <= kMaxSigma)) return false;
-    top = next * 1.01;  // between the samples, and roundings
+    if (!(most <= kMaxPoly) || !(next <= kMaxSigma)) return false;
+    top = next * 1.01;  // roundings
+  }
+  // |X_t|_F^2 is the sum over the singular values s of X_0, whose squares add up to
+  // 1, of s^2 times the square of the product of p's that it has met: no less than
+  // the least such product.  Where its sign changes from one s to the next it is 0
+  // between them.
+  uint32_t negative = 0;
+  for (int i = 0; i <= 256; ++i) {
+    double s = (i / 256.0) * (i / 256.0), left = 1.0;
+    uint32_t signs = 0;
+    for (int t = 0; t + 1 < c.steps; ++t) {
+      const double p = c.a[t] + (c.b[t] + c.c[t] * s * s) * s * s;
+      left *= p;
+      s *= p;
+      signs |= (left < 0.0 ? 1u : 0u) << t;
+      if (std::fabs(left) < kMinNorm) return false;
+    }
+    if (i > 0 && signs != negative) return false;
+    negative = signs;
   }
   return true;
 }

@@ -190,6 +190,24 @@ def test_orthogonalize_other_coefficients(P, coeffs, dtype):
     _check(P.orthogonalize(g, coeffs=coeffs), g, coeffs, where=f"{len(coeffs)} steps")
 
 
+@pytest.mark.parametrize("coeffs", [((0.1, 0.0, 0.0), (1.5, -0.5, 0.0)),
+                                    ((0.07, 0.0, 0.0), (2.0, 0.0, 0.0)), ((1e-3, 0.0, 0.0),),
+                                    ((0.26, 0.0, 0.0),) * 3, ((8.0, -8.0, 2.0), (0.01, 0.0, 0.0))])
+def test_orthogonalize_steps_that_shrink(P, coeffs):
+    """Down to a sixteenth of the norm in an iterate, as far as one likes in the
+    result: full spectra, rank one, all singular values equal.  Less is refused."""
+    import torch
+    gen = torch.Generator("cuda")
+    gen.manual_seed(6)
+    a, b = (torch.randn(n, generator=gen, device="cuda") for n in (700, 900))
+    flat = torch.linalg.qr(torch.randn(500, 400, generator=gen, device="cuda"))[0].contiguous()
+    for g in (_gradient(90, 140, 3), torch.outer(a, b).contiguous(), flat):
+        _check(P.orthogonalize(g, coeffs=coeffs), g, coeffs, where=f"{coeffs[0]}")
+    for less in (((0.06, 0.0, 0.0),) + coeffs, ((0.1, 0.0, 0.0),) * 8):
+        with pytest.raises(P.OscarsError):
+            P.orthogonalize(flat, coeffs=less)
+
+
 @pytest.mark.parametrize("scale", [1e-30, 1e-8, 1e8, 1e30])
 def test_orthogonalize_is_free_of_scale(P, scale):
     g = _gradient(96, 200, 9) * scale

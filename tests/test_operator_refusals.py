@@ -79,6 +79,15 @@ def test_one_step_past_the_range_is_refused(step):
     assert _orth(_mats(GOOD), coeffs=P._coeffs((step,))) == P.E_INVALID
 
 
+@pytest.mark.parametrize("steps", [
+    ((0.1, 0.0, 0.0),) * 8, ((0.1, 0.0, 0.0),) * 3, ((0.01, 1.0, 0.0), (1.5, -0.5, 0.0)),
+    ((1.0, -1.0, 0.0), (1.5, -0.5, 0.0)), ((1.0, -1e-3, 0.0), (0.0, 0.0, 0.0), (1.0, 0.0, 0.0))])
+def test_steps_that_shrink_are_refused(steps):
+    """Iterates far below 1 fall out of fp16's range: by every step, for the small
+    singular values only, for the largest one only, and all."""
+    assert _orth(_mats(GOOD), coeffs=P._coeffs(steps)) == P.E_INVALID
+
+
 def test_server_step_refuses_null():
     w = (ctypes.c_float * 1)(1.0)
     o = P._ServerOptions(0.1, 0.9, 0.0, 1.0, 1, 0, COEFFS[0], COEFFS[1])
