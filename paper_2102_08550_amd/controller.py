@@ -421,7 +421,7 @@ def main(argv=None):
     ap.add_argument("--server-lr", type=float, default=None, metavar="LR",
                     help="end every round with the server's step: a momentum and orthogonalised "
                          "updates of this learning rate in the place of the average")
-    ap.add_argument("--server-beta", type=float, default=0.9, help="its momentum")
+    ap.add_argument("--server-beta", type=float, default=None, help="its momentum (0.9)")
     ap.add_argument("--int8-eval", action="store_true",
                     help="evaluate the global model in 8-bit integers too")
     ap.add_argument("--out", default=None, help="also write the JSON here")
@@ -430,7 +430,12 @@ def main(argv=None):
                          "1024-2048-2048-10 fp32 MLP, 4 workers with batches 64, 128, 512, 1024 "
                          "reversed half way")
     args = ap.parse_args(argv)
+    if args.server_beta is not None and args.server_lr is None:
+        ap.error("--server-beta belongs to --server-lr")
     if args.measured > 0:
+        if args.server_lr is not None or args.int8_eval:
+            ap.error("--measured rounds end with the average and evaluate nothing: "
+                     "no --server-lr, no --int8-eval")
         cfg = _measured_cfg()
         sched = BatchSchedule(MEASURED_BATCHES,
                               {args.measured // 2: tuple(reversed(MEASURED_BATCHES))})
@@ -448,8 +453,9 @@ def main(argv=None):
                              jitter=args.jitter, seed=cfg.seed)
     res = compare(cfg, schedule, args.budget, local_steps=args.local_steps,
                   resolution=args.resolution, eval_every=args.eval_every,
-                  server=None if args.server_lr is None else {"lr": args.server_lr,
-                                                              "beta": args.server_beta},
+                  server=None if args.server_lr is None else {
+                      "lr": args.server_lr,
+                      "beta": 0.9 if args.server_beta is None else args.server_beta},
                   int8_eval=args.int8_eval)
     line = json.dumps(res)
     print(line)

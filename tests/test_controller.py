@@ -98,3 +98,22 @@ def test_command_line_takes_the_servers_step_and_int8(C, monkeypatch, capsys):
     capsys.readouterr()
     assert seen[0]["server"] is None and seen[0]["int8_eval"] is False
     assert seen[1]["server"] == {"lr": 0.02, "beta": 0.5} and seen[1]["int8_eval"] is True
+
+
+def test_command_line_refuses_options_that_would_not_count(C, monkeypatch, capsys):
+    """--measured has no server's step and no evaluation, a momentum without the step
+    nothing to belong to: an error, and nothing is run."""
+    def never(*a, **kw):
+        raise AssertionError("run in spite of the error")
+
+    for name in ("compare", "run_measured"):
+        monkeypatch.setattr(C, name, never)
+    for argv in (["--measured", "2", "--server-lr", "0.02"], ["--measured", "2", "--int8-eval"],
+                 ["--server-beta", "0.5"], ["--measured", "2", "--server-beta", "0.5"]):
+        with pytest.raises(SystemExit) as e:
+            C.main(argv)
+        assert e.value.code == 2 and "--server-lr" in capsys.readouterr().err
+    seen = []
+    monkeypatch.setattr(C, "compare", lambda cfg, schedule, budget, **kw: seen.append(kw) or {})
+    assert C.main(["--server-lr", "0.02"]) == 0
+    assert seen[0]["server"] == {"lr": 0.02, "beta": 0.9}
