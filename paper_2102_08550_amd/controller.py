@@ -174,6 +174,11 @@ def measure_step_ms(cfg, dataset, init, reps: int = 5) -> float:
     return float(np.median(times))
 
 
+def _check_int8(cfg, int8_eval: bool):
+    if int8_eval and cfg.is_cnn:
+        raise ValueError(f"{cfg.name}: evaluation in 8-bit integers is for fully connected models")
+
+
 def run_paradigm(cfg, dataset, init, eval_set, paradigm: str, schedule: SpeedSchedule,
                  base: float, time_budget: float, local_steps: int = 4, resolution: int = 8,
                  max_rounds: int = 100000, eval_every: int = 1,
@@ -184,10 +189,11 @@ def run_paradigm(cfg, dataset, init, eval_set, paradigm: str, schedule: SpeedSch
     the final global model as layers when ``return_model``).  ``server``: the
     arguments of OscarsRun.round_server, which then ends every round in the
     place of the average.  ``int8_eval``: every evaluation also with the model
-    in 8-bit integers (eval_loss_i8, eval_acc_i8)."""
+    in 8-bit integers (eval_loss_i8, eval_acc_i8); of fully connected models only."""
     import torch
 
     from .rounds import OscarsRun
+    _check_int8(cfg, int8_eval)
     K = cfg.K
     if schedule.K != K:
         raise ValueError("schedule and workload disagree on K")
@@ -352,6 +358,7 @@ def compare(cfg, schedule: SpeedSchedule, time_budget_steps: float, local_steps:
     budget is in units of the speed-1 step time; ``server`` and ``int8_eval`` as
     for run_paradigm."""
     import workload
+    _check_int8(cfg, int8_eval)
     dataset = workload.gen_dataset(cfg)
     init = workload.gen_init(cfg)
     eval_set = workload.gen_eval_set(cfg, n_eval)

@@ -117,3 +117,16 @@ def test_command_line_refuses_options_that_would_not_count(C, monkeypatch, capsy
     monkeypatch.setattr(C, "compare", lambda cfg, schedule, budget, **kw: seen.append(kw) or {})
     assert C.main(["--server-lr", "0.02"]) == 0
     assert seen[0]["server"] == {"lr": 0.02, "beta": 0.9}
+
+
+def test_int8_evaluation_of_a_convolutional_model_is_refused(C, monkeypatch):
+    """By name and before anything is made or run."""
+    import workload
+    cfg = workload.Config("small-cnn", (8 * 8 * 3, 10), workload.FP32, K=1, n_rows=10, batch=4,
+                          tau_rule="given", tau_given=(1,), image=(8, 8, 3), conv=((16, 1),))
+    sched = C.SpeedSchedule([1])
+    monkeypatch.setattr(workload, "gen_dataset", lambda cfg: pytest.fail("data made"))
+    with pytest.raises(ValueError, match="fully connected"):
+        C.run_paradigm(cfg, None, None, None, "bsp", sched, 1.0, 1.0, int8_eval=True)
+    with pytest.raises(ValueError, match="fully connected"):
+        C.compare(cfg, sched, 1.0, int8_eval=True)
