@@ -85,11 +85,13 @@ class OscarsRun:
         difference.  The momentum (``momentum``) starts at zero."""
         import torch
         stream = self.ctx._stream  # of the steps that follow
-        if self.momentum is None:
-            with torch.cuda.stream(stream):
-                self.momentum = torch.zeros_like(self.g)
         broadcast(self.g, self.replicas, self.cfg.K, self.n, self.n, stream=stream)
         self.local_steps(tau)
+        if self.momentum is None:
+            # behind the steps: where those are refused (into a graph they always are)
+            # no momentum stays that nothing has set to zero
+            with torch.cuda.stream(stream):
+                self.momentum = torch.zeros_like(self.g)
         self.ctx.server_step(self.g, self.replicas, self.weights, self.momentum, lr, beta=beta,
                              nesterov=nesterov, weight_decay=weight_decay, plain_lr=plain_lr,
                              plain_layers=plain_layers)

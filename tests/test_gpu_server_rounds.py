@@ -213,3 +213,31 @@ def test_rounds_on_the_contexts_own_stream(R):
         torch.cuda.synchronize()
         run.close()
         want.close()
+
+
+def test_a_round_refused_under_capture_leaves_the_run_as_it_was(R):
+    """The first round into a graph: the local steps refuse it, and the rounds after
+    it are those of a run that never tried."""
+    import torch
+    cfg = MLP32
+    ds, init = workload.gen_dataset(cfg), workload.gen_init(cfg)
+    run, want = R.OscarsRun(cfg, ds, init), R.OscarsRun(cfg, ds, init)
+    side, main = torch.cuda.Stream(), torch.cuda.current_stream()
+    try:
+        torch.cuda.synchronize()
+        run.ctx.set_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            with pytest.raises(Exception) as ei:
+                run.round_server(cfg.tau_given, **OPTS)
+        assert "oscars_local_steps" in str(ei.value) and run.momentum is None
+        run.ctx.set_stream(main)
+        for _ in range(2):
+            run.round_server(cfg.tau_given, **OPTS)
+            want.round_server(cfg.tau_given, **OPTS)
+        torch.cuda.synchronize()
+        assert torch.equal(run.g, want.g) and torch.equal(run.momentum, want.momentum)
+    finally:
+        torch.cuda.synchronize()
+        run.close()
+        want.close()

@@ -123,6 +123,28 @@ def test_numbers_of_the_default_steps():
     assert np.allclose(P.NEWTON_SCHULZ, ((3.4445, -4.7750, 2.0315),) * 5)
 
 
+def test_a_refused_round_leaves_no_momentum(monkeypatch):
+    """The local steps' refusal comes before the momentum is made: under a stream's
+    capture its zeros would never have been written."""
+    import types
+
+    import torch
+
+    from paper_2102_08550_amd import rounds as R
+    monkeypatch.setattr(R, "broadcast", lambda *a, **kw: None)
+    run = R.OscarsRun.__new__(R.OscarsRun)
+    run.ctx, run.cfg = types.SimpleNamespace(_stream=None), types.SimpleNamespace(K=2)
+    run.g, run.replicas, run.n, run.momentum = torch.zeros(64), torch.zeros(128), 64, None
+
+    def refuse(tau):
+        raise P.OscarsError(P.E_STATE, "oscars_local_steps")
+
+    run.local_steps = refuse
+    with pytest.raises(P.OscarsError):
+        run.round_server([1, 1], lr=0.1)
+    assert run.momentum is None
+
+
 # ------------------------------------------------------------------ 8 bits
 
 Q, X, W, S, OUT = (BASE + k * 0x1000000 for k in range(2, 7))
