@@ -310,6 +310,16 @@ def _workspace(nbytes: int, device, stream=None):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+def _used_on(stream, *tensors):
+    """What a call on ``stream`` reads or writes (None: the current one, whose work
+    torch orders by itself): dropped by the caller, it is not given to other
+    streams' work before the call has run."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 @functools.lru_cache(maxsize=16)
 def _coeffs(coeffs):
     """((a, b, c), ...) as a C array, kept with its number of steps."""
@@ -381,6 +391,7 @@ def orthogonalize(x, out=None, coeffs=NEWTON_SCHULZ, stream=None):
         _check(_lib().oscars_orthogonalize(mats, len(xs), FP32 if dt == torch.float32 else BF16,
                                            ca, steps, ws.data_ptr(), need,
                                            _stream_handle(stream)), "oscars_orthogonalize")
+    _used_on(stream, *xs, *outs)
     return outs[0] if single else outs
 
 
@@ -450,6 +461,7 @@ def quantize_rows(x, out=None, stream=None):
     with _on_device(dev):
         _check(_lib().oscars_quantize_rows(qp, qld, _vector(scale, n, dev, "scale"), xp, ld, dt, n,
                                            cols, _stream_handle(stream)), "oscars_quantize_rows")
+    _used_on(stream, x, q, scale)
     return out
 
 
@@ -479,6 +491,7 @@ def matmul_i8(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool = 
             wld, _vector(wscale, outs, dev, "wscale"), _vector(bias, outs, dev, "bias"),
             int(bool(relu)), n, int(in_features), outs, _stream_handle(stream)),
             "oscars_matmul_quantized")
+    _used_on(stream, xq, xscale, wq, wscale, bias, out)
     return out
 
 
@@ -512,6 +525,7 @@ def linear_i8(x, wq, wscale, bias=None, relu: bool = False, out_dtype=None, out=
             _vector(wscale, outs, dev, "wscale"), _vector(bias, outs, dev, "bias"),
             int(bool(relu)), n, cols, outs, ws.data_ptr() if need else None, need,
             _stream_handle(stream)), "oscars_linear_quantized")
+    _used_on(stream, x, wq, wscale, bias, out)
     return out
 
 
@@ -674,6 +688,7 @@ class Context:
         if out.numel() < need:
             raise ValueError(f"a quantised model takes {need} bytes")
         _check(_lib().oscars_quantize_model(self._h, pp, op), "oscars_quantize_model")
+        _used_on(self._stream, params, out)
         return out
 
     def evaluate_i8(self, model, x, y, n_rows: Optional[int] = None):
@@ -732,6 +747,7 @@ class Context:
         _check(_lib().oscars_server_step(self._h, ptrs[0], ptrs[1], wp, ptrs[2], ptrs[3], ptrs[4],
                                          ctypes.byref(o), ws.data_ptr(), need),
                "oscars_server_step")
+        _used_on(self._stream, global_, replicas, momentum, g_out, m_out)
         return g_out, m_out
 
     def cursors(self) -> List[int]:

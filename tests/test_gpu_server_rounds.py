@@ -241,3 +241,63 @@ def test_a_round_refused_under_capture_leaves_the_run_as_it_was(R):
         torch.cuda.synchronize()
         run.close()
         want.close()
+
+
+def _late(side):
+    """Some milliseconds of work, so that what follows on ``side`` runs late."""
+    import torch
+    with torch.cuda.stream(side):
+        a = torch.randn(4096, 4096, device="cuda")
+        for _ in range(40):
+            a = (a @ a).clamp(-1, 1)
+    return a
+
+
+def test_inputs_dropped_behind_a_call_on_another_stream(R):
+    """Tensors that the caller drops while a call on another stream has yet to read
+    them: their memory is not given to the caller's own stream meanwhile."""
+    import torch
+    import paper_2102_08550_amd as P
+    torch.manual_seed(3)
+    x, g = torch.randn(777, 1000, device="cuda"), torch.randn(500, 640, device="cuda")
+    w, ws = P.quantize_rows(torch.randn(300, 1000, device="cuda"))
+    xq, xs = P.quantize_rows(x)
+    cfg = MLP32
+    run = R.OscarsRun(cfg, workload.gen_dataset(cfg), workload.gen_init(cfg))
+    side = torch.cuda.Stream()
+    mom = torch.zeros_like(run.g)
+    reps = run.replicas + 0.01 * torch.randn_like(run.replicas)
+
+    def step(*tensors):
+        return run.ctx.server_step(tensors[0], tensors[1], run.weights, tensors[2], lr=0.05,
+                                   out=(torch.empty_like(run.g), torch.empty_like(run.g)))
+
+    calls = [("linear_i8", lambda s, a: P.linear_i8(a, w, ws, stream=s), (x,)),
+             ("quantize_rows", lambda s, a: P.quantize_rows(a, stream=s), (x,)),
+             ("matmul_i8", lambda s, a, b: P.matmul_i8(a, b, w, ws, 1000, stream=s), (xq, xs)),
+             ("orthogonalize", lambda s, a: P.orthogonalize(a, stream=s), (g,)),
+             ("quantize_model", lambda s, a: run.ctx.quantize_model(a), (run.g,)),
+             ("server_step", lambda s, *t: step(*t), (run.g, reps, mom))]
+    try:
+        for name, call, args in calls:
+            run.ctx.set_stream(None)
+            want = call(None, *args)
+            torch.cuda.synchronize()
+            run.ctx.set_stream(side)
+            keep = _late(side)
+            mine = [a.clone() for a in args]
+            side.wait_stream(torch.cuda.current_stream())  # the copies are there
+            got = call(side, *mine)
+            shapes = [(a.shape, a.dtype) for a in mine]
+            del mine
+            junk = [torch.full(s, 100, dtype=d, device="cuda") for s, d in shapes]
+            torch.cuda.synchronize()
+            pairs = zip(want, got) if isinstance(want, tuple) else [(want, got)]
+            for a, b in pairs:
+                if name == "quantize_model":  # integers of the first layer; the rest has gaps
+                    a, b = a[:72 * 128], b[:72 * 128]
+                assert torch.equal(a, b), name
+            del keep, junk
+    finally:
+        torch.cuda.synchronize()
+        run.close()
