@@ -49,8 +49,9 @@ __device__ __forceinline__ typename NtAcc<F>::type nt_mfma(nt_u32x4 a, nt_u32x4 
 // there are registers for it: NT_SPLIT's products with a lo plane have accumulators
 // of their own, added at the end.  Every product rounds the sum it goes into, and
 // the small ones would round the large sum two more times.  Five Newton-Schulz
-// steps of 10 x 256 matrices, error in 2-norm, median and worst of 24: 1.2e-6 and
-// 1.5e-6 without, 7.3e-7 and 1.3e-6 with; in fp32 6.1e-7 and 7.7e-7.
+// steps in 128 x 128 tiles, error in the Frobenius norm, without and with: 1024 x
+// 4096 1.70e-6 and 1.07e-6, 2048 x 2048 2.68e-6 and 1.55e-6, 2900 x 2950 2.91e-6 and
+// 1.67e-6; the calls take 0.3 to 0.5% longer.
 template <int BM_, int BN_, int WM_, int WN_, bool EXACT_ = false>
 struct NtShape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;

@@ -33,7 +33,7 @@ struct OrthCoeffs {
 // Whether the polynomials keep every intermediate, from singular values in [0, 1]
 // on, within the range of the fp16 planes, at both of its ends.
 bool orth_coeffs_ok(const OrthCoeffs& c);
-// Device bytes of a call's temporaries (256-byte aligned base).
+// Device bytes of a call's temporaries (their base 16-byte aligned).
 int64_t orth_workspace(const OrthMat* mats, int count);
 // norms_done: the sums of squares of every matrix are in the workspace already
 // (launch_server_pass).
