@@ -347,9 +347,10 @@ oscars_status oscars_broadcast(const float* global, float* replicas, int32_t K, 
  *            is rounded once, at the end;
  *   coeffs   host [steps][3], 1 <= steps <= OSCARS_MAX_ORTH_STEPS; refused where
  *            a step's polynomial a + b s^2 + c s^4 passes 400, or a singular
- *            value 16, from singular values s in [0, 1] on, or where the steps
- *            before the last can leave less than 1/16 of the Frobenius norm
- *            (iterates are held in fp16's range);
+ *            value 16, from singular values s in [0, 1] on (each step's largest
+ *            and 1% to spare go into the next), or where the steps before the
+ *            last can leave less than 1/16 of the Frobenius norm (iterates are
+ *            held in fp16's range);
  *   workspace  device, 16-byte aligned, oscars_orthogonalize_workspace bytes,
  *            no part of a matrix; the call's own until the stream has run it.
  * A matrix of zeros gives zeros, one with a NaN or an infinity gives NaN; the

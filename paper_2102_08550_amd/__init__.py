@@ -352,7 +352,8 @@ def orthogonalize(x, out=None, coeffs=NEWTON_SCHULZ, stream=None):
     or of every matrix of a sequence, in one call: fp32 or bf16 device tensors
     of one type, stored by rows or by columns, with any stride between them.
     ``out``: where the results go (``x`` itself is allowed), stored the same
-    way; new tensors by default.  Returns ``out``."""
+    way; new tensors by default.  ``coeffs``: each step's (a, b, c); steps that
+    leave fp16's range are refused.  Returns ``out``."""
     import torch
     single = isinstance(x, torch.Tensor)
     xs = [x] if single else list(x)
