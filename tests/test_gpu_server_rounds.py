@@ -301,3 +301,36 @@ def test_inputs_dropped_behind_a_call_on_another_stream(R):
     finally:
         torch.cuda.synchronize()
         run.close()
+
+
+def test_a_named_stream_under_capture(R):
+    """The operators captured with the capture's stream as an argument, on tensors of
+    the default stream and on ones made and dropped during the capture."""
+    import torch
+    import paper_2102_08550_amd as P
+    torch.manual_seed(4)
+    x, g = torch.randn(90, 300, device="cuda"), torch.randn(70, 130, device="cuda")
+    w, ws = P.quantize_rows(torch.randn(40, 300, device="cuda"))
+    out = [torch.empty(90, 40, device="cuda"), torch.empty(90, 40, device="cuda"),
+           torch.empty_like(g)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        P.linear_i8(x, w, ws, out=out[0], stream=side)
+        xq, xs = P.quantize_rows(x * 2, stream=side)
+        P.matmul_i8(xq, xs, w, ws, 300, out=out[1], stream=side)
+        del xq, xs
+        P.orthogonalize(g + 1, out=out[2], stream=side)
+    for k in range(4):
+        x.normal_()
+        g.normal_()
+        want = [P.linear_i8(x, w, ws), P.linear_i8(x * 2, w, ws), P.orthogonalize(g + 1)]
+        for o in out:
+            o.fill_(-3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, out)), f"replay {k}"
+    del x, g
+    torch.cuda.synchronize()
