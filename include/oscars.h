@@ -470,6 +470,114 @@ oscars_status oscars_evaluate_quantized(oscars_ctx* ctx, const void* model, cons
                                         const int32_t* y, int64_t n_rows, double* loss_sum,
                                         int64_t* correct);
 
+/* The linear layer in microscaled 4-bit floating point, for answers and for
+ * training.  Rows in 4 bits: 32 consecutive entries share a scale, the least power
+ * of two s from 2^-127 on with max |x| < 7 s, or 2^125 (so that no finite entry
+ * becomes infinite); an entry is x / s rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, ties to the even code.
+ * An entry's code is its magnitude's place in that list, plus 8 where it is
+ * negative; two codes a byte, the first entry's in the low half.  A scale is the byte
+ * log2(s) + 127.  A block whose largest magnitude is below 2^-126 counts as zeros
+ * (scale byte 0); one with a NaN or an infinity has zeros and scale byte 255, NaN,
+ * so that what it enters is NaN.  Behind a row's entries the bytes are 0 to the next
+ * multiple of 128 (256 entries), the scales to the next multiple of 16 (512 entries);
+ * both are part of the row and have to be there:
+ *   q      device [rows][q_ld], 16-byte aligned, q_ld % 16 == 0, q_ld <= 2^23;
+ *   scale  device [rows][s_ld], likewise.
+ * Rows have at most 2^24 entries.  No call allocates, all may be captured into a
+ * graph, results do not differ from run to run; an output overlaps no other argument.
+ *
+ * Dropout in a layer or by itself: t = round(65536 p), half to even; entry (r, c) is
+ * dropped (0) where its 16 bits of Philox4x32-10 are below t, and multiplied by
+ * 65536 / (65536 - t) in fp32 elsewhere (p = 1: all are dropped).  Key: seed (low
+ * word first).  Counter: c / 8, r, and the sum of offset and *offset_device (device,
+ * 8-byte aligned, read when the call runs, or NULL), low word first; the entry's bits
+ * are half c mod 2 (low first) of word (c mod 8) / 2.  A captured step draws another
+ * mask at each replay where the program counts *offset_device up in between. */
+typedef struct {
+  double p; /* 0 .. 1 */
+  uint64_t seed, offset;
+  const uint64_t* offset_device;
+} oscars_dropout_options;
+
+/* oscars_quantize_micro: the rows of x in 4 bits, or with `transposed` the rows of
+ *   x', one per column of x.
+ *   x      device [rows][x_ld], dtype OSCARS_FP32 or OSCARS_BF16, aligned to its
+ *          elements, x_ld >= cols;  0 <= rows < 2^31, 1 <= cols; the entries of a
+ *          quantised row at most 2^24, with `transposed` fewer than 2^37 in all.
+ * oscars_dequantize_micro: the values of quantised rows, in fp32 or rounded to bf16.
+ * oscars_matmul_micro: the product of quantised rows and weights,
+ *   y[r][o] = drop(relu(sum_k x[r][k] w[o][k] + bias[o])),  sums, bias and dropout's
+ *   factor in fp32, then the output's type; ReLU keeps a NaN.
+ *   xq, xscale  [rows] quantised rows of `in` entries;  wq, wscale  [outs] of them;
+ *   bias   device [outs] fp32 or NULL;  out  device [rows][out_ld] of out_dtype,
+ *          out_ld >= outs, aligned to its elements; 1 <= in <= 2^24,
+ *          1 <= outs <= 2^24;  dropout  host, or NULL: none.
+ * oscars_linear_micro: both, x [rows][x_ld] of `dtype` as for oscars_quantize_micro, in
+ *   <= OSCARS_MAX_WIDTH; one row, or up to 16 of together 16384 entries, in one
+ *   launch.  workspace: device, 16-byte aligned, oscars_linear_micro_workspace bytes
+ *   (NULL where those are 0), the call's own until the stream has run it. */
+oscars_status oscars_quantize_micro(uint8_t* q, int64_t q_ld, uint8_t* scale, int64_t s_ld,
+                                    const void* x, int64_t x_ld, int32_t dtype, int64_t rows,
+                                    int64_t cols, int32_t transposed, void* hip_stream);
+oscars_status oscars_dequantize_micro(void* out, int64_t out_ld, int32_t out_dtype,
+                                      const uint8_t* q, int64_t q_ld, const uint8_t* scale,
+                                      int64_t s_ld, int64_t rows, int64_t cols, void* hip_stream);
+oscars_status oscars_matmul_micro(void* out, int64_t out_ld, int32_t out_dtype, const uint8_t* xq,
+                                  int64_t x_ld, const uint8_t* xscale, int64_t xs_ld,
+                                  const uint8_t* wq, int64_t w_ld, const uint8_t* wscale,
+                                  int64_t ws_ld, const float* bias, int32_t relu,
+                                  const oscars_dropout_options* dropout, int64_t rows, int64_t in,
+                                  int64_t outs, void* hip_stream);
+int64_t oscars_linear_micro_workspace(int64_t rows, int64_t in);
+oscars_status oscars_linear_micro(void* out, int64_t out_ld, int32_t out_dtype, const void* x,
+                                  int64_t x_ld, int32_t dtype, const uint8_t* wq, int64_t w_ld,
+                                  const uint8_t* wscale, int64_t ws_ld, const float* bias,
+                                  int32_t relu, const oscars_dropout_options* dropout,
+                                  int64_t rows, int64_t in, int64_t outs, void* workspace,
+                                  int64_t workspace_bytes, void* hip_stream);
+
+/* The gradients of oscars_linear_micro's layer, straight through the rounding to 4 bits
+ * Q:  dz = dy where the layer passed its output on, times dropout's factor (fp32);
+ *   dx = Q(dz) Q(w')  along the outputs,  dw = Q(dz') Q(x')  along the rows,
+ *   db[o] = sum_r dz[r][o].
+ * What the layer passed on is y > 0 (or NaN) where its output y is given, which a layer with
+ * a ReLU needs and dropout then asks for nothing else; without y dropout's choice is
+ * drawn again from the options of the forward call.
+ *   dy, y    device [rows][..ld], y_dtype; y NULL for a layer without ReLU;
+ *   x        device [rows][x_ld], x_dtype: the layer's input;
+ *   wtq, wtscale  the weights' columns in 4 bits (oscars_quantize_micro of w [outs][in],
+ *            transposed): [in] quantised rows of `outs` entries;
+ *   dx       device [rows][dx_ld], x_dtype, or NULL: not wanted (wtq, wtscale unused);
+ *   dw       device [outs][dw_ld] fp32;  db  device [outs] fp32, or NULL;
+ *   0 <= rows <= 2^24 (0: dw and db are 0), 1 <= in, outs <= OSCARS_MAX_WIDTH;
+ *   workspace  device, 16-byte aligned, oscars_linear_micro_backward_workspace bytes,
+ *            the call's own until the stream has run it. */
+typedef struct {
+  int64_t rows, in, outs;
+  const void *dy, *y, *x;
+  int64_t dy_ld, y_ld, x_ld;
+  int32_t y_dtype, x_dtype;
+  const uint8_t *wtq, *wtscale;
+  int64_t wt_ld, wts_ld;
+  void* dx;
+  float *dw, *db;
+  int64_t dx_ld, dw_ld;
+  const oscars_dropout_options* dropout;
+} oscars_micro_gradients;
+int64_t oscars_linear_micro_backward_workspace(int64_t rows, int64_t in, int64_t outs,
+                                               int32_t want_dx);
+oscars_status oscars_linear_micro_backward(const oscars_micro_gradients* g, void* workspace,
+                                           int64_t workspace_bytes, void* hip_stream);
+
+/* Dropout by itself: out[r][c] = x[r][c] times the factor, rounded to the type, where
+ * kept, else 0 (whatever x holds).  Its gradient is the same call on the output's.
+ *   x, out  device [rows][..ld] of dtype, aligned to its elements; out may be x, with
+ *           the same stride, and overlaps it in no other way;  0 <= rows < 2^31,
+ *           1 <= cols < 2^31. */
+oscars_status oscars_dropout(void* out, int64_t out_ld, const void* x, int64_t x_ld, int32_t dtype,
+                             const oscars_dropout_options* options, int64_t rows, int64_t cols,
+                             void* hip_stream);
+
 /* Resume support: per-worker count of local steps done so far. host [K]. */
 oscars_status oscars_get_cursors(const oscars_ctx* ctx, int64_t* steps_done);
 oscars_status oscars_set_cursors(oscars_ctx* ctx, const int64_t* steps_done);

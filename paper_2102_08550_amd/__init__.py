@@ -70,6 +70,18 @@ class _ServerOptions(ctypes.Structure):
                 ("steps", _i32)]
 
 
+class _Dropout(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", _u64), ("offset", _u64), ("offset_device", _vp)]
+
+
+class _Gradients(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("inputs", _i64), ("outs", _i64), ("dy", _vp), ("y", _vp),
+                ("x", _vp), ("dy_ld", _i64), ("y_ld", _i64), ("x_ld", _i64), ("y_dtype", _i32),
+                ("x_dtype", _i32), ("wtq", _vp), ("wtscale", _vp), ("wt_ld", _i64),
+                ("wts_ld", _i64), ("dx", _vp), ("dw", _vp), ("db", _vp), ("dx_ld", _i64),
+                ("dw_ld", _i64), ("dropout", _P(_Dropout))]
+
+
 class _Shards(ctypes.Structure):
     _fields_ = [("x", _vp), ("y", _vp), ("n_rows", _i64), ("offsets", _P(_i64)), ("seed", _u64)]
 
@@ -117,6 +129,16 @@ _SIGS = {
     "oscars_linear_quantized_workspace": (_i64, [_i64, _i32]),
     "oscars_linear_quantized": (_i32, [_vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _i32,
                                        _i64, _i32, _i32, _vp, _i64, _vp]),
+    "oscars_quantize_micro": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i64, _i64, _i32, _vp]),
+    "oscars_dequantize_micro": (_i32, [_vp, _i64, _i32, _vp, _i64, _vp, _i64, _i64, _i64, _vp]),
+    "oscars_matmul_micro": (_i32, [_vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp,
+                                   _i32, _P(_Dropout), _i64, _i64, _i64, _vp]),
+    "oscars_linear_micro_workspace": (_i64, [_i64, _i64]),
+    "oscars_linear_micro": (_i32, [_vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp,
+                                   _i32, _P(_Dropout), _i64, _i64, _i64, _vp, _i64, _vp]),
+    "oscars_linear_micro_backward_workspace": (_i64, [_i64, _i64, _i64, _i32]),
+    "oscars_linear_micro_backward": (_i32, [_P(_Gradients), _vp, _i64, _vp]),
+    "oscars_dropout": (_i32, [_vp, _i64, _vp, _i64, _i32, _P(_Dropout), _i64, _i64, _vp]),
     "oscars_quantized_model_bytes": (_i64, [_vp]),
     "oscars_quantize_model": (_i32, [_vp, _vp, _vp]),
     "oscars_evaluate_quantized": (_i32, [_vp, _vp, _vp, _vp, _i64, _P(ctypes.c_double), _P(_i64)]),
@@ -527,6 +549,239 @@ def linear_i8(x, wq, wscale, bias=None, relu: bool = False, out_dtype=None, out=
             int(bool(relu)), n, cols, outs, ws.data_ptr() if need else None, need,
             _stream_handle(stream)), "oscars_linear_quantized")
     _used_on(stream, x, wq, wscale, bias, out)
+    return out
+
+
+def _micro_shapes(rows: int, cols: int):
+    """The shapes of ``rows`` rows of ``cols`` entries in 4 bits and of their scales."""
+    return (rows, (cols + 255) // 256 * 128), (rows, (cols + 511) // 512 * 16)
+
+
+def _micro_rows(q, scale, rows, cols, device, what):
+    """(pointer, row stride, scales' pointer, row stride) of quantised rows."""
+    import torch
+    qp, n, qld, qc = _rows(q, torch.uint8, device, what)
+    sp, sn, sld, sc = _rows(scale, torch.uint8, device, what + "'s scales")
+    (_, width), (_, blocks) = _micro_shapes(rows, cols)
+    if n != rows or sn != rows or qc < width or sc < blocks:
+        raise ValueError(f"{what} must hold {rows} rows of {width} bytes and {blocks} scales")
+    # the stride of a single row says nothing
+    return qp, qld if n > 1 else width, sp, sld if n > 1 else blocks
+
+
+def _dropout_options(dropout, device):
+    """(options, the offset's tensor) of ``(p, seed[, offset])``; Nones for None."""
+    import torch
+    if dropout is None:
+        return None, None
+    p, seed, offset = dropout if len(dropout) == 3 else (*dropout, 0)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("dropout's p must be from 0 to 1")
+    if not 0 <= seed < 1 << 64:
+        raise ValueError("dropout's seed must be of 64 bits, not negative")
+    if isinstance(offset, torch.Tensor):
+        if not offset.is_cuda or offset.device != device or offset.dtype != torch.int64:
+            raise TypeError("dropout's offset must be an int, or int64 on the input's device")
+        if offset.numel() != 1:
+            raise ValueError("dropout's offset must be one number")
+        return _Dropout(p, seed, 0, offset.data_ptr()), offset
+    if not 0 <= offset < 1 << 64:
+        raise ValueError("dropout's offset must be of 64 bits, not negative")
+    return _Dropout(p, seed, offset, None), None
+
+
+def quantize_mx4(x, transposed: bool = False, out=None, stream=None):
+    """The rows of ``x`` (fp32 or bf16 matrix, any row stride) in microscaled 4-bit
+    floating point (oscars_quantize_micro), or with ``transposed`` the rows of its
+    transpose: ``(q, scale)``, uint8, two entries a byte and a scale for every 32.
+    ``out``: such a pair to write into, row strides multiples of 16."""
+    import torch
+    dev = x.device
+    xp, n, ld, cols = _rows(x, x.dtype, dev, "x")
+    dt = _float_type(x.dtype, "x")
+    count, along = (cols, n) if transposed else (n, cols)
+    if out is None:
+        qs, ss = _micro_shapes(count, along)
+        out = _new(qs, torch.uint8, dev, stream), _new(ss, torch.uint8, dev, stream)
+    q, scale = out
+    qp, qld, sp, sld = _micro_rows(q, scale, count, along, dev, "q")
+    if n == 0:
+        return out
+    with _on_device(dev):
+        _check(_lib().oscars_quantize_micro(qp, qld, sp, sld, xp, ld, dt, n, cols,
+                                            int(bool(transposed)), _stream_handle(stream)),
+               "oscars_quantize_micro")
+    _used_on(stream, x, q, scale)
+    return out
+
+
+def dequantize_mx4(q, scale, columns: int, dtype=None, out=None, stream=None):
+    """The values of quantised rows of ``columns`` entries (oscars_dequantize_micro), in
+    fp32 by default."""
+    import torch
+    dev = q.device
+    n = q.shape[0]
+    qp, qld, sp, sld = _micro_rows(q, scale, n, int(columns), dev, "q")
+    if out is None:
+        out = _new((n, int(columns)), dtype or torch.float32, dev, stream)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError("out has another dtype than dtype")
+    op, on, old, oc = _rows(out, out.dtype, dev, "out")
+    if (on, oc) != (n, columns):
+        raise ValueError("out must be [rows][columns]")
+    if n == 0:
+        return out
+    with _on_device(dev):
+        _check(_lib().oscars_dequantize_micro(op, old, _float_type(out.dtype, "out"), qp, qld, sp,
+                                              sld, n, int(columns), _stream_handle(stream)),
+               "oscars_dequantize_micro")
+    _used_on(stream, q, scale, out)
+    return out
+
+
+def matmul_mx4(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool = False,
+               dropout=None, out_dtype=None, out=None, stream=None):
+    """drop(relu(x w' + bias)) (oscars_matmul_micro) of quantised rows ``xq`` [rows][..]
+    and weights ``wq`` [outputs][..] as quantize_mx4 gives them, of ``in_features``
+    entries each; ``dropout``: ``(p, seed)`` or ``(p, seed, offset)`` as in ``dropout``;
+    fp32 by default.  Returns ``out``."""
+    import torch
+    dev = xq.device
+    n, outs, cols = xq.shape[0], wq.shape[0], int(in_features)
+    xp, xld, xsp, xsld = _micro_rows(xq, xscale, n, cols, dev, "xq")
+    wp, wld, wsp, wsld = _micro_rows(wq, wscale, outs, cols, dev, "wq")
+    if out is None:
+        out = _new((n, outs), out_dtype or torch.float32, dev, stream)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError("out has another dtype than out_dtype")
+    op, on, old, oc = _rows(out, out.dtype, dev, "out")
+    if (on, oc) != (n, outs):
+        raise ValueError("out must be [rows][outputs]")
+    drop, offset = _dropout_options(dropout, dev)
+    if n == 0:
+        return out
+    with _on_device(dev):
+        _check(_lib().oscars_matmul_micro(
+            op, old, _float_type(out.dtype, "out"), xp, xld, xsp, xsld, wp, wld, wsp, wsld,
+            _vector(bias, outs, dev, "bias"), int(bool(relu)), drop, n, cols, outs,
+            _stream_handle(stream)), "oscars_matmul_micro")
+    _used_on(stream, xq, xscale, wq, wscale, bias, offset, out)
+    return out
+
+
+def linear_mx4(x, wq, wscale, bias=None, relu: bool = False, dropout=None, out_dtype=None,
+               out=None, stream=None):
+    """A linear layer in microscaled 4-bit floating point (oscars_linear_micro): the rows of
+    ``x`` (fp32 or bf16) are quantised on the way, ``wq`` and ``wscale`` are a weight
+    matrix's quantize_mx4.  ``dropout`` (training): ``(p, seed)`` or ``(p, seed,
+    offset)`` as in ``dropout``.  The result has ``x``'s type by default.  Returns
+    ``out``; linear_mx4_backward has the gradients."""
+    import torch
+    dev = x.device
+    xp, n, xld, cols = _rows(x, x.dtype, dev, "x")
+    dt = _float_type(x.dtype, "x")
+    outs = wq.shape[0]
+    wp, wld, wsp, wsld = _micro_rows(wq, wscale, outs, cols, dev, "wq")
+    if out is None:
+        out = _new((n, outs), out_dtype or x.dtype, dev, stream)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError("out has another dtype than out_dtype")
+    op, on, old, oc = _rows(out, out.dtype, dev, "out")
+    if (on, oc) != (n, outs):
+        raise ValueError("out must be [rows][outputs]")
+    drop, offset = _dropout_options(dropout, dev)
+    if n == 0:
+        return out
+    lib = _lib()
+    need = lib.oscars_linear_micro_workspace(n, cols)
+    ws = _workspace(need, dev, stream) if need else None
+    with _on_device(dev):
+        _check(lib.oscars_linear_micro(
+            op, old, _float_type(out.dtype, "out"), xp, xld, dt, wp, wld, wsp, wsld,
+            _vector(bias, outs, dev, "bias"), int(bool(relu)), drop, n, cols, outs,
+            ws.data_ptr() if need else None, need, _stream_handle(stream)),
+            "oscars_linear_micro")
+    _used_on(stream, x, wq, wscale, bias, offset, out)
+    return out
+
+
+def linear_mx4_backward(dy, x, wtq=None, wtscale=None, y=None, dropout=None, want_dx: bool = True,
+                        out=None, stream=None):
+    """The gradients of linear_mx4's layer (oscars_linear_micro_backward), straight through the
+    rounding to 4 bits: ``(dx, dw, db)`` from the output's gradient ``dy``, the
+    layer's input ``x`` and ``quantize_mx4(w, transposed=True)``.  ``y``: the layer's
+    output, for a layer with a ReLU.  ``dropout``: as in the forward call.  dx has
+    ``x``'s type (None without ``want_dx``, which needs no weights), dw and db are
+    fp32.  ``out``: such a triple to write into."""
+    import torch
+    dev = dy.device
+    dyp, n, dyld, outs = _rows(dy, dy.dtype, dev, "dy")
+    xp, xn, xld, cols = _rows(x, x.dtype, dev, "x")
+    if xn != n:
+        raise ValueError("dy and x must have as many rows")
+    g = _Gradients(rows=n, inputs=cols, outs=outs, dy=dyp, dy_ld=dyld, x=xp, x_ld=xld,
+                   y_dtype=_float_type(dy.dtype, "dy"), x_dtype=_float_type(x.dtype, "x"))
+    if y is not None:
+        g.y, yn, g.y_ld, yc = _rows(y, dy.dtype, dev, "y")
+        if (yn, yc) != (n, outs):
+            raise ValueError("y must have dy's shape")
+    if out is None:
+        out = (_new((n, cols), x.dtype, dev, stream) if want_dx else None,
+               _new((outs, cols), torch.float32, dev, stream),
+               _new((outs,), torch.float32, dev, stream))
+    dx, dw, db = out
+    if (dx is not None) != bool(want_dx):
+        raise ValueError("out must hold a dx where it is wanted, and None where it is not")
+    if want_dx:
+        if wtq is None or wtscale is None:
+            raise ValueError("dx needs the weights' columns in 4 bits")
+        g.wtq, g.wt_ld, g.wtscale, g.wts_ld = _micro_rows(wtq, wtscale, cols, outs, dev, "wtq")
+        g.dx, dn, g.dx_ld, dc = _rows(dx, x.dtype, dev, "dx")
+        if (dn, dc) != (n, cols):
+            raise ValueError("dx must have x's shape")
+    g.dw, wn, g.dw_ld, wc = _rows(dw, torch.float32, dev, "dw")
+    if (wn, wc) != (outs, cols):
+        raise ValueError("dw must be [outputs][inputs]")
+    g.db = _vector(db, outs, dev, "db")
+    drop, offset = _dropout_options(dropout, dev)
+    if drop is not None:
+        g.dropout = ctypes.pointer(drop)
+    if n == 0:  # what empty tensors point at
+        g.dy = g.x = g.dw
+        g.y, g.dx = None, None
+    lib = _lib()
+    need = lib.oscars_linear_micro_backward_workspace(n, cols, outs, int(g.dx is not None))
+    ws = _workspace(need, dev, stream) if need else None
+    with _on_device(dev):
+        _check(lib.oscars_linear_micro_backward(
+            ctypes.byref(g), ws.data_ptr() if need else None, need, _stream_handle(stream)),
+            "oscars_linear_micro_backward")
+    _used_on(stream, dy, x, wtq, wtscale, y, offset, dx, dw, db)
+    return out
+
+
+def dropout(x, p: float, seed: int, offset=0, out=None, stream=None):
+    """Dropout from a counter-based generator (oscars_dropout) of ``x`` (fp32 or bf16
+    matrix, any row stride): entries are 0 with probability ``p`` (to 16 bits),
+    multiplied by 1 / (1 - p) otherwise.  The mask is a function of ``seed``,
+    ``offset`` (the call's number in a training run; an int64 tensor of one element
+    on the device is read when the call runs) and the place, so the gradient is
+    ``dropout(dy, p, seed, offset)``.  ``out``: ``x`` itself is allowed."""
+    dev = x.device
+    xp, n, ld, cols = _rows(x, x.dtype, dev, "x")
+    dt = _float_type(x.dtype, "x")
+    if out is None:
+        out = _new((n, cols), x.dtype, dev, stream)
+    op, on, old, oc = _rows(out, x.dtype, dev, "out")
+    if (on, oc) != (n, cols):
+        raise ValueError("out must have x's shape")
+    options, more = _dropout_options((p, seed, offset), dev)
+    if n == 0:
+        return out
+    with _on_device(dev):
+        _check(_lib().oscars_dropout(op, old, xp, ld, dt, options, n, cols,
+                                     _stream_handle(stream)), "oscars_dropout")
+    _used_on(stream, x, more, out)
     return out
 
 

@@ -1,0 +1,941 @@
+// The linear layer in microscaled 4-bit floating point (mx4.h has the format):
+//   y[r][o] = drop(relu(sum_k Q(x)[r][k] Q(w)[o][k] + b[o])),
+// and what its gradients take.  A product of two entries is exact, and so is its
+// scale; the matrix units add them into fp32.
+//
+//   mx4_rows      rows into 4 bits, one pass;
+//   mx4_columns   columns into 4 bits (the rows of x'), and their sums;
+//   mx4_values    4 bits back into values;
+//   mx4_product   tiles on 32x32x64 block-scaled matrix instructions: a lane's 16
+//                 bytes of an operand are one block of 32 with one scale;
+//   mx4_few       one row, or up to 16 short ones: a stream of the weights, with the
+//                 rows' quantisation in front of it in every workgroup.
+#include "mx4.h"
+
+#include "mx4_plan.h"
+#include "nt_mma.h"
+
+namespace oscars {
+namespace {
+
+typedef int mx_i32x8 __attribute__((ext_vector_type(8)));
+typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float mx_bf16(uint32_t v) {
+  return __builtin_bit_cast(float, v << 16);
+}
+__device__ __forceinline__ uint16_t mx_to_bf16(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return static_cast<uint16_t>(u >> 16) | 0x40;
+  return static_cast<uint16_t>((u + 0x7FFF + ((u >> 16) & 1)) >> 16);
+}
+__device__ __forceinline__ uint32_t mx_abs(float v) {
+  return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
+}
+
+// A block's scale from its largest |x| as bits.  Adding a quarter of the significand's
+// range carries into the exponent from 7/4 on: then the largest entry would be
+// rounded to 8, which is not there, and the scale is twice as large.  (Scales by the
+// exponent alone, with what is above 6 cut to 6, have 1.06 times the squared error for
+// normal entries, 1.04 where channels differ, 2.1 for uniform ones; scales that bring
+// the largest to 6 or below 1.06, 1.10 and 1.00 times.)  Scales end at 2^125: what is
+// left above 6 is cut to 6, where 2^126 would make it 2^128.
+// inv: what an entry is multiplied with, exactly; 0 where the block counts as zeros:
+// with no normal number in it, or with a NaN or an infinity (scale byte 255: NaN).
+struct MxScale {
+  uint32_t byte;
+  float inv;
+};
+__device__ __forceinline__ MxScale mx_scale(uint32_t top) {
+  const uint32_t e = (top + 0x00200000u) >> 23;
+  const uint32_t byte = e > 254 ? 252 : e > 2 ? e - 2 : 0;
+  MxScale r{byte, __builtin_bit_cast(float, (254u - byte) << 23)};
+  if (top >= 0x7F800000u) r = MxScale{255u, 0.0f};
+  if (top < 0x00800000u) r = MxScale{0u, 0.0f};
+  return r;
+}
+// Eight entries, first in the low half of the lowest byte.  v inv is exact; the
+// conversion rounds to nearest, ties to even.
+__device__ __forceinline__ uint32_t mx_pack8(const float* v, float inv) {
+  uint32_t w = 0;
+  if (inv > 0.0f) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * inv, v[1] * inv, 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * inv, v[3] * inv, 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * inv, v[5] * inv, 1.0f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * inv, v[7] * inv, 1.0f, 3);
+  }
+  return w;
+}
+
+// Eight consecutive entries from column c (a multiple of 8); zeros from `cols` on.
+template <bool BF16, bool VEC>
+__device__ __forceinline__ void mx_load8(const void* row, int c, int cols, float* v) {
+  if (VEC && c + 8 <= cols) {
+    if constexpr (BF16) {
+      const nt_u32x4 w =
+          *reinterpret_cast<const nt_u32x4*>(static_cast<const uint16_t*>(row) + c);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        v[2 * t] = mx_bf16(w[t] & 0xFFFFu);
+        v[2 * t + 1] = mx_bf16(w[t] >> 16);
+      }
+    } else {
+      const nt_f32x4* p = reinterpret_cast<const nt_f32x4*>(static_cast<const float*>(row) + c);
+      const nt_f32x4 a = p[0], b = p[1];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        v[t] = a[t];
+        v[4 + t] = b[t];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      v[t] = 0.0f;
+      if (c + t < cols) {
+        if constexpr (BF16) v[t] = mx_bf16(static_cast<const uint16_t*>(row)[c + t]);
+        else v[t] = static_cast<const float*>(row)[c + t];
+      }
+    }
+  }
+}
+
+// The gradient behind the layer's epilogue (mx4.h).  A NaN in y passes it on.
+__device__ __forceinline__ float mx_pass(float dy, float y, const DropArgs& d) {
+  const float g = d.below ? dy * d.factor : dy;
+  return y <= 0.0f ? 0.0f : g;
+}
+
+// MODE 0: x as it is, 1: with y, 2: with the generator.
+template <bool BF16, bool VEC, int MODE>
+__device__ __forceinline__ void mx_source8(const Mx4Source& a, int64_t row, int c, uint64_t offset,
+                                           float* v) {
+  constexpr int ES = BF16 ? 2 : 4;
+  mx_load8<BF16, VEC>(static_cast<const char*>(a.x) + row * a.x_ld * ES, c, a.cols, v);
+  if constexpr (MODE == 1) {
+    float y[8];
+    mx_load8<BF16, VEC>(static_cast<const char*>(a.y) + row * a.y_ld * ES, c, a.cols, y);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = mx_pass(v[t], y[t], a.drop);
+  }
+  if constexpr (MODE == 2) {
+    const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(row), c / 8);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = drop_keeps(a.drop, w, t) ? v[t] * a.drop.factor : 0.0f;
+  }
+}
+
+// A wave takes 512 columns of a row, a lane eight of them, four lanes a block.
+template <bool BF16, bool VEC, int MODE>
+__global__ __launch_bounds__(256) void mx4_rows_kernel(Mx4Source a, Mx4Rows to, int pieces) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t offset = MODE == 2 ? drop_offset(a.drop) : 0;
+  const int64_t units = a.rows * pieces, step = static_cast<int64_t>(gridDim.x) * 4;
+  const int end = static_cast<int>(mx4_bytes(a.cols)) * 2;
+  for (int64_t u = static_cast<int64_t>(blockIdx.x) * 4 + wave; u < units; u += step) {
+    const int64_t row = u / pieces;
+    const int c = static_cast<int>(u - row * pieces) * 512 + 8 * lane;
+    float v[8];
+    mx_source8<BF16, VEC, MODE>(a, row, c, offset, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) top = max(top, mx_abs(v[t]));
+    top = max(top, static_cast<uint32_t>(__shfl_xor(top, 1)));
+    top = max(top, static_cast<uint32_t>(__shfl_xor(top, 2)));
+    const MxScale s = mx_scale(top);
+    if (c < end)
+      *reinterpret_cast<uint32_t*>(to.q + row * to.q_ld + c / 2) = mx_pack8(v, s.inv);
+    if ((lane & 3) == 0) to.scale[row * to.s_ld + c / 32] = static_cast<uint8_t>(s.byte);
+  }
+}
+
+// 256 rows x 128 columns a workgroup, eight waves of 32 rows; a lane has two
+// neighbouring columns of its wave's rows, a block of each, and turns them by LDS
+// so that a column's 128 bytes are stored by eight neighbouring lanes.
+constexpr int MXC_ROWS = 256, MXC_COLS = 128;
+
+template <bool BF16, bool VEC, int MODE>
+__global__ __launch_bounds__(512) void mx4_columns_kernel(Mx4Source a, Mx4Rows to, float* sums) {
+  constexpr int LD = 128 + 16;  // 16 more: neighbouring columns start in other banks
+  __shared__ __attribute__((aligned(16))) uint8_t q[MXC_COLS * LD];
+  __shared__ uint8_t sc[MXC_COLS][8];
+  __shared__ float part[8][MXC_COLS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int across = (a.cols + MXC_COLS - 1) / MXC_COLS;
+  const int64_t tile = blockIdx.x / across;
+  const int c0 = static_cast<int>(blockIdx.x % across) * MXC_COLS, c = c0 + 2 * lane;
+  const int64_t r0 = tile * MXC_ROWS + 32 * wave;
+  const uint64_t offset = MODE == 2 ? drop_offset(a.drop) : 0;
+  constexpr int ES = BF16 ? 2 : 4;
+  auto load2 = [&](const void* p, int64_t ld, int64_t r) {
+    const char* row = static_cast<const char*>(p) + r * ld * ES;
+    mx_f32x2 v = {0.0f, 0.0f};
+    if (r >= a.rows) return v;
+    if (VEC && c + 2 <= a.cols) {
+      if constexpr (BF16) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(row + 2 * c);
+        v = mx_f32x2{mx_bf16(w & 0xFFFFu), mx_bf16(w >> 16)};
+      } else {
+        v = *reinterpret_cast<const mx_f32x2*>(row + 4 * static_cast<int64_t>(c));
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (c + t < a.cols) {
+          if constexpr (BF16) v[t] = mx_bf16(reinterpret_cast<const uint16_t*>(row)[c + t]);
+          else v[t] = reinterpret_cast<const float*>(row)[c + t];
+        }
+    }
+    return v;
+  };
+  float v[2][32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const mx_f32x2 x = load2(a.x, a.x_ld, r0 + i);
+    v[0][i] = x[0];
+    v[1][i] = x[1];
+  }
+  if constexpr (MODE == 1) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const mx_f32x2 y = load2(a.y, a.y_ld, r0 + i);
+      v[0][i] = mx_pass(v[0][i], y[0], a.drop);
+      v[1][i] = mx_pass(v[1][i], y[1], a.drop);
+    }
+  }
+  if constexpr (MODE == 2) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(r0 + i), c / 8);
+      const uint32_t mine = w.w[lane & 3];
+      v[0][i] = (mine & 0xFFFFu) >= a.drop.below ? v[0][i] * a.drop.factor : 0.0f;
+      v[1][i] = mine >> 16 >= a.drop.below ? v[1][i] * a.drop.factor : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    uint32_t top = 0;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      top = max(top, mx_abs(v[t][i]));
+      sum += v[t][i];
+    }
+    const MxScale s = mx_scale(top);
+    const int col = 2 * lane + t;
+    *reinterpret_cast<nt_u32x4*>(q + col * LD + 16 * wave) =
+        nt_u32x4{mx_pack8(v[t], s.inv), mx_pack8(v[t] + 8, s.inv), mx_pack8(v[t] + 16, s.inv),
+                 mx_pack8(v[t] + 24, s.inv)};
+    sc[col][wave] = static_cast<uint8_t>(s.byte);
+    part[wave][col] = sum;
+  }
+  __syncthreads();
+  for (int i = tid; i < MXC_COLS * 8; i += 512) {
+    const int col = i >> 3, k = i & 7;
+    if (c0 + col < a.cols)
+      *reinterpret_cast<nt_u32x4*>(to.q + (c0 + col) * to.q_ld + tile * 128 + 16 * k) =
+          *reinterpret_cast<const nt_u32x4*>(q + col * LD + 16 * k);
+  }
+  if (tid < MXC_COLS && c0 + tid < a.cols) {
+    uint8_t* s = to.scale + (c0 + tid) * to.s_ld + tile * 8;
+    *reinterpret_cast<nt_u32x2*>(s) = *reinterpret_cast<const nt_u32x2*>(sc[tid]);
+    // the last tile fills the scales to a whole 16
+    if ((tile & 1) == 0 && (tile + 1) * MXC_ROWS >= a.rows)
+      *reinterpret_cast<nt_u32x2*>(s + 8) = nt_u32x2{0, 0};
+    if (sums) {
+      float t = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) t += part[w][tid];
+      sums[tile * a.cols + c0 + tid] = t;
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void mx4_sum_kernel(const float* part, int64_t parts, int cols,
+                                                      float* sums) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= cols) return;
+  float s = 0.0f;
+  for (int64_t i = 0; i < parts; ++i) s += part[i * cols + c];
+  sums[c] = s;
+}
+
+// Values: eight a thread.
+template <bool OUT_BF16>
+__global__ __launch_bounds__(256) void mx4_values_kernel(Mx4Values a, uint32_t groups) {
+  const int64_t units = a.rows * groups, step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t u = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; u < units; u += step) {
+    const int64_t row = u / groups;
+    const int c = static_cast<int>(u - row * groups) * 8;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(a.q + row * a.q_ld + c / 2);
+    const uint32_t e = a.scale[row * a.s_ld + c / 32];
+    // 2^-127 is no normal number; 2^-126 / 2 is the same
+    const float s = __builtin_bit_cast(float, e == 0 ? 0x00400000u
+                                                     : e == 255 ? 0x7FC00000u : e << 23);
+    float v[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const uint32_t n = w >> (4 * t) & 15u, m = n & 7u;
+      const float x = m < 4 ? 0.5f * static_cast<float>(m)
+                            : static_cast<float>((2 + (m & 1u)) << (m >> 1)) * 0.25f;
+      v[t] = (n & 8u ? -x : x) * s;
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      if (c + t < a.cols) {
+        if constexpr (OUT_BF16)
+          static_cast<uint16_t*>(a.out)[row * a.out_ld + c + t] = mx_to_bf16(v[t]);
+        else
+          static_cast<float*>(a.out)[row * a.out_ld + c + t] = v[t];
+      }
+  }
+}
+
+__global__ __launch_bounds__(256) void mx4_zero_kernel(float* p, int64_t ld, int64_t rows,
+                                                       int cols) {
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int c = threadIdx.x; c < cols; c += 256) p[r * ld + c] = 0.0f;
+}
+
+// ------------------------------------------------------------------ products
+
+__device__ __forceinline__ float mx_finish(const Mx4Product& a, float acc, float b) {
+  float y = acc + b;
+  if (a.relu) y = y < 0.0f ? 0.0f : y;  // keeps a NaN
+  return y;
+}
+// N (4 or 8) outputs of a row from o (a multiple of N) on.
+template <int N>
+__device__ __forceinline__ void mx_drop(const Mx4Product& a, uint64_t offset, int64_t row, int o,
+                                        float* v) {
+  const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(row), o / 8);
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    const bool keep = N == 8 || !(o & 4) ? drop_keeps(a.drop, w, t)
+                                         : drop_keeps(a.drop, w, (t + 4) & 7);
+    v[t] = keep ? v[t] * a.drop.factor : 0.0f;
+  }
+}
+
+// N channels from o on of an output row.
+template <int N, bool OUT_BF16, bool VEC>
+__device__ __forceinline__ void mx_store(const Mx4Product& a, int64_t row, int o, const float* v) {
+  if constexpr (OUT_BF16) {
+    uint16_t* p = static_cast<uint16_t*>(a.out) + row * a.out_ld + o;
+    if (VEC && o + N <= a.outs) {
+      uint32_t w[N / 2];
+#pragma unroll
+      for (int e = 0; e < N / 2; ++e)
+        w[e] = mx_to_bf16(v[2 * e]) | static_cast<uint32_t>(mx_to_bf16(v[2 * e + 1])) << 16;
+      if constexpr (N == 8)
+        *reinterpret_cast<nt_u32x4*>(p) = nt_u32x4{w[0], w[1], w[2], w[3]};
+      else
+        *reinterpret_cast<nt_u32x2*>(p) = nt_u32x2{w[0], w[1]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (o + e < a.outs) p[e] = mx_to_bf16(v[e]);
+    }
+  } else {
+    float* p = static_cast<float*>(a.out) + row * a.out_ld + o;
+    if (VEC && o + N <= a.outs) {
+#pragma unroll
+      for (int e = 0; e < N; e += 4)
+        *reinterpret_cast<nt_f32x4*>(p + e) = nt_f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (o + e < a.outs) p[e] = v[e];
+    }
+  }
+}
+
+template <int BYTE>
+__device__ __forceinline__ nt_f32x16 mx_mfma(nt_u32x4 a, nt_u32x4 b, nt_f32x16 c, uint32_t sa,
+                                             uint32_t sb) {
+  const mx_i32x8 x = {static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]),
+                      static_cast<int>(a[3]), 0, 0, 0, 0};
+  const mx_i32x8 y = {static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]),
+                      static_cast<int>(b[3]), 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, BYTE,
+                                                         static_cast<int>(sa), BYTE,
+                                                         static_cast<int>(sb));
+}
+
+typedef NtShape<256, 256, 2, 4> MxL;
+typedef NtShape<128, 128, 2, 2> MxM;
+static_assert(mx4_threads(MxL::BM) == MxL::NT && mx4_threads(MxM::BM) == MxM::NT, "mx4_plan.h");
+
+// A stage is 256 entries of K, 128 bytes a row; of its eight blocks a lane takes 4 h +
+// c in group c (h: its half of the wave), so that its four scales are four
+// neighbouring bytes and the instruction picks byte c.  The order of K within a stage
+// is free, both operands have the same.
+// Scales come in pairs of stages, 16 bytes a row, a row a lane: half of the waves
+// fetch A's, the others B's.
+template <class S>
+struct MxScales {
+  static constexpr int BYTES = 2 * (S::BM + S::BN) * 16;
+  static_assert((S::BM + S::BN) / 64 == S::NT / 64 && S::BM == S::BN, "a wave's load each");
+  __amdgpu_buffer_rsrc_t rsrc;
+  int voff;
+  __device__ __forceinline__ void init(const uint8_t* sa, int64_t a_ld, int64_t a_bytes, int a_row,
+                                       int a_rows, const uint8_t* sb, int64_t b_ld,
+                                       int64_t b_bytes, int b_rows, int tid) {
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool first = wave < S::NT / 128;
+    const int64_t ld = first ? a_ld : b_ld, at = first ? a_row * a_ld : 0;
+    const int64_t left = (first ? a_bytes : b_bytes) - at;
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>((first ? sa : sb) + at), 0,
+                                             static_cast<int>(left < 0x7FFFFFFF ? left : 0x7FFFFFFF),
+                                             0x00020000u);
+    const int r = first ? tid : tid - S::NT / 2, n = first ? a_rows - a_row : b_rows;
+    voff = static_cast<int>((r < n ? r : n - 1) * ld);
+  }
+  // lds: the tile's scales, A's rows and then B's, of two pairs
+  __device__ __forceinline__ void issue(char* lds, int pair, int tid) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc,
+        (__attribute__((address_space(3))) void*)(lds + (pair & 1) * (BYTES / 2) +
+                                                  (tid & ~63) * 16),
+        16, voff, pair * 16, 0, 0);
+  }
+};
+
+// acc[i][j] += the tile's products over `blocks` stages, in the order of nt_tile's.
+template <class S>
+__device__ __forceinline__ void mx_tile(const NtRows<S::NT, S::BM>& a,
+                                        const NtRows<S::NT, S::BN>& b, const MxScales<S>& sc,
+                                        int blocks, char* lds, int tid,
+                                        nt_f32x16 (&acc)[S::MI][S::NJ]) {
+  constexpr int ABYTES = S::BM * NT_BLOCK, STAGE = (S::BM + S::BN) * NT_BLOCK;
+  char* scales = lds + 2 * STAGE;
+  const int lane = tid & 63, wave = tid >> 6;
+  const int arow = (wave / S::WN) * 32 * S::MI + (lane & 31);
+  const int brow = (wave % S::WN) * 32 * S::NJ + (lane & 31), h = lane >> 5;
+  constexpr bool SPREAD = S::NT == 512;
+  const int pairs = (blocks + 1) / 2;
+  auto issue = [&](int s) {
+    char* t = lds + (s & 1) * STAGE;
+    a.issue(t, s * NT_BLOCK, tid);
+    b.issue(t + ABYTES, s * NT_BLOCK, tid);
+  };
+  auto issue_part = [&](int s, int part) {
+    if (!SPREAD || s >= blocks) return;
+    char* t = lds + (s & 1) * STAGE;
+    a.issue(t, s * NT_BLOCK, tid, part);
+    b.issue(t + ABYTES, s * NT_BLOCK, tid, part);
+  };
+  auto load = [&](const char* t, int c, nt_u32x4(&fa)[S::MI], nt_u32x4(&fb)[S::NJ]) {
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) fa[i] = nt_read(t, arow + 32 * i, 4 * h + c);
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) fb[j] = nt_read(t + ABYTES, brow + 32 * j, 4 * h + c);
+  };
+  auto load_scales = [&](int s, uint32_t(&sa)[S::MI], uint32_t(&sb)[S::NJ]) {
+    const char* t = scales + ((s >> 1) & 1) * (MxScales<S>::BYTES / 2) + 8 * (s & 1) + 4 * h;
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+      sa[i] = *reinterpret_cast<const uint32_t*>(t + (arow + 32 * i) * 16);
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j)
+      sb[j] = *reinterpret_cast<const uint32_t*>(t + (S::BM + brow + 32 * j) * 16);
+  };
+  uint32_t sa[S::MI], sb[S::NJ], na[S::MI], nb[S::NJ];
+  // the scheduler keeps loads and products in the order written
+#define OSCARS_MUL(C, FA, FB)                                                               \
+  do {                                                                                      \
+    __builtin_amdgcn_sched_barrier(0);                                                      \
+    _Pragma("unroll") for (int i = 0; i < S::MI; ++i)                                       \
+        _Pragma("unroll") for (int j = 0; j < S::NJ; ++j) acc[i][j] =                       \
+            mx_mfma<C>(FA[i], FB[j], acc[i][j], sa[i], sb[j]);                              \
+    __builtin_amdgcn_sched_barrier(0);                                                      \
+  } while (0)
+  nt_u32x4 a0[S::MI], a1[S::MI], b0[S::NJ], b1[S::NJ];
+  issue(0);
+  sc.issue(scales, 0, tid);
+  nt_wait_vm<0>();
+  nt_barrier();
+  if constexpr (SPREAD) issue_part(1, 0);
+  else if (blocks > 1) issue(1);
+  if (pairs > 1) sc.issue(scales, 1, tid);
+  load(lds, 0, a0, b0);
+  load_scales(0, sa, sb);
+  for (int s = 0; s < blocks; ++s) {
+    const char* t = lds + (s & 1) * STAGE;
+    const char* next = lds + ((s + 1) & 1) * STAGE;
+    issue_part(s + 1, 1);
+    load(t, 1, a1, b1);
+    OSCARS_MUL(0, a0, b0);
+    issue_part(s + 1, 2);
+    issue_part(s + 1, 3);
+    load(t, 2, a0, b0);
+    OSCARS_MUL(1, a1, b1);
+    load(t, 3, a1, b1);
+    OSCARS_MUL(2, a0, b0);
+    nt_wait_vm<0>();  // the next stage is there,
+    nt_barrier();     // and this one read by every wave
+    if constexpr (SPREAD) issue_part(s + 2, 0);
+    else if (s + 2 < blocks) issue(s + 2);
+    // stage s was the last of pair s / 2: its buffer takes the pair after the next
+    if ((s & 1) && (s >> 1) + 2 < pairs) sc.issue(scales, (s >> 1) + 2, tid);
+    load(next, 0, a0, b0);
+    load_scales(s + 1, na, nb);
+    OSCARS_MUL(3, a1, b1);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) sa[i] = na[i];
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) sb[j] = nb[j];
+  }
+  nt_wait_vm<0>();
+#undef OSCARS_MUL
+}
+
+// Output rows are input rows; the tile's own rows (R) are output channels, four
+// consecutive ones a lane.  Two blocks of 32 channels go through LDS so that
+// neighbouring lanes store whole 128-byte lines of an output row.  VEC: 16-byte
+// stores.
+template <class S, bool OUT_BF16, bool VEC>
+__global__ __launch_bounds__(S::NT, 2) void mx4_product_kernel(Mx4Product a) {
+#if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
+  constexpr int TURN = 68;  // 64 channels of a row
+  static_assert(S::LDS_BYTES >= S::WM * S::WN * 32 * TURN * 4 && S::MI % 2 == 0, "turned blocks");
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS_BYTES + MxScales<S>::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+  const int tr = (a.outs + S::BM - 1) / S::BM;
+  const int tc = static_cast<int>((a.rows + S::BN - 1) / S::BN);
+  const int total = tr * tc;
+  int id;
+  {  // the workgroups of one XCD (index mod 8) take neighbouring tiles
+    const int per = total >> 3, rem = total & 7, x = blockIdx.x & 7, q = blockIdx.x >> 3;
+    id = x * per + (x < rem ? x : rem) + q;
+  }
+  // bands of four tile columns (rows of the input), channel tile by channel tile
+  constexpr int BAND = 4;
+  const int band = id / (BAND * tr), cols = tc - band * BAND < BAND ? tc - band * BAND : BAND;
+  const int at = id - band * BAND * tr;
+  const int r0 = (at / cols) * S::BM;
+  const int64_t c0 = static_cast<int64_t>(band * BAND + at % cols) * S::BN;
+
+  const int blocks = (a.in + 255) / 256;
+  const int64_t left = a.rows - c0;
+  const int here = static_cast<int>(left < S::BN ? left : S::BN);
+  NtRows<S::NT, S::BM> ra;
+  NtRows<S::NT, S::BN> rb;
+  MxScales<S> sc;
+  const int64_t qb = mx4_bytes(a.in), sb = mx4_scales(a.in);
+  ra.init(a.wq, a.w_ld, (a.outs - 1) * a.w_ld + qb, r0, a.outs, tid);
+  rb.init(a.xq + c0 * a.x_ld, a.x_ld, (here - 1) * a.x_ld + qb, 0, here, tid);
+  sc.init(a.ws, a.ws_ld, (a.outs - 1) * a.ws_ld + sb, r0, a.outs, a.xs + c0 * a.xs_ld, a.xs_ld,
+          (here - 1) * a.xs_ld + sb, here, tid);
+  nt_f32x16 acc[S::MI][S::NJ];
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+  mx_tile<S>(ra, rb, sc, blocks, lds, tid, acc);
+
+  const int rw = r0 + (wave / S::WN) * 32 * S::MI;
+  const int64_t cw = c0 + (wave % S::WN) * 32 * S::NJ;
+  float* turn = reinterpret_cast<float*>(lds) + wave * 32 * TURN;
+  constexpr int PER = OUT_BF16 ? 8 : 4, LANES = 64 / PER;  // 16 bytes a lane
+  const int k = PER * (lane % LANES);
+  const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0;
+  nt_barrier();  // the stages are read: LDS is free
+#pragma nounroll
+  for (int i = 0; i < S::MI; i += 2) {
+    const int o = rw + 32 * i + k;  // the lane's channels
+    if (rw + 32 * i >= a.outs) continue;
+    float bias[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int oc = o + e < a.outs ? o + e : a.outs - 1;
+      bias[e] = a.bias ? a.bias[oc] : 0.0f;
+    }
+#pragma nounroll
+    for (int j = 0; j < S::NJ; ++j) {
+      const int64_t row0 = cw + 32 * j;
+      if (row0 >= a.rows) continue;  // uniform over the wave
+#pragma unroll
+      for (int ii = 0; ii < S::MI; ++ii)
+#pragma unroll
+        for (int jj = 0; jj < S::NJ; ++jj)
+          if ((ii & ~1) == i && jj == j) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<nt_f32x4*>(turn + (lane & 31) * TURN + 32 * (ii & 1) + 8 * q +
+                                           4 * h) =
+                  nt_f32x4{acc[ii][jj][4 * q], acc[ii][jj][4 * q + 1], acc[ii][jj][4 * q + 2],
+                           acc[ii][jj][4 * q + 3]};
+          }
+      nt_wave_sync();
+      for (int r = lane / LANES; r < 32; r += 64 / LANES) {
+        const int64_t row = row0 + r;
+        float v[PER];
+#pragma unroll
+        for (int e = 0; e < PER; e += 4) {
+          const nt_f32x4 t = *reinterpret_cast<const nt_f32x4*>(turn + r * TURN + k + e);
+#pragma unroll
+          for (int f = 0; f < 4; ++f) v[e + f] = mx_finish(a, t[f], bias[e + f]);
+        }
+        if (a.drop.below) mx_drop<PER>(a, offset, row, o, v);
+        if (row < a.rows && o < a.outs) mx_store<PER, OUT_BF16, VEC>(a, row, o, v);
+      }
+      nt_wave_sync();
+    }
+  }
+#endif
+}
+
+// Few tiles: 32 x 32 outputs a workgroup, K dealt to its four waves block by block.
+// A wave streams its blocks and their scales through LDS of its own (RING of them),
+// into registers, and waits for no other wave until the four sums meet, in order.
+constexpr int MX_SMALL_RING = 2;
+
+template <bool OUT_BF16, bool VEC>
+__global__ __launch_bounds__(256) void mx4_small_kernel(Mx4Product a) {
+#if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
+  constexpr int DATA = 64 * NT_BLOCK, STAGE = DATA + 512, RING = MX_SMALL_RING;
+  __shared__ __attribute__((aligned(16))) char lds[4 * RING * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // scalar addresses below
+  const int tr = (a.outs + 31) / 32;
+  const int r0 = static_cast<int>(blockIdx.x % tr) * 32;
+  const int64_t c0 = static_cast<int64_t>(blockIdx.x / tr) * 32;
+  const int blocks = (a.in + 255) / 256;
+  const int64_t left = a.rows - c0;
+  const int here = static_cast<int>(left < 32 ? left : 32);
+  NtRows<64, 32> ra, rb;
+  const int64_t qb = mx4_bytes(a.in), sb = mx4_scales(a.in);
+  ra.init(a.wq, a.w_ld, (a.outs - 1) * a.w_ld + qb, r0, a.outs, lane);
+  rb.init(a.xq + c0 * a.x_ld, a.x_ld, (here - 1) * a.x_ld + qb, 0, here, lane);
+  // a block's scales: 8 bytes a row, four of them a lane
+  auto scale_rsrc = [](const uint8_t* p, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(p), 0, static_cast<int>(bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF),
+        0x00020000u);
+  };
+  const int na = a.outs - r0 < 32 ? a.outs - r0 : 32;
+  const __amdgpu_buffer_rsrc_t rsa = scale_rsrc(a.ws + r0 * a.ws_ld, (na - 1) * a.ws_ld + sb);
+  const __amdgpu_buffer_rsrc_t rsb = scale_rsrc(a.xs + c0 * a.xs_ld, (here - 1) * a.xs_ld + sb);
+  const int row = lane & 31;
+  const int va = static_cast<int>((row < na ? row : na - 1) * a.ws_ld) + 4 * h;
+  const int vb = static_cast<int>((row < here ? row : here - 1) * a.xs_ld) + 4 * h;
+  char* ring = lds + wave * RING * STAGE;
+  typedef __attribute__((address_space(3))) void* lds_ptr;
+  auto issue = [&](int i) {  // the wave's block i
+    const int k = wave + 4 * i;
+    char* t = ring + (i % RING) * STAGE;
+    const int block = k < blocks ? k : blocks - 1;
+    ra.issue(t, block * NT_BLOCK, lane);
+    rb.issue(t + DATA / 2, block * NT_BLOCK, lane);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (lds_ptr)(t + DATA), 4, va, block * 8, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsb, (lds_ptr)(t + DATA + 256), 4, vb, block * 8, 0,
+                                             0);
+  };
+  nt_f32x16 acc;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+  constexpr int PER = NtRows<64, 32>::P * 2 + 2;
+  for (int i = 0; i < RING; ++i) issue(i);
+  for (int i = 0; wave + 4 * i < blocks; ++i) {
+    nt_wait_vm<(RING - 1) * PER>();
+    const char* ta = ring + (i % RING) * STAGE;
+    const char* tb = ta + DATA / 2;
+    nt_u32x4 fa[4], fb[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      fa[c] = nt_read(ta, lane & 31, 4 * h + c);
+      fb[c] = nt_read(tb, lane & 31, 4 * h + c);
+    }
+    const uint32_t sa = *reinterpret_cast<const uint32_t*>(ta + DATA + 4 * lane);
+    const uint32_t sb4 = *reinterpret_cast<const uint32_t*>(ta + DATA + 256 + 4 * lane);
+    // the stage is in registers: refill it
+    __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    issue(i + RING);
+    acc = mx_mfma<0>(fa[0], fb[0], acc, sa, sb4);
+    acc = mx_mfma<1>(fa[1], fb[1], acc, sa, sb4);
+    acc = mx_mfma<2>(fa[2], fb[2], acc, sa, sb4);
+    acc = mx_mfma<3>(fa[3], fb[3], acc, sa, sb4);
+  }
+  nt_wait_vm<0>();
+  __syncthreads();  // every wave is through with LDS: now the four sums
+  float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) sums[(wave * 16 + e) * 64 + lane] = acc[e];
+  __syncthreads();
+  // wave w finishes channels 8 w + 4 h .. + 3 of row (lane & 31)
+  const int o = r0 + 8 * wave + 4 * h;
+  const int64_t r = c0 + row;
+  if (r >= a.rows || o >= a.outs) return;
+  float v[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s += sums[(w * 16 + 4 * wave + t) * 64 + lane];
+    const int oc = o + t < a.outs ? o + t : a.outs - 1;
+    v[t] = mx_finish(a, s, a.bias ? a.bias[oc] : 0.0f);
+  }
+  if (a.drop.below) mx_drop<4>(a, drop_offset(a.drop), r, o, v);
+  mx_store<4, OUT_BF16, VEC>(a, r, o, v);
+#endif
+}
+
+template <bool OUT_BF16, bool VEC>
+hipError_t product_launch(const Mx4Product& a, int tile, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>((a.outs + tile - 1) / tile * ((a.rows + tile - 1) / tile)));
+  if (tile == MxL::BM)
+    hipLaunchKernelGGL((mx4_product_kernel<MxL, OUT_BF16, VEC>), grid, dim3(MxL::NT), 0, s, a);
+  else if (tile == MxM::BM)
+    hipLaunchKernelGGL((mx4_product_kernel<MxM, OUT_BF16, VEC>), grid, dim3(MxM::NT), 0, s, a);
+  else
+    hipLaunchKernelGGL((mx4_small_kernel<OUT_BF16, VEC>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+bool aligned_rows(const void* p, int64_t row_bytes, int to) {
+  return reinterpret_cast<uintptr_t>(p) % to == 0 && row_bytes % to == 0;
+}
+
+// ------------------------------------------------------------------ a few rows
+
+// Up to 16 rows.  A workgroup takes 16 output channels, its eight waves slices of 512
+// of K in turn: four 16x16x128 instructions, lane l channel or row l & 15, block l >> 4
+// of 128 entries.  While the weights are on their way every workgroup quantises all
+// rows into LDS for itself (they come from the L2).  The eight partial sums meet in
+// LDS, in order.
+constexpr int FEW_ROWS = 16;
+constexpr int FEW_WAVES = 8;
+constexpr int FEW_ENTRIES = 16384;  // of more than one row
+
+__host__ __device__ __forceinline__ int few_row_bytes(int in) {
+  return (in + 511) / 512 * 256 + 16;  // 16 more: consecutive rows start in other banks
+}
+__host__ __device__ __forceinline__ int few_row_scales(int in) { return (in + 511) / 512 * 16; }
+// quantised rows and scales: FEW_ENTRIES of 16 rows, or 65536 of one
+constexpr int FEW_LDS_S = 13 << 10, FEW_LDS_L = 35 << 10;
+
+template <int LDS, bool X_BF16, bool VEC, bool OUT_BF16>
+__global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(Mx4Product a, const void* x,
+                                                                 int64_t x_ld) {
+  __shared__ __attribute__((aligned(16))) char few_lds[LDS];
+  __shared__ float part[FEW_WAVES][64][4];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = static_cast<int>(a.rows), in = a.in, ld = few_row_bytes(in);
+  const int sld = few_row_scales(in), slices = (in + 511) / 512;
+  char* scales = few_lds + rows * ld;
+  const int ch = blockIdx.x * 16 + (lane & 15), chc = ch < a.outs ? ch : a.outs - 1;
+  const int g = lane >> 4;
+  const uint8_t* w = a.wq + chc * a.w_ld + 16 * g;
+  const uint8_t* ws = a.ws + chc * a.ws_ld;
+  const int64_t qb = mx4_bytes(in);
+  nt_u32x4 cur[4], cur_s;
+  auto load_w = [&](int sl) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      // the second half of the last slice may not be there: zeros of x meet the first's
+      const int at = sl * 256 + 64 * c;
+      cur[c] = *reinterpret_cast<const nt_u32x4*>(w + (at + 64 <= qb ? at : at - 128));
+    }
+    cur_s = *reinterpret_cast<const nt_u32x4*>(ws + sl * 16);
+  };
+  if (wave < slices) load_w(wave);
+  // the rows, eight entries a thread, four threads a block
+  const int per = slices * 64;  // threads' work of a row
+  for (int i = tid; i < rows * per; i += 64 * FEW_WAVES) {
+    const int r = i / per, c = 8 * (i - r * per);
+    float v[8];
+    mx_load8<X_BF16, VEC>(static_cast<const char*>(x) + r * x_ld * (X_BF16 ? 2 : 4), c, in, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) top = max(top, mx_abs(v[t]));
+    top = max(top, static_cast<uint32_t>(__shfl_xor(top, 1)));
+    top = max(top, static_cast<uint32_t>(__shfl_xor(top, 2)));
+    const MxScale s = mx_scale(top);
+    *reinterpret_cast<uint32_t*>(few_lds + r * ld + c / 2) = mx_pack8(v, s.inv);
+    if ((lane & 3) == 0) scales[r * sld + c / 32] = static_cast<char>(s.byte);
+  }
+  __syncthreads();
+  nt_f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  // lanes of rows that are not there read the last one; their sums are not used
+  const int r = (lane & 15) < rows ? (lane & 15) : rows - 1;
+  const char* b = few_lds + r * ld + 16 * g;
+  const char* bs = scales + r * sld;
+  for (int sl = wave; sl < slices; sl += FEW_WAVES) {
+    nt_u32x4 wv[4] = {cur[0], cur[1], cur[2], cur[3]};
+    const nt_u32x4 wsc = cur_s;
+    if (sl + FEW_WAVES < slices) load_w(sl + FEW_WAVES);
+    const nt_u32x4 xsc = *reinterpret_cast<const nt_u32x4*>(bs + sl * 16);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const nt_u32x4 xv = *reinterpret_cast<const nt_u32x4*>(b + sl * 256 + 64 * c);
+      const mx_i32x8 p = {static_cast<int>(wv[c][0]), static_cast<int>(wv[c][1]),
+                          static_cast<int>(wv[c][2]), static_cast<int>(wv[c][3]), 0, 0, 0, 0};
+      const mx_i32x8 q = {static_cast<int>(xv[0]), static_cast<int>(xv[1]),
+                          static_cast<int>(xv[2]), static_cast<int>(xv[3]), 0, 0, 0, 0};
+      // the lane's scale to the lowest byte
+      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+          p, q, acc, 4, 4, 0, static_cast<int>(wsc[c] >> (8 * g)), 0,
+          static_cast<int>(xsc[c] >> (8 * g)));
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) part[wave][lane][e] = acc[e];
+  __syncthreads();
+  // lane l, element e: channel 4 (l >> 4) + e, row l & 15; a thread finishes one output
+  if (tid < 256) {
+    const int e = tid & 3, l = tid >> 2;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < FEW_WAVES; ++i) sum += part[i][l][e];
+    const int q = l & 15, o = blockIdx.x * 16 + 4 * (l >> 4) + e;
+    if (q < rows && o < a.outs) {
+      float y = mx_finish(a, sum, a.bias ? a.bias[o] : 0.0f);
+      if (a.drop.below) {
+        const Words4 d = drop_words(a.drop, drop_offset(a.drop), q, o / 8);
+        const uint32_t d01 = o & 2 ? d.w[1] : d.w[0], d23 = o & 2 ? d.w[3] : d.w[2];
+        const uint32_t word = o & 4 ? d23 : d01;
+        y = (o & 1 ? word >> 16 : word & 0xFFFFu) >= a.drop.below ? y * a.drop.factor : 0.0f;
+      }
+      if constexpr (OUT_BF16) static_cast<uint16_t*>(a.out)[q * a.out_ld + o] = mx_to_bf16(y);
+      else static_cast<float*>(a.out)[q * a.out_ld + o] = y;
+    }
+  }
+}
+
+template <int LDS, bool X_BF16, bool VEC>
+hipError_t few_launch(const Mx4Product& a, const void* x, int64_t x_ld, hipStream_t s) {
+  const dim3 grid((a.outs + 15) / 16), wg(64 * FEW_WAVES);
+  if (a.out_bf16)
+    hipLaunchKernelGGL((mx4_few_kernel<LDS, X_BF16, VEC, true>), grid, wg, 0, s, a, x, x_ld);
+  else
+    hipLaunchKernelGGL((mx4_few_kernel<LDS, X_BF16, VEC, false>), grid, wg, 0, s, a, x, x_ld);
+  return hipGetLastError();
+}
+
+template <bool X_BF16, bool VEC>
+hipError_t few_launch(const Mx4Product& a, const void* x, int64_t x_ld, hipStream_t s) {
+  return a.rows * (few_row_bytes(a.in) + few_row_scales(a.in)) <= FEW_LDS_S
+             ? few_launch<FEW_LDS_S, X_BF16, VEC>(a, x, x_ld, s)
+             : few_launch<FEW_LDS_L, X_BF16, VEC>(a, x, x_ld, s);
+}
+
+int source_mode(const Mx4Source& a) { return a.y ? 1 : a.drop.below ? 2 : 0; }
+
+template <bool BF16, bool VEC>
+hipError_t rows_launch(const Mx4Source& a, const Mx4Rows& to, hipStream_t s) {
+  const int pieces = (a.cols + 511) / 512;
+  const int64_t want = (a.rows * pieces + 3) / 4;
+  const dim3 grid(static_cast<unsigned>(want < 4096 ? want : 4096)), wg(256);
+  const int mode = source_mode(a);
+  if (mode == 0) hipLaunchKernelGGL((mx4_rows_kernel<BF16, VEC, 0>), grid, wg, 0, s, a, to, pieces);
+  else if (mode == 1)
+    hipLaunchKernelGGL((mx4_rows_kernel<BF16, VEC, 1>), grid, wg, 0, s, a, to, pieces);
+  else hipLaunchKernelGGL((mx4_rows_kernel<BF16, VEC, 2>), grid, wg, 0, s, a, to, pieces);
+  return hipGetLastError();
+}
+
+template <bool BF16, bool VEC>
+hipError_t columns_launch(const Mx4Source& a, const Mx4Rows& to, float* sums, hipStream_t s) {
+  const int64_t n = (a.rows + MXC_ROWS - 1) / MXC_ROWS * ((a.cols + MXC_COLS - 1) / MXC_COLS);
+  const dim3 grid(static_cast<unsigned>(n)), wg(512);
+  const int mode = source_mode(a);
+  if (mode == 0)
+    hipLaunchKernelGGL((mx4_columns_kernel<BF16, VEC, 0>), grid, wg, 0, s, a, to, sums);
+  else if (mode == 1)
+    hipLaunchKernelGGL((mx4_columns_kernel<BF16, VEC, 1>), grid, wg, 0, s, a, to, sums);
+  else
+    hipLaunchKernelGGL((mx4_columns_kernel<BF16, VEC, 2>), grid, wg, 0, s, a, to, sums);
+  return hipGetLastError();
+}
+
+bool source_aligned(const Mx4Source& a, int to) {
+  const int64_t es = a.bf16 ? 2 : 4;
+  return aligned_rows(a.x, a.x_ld * es, to) && (!a.y || aligned_rows(a.y, a.y_ld * es, to));
+}
+
+}  // namespace
+
+hipError_t launch_mx4_rows(const Mx4Source& a, const Mx4Rows& to, hipStream_t s) {
+  const bool vec = source_aligned(a, 16);
+  if (a.bf16) return vec ? rows_launch<true, true>(a, to, s) : rows_launch<true, false>(a, to, s);
+  return vec ? rows_launch<false, true>(a, to, s) : rows_launch<false, false>(a, to, s);
+}
+
+int64_t mx4_sum_parts(int64_t rows) {
+  const int64_t n = (rows + MXC_ROWS - 1) / MXC_ROWS;
+  return n > 1 ? n : 0;
+}
+
+hipError_t launch_mx4_columns(const Mx4Source& a, const Mx4Rows& to, float* sums, float* part,
+                              hipStream_t s) {
+  const bool vec = source_aligned(a, a.bf16 ? 4 : 8);
+  const int64_t parts = mx4_sum_parts(a.rows);
+  float* first = sums && parts ? part : sums;
+  hipError_t e;
+  if (a.bf16)
+    e = vec ? columns_launch<true, true>(a, to, first, s)
+            : columns_launch<true, false>(a, to, first, s);
+  else
+    e = vec ? columns_launch<false, true>(a, to, first, s)
+            : columns_launch<false, false>(a, to, first, s);
+  if (e != hipSuccess || first == sums) return e;
+  hipLaunchKernelGGL(mx4_sum_kernel, dim3((a.cols + 255) / 256), dim3(256), 0, s, part, parts,
+                     a.cols, sums);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_values(const Mx4Values& a, hipStream_t s) {
+  const uint32_t groups = static_cast<uint32_t>((static_cast<int64_t>(a.cols) + 7) / 8);
+  const int64_t want = (a.rows * groups + 255) / 256;
+  const dim3 grid(static_cast<unsigned>(want < 8192 ? want : 8192));
+  if (a.out_bf16) hipLaunchKernelGGL((mx4_values_kernel<true>), grid, dim3(256), 0, s, a, groups);
+  else hipLaunchKernelGGL((mx4_values_kernel<false>), grid, dim3(256), 0, s, a, groups);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_product(const Mx4Product& args, hipStream_t s) {
+  const bool vec = aligned_rows(args.out, args.out_ld * (args.out_bf16 ? 2 : 4), 16);
+  hipError_t e = hipSuccess;
+  mx4_launches(args.rows, args.in, args.outs, [&](int tile, int64_t at, int64_t rows) {
+    Mx4Product a = args;
+    a.rows = rows;
+    a.xq += at * a.x_ld;
+    a.xs += at * a.xs_ld;
+    a.out = static_cast<char*>(a.out) + at * a.out_ld * (a.out_bf16 ? 2 : 4);
+    if (a.out_bf16)
+      e = vec ? product_launch<true, true>(a, tile, s) : product_launch<true, false>(a, tile, s);
+    else
+      e = vec ? product_launch<false, true>(a, tile, s) : product_launch<false, false>(a, tile, s);
+    return e == hipSuccess;
+  });
+  return e;
+}
+
+bool mx4_one_launch(int64_t rows, int in) {
+  static_assert(FEW_LDS_S >= FEW_ENTRIES * 17 / 32 + FEW_ROWS * (256 + 32) &&
+                    FEW_LDS_L >= 65536 / 512 * 272 + 16,
+                "room for the rows");
+  return rows == 1 || (rows <= FEW_ROWS && rows * in <= FEW_ENTRIES);
+}
+
+hipError_t launch_mx4_few(const Mx4Product& a, const void* x, int64_t x_ld, bool x_bf16,
+                          hipStream_t s) {
+  const bool vec = aligned_rows(x, x_ld * (x_bf16 ? 2 : 4), 16);
+  if (x_bf16)
+    return vec ? few_launch<true, true>(a, x, x_ld, s) : few_launch<true, false>(a, x, x_ld, s);
+  return vec ? few_launch<false, true>(a, x, x_ld, s) : few_launch<false, false>(a, x, x_ld, s);
+}
+
+hipError_t launch_mx4_zero(float* p, int64_t ld, int64_t rows, int cols, hipStream_t s) {
+  hipLaunchKernelGGL(mx4_zero_kernel, dim3(static_cast<unsigned>(rows < 4096 ? rows : 4096)),
+                     dim3(256), 0, s, p, ld, rows, cols);
+  return hipGetLastError();
+}
+
+}  // namespace oscars

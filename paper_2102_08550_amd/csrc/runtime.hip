@@ -24,6 +24,7 @@
 #include "host_logic.h"
 #include "int8.h"
 #include "kernels.h"
+#include "mx4.h"
 #include "orthogonalize.h"
 
 using namespace oscars;
@@ -2136,6 +2137,287 @@ oscars_status oscars_evaluate_quantized(oscars_ctx* c, const void* model, const 
   e = run_evaluate_i8(c, model, x, y, n_rows, buf, loss_sum, correct);
   const hipError_t f = hipFree(buf);  // waits for the device
   if (e == hipSuccess) e = f;
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+namespace {
+
+// Rows in 4 bits of `cols` entries (mx4.h): their bytes and scales are all there.
+bool mx4_rows_ok(const uint8_t* q, int64_t q_ld, const uint8_t* s, int64_t s_ld, int64_t cols) {
+  return q && aligned16(q) && q_ld % 16 == 0 && q_ld >= mx4_bytes(cols) && q_ld <= kMaxI8Ld &&
+         s && aligned16(s) && s_ld % 16 == 0 && s_ld >= mx4_scales(cols) && s_ld <= kMaxI8Ld;
+}
+bool mx4_cols_ok(int64_t cols) { return cols >= 1 && cols <= MX4_MAX_COLS; }
+constexpr int64_t kMaxRows = (int64_t{1} << 31) - 1;
+
+// The options as the kernels take them; false: not valid.
+bool drop_args(const oscars_dropout_options* o, DropArgs* d) {
+  *d = DropArgs{};
+  if (!o) return true;
+  if (!(o->p >= 0.0 && o->p <= 1.0) || !aligned_to(o->offset_device, 8)) return false;
+  const double t = std::nearbyint(65536.0 * o->p);
+  d->below = static_cast<uint32_t>(t);
+  d->factor = t < 65536.0 ? static_cast<float>(65536.0 / (65536.0 - t)) : 0.0f;
+  d->key[0] = static_cast<uint32_t>(o->seed);
+  d->key[1] = static_cast<uint32_t>(o->seed >> 32);
+  d->offset = o->offset;
+  d->more = o->offset_device;
+  return true;
+}
+
+// Memory that a call touches.
+struct Range {
+  const void* p;
+  int64_t bytes;
+};
+// No output (the first `outs` of them) shares memory with another argument.
+bool apart(const Range* r, int outs, int n) {
+  for (int i = 0; i < outs; ++i)
+    for (int j = i + 1; j < n; ++j)
+      if (r[i].p && r[j].p && r[i].bytes > 0 && r[j].bytes > 0 &&
+          overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes))
+        return false;
+  return true;
+}
+
+// What the product and the fused layer have in common.
+bool mx4_product_ok(const Mx4Product& a, int64_t in, int64_t outs) {
+  return a.rows >= 0 && a.rows <= kMaxRows && mx4_cols_ok(in) && mx4_cols_ok(outs) &&
+         mx4_rows_ok(a.wq, a.w_ld, a.ws, a.ws_ld, in) && aligned_to(a.bias, 4) &&
+         rows_ok(a.out, a.out_ld, outs, a.out_bf16 ? 2 : 4);
+}
+Range mx4_range(const uint8_t* p, int64_t ld, int64_t rows, int64_t width) {
+  return Range{p, rows_span(rows, ld, width, 1)};
+}
+
+// The gradients' workspace: dz by rows (only for dx) and by columns, x by columns, the
+// parts of db's sums.
+struct Mx4Grads {
+  int64_t zq, zs, ztq, zts, xtq, xts, part, end;
+  Mx4Grads(int64_t rows, int64_t in, int64_t outs, bool dx) {
+    zq = 0;
+    zs = zq + (dx ? round_up(rows * mx4_bytes(outs), 256) : 0);
+    ztq = zs + (dx ? round_up(rows * mx4_scales(outs), 256) : 0);
+    zts = ztq + round_up(outs * mx4_bytes(rows), 256);
+    xtq = zts + round_up(outs * mx4_scales(rows), 256);
+    xts = xtq + round_up(in * mx4_bytes(rows), 256);
+    part = xts + round_up(in * mx4_scales(rows), 256);
+    end = part + round_up(mx4_sum_parts(rows) * outs * 4, 256);
+  }
+};
+bool mx4_grad_sizes_ok(int64_t rows, int64_t in, int64_t outs) {
+  return rows >= 0 && rows <= MX4_MAX_COLS && in >= 1 && in <= OSCARS_MAX_WIDTH && outs >= 1 &&
+         outs <= OSCARS_MAX_WIDTH;
+}
+
+}  // namespace
+
+oscars_status oscars_quantize_micro(uint8_t* q, int64_t q_ld, uint8_t* scale, int64_t s_ld,
+                                    const void* x, int64_t x_ld, int32_t dtype, int64_t rows,
+                                    int64_t cols, int32_t transposed, void* hip_stream) {
+  if (!is_dtype(dtype) || rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxRows)
+    return OSCARS_E_INVALID;
+  const int64_t along = transposed ? rows : cols, count = transposed ? cols : rows;
+  if (along > MX4_MAX_COLS || (transposed && rows * cols >= (int64_t{1} << 37)))
+    return OSCARS_E_INVALID;
+  const int64_t es = dtype_bytes(dtype);
+  if (!rows_ok(x, x_ld, cols, es)) return OSCARS_E_INVALID;
+  if (rows == 0) return OSCARS_OK;
+  if (!mx4_rows_ok(q, q_ld, scale, s_ld, along)) return OSCARS_E_INVALID;
+  const Range r[] = {mx4_range(q, q_ld, count, mx4_bytes(along)),
+                     mx4_range(scale, s_ld, count, mx4_scales(along)),
+                     {x, rows_span(rows, x_ld, cols, es)}};
+  if (!apart(r, 2, 3)) return OSCARS_E_INVALID;
+  const Mx4Source a{x, x_ld, dtype == OSCARS_BF16, rows, static_cast<int>(cols), nullptr, 0,
+                    DropArgs{}};
+  const Mx4Rows to{q, q_ld, scale, s_ld};
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t e = transposed ? launch_mx4_columns(a, to, nullptr, nullptr, s)
+                                  : launch_mx4_rows(a, to, s);
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+oscars_status oscars_dequantize_micro(void* out, int64_t out_ld, int32_t out_dtype,
+                                      const uint8_t* q, int64_t q_ld, const uint8_t* scale,
+                                      int64_t s_ld, int64_t rows, int64_t cols, void* hip_stream) {
+  if (!is_dtype(out_dtype) || rows < 0 || rows > kMaxRows || !mx4_cols_ok(cols) ||
+      !mx4_rows_ok(q, q_ld, scale, s_ld, cols))
+    return OSCARS_E_INVALID;
+  const int64_t es = dtype_bytes(out_dtype);
+  if (!rows_ok(out, out_ld, cols, es)) return OSCARS_E_INVALID;
+  const Range r[] = {{out, rows_span(rows, out_ld, cols, es)},
+                     mx4_range(q, q_ld, rows, mx4_bytes(cols)),
+                     mx4_range(scale, s_ld, rows, mx4_scales(cols))};
+  if (!apart(r, 1, 3)) return OSCARS_E_INVALID;
+  if (rows == 0) return OSCARS_OK;
+  const hipError_t e = launch_mx4_values(
+      Mx4Values{q, q_ld, scale, s_ld, rows, static_cast<int>(cols), out, out_ld,
+                out_dtype == OSCARS_BF16},
+      static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+oscars_status oscars_matmul_micro(void* out, int64_t out_ld, int32_t out_dtype, const uint8_t* xq,
+                                  int64_t x_ld, const uint8_t* xscale, int64_t xs_ld,
+                                  const uint8_t* wq, int64_t w_ld, const uint8_t* wscale,
+                                  int64_t ws_ld, const float* bias, int32_t relu,
+                                  const oscars_dropout_options* dropout, int64_t rows, int64_t in,
+                                  int64_t outs, void* hip_stream) {
+  DropArgs drop;
+  if (!is_dtype(out_dtype) || !drop_args(dropout, &drop)) return OSCARS_E_INVALID;
+  const Mx4Product a{xq,    x_ld, xscale, xs_ld, wq, w_ld, wscale, ws_ld, bias, relu != 0,
+                     rows,  static_cast<int>(in), static_cast<int>(outs), out, out_ld,
+                     out_dtype == OSCARS_BF16, drop};
+  if (!mx4_product_ok(a, in, outs) || !mx4_rows_ok(xq, x_ld, xscale, xs_ld, in))
+    return OSCARS_E_INVALID;
+  const Range r[] = {{out, rows_span(rows, out_ld, outs, dtype_bytes(out_dtype))},
+                     mx4_range(xq, x_ld, rows, mx4_bytes(in)),
+                     mx4_range(xscale, xs_ld, rows, mx4_scales(in)),
+                     mx4_range(wq, w_ld, outs, mx4_bytes(in)),
+                     mx4_range(wscale, ws_ld, outs, mx4_scales(in)),
+                     {bias, outs * 4},
+                     {drop.more, 8}};
+  if (!apart(r, 1, 7)) return OSCARS_E_INVALID;
+  if (rows == 0) return OSCARS_OK;
+  const hipError_t e = launch_mx4_product(a, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+int64_t oscars_linear_micro_workspace(int64_t rows, int64_t in) {
+  if (rows < 0 || rows > kMaxRows || in < 1 || in > OSCARS_MAX_WIDTH ||
+      mx4_one_launch(rows, static_cast<int>(in)))
+    return 0;
+  return round_up(rows * mx4_bytes(in), 256) + rows * mx4_scales(in);
+}
+
+oscars_status oscars_linear_micro(void* out, int64_t out_ld, int32_t out_dtype, const void* x,
+                                  int64_t x_ld, int32_t dtype, const uint8_t* wq, int64_t w_ld,
+                                  const uint8_t* wscale, int64_t ws_ld, const float* bias,
+                                  int32_t relu, const oscars_dropout_options* dropout,
+                                  int64_t rows, int64_t in, int64_t outs, void* workspace,
+                                  int64_t workspace_bytes, void* hip_stream) {
+  DropArgs drop;
+  if (!is_dtype(dtype) || !is_dtype(out_dtype) || !drop_args(dropout, &drop))
+    return OSCARS_E_INVALID;
+  Mx4Product a{nullptr, 0, nullptr, 0, wq, w_ld, wscale, ws_ld, bias, relu != 0,
+               rows, static_cast<int>(in), static_cast<int>(outs), out, out_ld,
+               out_dtype == OSCARS_BF16, drop};
+  const int64_t es = dtype_bytes(dtype);
+  if (!mx4_product_ok(a, in, outs) || in > OSCARS_MAX_WIDTH || !rows_ok(x, x_ld, in, es))
+    return OSCARS_E_INVALID;
+  const int64_t need = oscars_linear_micro_workspace(rows, in);
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+    return OSCARS_E_INVALID;
+  const Range r[] = {{out, rows_span(rows, out_ld, outs, dtype_bytes(out_dtype))},
+                     {need > 0 ? workspace : nullptr, need},
+                     {x, rows_span(rows, x_ld, in, es)},
+                     mx4_range(wq, w_ld, outs, mx4_bytes(in)),
+                     mx4_range(wscale, ws_ld, outs, mx4_scales(in)),
+                     {bias, outs * 4},
+                     {drop.more, 8}};
+  if (!apart(r, 2, 7)) return OSCARS_E_INVALID;
+  if (rows == 0) return OSCARS_OK;
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const bool bf16 = dtype == OSCARS_BF16;
+  hipError_t e;
+  if (need == 0) {
+    e = launch_mx4_few(a, x, x_ld, bf16, s);
+  } else {
+    uint8_t* q = static_cast<uint8_t*>(workspace);
+    const Mx4Rows to{q, mx4_bytes(in), q + round_up(rows * mx4_bytes(in), 256), mx4_scales(in)};
+    e = launch_mx4_rows(
+        Mx4Source{x, x_ld, bf16, rows, static_cast<int>(in), nullptr, 0, DropArgs{}}, to, s);
+    a.xq = to.q;
+    a.x_ld = to.q_ld;
+    a.xs = to.scale;
+    a.xs_ld = to.s_ld;
+    if (e == hipSuccess) e = launch_mx4_product(a, s);
+  }
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+int64_t oscars_linear_micro_backward_workspace(int64_t rows, int64_t in, int64_t outs,
+                                               int32_t want_dx) {
+  return mx4_grad_sizes_ok(rows, in, outs) ? Mx4Grads(rows, in, outs, want_dx != 0).end : 0;
+}
+
+oscars_status oscars_linear_micro_backward(const oscars_micro_gradients* g, void* workspace,
+                                           int64_t workspace_bytes, void* hip_stream) {
+  DropArgs drop;
+  if (!g || !is_dtype(g->y_dtype) || !is_dtype(g->x_dtype) || !drop_args(g->dropout, &drop) ||
+      !mx4_grad_sizes_ok(g->rows, g->in, g->outs))
+    return OSCARS_E_INVALID;
+  const int64_t rows = g->rows, ye = dtype_bytes(g->y_dtype), xe = dtype_bytes(g->x_dtype);
+  const int in = static_cast<int>(g->in), outs = static_cast<int>(g->outs);
+  const bool dx = g->dx != nullptr;
+  if (!rows_ok(g->dy, g->dy_ld, outs, ye) || !rows_ok(g->x, g->x_ld, in, xe) ||
+      (g->y && !rows_ok(g->y, g->y_ld, outs, ye)) || !rows_ok(g->dw, g->dw_ld, in, 4) ||
+      !aligned_to(g->db, 4))
+    return OSCARS_E_INVALID;
+  if (dx && (!rows_ok(g->dx, g->dx_ld, in, xe) ||
+             !mx4_rows_ok(g->wtq, g->wt_ld, g->wtscale, g->wts_ld, outs)))
+    return OSCARS_E_INVALID;
+  const Mx4Grads lay(rows, in, outs, dx);
+  if (lay.end > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < lay.end))
+    return OSCARS_E_INVALID;
+  const Range r[] = {{workspace, lay.end},
+                     {g->dx, rows_span(rows, g->dx_ld, in, xe)},
+                     {g->dw, rows_span(outs, g->dw_ld, in, 4)},
+                     {g->db, outs * int64_t{4}},
+                     {g->dy, rows_span(rows, g->dy_ld, outs, ye)},
+                     {g->y, rows_span(rows, g->y_ld, outs, ye)},
+                     {g->x, rows_span(rows, g->x_ld, in, xe)},
+                     {dx ? g->wtq : nullptr, rows_span(in, g->wt_ld, mx4_bytes(outs), 1)},
+                     {dx ? g->wtscale : nullptr, rows_span(in, g->wts_ld, mx4_scales(outs), 1)},
+                     {drop.more, 8}};
+  if (!apart(r, 4, 10)) return OSCARS_E_INVALID;
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  hipError_t e = hipSuccess;
+  if (rows == 0) {
+    e = launch_mx4_zero(g->dw, g->dw_ld, outs, in, s);
+    if (e == hipSuccess && g->db) e = launch_mx4_zero(g->db, outs, 1, outs, s);
+    return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+  }
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const Mx4Source z{g->dy, g->dy_ld, g->y_dtype == OSCARS_BF16, rows, outs, g->y, g->y_ld, drop};
+  const Mx4Source x{g->x, g->x_ld, g->x_dtype == OSCARS_BF16, rows, in, nullptr, 0, DropArgs{}};
+  const Mx4Rows zr{ws + lay.zq, mx4_bytes(outs), ws + lay.zs, mx4_scales(outs)};
+  const Mx4Rows zc{ws + lay.ztq, mx4_bytes(rows), ws + lay.zts, mx4_scales(rows)};
+  const Mx4Rows xc{ws + lay.xtq, mx4_bytes(rows), ws + lay.xts, mx4_scales(rows)};
+  e = launch_mx4_columns(z, zc, g->db, reinterpret_cast<float*>(ws + lay.part), s);
+  if (e == hipSuccess) e = launch_mx4_columns(x, xc, nullptr, nullptr, s);
+  if (e == hipSuccess && dx) e = launch_mx4_rows(z, zr, s);
+  if (e == hipSuccess && dx)
+    e = launch_mx4_product(
+        Mx4Product{zr.q, zr.q_ld, zr.scale, zr.s_ld, g->wtq, g->wt_ld, g->wtscale, g->wts_ld,
+                   nullptr, false, rows, outs, in, g->dx, g->dx_ld, g->x_dtype == OSCARS_BF16,
+                   DropArgs{}},
+        s);
+  if (e == hipSuccess)
+    e = launch_mx4_product(
+        Mx4Product{zc.q, zc.q_ld, zc.scale, zc.s_ld, xc.q, xc.q_ld, xc.scale, xc.s_ld, nullptr,
+                   false, outs, static_cast<int>(rows), in, g->dw, g->dw_ld, false, DropArgs{}},
+        s);
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+oscars_status oscars_dropout(void* out, int64_t out_ld, const void* x, int64_t x_ld, int32_t dtype,
+                             const oscars_dropout_options* options, int64_t rows, int64_t cols,
+                             void* hip_stream) {
+  DropArgs drop;
+  if (!options || !is_dtype(dtype) || !drop_args(options, &drop) || rows < 0 || rows > kMaxRows ||
+      cols < 1 || cols > kMaxRows)
+    return OSCARS_E_INVALID;
+  const int64_t es = dtype_bytes(dtype);
+  if (!rows_ok(x, x_ld, cols, es) || !rows_ok(out, out_ld, cols, es)) return OSCARS_E_INVALID;
+  const Range r[] = {{out, rows_span(rows, out_ld, cols, es)},
+                     {out == x && out_ld == x_ld ? nullptr : x, rows_span(rows, x_ld, cols, es)},
+                     {drop.more, 8}};
+  if (!apart(r, 1, 3)) return OSCARS_E_INVALID;
+  if (rows == 0) return OSCARS_OK;
+  const hipError_t e = launch_dropout(
+      DropoutArgs{x, x_ld, out, out_ld, dtype == OSCARS_BF16, rows, static_cast<int>(cols), drop},
+      static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
 
