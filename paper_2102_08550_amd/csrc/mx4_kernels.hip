@@ -301,9 +301,8 @@ __global__ __launch_bounds__(256) void mx4_zero_kernel(float* p, int64_t ld, int
 // ------------------------------------------------------------------ products
 
 __device__ __forceinline__ float mx_finish(const Mx4Product& a, float acc, float b) {
-  float y = acc + b;
-  if (a.relu) y = y < 0.0f ? 0.0f : y;  // keeps a NaN
-  return y;
+  const float y = acc + b;
+  return a.relu ? __builtin_elementwise_maximum(y, 0.0f) : y;  // keeps a NaN
 }
 // N (4 or 8) outputs of a row from o (a multiple of N) on.
 template <int N>
@@ -351,6 +350,36 @@ __device__ __forceinline__ void mx_store(const Mx4Product& a, int64_t row, int o
   }
 }
 
+// Two values in bf16, rounded to nearest even, by the one instruction there is for it.
+__device__ __forceinline__ uint32_t mx_bf16_pair(float lo, float hi) {
+  typedef __bf16 pair __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((mx_f32x2{lo, hi}), pair));
+}
+// 16 bytes of an output row in its type, from channel o on.
+template <bool OUT_BF16, bool VEC>
+__device__ __forceinline__ void mx_store16(const Mx4Product& a, int64_t row, int o, nt_u32x4 w) {
+  constexpr int N = OUT_BF16 ? 8 : 4;
+  if constexpr (OUT_BF16) {
+    uint16_t* p = static_cast<uint16_t*>(a.out) + row * a.out_ld + o;
+    if (VEC && o + N <= a.outs) {
+      __builtin_nontemporal_store(w, reinterpret_cast<nt_u32x4*>(p));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (o + e < a.outs) p[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+    }
+  } else {
+    uint32_t* p = static_cast<uint32_t*>(a.out) + row * a.out_ld + o;
+    if (VEC && o + N <= a.outs) {
+      __builtin_nontemporal_store(w, reinterpret_cast<nt_u32x4*>(p));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (o + e < a.outs) p[e] = w[e];
+    }
+  }
+}
+
 template <int BYTE>
 __device__ __forceinline__ nt_f32x16 mx_mfma(nt_u32x4 a, nt_u32x4 b, nt_f32x16 c, uint32_t sa,
                                              uint32_t sb) {
@@ -363,171 +392,206 @@ __device__ __forceinline__ nt_f32x16 mx_mfma(nt_u32x4 a, nt_u32x4 b, nt_f32x16 c
                                                          static_cast<int>(sb));
 }
 
-typedef NtShape<256, 256, 2, 4> MxL;
-typedef NtShape<128, 128, 2, 2> MxM;
+// Workgroup tile: BM x BN outputs, WM x WN waves.  A stage is 128 bytes of a row, 256
+// entries of K; two stages in LDS, and scales for two times two.
+template <int BM_, int BN_, int WM_, int WN_>
+struct MxShape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int NT = 64 * WM * WN, MI = BM / WM / 32, NJ = BN / WN / 32;
+  static constexpr int STAGE = (BM + BN) * NT_BLOCK, SCALES = (BM + BN) * 16;
+  static constexpr int LDS_BYTES = 2 * STAGE + 2 * SCALES;
+  static constexpr int EU = NT / 256 * (LDS_BYTES > (80 << 10) ? 1 : 2);  // waves of a SIMD
+  static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0, "whole blocks");
+  static_assert(BM + BN == NT, "a wave's load of scales each");
+};
+typedef MxShape<256, 256, 2, 4> MxL;
+typedef MxShape<128, 128, 2, 2> MxM;
 static_assert(mx4_threads(MxL::BM) == MxL::NT && mx4_threads(MxM::BM) == MxM::NT, "mx4_plan.h");
 
-// A stage is 256 entries of K, 128 bytes a row; of its eight blocks a lane takes 4 h +
-// c in group c (h: its half of the wave), so that its four scales are four
-// neighbouring bytes and the instruction picks byte c.  The order of K within a stage
-// is free, both operands have the same.
-// Scales come in pairs of stages, 16 bytes a row, a row a lane: half of the waves
-// fetch A's, the others B's.
+// p and bytes are the same for the wave; where the compiler computes them on the vector unit
+// (64-bit comparisons are its), it would loop over the lanes' buffers around every load.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_buffer(const uint8_t* p, int64_t bytes) {
+  const int n = static_cast<int>(bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF);
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(
+      reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0,
+      __builtin_amdgcn_readfirstlane(n), 0x00020000u);
+}
+typedef __attribute__((address_space(3))) void* mx_lds;
+
+// Rows and scales of a tile's operands as buffers that end behind the last row: what
+// lies behind it reads as zeros.
+struct MxTile {
+  __amdgpu_buffer_rsrc_t a, b, scales;
+};
+// The part of the addresses that is the same for every tile.  A lane's 16 bytes of a
+// stage: row r, chunk p at LDS byte 128 r + 16 p holds chunk p ^ turn(r) of the row:
+// 16 consecutive rows' chunks lie in different banks.
+__device__ __forceinline__ int mx_turn(int r) { return (r ^ ((r >> 3) & 3)) & 7; }
 template <class S>
-struct MxScales {
-  static constexpr int BYTES = 2 * (S::BM + S::BN) * 16;
-  static_assert((S::BM + S::BN) / 64 == S::NT / 64 && S::BM == S::BN, "a wave's load each");
-  __amdgpu_buffer_rsrc_t rsrc;
-  int voff;
-  __device__ __forceinline__ void init(const uint8_t* sa, int64_t a_ld, int64_t a_bytes, int a_row,
-                                       int a_rows, const uint8_t* sb, int64_t b_ld,
-                                       int64_t b_bytes, int b_rows, int tid) {
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const bool first = wave < S::NT / 128;
-    const int64_t ld = first ? a_ld : b_ld, at = first ? a_row * a_ld : 0;
-    const int64_t left = (first ? a_bytes : b_bytes) - at;
-    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>((first ? sa : sb) + at), 0,
-                                             static_cast<int>(left < 0x7FFFFFFF ? left : 0x7FFFFFFF),
-                                             0x00020000u);
-    const int r = first ? tid : tid - S::NT / 2, n = first ? a_rows - a_row : b_rows;
-    voff = static_cast<int>((r < n ? r : n - 1) * ld);
-  }
-  // lds: the tile's scales, A's rows and then B's, of two pairs
-  __device__ __forceinline__ void issue(char* lds, int pair, int tid) const {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        rsrc,
-        (__attribute__((address_space(3))) void*)(lds + (pair & 1) * (BYTES / 2) +
-                                                  (tid & ~63) * 16),
-        16, voff, pair * 16, 0, 0);
+struct MxPlace {
+  static constexpr int PA = S::BM * 8 / S::NT, PB = S::BN * 8 / S::NT, STEP = S::NT / 8;
+  static_assert(STEP % 32 == 0, "the same turn in every part");
+  int a, a_step, b, b_step, scales;
+  __device__ __forceinline__ MxPlace(const Mx4Product& p, int tid, int wave) {
+    const int r = tid / 8, c = 16 * ((tid % 8) ^ mx_turn(r));
+    a = static_cast<int>(r * p.w_ld) + c;
+    b = static_cast<int>(r * p.x_ld) + c;
+    a_step = static_cast<int>(STEP * p.w_ld);
+    b_step = static_cast<int>(STEP * p.x_ld);
+    // a row a lane, A's rows and then B's
+    scales = static_cast<int>(64 * wave < S::BM ? tid * p.ws_ld : (tid - S::BM) * p.xs_ld);
   }
 };
-
-// acc[i][j] += the tile's products over `blocks` stages, in the order of nt_tile's.
-template <class S>
-__device__ __forceinline__ void mx_tile(const NtRows<S::NT, S::BM>& a,
-                                        const NtRows<S::NT, S::BN>& b, const MxScales<S>& sc,
-                                        int blocks, char* lds, int tid,
-                                        nt_f32x16 (&acc)[S::MI][S::NJ]) {
-  constexpr int ABYTES = S::BM * NT_BLOCK, STAGE = (S::BM + S::BN) * NT_BLOCK;
-  char* scales = lds + 2 * STAGE;
-  const int lane = tid & 63, wave = tid >> 6;
-  const int arow = (wave / S::WN) * 32 * S::MI + (lane & 31);
-  const int brow = (wave % S::WN) * 32 * S::NJ + (lane & 31), h = lane >> 5;
-  constexpr bool SPREAD = S::NT == 512;
-  const int pairs = (blocks + 1) / 2;
-  auto issue = [&](int s) {
-    char* t = lds + (s & 1) * STAGE;
-    a.issue(t, s * NT_BLOCK, tid);
-    b.issue(t + ABYTES, s * NT_BLOCK, tid);
-  };
-  auto issue_part = [&](int s, int part) {
-    if (!SPREAD || s >= blocks) return;
-    char* t = lds + (s & 1) * STAGE;
-    a.issue(t, s * NT_BLOCK, tid, part);
-    b.issue(t + ABYTES, s * NT_BLOCK, tid, part);
-  };
-  auto load = [&](const char* t, int c, nt_u32x4(&fa)[S::MI], nt_u32x4(&fb)[S::NJ]) {
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i) fa[i] = nt_read(t, arow + 32 * i, 4 * h + c);
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j) fb[j] = nt_read(t + ABYTES, brow + 32 * j, 4 * h + c);
-  };
-  auto load_scales = [&](int s, uint32_t(&sa)[S::MI], uint32_t(&sb)[S::NJ]) {
-    const char* t = scales + ((s >> 1) & 1) * (MxScales<S>::BYTES / 2) + 8 * (s & 1) + 4 * h;
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i)
-      sa[i] = *reinterpret_cast<const uint32_t*>(t + (arow + 32 * i) * 16);
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j)
-      sb[j] = *reinterpret_cast<const uint32_t*>(t + (S::BM + brow + 32 * j) * 16);
-  };
-  uint32_t sa[S::MI], sb[S::NJ], na[S::MI], nb[S::NJ];
-  // the scheduler keeps loads and products in the order written
-#define OSCARS_MUL(C, FA, FB)                                                               \
-  do {                                                                                      \
-    __builtin_amdgcn_sched_barrier(0);                                                      \
-    _Pragma("unroll") for (int i = 0; i < S::MI; ++i)                                       \
-        _Pragma("unroll") for (int j = 0; j < S::NJ; ++j) acc[i][j] =                       \
-            mx_mfma<C>(FA[i], FB[j], acc[i][j], sa[i], sb[j]);                              \
-    __builtin_amdgcn_sched_barrier(0);                                                      \
-  } while (0)
-  nt_u32x4 a0[S::MI], a1[S::MI], b0[S::NJ], b1[S::NJ];
-  issue(0);
-  sc.issue(scales, 0, tid);
-  nt_wait_vm<0>();
-  nt_barrier();
-  if constexpr (SPREAD) issue_part(1, 0);
-  else if (blocks > 1) issue(1);
-  if (pairs > 1) sc.issue(scales, 1, tid);
-  load(lds, 0, a0, b0);
-  load_scales(0, sa, sb);
-  for (int s = 0; s < blocks; ++s) {
-    const char* t = lds + (s & 1) * STAGE;
-    const char* next = lds + ((s + 1) & 1) * STAGE;
-    issue_part(s + 1, 1);
-    load(t, 1, a1, b1);
-    OSCARS_MUL(0, a0, b0);
-    issue_part(s + 1, 2);
-    issue_part(s + 1, 3);
-    load(t, 2, a0, b0);
-    OSCARS_MUL(1, a1, b1);
-    load(t, 3, a1, b1);
-    OSCARS_MUL(2, a0, b0);
-    nt_wait_vm<0>();  // the next stage is there,
-    nt_barrier();     // and this one read by every wave
-    if constexpr (SPREAD) issue_part(s + 2, 0);
-    else if (s + 2 < blocks) issue(s + 2);
-    // stage s was the last of pair s / 2: its buffer takes the pair after the next
-    if ((s & 1) && (s >> 1) + 2 < pairs) sc.issue(scales, (s >> 1) + 2, tid);
-    load(next, 0, a0, b0);
-    load_scales(s + 1, na, nb);
-    OSCARS_MUL(3, a1, b1);
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i) sa[i] = na[i];
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j) sb[j] = nb[j];
-  }
-  nt_wait_vm<0>();
-#undef OSCARS_MUL
+__device__ __forceinline__ nt_u32x4 mx_read(const char* tile, int row, int chunk) {
+  return *reinterpret_cast<const nt_u32x4*>(tile + row * NT_BLOCK + 16 * (chunk ^ mx_turn(row)));
 }
 
-// Output rows are input rows; the tile's own rows (R) are output channels, four
-// consecutive ones a lane.  Two blocks of 32 channels go through LDS so that
-// neighbouring lanes store whole 128-byte lines of an output row.  VEC: 16-byte
-// stores.
+// A wave's 32 x 32 block of sums into outputs: acc[4 q + t] is channel o + 8 q + 4 h + t
+// (h: the lane's half of the wave) of row `row`.
+__device__ __forceinline__ void mx_epilogue(const Mx4Product& a, uint64_t offset, int64_t row,
+                                            int o, int h, const nt_f32x4 (&bias)[4],
+                                            const nt_f32x16& acc, float (&v)[16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = mx_finish(a, acc[e], bias[e >> 2][e & 3]);
+  if (a.drop.below) {
+    // eight channels share a call of the generator, and four of them are the other half's:
+    // each half makes one of two calls, and they swap words
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(row), o / 8 + 2 * p + h);
+      const auto x = __builtin_amdgcn_permlane32_swap(w.w[0], w.w[2], false, false);
+      const auto y = __builtin_amdgcn_permlane32_swap(w.w[1], w.w[3], false, false);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const uint32_t lo = x[q], hi = y[q];
+        float* u = v + 4 * (2 * p + q);
+        u[0] = (lo & 0xFFFFu) >= a.drop.below ? u[0] * a.drop.factor : 0.0f;
+        u[1] = lo >> 16 >= a.drop.below ? u[1] * a.drop.factor : 0.0f;
+        u[2] = (hi & 0xFFFFu) >= a.drop.below ? u[2] * a.drop.factor : 0.0f;
+        u[3] = hi >> 16 >= a.drop.below ? u[3] * a.drop.factor : 0.0f;
+      }
+    }
+  }
+}
+
+// Four channels 8 q + 4 h .. + 3 of each of a block's four q.
+__device__ __forceinline__ void mx_bias(const Mx4Product& a, int o, int h, nt_f32x4 (&bias)[4]) {
+  if (a.bias && o + 32 <= a.outs) {
+    // the same for the wave but for its halves: loaded by the scalar unit
+    const auto* p = (const __attribute__((address_space(4))) float*)(a.bias + o);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float lo = p[8 * q + t], hi = p[8 * q + 4 + t];
+        bias[q][t] = h ? hi : lo;
+      }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int c = o + 8 * q + 4 * h + t;
+        bias[q][t] = a.bias ? a.bias[c < a.outs ? c : a.outs - 1] : 0.0f;
+      }
+  }
+}
+
+// Output rows are input rows; the tile's own rows (A's) are output channels, four
+// consecutive ones a lane.
+// The last products of a stage are issued behind the barrier that ends it, with the
+// next stage's first operands on their way; then the loads into the stage that is
+// free go out, a whole stage ahead.  The empty asm keeps each group's products where
+// they are written: without it they sink below the loads of the groups behind
+// them, whose operands then do not fit the registers (8192 x 4096 x 4096: 139 us instead
+// of 78).  A 256 x 256 tile's stage takes 3250 cycles at 1.7 GHz, where 32 products a
+// wave are 2048: instructions from registers alone run at 6.5 PFLOP/s, 1.55 GHz, so it
+// is power that bounds both.  Stages of 64 bytes, four of them in LDS: 88 us; four waves
+// of 128 x 128 outputs: 87 us; workgroups that take one tile after the other, the next
+// one's loads ahead of the stores: 76 us, but 55 instead of 51 where there is one tile a
+// CU (2048 x 8192 x 4096).
+// Of a stage's eight chunks a lane takes 4 h + c in group c (h: its half of the wave), so
+// that its four scales are neighbouring bytes and the instruction picks byte c.  The order
+// of K within a stage is free, both operands have the same.  Scales come in parts of
+// 16 bytes a row, two stages'.
+// VEC: 16-byte stores.
 template <class S, bool OUT_BF16, bool VEC>
-__global__ __launch_bounds__(S::NT, 2) void mx4_product_kernel(Mx4Product a) {
+__global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a) {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
-  constexpr int TURN = 68;  // 64 channels of a row
-  static_assert(S::LDS_BYTES >= S::WM * S::WN * 32 * TURN * 4 && S::MI % 2 == 0, "turned blocks");
-  __shared__ __attribute__((aligned(16))) char lds[S::LDS_BYTES + MxScales<S>::BYTES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+  constexpr int ABYTES = S::BM * NT_BLOCK, ES = OUT_BF16 ? 2 : 4;
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS_BYTES];
+  char* const scales = lds + 2 * S::STAGE;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int am = (wave / S::WN) * 32 * S::MI, bm = (wave % S::WN) * 32 * S::NJ;
   const int tr = (a.outs + S::BM - 1) / S::BM;
   const int tc = static_cast<int>((a.rows + S::BN - 1) / S::BN);
-  const int total = tr * tc;
-  int id;
+  int r0;
+  int64_t c0;
   {  // the workgroups of one XCD (index mod 8) take neighbouring tiles
-    const int per = total >> 3, rem = total & 7, x = blockIdx.x & 7, q = blockIdx.x >> 3;
-    id = x * per + (x < rem ? x : rem) + q;
+    const int total = tr * tc, per = total >> 3, rem = total & 7;
+    const int x = blockIdx.x & 7, q = blockIdx.x >> 3;
+    const int id = x * per + (x < rem ? x : rem) + q;
+    // bands of four tile columns (rows of the input), channel tile by channel tile
+    constexpr int BAND = 4;
+    const int band = id / (BAND * tr), cols = tc - band * BAND < BAND ? tc - band * BAND : BAND;
+    const int in_band = id - band * BAND * tr;
+    r0 = (in_band / cols) * S::BM;
+    c0 = static_cast<int64_t>(band * BAND + in_band % cols) * S::BN;
   }
-  // bands of four tile columns (rows of the input), channel tile by channel tile
-  constexpr int BAND = 4;
-  const int band = id / (BAND * tr), cols = tc - band * BAND < BAND ? tc - band * BAND : BAND;
-  const int at = id - band * BAND * tr;
-  const int r0 = (at / cols) * S::BM;
-  const int64_t c0 = static_cast<int64_t>(band * BAND + at % cols) * S::BN;
-
   const int blocks = (a.in + 255) / 256;
-  const int64_t left = a.rows - c0;
-  const int here = static_cast<int>(left < S::BN ? left : S::BN);
-  NtRows<S::NT, S::BM> ra;
-  NtRows<S::NT, S::BN> rb;
-  MxScales<S> sc;
-  const int64_t qb = mx4_bytes(a.in), sb = mx4_scales(a.in);
-  ra.init(a.wq, a.w_ld, (a.outs - 1) * a.w_ld + qb, r0, a.outs, tid);
-  rb.init(a.xq + c0 * a.x_ld, a.x_ld, (here - 1) * a.x_ld + qb, 0, here, tid);
-  sc.init(a.ws, a.ws_ld, (a.outs - 1) * a.ws_ld + sb, r0, a.outs, a.xs + c0 * a.xs_ld, a.xs_ld,
-          (here - 1) * a.xs_ld + sb, here, tid);
+  const MxPlace<S> at(a, tid, wave);
+  MxTile t;
+  {
+    const int64_t left = a.rows - c0, qb = mx4_bytes(a.in), sb = mx4_scales(a.in);
+    const int nb = __builtin_amdgcn_readfirstlane(static_cast<int>(left < S::BN ? left : S::BN));
+    const int na = a.outs - r0 < S::BM ? a.outs - r0 : S::BM;
+    const bool first = 64 * wave < S::BM;
+    t.a = mx_buffer(a.wq + r0 * a.w_ld, (na - 1) * a.w_ld + qb);
+    t.b = mx_buffer(a.xq + c0 * a.x_ld, (nb - 1) * a.x_ld + qb);
+    t.scales = mx_buffer(first ? a.ws + r0 * a.ws_ld : a.xs + c0 * a.xs_ld,
+                         first ? (na - 1) * a.ws_ld + sb : (nb - 1) * a.xs_ld + sb);
+  }
+  // stage s, and with an even one its part of the scales
+  auto issue = [&](int s) {
+    if (s >= blocks) return;
+    char* to = lds + (s & 1) * S::STAGE + wave * 1024;
+    const int k = s * NT_BLOCK;
+#pragma unroll
+    for (int p = 0; p < MxPlace<S>::PA; ++p)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(t.a, (mx_lds)(to + S::NT * 16 * p), 16, at.a,
+                                               k + p * at.a_step, 0, 0);
+#pragma unroll
+    for (int p = 0; p < MxPlace<S>::PB; ++p)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(t.b, (mx_lds)(to + ABYTES + S::NT * 16 * p), 16,
+                                               at.b, k + p * at.b_step, 0, 0);
+    if ((s & 1) == 0)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          t.scales, (mx_lds)(scales + ((s >> 1) & 1) * S::SCALES + wave * 1024), 16, at.scales,
+          8 * s, 0, 0);
+  };
+  auto load = [&](int s, int c, nt_u32x4(&fa)[S::MI], nt_u32x4(&fb)[S::NJ]) {
+    const char* from = lds + (s & 1) * S::STAGE;
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) fa[i] = mx_read(from + (am + 32 * i) * NT_BLOCK, r, 4 * h + c);
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j)
+      fb[j] = mx_read(from + ABYTES + (bm + 32 * j) * NT_BLOCK, r, 4 * h + c);
+  };
+  auto load_scales = [&](int s, uint32_t(&sa)[S::MI], uint32_t(&sb)[S::NJ]) {
+    const char* from = scales + ((s >> 1) & 1) * S::SCALES + 16 * r + 8 * (s & 1) + 4 * h;
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+      sa[i] = *reinterpret_cast<const uint32_t*>(from + (am + 32 * i) * 16);
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j)
+      sb[j] = *reinterpret_cast<const uint32_t*>(from + (S::BM + bm + 32 * j) * 16);
+  };
+  uint32_t sa[2][S::MI], sb[2][S::NJ];
+  nt_u32x4 fa[2][S::MI], fb[2][S::NJ];
   nt_f32x16 acc[S::MI][S::NJ];
 #pragma unroll
   for (int i = 0; i < S::MI; ++i)
@@ -535,53 +599,90 @@ __global__ __launch_bounds__(S::NT, 2) void mx4_product_kernel(Mx4Product a) {
     for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  mx_tile<S>(ra, rb, sc, blocks, lds, tid, acc);
+  issue(0);
+  issue(1);
+  nt_wait_vm<0>();
+  nt_barrier();
+  load(0, 0, fa[0], fb[0]);
+  load_scales(0, sa[0], sb[0]);
+  // a stage; its scales are sa[E], sb[E], the next one's go to the others
+#define OSCARS_STAGE(STAGE, E)                                                                  \
+  {                                                                                             \
+    const int now = STAGE;                                                                      \
+    _Pragma("unroll") for (int c = 0; c < 4; ++c) {                                             \
+      if (c < 3) {                                                                              \
+        load(now, c + 1, fa[(c + 1) & 1], fb[(c + 1) & 1]);                                     \
+      } else {                                                                                  \
+        nt_wait_vm<0>(); /* the next stage is there, */                                         \
+        nt_barrier();    /* and this one read by every wave */                                  \
+        load(now + 1, 0, fa[0], fb[0]);                                                         \
+        load_scales(now + 1, sa[1 - (E)], sb[1 - (E)]);                                         \
+        issue(now + 2);                                                                         \
+      }                                                                                         \
+      __builtin_amdgcn_sched_barrier(0);                                                        \
+      _Pragma("unroll") for (int i = 0; i < S::MI; ++i)                                         \
+          _Pragma("unroll") for (int j = 0; j < S::NJ; ++j) {                                   \
+        if (c == 0) acc[i][j] = mx_mfma<0>(fa[0][i], fb[0][j], acc[i][j], sa[E][i], sb[E][j]);  \
+        if (c == 1) acc[i][j] = mx_mfma<1>(fa[1][i], fb[1][j], acc[i][j], sa[E][i], sb[E][j]);  \
+        if (c == 2) acc[i][j] = mx_mfma<2>(fa[0][i], fb[0][j], acc[i][j], sa[E][i], sb[E][j]);  \
+        if (c == 3) acc[i][j] = mx_mfma<3>(fa[1][i], fb[1][j], acc[i][j], sa[E][i], sb[E][j]);  \
+      }                                                                                         \
+      _Pragma("unroll") for (int i = 0; i < S::MI; ++i)                                         \
+          _Pragma("unroll") for (int j = 0; j < S::NJ; ++j) asm volatile("" : "+v"(acc[i][j])); \
+      __builtin_amdgcn_sched_barrier(0);                                                        \
+    }                                                                                           \
+  }
+  int stage = 0;
+  for (; stage + 1 < blocks; stage += 2) {
+    OSCARS_STAGE(stage, 0)
+    OSCARS_STAGE(stage + 1, 1)
+  }
+  if (stage < blocks) OSCARS_STAGE(stage, 0)
+#undef OSCARS_STAGE
 
-  const int rw = r0 + (wave / S::WN) * 32 * S::MI;
-  const int64_t cw = c0 + (wave % S::WN) * 32 * S::NJ;
-  float* turn = reinterpret_cast<float*>(lds) + wave * 32 * TURN;
-  constexpr int PER = OUT_BF16 ? 8 : 4, LANES = 64 / PER;  // 16 bytes a lane
-  const int k = PER * (lane % LANES);
+  // The outputs of 32 rows, two blocks of 32 channels of them, go through LDS in their type,
+  // so that neighbouring lanes store whole lines of an output row.
+  constexpr int TURN = 64 * ES + 16;              // bytes of a row's channels
+  constexpr int PER = 16 / ES, LANES = 64 / PER;  // channels of a lane, lanes of a row
+  static_assert(S::LDS_BYTES >= S::WM * S::WN * 32 * TURN && S::MI % 2 == 0, "turned blocks");
+  char* const turn = lds + wave * 32 * TURN;
   const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0;
   nt_barrier();  // the stages are read: LDS is free
-#pragma nounroll
-  for (int i = 0; i < S::MI; i += 2) {
-    const int o = rw + 32 * i + k;  // the lane's channels
-    if (rw + 32 * i >= a.outs) continue;
-    float bias[PER];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const int oc = o + e < a.outs ? o + e : a.outs - 1;
-      bias[e] = a.bias ? a.bias[oc] : 0.0f;
-    }
-#pragma nounroll
+  for (int i = 0; i < S::MI; i += 2) {
+    const int o = r0 + am + 32 * i;
+    if (o >= a.outs) continue;  // uniform over the wave
+    nt_f32x4 bias[2][4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) mx_bias(a, o + 32 * k, h, bias[k]);
+#pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
-      const int64_t row0 = cw + 32 * j;
+      const int64_t row0 = c0 + bm + 32 * j;
       if (row0 >= a.rows) continue;  // uniform over the wave
 #pragma unroll
-      for (int ii = 0; ii < S::MI; ++ii)
+      for (int k = 0; k < 2; ++k) {
+        float v[16];
+        mx_epilogue(a, offset, row0 + r, o + 32 * k, h, bias[k], acc[i + k][j], v);
+        char* to = turn + r * TURN + (32 * k + 4 * h) * ES;
 #pragma unroll
-        for (int jj = 0; jj < S::NJ; ++jj)
-          if ((ii & ~1) == i && jj == j) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              *reinterpret_cast<nt_f32x4*>(turn + (lane & 31) * TURN + 32 * (ii & 1) + 8 * q +
-                                           4 * h) =
-                  nt_f32x4{acc[ii][jj][4 * q], acc[ii][jj][4 * q + 1], acc[ii][jj][4 * q + 2],
-                           acc[ii][jj][4 * q + 3]};
-          }
-      nt_wave_sync();
-      for (int r = lane / LANES; r < 32; r += 64 / LANES) {
-        const int64_t row = row0 + r;
-        float v[PER];
-#pragma unroll
-        for (int e = 0; e < PER; e += 4) {
-          const nt_f32x4 t = *reinterpret_cast<const nt_f32x4*>(turn + r * TURN + k + e);
-#pragma unroll
-          for (int f = 0; f < 4; ++f) v[e + f] = mx_finish(a, t[f], bias[e + f]);
+        for (int q = 0; q < 4; ++q) {
+          if constexpr (OUT_BF16)
+            *reinterpret_cast<nt_u32x2*>(to + 8 * q * ES) =
+                nt_u32x2{mx_bf16_pair(v[4 * q], v[4 * q + 1]),
+                         mx_bf16_pair(v[4 * q + 2], v[4 * q + 3])};
+          else
+            *reinterpret_cast<nt_f32x4*>(to + 8 * q * ES) =
+                nt_f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
         }
-        if (a.drop.below) mx_drop<PER>(a, offset, row, o, v);
-        if (row < a.rows && o < a.outs) mx_store<PER, OUT_BF16, VEC>(a, row, o, v);
+      }
+      nt_wave_sync();
+      const int mine = o + PER * (lane % LANES);
+#pragma unroll
+      for (int n = 0; n < 32; n += 64 / LANES) {
+        const int64_t row = row0 + n + lane / LANES;
+        const nt_u32x4 w = *reinterpret_cast<const nt_u32x4*>(
+            turn + (n + lane / LANES) * TURN + 16 * (lane % LANES));
+        if (row < a.rows && mine < a.outs) mx_store16<OUT_BF16, VEC>(a, row, mine, w);
       }
       nt_wave_sync();
     }
