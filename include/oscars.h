@@ -503,7 +503,8 @@ typedef struct {
  *   x', one per column of x.
  *   x      device [rows][x_ld], dtype OSCARS_FP32 or OSCARS_BF16, aligned to its
  *          elements, x_ld >= cols;  0 <= rows < 2^31, 1 <= cols; the entries of a
- *          quantised row at most 2^24, with `transposed` fewer than 2^37 in all.
+ *          quantised row at most 2^24, with `transposed` fewer than 2^37 in all, rows
+ *          counted to a whole 256 and columns to a whole 64.
  * oscars_dequantize_micro: the values of quantised rows, in fp32 or rounded to bf16.
  * oscars_matmul_micro: the product of quantised rows and weights,
  *   y[r][o] = drop(relu(sum_k x[r][k] w[o][k] + bias[o])),  sums, bias and dropout's
@@ -549,7 +550,8 @@ oscars_status oscars_linear_micro(void* out, int64_t out_ld, int32_t out_dtype, 
  *            transposed): [in] quantised rows of `outs` entries;
  *   dx       device [rows][dx_ld], x_dtype, or NULL: not wanted (wtq, wtscale unused);
  *   dw       device [outs][dw_ld] fp32;  db  device [outs] fp32, or NULL;
- *   0 <= rows <= 2^24 (0: dw and db are 0), 1 <= in, outs <= OSCARS_MAX_WIDTH;
+ *   0 <= rows <= 2^24 (0: dw and db are 0), 1 <= in, outs <= OSCARS_MAX_WIDTH, x and dy
+ *            together fewer than 2^37 entries, counted as for oscars_quantize_micro;
  *   workspace  device, 16-byte aligned, oscars_linear_micro_backward_workspace bytes,
  *            the call's own until the stream has run it. */
 typedef struct {

@@ -560,13 +560,24 @@ def _micro_shapes(rows: int, cols: int):
 def _micro_rows(q, scale, rows, cols, device, what):
     """(pointer, row stride, scales' pointer, row stride) of quantised rows."""
     import torch
-    qp, n, qld, qc = _rows(q, torch.uint8, device, what)
-    sp, sn, sld, sc = _rows(scale, torch.uint8, device, what + "'s scales")
-    (_, width), (_, blocks) = _micro_shapes(rows, cols)
-    if n != rows or sn != rows or qc < width or sc < blocks:
+    if (not isinstance(q, torch.Tensor) or not isinstance(scale, torch.Tensor)
+            or q.device != device or scale.device != device or not q.is_cuda):
+        raise TypeError(f"{what} and its scales must be tensors on the input's CUDA (HIP) device")
+    if q.dtype != torch.uint8 or scale.dtype != torch.uint8:
+        raise TypeError(f"{what} and its scales must have dtype uint8")
+    width, blocks = (cols + 255) // 256 * 128, (cols + 511) // 512 * 16
+    qs, ss = q.shape, scale.shape
+    if (len(qs) != 2 or len(ss) != 2 or qs[0] != rows or ss[0] != rows or qs[1] < width
+            or ss[1] < blocks):
         raise ValueError(f"{what} must hold {rows} rows of {width} bytes and {blocks} scales")
-    # the stride of a single row says nothing
-    return qp, qld if n > 1 else width, sp, sld if n > 1 else blocks
+    if rows <= 1:  # the stride of a single row says nothing
+        if (qs[1] > 1 and q.stride(1) != 1) or (ss[1] > 1 and scale.stride(1) != 1):
+            raise ValueError(f"{what} must be stored by rows")
+        return q.data_ptr(), width, scale.data_ptr(), blocks
+    (qld, qstep), (sld, sstep) = q.stride(), scale.stride()
+    if ((qs[1] > 1 and qstep != 1) or (ss[1] > 1 and sstep != 1) or qld < qs[1] or sld < ss[1]):
+        raise ValueError(f"{what} must be stored by rows that do not overlap")
+    return q.data_ptr(), qld, scale.data_ptr(), sld
 
 
 def _dropout_options(dropout, device):
@@ -588,6 +599,20 @@ def _dropout_options(dropout, device):
     if not 0 <= offset < 1 << 64:
         raise ValueError("dropout's offset must be of 64 bits, not negative")
     return _Dropout(p, seed, offset, None), None
+
+
+def _result(out, rows, cols, dtype, asked, device, stream):
+    """(out, pointer, row stride, type): a new tensor of ``asked`` or ``dtype``, or
+    the caller's, checked."""
+    if out is None:
+        out = _new((rows, cols), asked or dtype, device, stream)
+        return out, out.data_ptr(), cols, _float_type(out.dtype, "out")
+    if asked is not None and out.dtype != asked:
+        raise TypeError("out has another dtype than the one asked for")
+    op, on, old, oc = _rows(out, out.dtype, device, "out")
+    if (on, oc) != (rows, cols):
+        raise ValueError(f"out must be [{rows}][{cols}]")
+    return out, op, old, _float_type(out.dtype, "out")
 
 
 def quantize_mx4(x, transposed: bool = False, out=None, stream=None):
@@ -622,17 +647,11 @@ def dequantize_mx4(q, scale, columns: int, dtype=None, out=None, stream=None):
     dev = q.device
     n = q.shape[0]
     qp, qld, sp, sld = _micro_rows(q, scale, n, int(columns), dev, "q")
-    if out is None:
-        out = _new((n, int(columns)), dtype or torch.float32, dev, stream)
-    elif dtype is not None and out.dtype != dtype:
-        raise TypeError("out has another dtype than dtype")
-    op, on, old, oc = _rows(out, out.dtype, dev, "out")
-    if (on, oc) != (n, columns):
-        raise ValueError("out must be [rows][columns]")
+    out, op, old, odt = _result(out, n, int(columns), torch.float32, dtype, dev, stream)
     if n == 0:
         return out
     with _on_device(dev):
-        _check(_lib().oscars_dequantize_micro(op, old, _float_type(out.dtype, "out"), qp, qld, sp,
+        _check(_lib().oscars_dequantize_micro(op, old, odt, qp, qld, sp,
                                               sld, n, int(columns), _stream_handle(stream)),
                "oscars_dequantize_micro")
     _used_on(stream, q, scale, out)
@@ -650,19 +669,13 @@ def matmul_mx4(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool =
     n, outs, cols = xq.shape[0], wq.shape[0], int(in_features)
     xp, xld, xsp, xsld = _micro_rows(xq, xscale, n, cols, dev, "xq")
     wp, wld, wsp, wsld = _micro_rows(wq, wscale, outs, cols, dev, "wq")
-    if out is None:
-        out = _new((n, outs), out_dtype or torch.float32, dev, stream)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise TypeError("out has another dtype than out_dtype")
-    op, on, old, oc = _rows(out, out.dtype, dev, "out")
-    if (on, oc) != (n, outs):
-        raise ValueError("out must be [rows][outputs]")
+    out, op, old, odt = _result(out, n, outs, torch.float32, out_dtype, dev, stream)
     drop, offset = _dropout_options(dropout, dev)
     if n == 0:
         return out
     with _on_device(dev):
         _check(_lib().oscars_matmul_micro(
-            op, old, _float_type(out.dtype, "out"), xp, xld, xsp, xsld, wp, wld, wsp, wsld,
+            op, old, odt, xp, xld, xsp, xsld, wp, wld, wsp, wsld,
             _vector(bias, outs, dev, "bias"), int(bool(relu)), drop, n, cols, outs,
             _stream_handle(stream)), "oscars_matmul_micro")
     _used_on(stream, xq, xscale, wq, wscale, bias, offset, out)
@@ -682,13 +695,7 @@ def linear_mx4(x, wq, wscale, bias=None, relu: bool = False, dropout=None, out_d
     dt = _float_type(x.dtype, "x")
     outs = wq.shape[0]
     wp, wld, wsp, wsld = _micro_rows(wq, wscale, outs, cols, dev, "wq")
-    if out is None:
-        out = _new((n, outs), out_dtype or x.dtype, dev, stream)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise TypeError("out has another dtype than out_dtype")
-    op, on, old, oc = _rows(out, out.dtype, dev, "out")
-    if (on, oc) != (n, outs):
-        raise ValueError("out must be [rows][outputs]")
+    out, op, old, odt = _result(out, n, outs, x.dtype, out_dtype, dev, stream)
     drop, offset = _dropout_options(dropout, dev)
     if n == 0:
         return out
@@ -697,7 +704,7 @@ def linear_mx4(x, wq, wscale, bias=None, relu: bool = False, dropout=None, out_d
     ws = _workspace(need, dev, stream) if need else None
     with _on_device(dev):
         _check(lib.oscars_linear_micro(
-            op, old, _float_type(out.dtype, "out"), xp, xld, dt, wp, wld, wsp, wsld,
+            op, old, odt, xp, xld, dt, wp, wld, wsp, wsld,
             _vector(bias, outs, dev, "bias"), int(bool(relu)), drop, n, cols, outs,
             ws.data_ptr() if need else None, need, _stream_handle(stream)),
             "oscars_linear_micro")
@@ -770,11 +777,7 @@ def dropout(x, p: float, seed: int, offset=0, out=None, stream=None):
     dev = x.device
     xp, n, ld, cols = _rows(x, x.dtype, dev, "x")
     dt = _float_type(x.dtype, "x")
-    if out is None:
-        out = _new((n, cols), x.dtype, dev, stream)
-    op, on, old, oc = _rows(out, x.dtype, dev, "out")
-    if (on, oc) != (n, cols):
-        raise ValueError("out must have x's shape")
+    out, op, old, _ = _result(out, n, cols, x.dtype, x.dtype, dev, stream)
     options, more = _dropout_options((p, seed, offset), dev)
     if n == 0:
         return out

@@ -28,7 +28,7 @@ struct Mx4Rows {
   int64_t s_ld;
 };
 
-// What is quantised: x, or with y or dropout the gradient behind a layer's epilogue:
+// What is quantised: x, or for the gradients what is behind a layer's epilogue:
 // 0 where y <= 0 or the generator dropped the entry (only asked without y), else
 // fl(x factor).
 struct Mx4Source {
@@ -37,16 +37,24 @@ struct Mx4Source {
   bool bf16;
   int64_t rows;
   int cols;
-  const void* y;  // of x's type, or nullptr
+  const void* y;  // of x's type, or nullptr; gradients only, like drop
   int64_t y_ld;
   DropArgs drop;
 };
 hipError_t launch_mx4_rows(const Mx4Source& a, const Mx4Rows& to, hipStream_t s);
-// The rows of x' in 4 bits; sums: the columns' sums in fp32, or nullptr; then part
-// holds mx4_sum_parts(rows) x cols floats.
+// The rows of x' in 4 bits; fewer than 2^23 tiles.
+int64_t mx4_column_tiles(int64_t rows, int cols);
+hipError_t launch_mx4_columns(const Mx4Source& a, const Mx4Rows& to, hipStream_t s);
+
+// What the gradients multiply: dz by columns and, with z_rows.q, by rows; x by columns;
+// and dz's columns' sums, or nullptr; then part holds mx4_sum_parts(rows) x cols floats.
+struct Mx4Gradient {
+  Mx4Source z, x;
+  Mx4Rows z_rows, z_columns, x_columns;
+  float *sums, *part;
+};
 int64_t mx4_sum_parts(int64_t rows);
-hipError_t launch_mx4_columns(const Mx4Source& a, const Mx4Rows& to, float* sums, float* part,
-                              hipStream_t s);
+hipError_t launch_mx4_gradient(const Mx4Gradient& g, hipStream_t s);
 
 struct Mx4Values {
   const uint8_t* q;
@@ -81,6 +89,8 @@ struct Mx4Product {
   DropArgs drop;
 };
 hipError_t launch_mx4_product(const Mx4Product& a, hipStream_t s);
+// One or two products that wait for nothing of each other, in one launch if they are small.
+hipError_t launch_mx4_products(const Mx4Product* p, int n, hipStream_t s);
 
 // A few rows: quantisation and product in one launch (x of the caller's type; xq,
 // x_ld, xs and xs_ld of `a` unused).

@@ -4,7 +4,9 @@
 // scale; the matrix units add them into fp32.
 //
 //   mx4_rows      rows into 4 bits, one pass;
-//   mx4_columns   columns into 4 bits (the rows of x'), and their sums;
+//   mx4_columns   columns into 4 bits (the rows of x');
+//   mx4_gradient  the output's gradient by columns, and rows, and its sums, and x by
+//                 columns: all that the gradients multiply;
 //   mx4_values    4 bits back into values;
 //   mx4_product   tiles on 32x32x64 block-scaled matrix instructions: a lane's 16
 //                 bytes of an operand are one block of 32 with one scale;
@@ -54,33 +56,37 @@ __device__ __forceinline__ MxScale mx_scale(uint32_t top) {
   if (top < 0x00800000u) r = MxScale{0u, 0.0f};
   return r;
 }
-// Eight entries, first in the low half of the lowest byte.  v inv is exact; the
-// conversion rounds to nearest, ties to even.
+// Two entries into byte B of w, the first in its low half.  v inv is exact; the conversion
+// rounds to nearest, ties to even.
+template <int B>
+__device__ __forceinline__ uint32_t mx_pack2(uint32_t w, float a, float b, float inv) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a * inv, b * inv, 1.0f, B);
+}
 __device__ __forceinline__ uint32_t mx_pack8(const float* v, float inv) {
-  uint32_t w = 0;
-  if (inv > 0.0f) {
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * inv, v[1] * inv, 1.0f, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * inv, v[3] * inv, 1.0f, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * inv, v[5] * inv, 1.0f, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * inv, v[7] * inv, 1.0f, 3);
-  }
-  return w;
+  uint32_t w = mx_pack2<0>(0u, v[0], v[1], inv);
+  w = mx_pack2<1>(w, v[2], v[3], inv);
+  w = mx_pack2<2>(w, v[4], v[5], inv);
+  w = mx_pack2<3>(w, v[6], v[7], inv);
+  return inv > 0.0f ? w : 0u;
 }
 
-// Eight consecutive entries from column c (a multiple of 8); zeros from `cols` on.
+// Eight consecutive entries from column c (a multiple of 8).  VEC: cols % 8 == 0, 16-byte loads.
+// Columns behind the last read the last ones again, so that no load waits behind a branch;
+// mx_clip8 makes them zeros.
 template <bool BF16, bool VEC>
 __device__ __forceinline__ void mx_load8(const void* row, int c, int cols, float* v) {
-  if (VEC && c + 8 <= cols) {
+  if constexpr (VEC) {
+    const int at = c < cols ? c : cols - 8;
     if constexpr (BF16) {
       const nt_u32x4 w =
-          *reinterpret_cast<const nt_u32x4*>(static_cast<const uint16_t*>(row) + c);
+          *reinterpret_cast<const nt_u32x4*>(static_cast<const uint16_t*>(row) + at);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         v[2 * t] = mx_bf16(w[t] & 0xFFFFu);
         v[2 * t + 1] = mx_bf16(w[t] >> 16);
       }
     } else {
-      const nt_f32x4* p = reinterpret_cast<const nt_f32x4*>(static_cast<const float*>(row) + c);
+      const nt_f32x4* p = reinterpret_cast<const nt_f32x4*>(static_cast<const float*>(row) + at);
       const nt_f32x4 a = p[0], b = p[1];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -91,13 +97,16 @@ __device__ __forceinline__ void mx_load8(const void* row, int c, int cols, float
   } else {
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
-      v[t] = 0.0f;
-      if (c + t < cols) {
-        if constexpr (BF16) v[t] = mx_bf16(static_cast<const uint16_t*>(row)[c + t]);
-        else v[t] = static_cast<const float*>(row)[c + t];
-      }
+      const int at = c + t < cols ? c + t : cols - 1;
+      if constexpr (BF16) v[t] = mx_bf16(static_cast<const uint16_t*>(row)[at]);
+      else v[t] = static_cast<const float*>(row)[at];
     }
   }
+}
+template <bool VEC>
+__device__ __forceinline__ void mx_clip8(int c, int cols, float* v) {
+#pragma unroll
+  for (int t = 0; t < 8; ++t) v[t] = (VEC ? c : c + t) < cols ? v[t] : 0.0f;
 }
 
 // The gradient behind the layer's epilogue (mx4.h).  A NaN in y passes it on.
@@ -106,163 +115,312 @@ __device__ __forceinline__ float mx_pass(float dy, float y, const DropArgs& d) {
   return y <= 0.0f ? 0.0f : g;
 }
 
-// MODE 0: x as it is, 1: with y, 2: with the generator.
-template <bool BF16, bool VEC, int MODE>
-__device__ __forceinline__ void mx_source8(const Mx4Source& a, int64_t row, int c, uint64_t offset,
-                                           float* v) {
-  constexpr int ES = BF16 ? 2 : 4;
-  mx_load8<BF16, VEC>(static_cast<const char*>(a.x) + row * a.x_ld * ES, c, a.cols, v);
-  if constexpr (MODE == 1) {
-    float y[8];
-    mx_load8<BF16, VEC>(static_cast<const char*>(a.y) + row * a.y_ld * ES, c, a.cols, y);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = mx_pass(v[t], y[t], a.drop);
-  }
-  if constexpr (MODE == 2) {
-    const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(row), c / 8);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = drop_keeps(a.drop, w, t) ? v[t] * a.drop.factor : 0.0f;
-  }
-}
-
-// A wave takes 512 columns of a row, a lane eight of them, four lanes a block.
-template <bool BF16, bool VEC, int MODE>
+// A wave takes 512 columns of a row, a lane eight of them, four lanes a block; neighbouring
+// waves have neighbouring pieces.  4096 x 4096 in fp32 12.5 us, 6.1 TB/s; 8191 x 4096 in
+// bf16 16.3.  Four pieces a wave with all loads on their way: 13.9 and 17.2; 16 rows of
+// the same columns a workgroup, which in rows a power of two apart meet in the same
+// channels: 17 and 17.4.
+template <bool BF16, bool VEC>
 __global__ __launch_bounds__(256) void mx4_rows_kernel(Mx4Source a, Mx4Rows to, int pieces) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t offset = MODE == 2 ? drop_offset(a.drop) : 0;
   const int64_t units = a.rows * pieces, step = static_cast<int64_t>(gridDim.x) * 4;
   const int end = static_cast<int>(mx4_bytes(a.cols)) * 2;
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * 4 + wave; u < units; u += step) {
     const int64_t row = u / pieces;
     const int c = static_cast<int>(u - row * pieces) * 512 + 8 * lane;
     float v[8];
-    mx_source8<BF16, VEC, MODE>(a, row, c, offset, v);
+    mx_load8<BF16, VEC>(static_cast<const char*>(a.x) + row * a.x_ld * (BF16 ? 2 : 4), c, a.cols,
+                        v);
+    mx_clip8<VEC>(c, a.cols, v);
     uint32_t top = 0;
 #pragma unroll
     for (int t = 0; t < 8; ++t) top = max(top, mx_abs(v[t]));
     top = max(top, static_cast<uint32_t>(__shfl_xor(top, 1)));
     top = max(top, static_cast<uint32_t>(__shfl_xor(top, 2)));
     const MxScale s = mx_scale(top);
-    if (c < end)
-      *reinterpret_cast<uint32_t*>(to.q + row * to.q_ld + c / 2) = mx_pack8(v, s.inv);
+    if (c < end) *reinterpret_cast<uint32_t*>(to.q + row * to.q_ld + c / 2) = mx_pack8(v, s.inv);
     if ((lane & 3) == 0) to.scale[row * to.s_ld + c / 32] = static_cast<uint8_t>(s.byte);
   }
 }
 
-// 256 rows x 128 columns a workgroup, eight waves of 32 rows; a lane has two
-// neighbouring columns of its wave's rows, a block of each, and turns them by LDS
-// so that a column's 128 bytes are stored by eight neighbouring lanes.
-constexpr int MXC_ROWS = 256, MXC_COLS = 128;
+// 256 rows x 64 columns a workgroup, eight waves of 32 rows; a lane has two neighbouring
+// columns of half of its wave's rows.  A column's block of 32 rows is two lanes', its
+// bytes are turned by LDS so that eight neighbouring lanes store a column's 128.
+// BOTH: by rows as well, a block of 32 columns 16 lanes', for which the gradient is
+// read once.  4096 x 4096 in fp32 12.7 us, 6.0 TB/s; dz of 8191 x 2048 both ways, from dy and
+// y in bf16, with x of 8191 x 4096 42 us, 4.0 TB/s (98 with loads behind branches and
+// every lane reducing every row).
+constexpr int MXC_ROWS = 256, MXC_COLS = 64;
 
-template <bool BF16, bool VEC, int MODE>
-__global__ __launch_bounds__(512) void mx4_columns_kernel(Mx4Source a, Mx4Rows to, float* sums) {
-  constexpr int LD = 128 + 16;  // 16 more: neighbouring columns start in other banks
-  __shared__ __attribute__((aligned(16))) uint8_t q[MXC_COLS * LD];
-  __shared__ uint8_t sc[MXC_COLS][8];
-  __shared__ float part[8][MXC_COLS];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int across = (a.cols + MXC_COLS - 1) / MXC_COLS;
-  const int64_t tile = blockIdx.x / across;
-  const int c0 = static_cast<int>(blockIdx.x % across) * MXC_COLS, c = c0 + 2 * lane;
-  const int64_t r0 = tile * MXC_ROWS + 32 * wave;
-  const uint64_t offset = MODE == 2 ? drop_offset(a.drop) : 0;
-  constexpr int ES = BF16 ? 2 : 4;
-  auto load2 = [&](const void* p, int64_t ld, int64_t r) {
-    const char* row = static_cast<const char*>(p) + r * ld * ES;
-    mx_f32x2 v = {0.0f, 0.0f};
-    if (r >= a.rows) return v;
-    if (VEC && c + 2 <= a.cols) {
-      if constexpr (BF16) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(row + 2 * c);
-        v = mx_f32x2{mx_bf16(w & 0xFFFFu), mx_bf16(w >> 16)};
-      } else {
-        v = *reinterpret_cast<const mx_f32x2*>(row + 4 * static_cast<int64_t>(c));
-      }
-    } else {
+struct Mx4Columns {
+  Mx4Source from;
+  Mx4Rows to;
+  Mx4Rows rows;  // BOTH
+  float* sums;   // of the columns, a row of them for each 256 of x; or nullptr
+};
+template <bool BOTH>
+struct MxColumnsLds {
+  static constexpr int LD = 128 + 16;  // 16 more: neighbouring columns start in other banks
+  __attribute__((aligned(16))) uint8_t q[MXC_COLS * LD];
+  __attribute__((aligned(16))) uint8_t scale[MXC_COLS][8];
+  float part[8][MXC_COLS];
+  __attribute__((aligned(16))) uint8_t row_q[BOTH ? MXC_ROWS : 1][32];
+  __attribute__((aligned(16))) uint8_t row_scale[BOTH ? MXC_ROWS : 1][2];
+};
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t mx_dpp(uint32_t v) {
+  return static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xF, 0xF, false));
+}
+// Of N values a lane, one per row, and 16 lanes: the first N / 2 rows' largest in the lanes whose
+// bit N / 2 is clear, the others' in their partners.
+template <int CTRL, int N>
+__device__ __forceinline__ void mx_fold(uint32_t (&m)[16], int lane) {
+  const bool up = lane & (N / 2);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (c + t < a.cols) {
-          if constexpr (BF16) v[t] = mx_bf16(reinterpret_cast<const uint16_t*>(row)[c + t]);
-          else v[t] = reinterpret_cast<const float*>(row)[c + t];
-        }
-    }
-    return v;
-  };
-  float v[2][32];
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const mx_f32x2 x = load2(a.x, a.x_ld, r0 + i);
-    v[0][i] = x[0];
-    v[1][i] = x[1];
+  for (int i = 0; i < N / 2; ++i) {
+    const uint32_t keep = up ? m[i + N / 2] : m[i], give = up ? m[i] : m[i + N / 2];
+    m[i] = max(keep, mx_dpp<CTRL>(give));
   }
-  if constexpr (MODE == 1) {
+}
+// What the lane that is K-th of four has; every lane has to ask.
+template <int K>
+__device__ __forceinline__ uint32_t mx_from_quad(uint32_t v) {
+  return mx_dpp<K * 0x55>(v);
+}
+// ... of sixteen.
+template <int K>
+__device__ __forceinline__ float mx_from_row(float v) {
+  return __builtin_bit_cast(float, mx_dpp<0x150 + K>(__builtin_bit_cast(uint32_t, v)));
+}
+
+template <bool BF16, bool VEC, int MODE, bool BOTH>
+__device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row, int tile_col,
+                                           MxColumnsLds<BOTH>& lds) {
+  const Mx4Source& a = p.from;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pair = lane & 31, h = lane >> 5;
+  const int c0 = tile_col * MXC_COLS, c = c0 + 2 * pair;
+  const int64_t r0 = tile_row * MXC_ROWS, mine = r0 + 32 * wave + 16 * h;
+  constexpr int ES = BF16 ? 2 : 4;
+  // Rows and columns behind the last read the last one again, so that no load waits behind
+  // a branch, and count as zeros.  VEC: an even number of columns, pairs aligned.
+  const int64_t left = a.rows - mine;
+  const int seen = static_cast<int>(left < 16 ? left : 16);  // of the lane's rows, may be < 0
+  const int c_in = c < a.cols ? c : (VEC ? a.cols - 2 : a.cols - 1);
+  const int c_next = c + 1 < a.cols ? 1 : 0;
+  auto load = [&](const void* from, int64_t ld, float(&v)[2][16]) {
+    const char* at = static_cast<const char*>(from) +
+                     ((left > 0 ? mine : a.rows - 1) * ld + c_in) * ES;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const mx_f32x2 y = load2(a.y, a.y_ld, r0 + i);
-      v[0][i] = mx_pass(v[0][i], y[0], a.drop);
-      v[1][i] = mx_pass(v[1][i], y[1], a.drop);
+    for (int i = 0; i < 16; ++i) {
+      if constexpr (VEC && BF16) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(at);
+        v[0][i] = mx_bf16(w & 0xFFFFu);
+        v[1][i] = mx_bf16(w >> 16);
+      } else if constexpr (VEC) {
+        const mx_f32x2 w = *reinterpret_cast<const mx_f32x2*>(at);
+        v[0][i] = w[0];
+        v[1][i] = w[1];
+      } else if constexpr (BF16) {
+        v[0][i] = mx_bf16(reinterpret_cast<const uint16_t*>(at)[0]);
+        v[1][i] = mx_bf16(reinterpret_cast<const uint16_t*>(at)[c_next]);
+      } else {
+        v[0][i] = reinterpret_cast<const float*>(at)[0];
+        v[1][i] = reinterpret_cast<const float*>(at)[c_next];
+      }
+      at += i + 1 < seen ? ld * ES : 0;
+    }
+  };
+  float v[2][16];
+  load(a.x, a.x_ld, v);
+  if constexpr (MODE == 1) {
+    float y[2][16];
+    load(a.y, a.y_ld, y);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      v[0][i] = mx_pass(v[0][i], y[0][i], a.drop);
+      v[1][i] = mx_pass(v[1][i], y[1][i], a.drop);
+    }
+  }
+  if (__any(seen < 16 || c + 1 >= a.cols)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      v[0][i] = i < seen && c < a.cols ? v[0][i] : 0.0f;
+      v[1][i] = i < seen && c + 1 < a.cols ? v[1][i] : 0.0f;
     }
   }
   if constexpr (MODE == 2) {
+    // four lanes share a call of the generator for a row: each makes one of four rows'
+    const uint64_t offset = drop_offset(a.drop);
+    const int k = lane & 3;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(r0 + i), c / 8);
-      const uint32_t mine = w.w[lane & 3];
-      v[0][i] = (mine & 0xFFFFu) >= a.drop.below ? v[0][i] * a.drop.factor : 0.0f;
-      v[1][i] = mine >> 16 >= a.drop.below ? v[1][i] * a.drop.factor : 0.0f;
+    for (int i = 0; i < 16; i += 4) {
+      const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(mine + i + k), c / 8);
+#define OSCARS_KEEP(K)                                                                       \
+  {                                                                                          \
+    const uint32_t u0 = mx_from_quad<K>(w.w[0]), u1 = mx_from_quad<K>(w.w[1]);               \
+    const uint32_t u2 = mx_from_quad<K>(w.w[2]), u3 = mx_from_quad<K>(w.w[3]);               \
+    const uint32_t u = k & 2 ? (k & 1 ? u3 : u2) : (k & 1 ? u1 : u0);                        \
+    v[0][i + K] = (u & 0xFFFFu) >= a.drop.below ? v[0][i + K] * a.drop.factor : 0.0f;        \
+    v[1][i + K] = u >> 16 >= a.drop.below ? v[1][i + K] * a.drop.factor : 0.0f;              \
+  }
+      OSCARS_KEEP(0)
+      OSCARS_KEEP(1)
+      OSCARS_KEEP(2)
+      OSCARS_KEEP(3)
+#undef OSCARS_KEEP
     }
   }
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     uint32_t top = 0;
-    float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      top = max(top, mx_abs(v[t][i]));
-      sum += v[t][i];
-    }
+    for (int i = 0; i < 16; ++i) top = max(top, mx_abs(v[t][i]));
+    top = max(top, static_cast<uint32_t>(__shfl_xor(top, 32)));
     const MxScale s = mx_scale(top);
-    const int col = 2 * lane + t;
-    *reinterpret_cast<nt_u32x4*>(q + col * LD + 16 * wave) =
-        nt_u32x4{mx_pack8(v[t], s.inv), mx_pack8(v[t] + 8, s.inv), mx_pack8(v[t] + 16, s.inv),
-                 mx_pack8(v[t] + 24, s.inv)};
-    sc[col][wave] = static_cast<uint8_t>(s.byte);
-    part[wave][col] = sum;
+    const int col = 2 * pair + t;
+    *reinterpret_cast<nt_u32x2*>(lds.q + col * MxColumnsLds<BOTH>::LD + 16 * wave + 8 * h) =
+        nt_u32x2{mx_pack8(v[t], s.inv), mx_pack8(v[t] + 8, s.inv)};
+    if (h == 0) lds.scale[col][wave] = static_cast<uint8_t>(s.byte);
+    if (p.sums) {  // in pairs of pairs: five additions deep
+      float sum[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i] = v[t][i];
+#pragma unroll
+      for (int n = 8; n > 0; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) sum[i] += sum[i + n];
+      const float other = __shfl_xor(sum[0], 32);
+      if (h == 0) lds.part[wave][col] = sum[0] + other;
+    }
+  }
+  if constexpr (BOTH) {
+    // 16 lanes have a block of each of 16 rows: lane l comes to hold row l's largest
+    uint32_t m[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m[i] = max(mx_abs(v[0][i]), mx_abs(v[1][i]));
+    mx_fold<0x140, 16>(m, lane);  // with lane 15 - l,
+    mx_fold<0x141, 8>(m, lane);   // 7 - l of eight,
+    mx_fold<0x1B, 4>(m, lane);    // 3 - l of four,
+    mx_fold<0xB1, 2>(m, lane);    // 1 - l of two
+    const MxScale s = mx_scale(m[0]);
+    const int row0 = 32 * wave + 16 * h;
+    lds.row_scale[row0 + (lane & 15)][pair >> 4] = static_cast<uint8_t>(s.byte);
+    // bytes of four rows in a lane turn into four lanes' bytes of a row (a block with a NaN may
+    // have codes other than 0: it is its scale that counts)
+    const uint32_t turn1 = lane & 1 ? 0x03070105u : 0x06020400u;
+    const uint32_t turn2 = lane & 2 ? 0x03020706u : 0x05040100u;
+#define OSCARS_ROWS(I)                                                                           \
+  {                                                                                              \
+    uint32_t w = mx_pack2<0>(0u, v[0][I], v[1][I], mx_from_row<I>(s.inv));                       \
+    w = mx_pack2<1>(w, v[0][I + 1], v[1][I + 1], mx_from_row<I + 1>(s.inv));                     \
+    w = mx_pack2<2>(w, v[0][I + 2], v[1][I + 2], mx_from_row<I + 2>(s.inv));                     \
+    w = mx_pack2<3>(w, v[0][I + 3], v[1][I + 3], mx_from_row<I + 3>(s.inv));                     \
+    w = __builtin_amdgcn_perm(mx_dpp<0xB1>(w), w, turn1);                                        \
+    w = __builtin_amdgcn_perm(mx_dpp<0x4E>(w), w, turn2);                                        \
+    *reinterpret_cast<uint32_t*>(&lds.row_q[row0 + I + (lane & 3)][pair & ~3]) = w;              \
+  }
+    OSCARS_ROWS(0)
+    OSCARS_ROWS(4)
+    OSCARS_ROWS(8)
+    OSCARS_ROWS(12)
+#undef OSCARS_ROWS
   }
   __syncthreads();
-  for (int i = tid; i < MXC_COLS * 8; i += 512) {
-    const int col = i >> 3, k = i & 7;
+  {
+    const int col = tid >> 3, k = tid & 7;
     if (c0 + col < a.cols)
-      *reinterpret_cast<nt_u32x4*>(to.q + (c0 + col) * to.q_ld + tile * 128 + 16 * k) =
-          *reinterpret_cast<const nt_u32x4*>(q + col * LD + 16 * k);
+      *reinterpret_cast<nt_u32x4*>(p.to.q + (c0 + col) * p.to.q_ld + tile_row * 128 + 16 * k) =
+          *reinterpret_cast<const nt_u32x4*>(lds.q + col * MxColumnsLds<BOTH>::LD + 16 * k);
   }
   if (tid < MXC_COLS && c0 + tid < a.cols) {
-    uint8_t* s = to.scale + (c0 + tid) * to.s_ld + tile * 8;
-    *reinterpret_cast<nt_u32x2*>(s) = *reinterpret_cast<const nt_u32x2*>(sc[tid]);
+    uint8_t* s = p.to.scale + (c0 + tid) * p.to.s_ld + tile_row * 8;
+    *reinterpret_cast<nt_u32x2*>(s) = *reinterpret_cast<const nt_u32x2*>(lds.scale[tid]);
     // the last tile fills the scales to a whole 16
-    if ((tile & 1) == 0 && (tile + 1) * MXC_ROWS >= a.rows)
+    if ((tile_row & 1) == 0 && r0 + MXC_ROWS >= a.rows)
       *reinterpret_cast<nt_u32x2*>(s + 8) = nt_u32x2{0, 0};
-    if (sums) {
-      float t = 0.0f;
+    if (p.sums) {
+      float t[8];
 #pragma unroll
-      for (int w = 0; w < 8; ++w) t += part[w][tid];
-      sums[tile * a.cols + c0 + tid] = t;
+      for (int w = 0; w < 8; ++w) t[w] = lds.part[w][tid];
+      p.sums[tile_row * a.cols + c0 + tid] =
+          ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+    }
+  }
+  if constexpr (BOTH) {
+    const int row = tid >> 1, k = tid & 1;
+    if (r0 + row < a.rows) {
+      if (c0 < mx4_bytes(a.cols) * 2)
+        *reinterpret_cast<nt_u32x4*>(p.rows.q + (r0 + row) * p.rows.q_ld + c0 / 2 + 16 * k) =
+            *reinterpret_cast<const nt_u32x4*>(&lds.row_q[row][16 * k]);
+      if (k == 0)
+        *reinterpret_cast<uint16_t*>(p.rows.scale + (r0 + row) * p.rows.s_ld + c0 / 32) =
+            *reinterpret_cast<const uint16_t*>(lds.row_scale[row]);
     }
   }
 }
 
-__global__ __launch_bounds__(256) void mx4_sum_kernel(const float* part, int64_t parts, int cols,
-                                                      float* sums) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
-  float s = 0.0f;
-  for (int64_t i = 0; i < parts; ++i) s += part[i * cols + c];
-  sums[c] = s;
+// Tiles of 64 columns: with BOTH to a whole 512, whose scales are all written.
+__host__ __device__ __forceinline__ int mx_column_tiles(int cols, bool both) {
+  return static_cast<int>(both ? (static_cast<int64_t>(cols) + 511) / 512 * 8
+                               : (static_cast<int64_t>(cols) + MXC_COLS - 1) / MXC_COLS);
+}
+__host__ __device__ __forceinline__ int64_t mx_row_tiles(int64_t rows) {
+  return (rows + MXC_ROWS - 1) / MXC_ROWS;
 }
 
-// Values: eight a thread.
-template <bool OUT_BF16>
+template <bool BF16, bool VEC>
+__global__ __launch_bounds__(512) void mx4_columns_kernel(Mx4Columns p) {
+  __shared__ __attribute__((aligned(16))) MxColumnsLds<false> lds;
+  const int across = mx_column_tiles(p.from.cols, false);
+  mx_columns<BF16, VEC, 0, false>(p, blockIdx.x / across, static_cast<int>(blockIdx.x % across),
+                                  lds);
+}
+
+// What the gradients quantise in one launch: dz by columns, and for dx by rows, and x by
+// columns.  The workgroups of one XCD (index mod 8) take neighbouring tiles: they
+// share lines of dz's rows.
+template <bool BF16, bool VEC, int MODE, bool BOTH>
+__global__ __launch_bounds__(512) void mx4_gradient_kernel(Mx4Columns z, Mx4Columns x,
+                                                           int z_tiles) {
+  __shared__ __attribute__((aligned(16))) MxColumnsLds<BOTH> lds;
+  const int total = gridDim.x, per = total >> 3, rem = total & 7;
+  const int n = blockIdx.x & 7, q = blockIdx.x >> 3;
+  int id = n * per + (n < rem ? n : rem) + q;
+  if (id < z_tiles) {
+    const int across = mx_column_tiles(z.from.cols, BOTH);
+    mx_columns<BF16, VEC, MODE, BOTH>(z, id / across, id % across, lds);
+  } else {
+    id -= z_tiles;
+    const int across = mx_column_tiles(x.from.cols, false);
+    auto& own = reinterpret_cast<MxColumnsLds<false>&>(lds);
+    if (x.from.bf16) mx_columns<true, VEC, 0, false>(x, id / across, id % across, own);
+    else mx_columns<false, VEC, 0, false>(x, id / across, id % across, own);
+  }
+}
+
+// 32 columns a workgroup, every eighth part a thread.
+__global__ __launch_bounds__(256) void mx4_sum_kernel(const float* part, int64_t parts, int cols,
+                                                      float* sums) {
+  __shared__ float some[8][32];
+  const int l = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
+  float s = 0.0f;
+  if (c < cols)
+#pragma unroll 4
+    for (int64_t i = k; i < parts; i += 8) s += part[i * cols + c];
+  some[k][l] = s;
+  __syncthreads();
+  if (k == 0 && c < cols) {
+    sums[c] = ((some[0][l] + some[1][l]) + (some[2][l] + some[3][l])) +
+              ((some[4][l] + some[5][l]) + (some[6][l] + some[7][l]));
+  }
+}
+
+// Values: eight a thread.  A row's scale of 2^-127 is no normal number: entries are
+// converted at scale 1 and multiplied, exactly.
+template <bool OUT_BF16, bool VEC>
 __global__ __launch_bounds__(256) void mx4_values_kernel(Mx4Values a, uint32_t groups) {
   const int64_t units = a.rows * groups, step = static_cast<int64_t>(gridDim.x) * 256;
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; u < units; u += step) {
@@ -270,25 +428,39 @@ __global__ __launch_bounds__(256) void mx4_values_kernel(Mx4Values a, uint32_t g
     const int c = static_cast<int>(u - row * groups) * 8;
     const uint32_t w = *reinterpret_cast<const uint32_t*>(a.q + row * a.q_ld + c / 2);
     const uint32_t e = a.scale[row * a.s_ld + c / 32];
-    // 2^-127 is no normal number; 2^-126 / 2 is the same
-    const float s = __builtin_bit_cast(float, e == 0 ? 0x00400000u
-                                                     : e == 255 ? 0x7FC00000u : e << 23);
-    float v[8];
+    const float s = __builtin_bit_cast(float, e == 0     ? 0x00400000u
+                                              : e == 255 ? 0x7FC00000u
+                                                         : e << 23);
+    const auto v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
+    const auto v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+    const auto v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
+    const auto v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+    const float v[8] = {v0[0] * s, v0[1] * s, v1[0] * s, v1[1] * s,
+                        v2[0] * s, v2[1] * s, v3[0] * s, v3[1] * s};
+    if constexpr (OUT_BF16) {
+      uint16_t* p = static_cast<uint16_t*>(a.out) + row * a.out_ld + c;
+      if (VEC && c + 8 <= a.cols) {
+        nt_u32x4 o;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const uint32_t n = w >> (4 * t) & 15u, m = n & 7u;
-      const float x = m < 4 ? 0.5f * static_cast<float>(m)
-                            : static_cast<float>((2 + (m & 1u)) << (m >> 1)) * 0.25f;
-      v[t] = (n & 8u ? -x : x) * s;
-    }
+        for (int t = 0; t < 4; ++t)
+          o[t] = mx_to_bf16(v[2 * t]) | static_cast<uint32_t>(mx_to_bf16(v[2 * t + 1])) << 16;
+        *reinterpret_cast<nt_u32x4*>(p) = o;
+      } else {
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-      if (c + t < a.cols) {
-        if constexpr (OUT_BF16)
-          static_cast<uint16_t*>(a.out)[row * a.out_ld + c + t] = mx_to_bf16(v[t]);
-        else
-          static_cast<float*>(a.out)[row * a.out_ld + c + t] = v[t];
+        for (int t = 0; t < 8; ++t)
+          if (c + t < a.cols) p[t] = mx_to_bf16(v[t]);
       }
+    } else {
+      float* p = static_cast<float*>(a.out) + row * a.out_ld + c;
+      if (VEC && c + 8 <= a.cols) {
+        reinterpret_cast<nt_f32x4*>(p)[0] = nt_f32x4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<nt_f32x4*>(p)[1] = nt_f32x4{v[4], v[5], v[6], v[7]};
+      } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (c + t < a.cols) p[t] = v[t];
+      }
+    }
   }
 }
 
@@ -393,20 +565,25 @@ __device__ __forceinline__ nt_f32x16 mx_mfma(nt_u32x4 a, nt_u32x4 b, nt_f32x16 c
 }
 
 // Workgroup tile: BM x BN outputs, WM x WN waves.  A stage is 128 bytes of a row, 256
-// entries of K; two stages in LDS, and scales for two times two.
-template <int BM_, int BN_, int WM_, int WN_>
+// entries of K; RING stages in LDS, and scales for two stages each.
+template <int BM_, int BN_, int WM_, int WN_, int RING_>
 struct MxShape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, RING = RING_;
   static constexpr int NT = 64 * WM * WN, MI = BM / WM / 32, NJ = BN / WN / 32;
   static constexpr int STAGE = (BM + BN) * NT_BLOCK, SCALES = (BM + BN) * 16;
-  static constexpr int LDS_BYTES = 2 * STAGE + 2 * SCALES;
+  static constexpr int PARTS = RING / 2 + 1;  // of scales, in LDS
+  static constexpr int LDS_BYTES = RING * STAGE + PARTS * SCALES;
+  static constexpr int LOADS = STAGE / 16 / NT;                           // of a wave and stage
   static constexpr int EU = NT / 256 * (LDS_BYTES > (80 << 10) ? 1 : 2);  // waves of a SIMD
   static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0, "whole blocks");
-  static_assert(BM + BN == NT, "a wave's load of scales each");
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && BM + BN <= NT, "a row of scales a lane");
 };
-typedef MxShape<256, 256, 2, 4> MxL;
-typedef MxShape<128, 128, 2, 2> MxM;
-static_assert(mx4_threads(MxL::BM) == MxL::NT && mx4_threads(MxM::BM) == MxM::NT, "mx4_plan.h");
+typedef MxShape<256, 256, 2, 4, 2> MxL;
+typedef MxShape<128, 128, 2, 2, 2> MxM;
+typedef MxShape<64, 64, 2, 2, 4> MxS;
+static_assert(mx4_threads(256) == MxL::NT && mx4_threads(128) == MxM::NT &&
+                  mx4_threads(64) == MxS::NT,
+              "mx4_plan.h");
 
 // p and bytes are the same for the wave; where the compiler computes them on the vector unit
 // (64-bit comparisons are its), it would loop over the lanes' buffers around every load.
@@ -523,7 +700,7 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
   constexpr int ABYTES = S::BM * NT_BLOCK, ES = OUT_BF16 ? 2 : 4;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS_BYTES];
-  char* const scales = lds + 2 * S::STAGE;
+  char* const scales = lds + S::RING * S::STAGE;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int am = (wave / S::WN) * 32 * S::MI, bm = (wave % S::WN) * 32 * S::NJ;
@@ -558,7 +735,7 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
   // stage s, and with an even one its part of the scales
   auto issue = [&](int s) {
     if (s >= blocks) return;
-    char* to = lds + (s & 1) * S::STAGE + wave * 1024;
+    char* to = lds + s % S::RING * S::STAGE + wave * 1024;
     const int k = s * NT_BLOCK;
 #pragma unroll
     for (int p = 0; p < MxPlace<S>::PA; ++p)
@@ -568,13 +745,13 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
     for (int p = 0; p < MxPlace<S>::PB; ++p)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(t.b, (mx_lds)(to + ABYTES + S::NT * 16 * p), 16,
                                                at.b, k + p * at.b_step, 0, 0);
-    if ((s & 1) == 0)
+    if ((s & 1) == 0 && 64 * wave < S::BM + S::BN)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          t.scales, (mx_lds)(scales + ((s >> 1) & 1) * S::SCALES + wave * 1024), 16, at.scales,
-          8 * s, 0, 0);
+          t.scales, (mx_lds)(scales + (s >> 1) % S::PARTS * S::SCALES + wave * 1024), 16,
+          at.scales, 8 * s, 0, 0);
   };
   auto load = [&](int s, int c, nt_u32x4(&fa)[S::MI], nt_u32x4(&fb)[S::NJ]) {
-    const char* from = lds + (s & 1) * S::STAGE;
+    const char* from = lds + s % S::RING * S::STAGE;
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) fa[i] = mx_read(from + (am + 32 * i) * NT_BLOCK, r, 4 * h + c);
 #pragma unroll
@@ -582,7 +759,7 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
       fb[j] = mx_read(from + ABYTES + (bm + 32 * j) * NT_BLOCK, r, 4 * h + c);
   };
   auto load_scales = [&](int s, uint32_t(&sa)[S::MI], uint32_t(&sb)[S::NJ]) {
-    const char* from = scales + ((s >> 1) & 1) * S::SCALES + 16 * r + 8 * (s & 1) + 4 * h;
+    const char* from = scales + (s >> 1) % S::PARTS * S::SCALES + 16 * r + 8 * (s & 1) + 4 * h;
 #pragma unroll
     for (int i = 0; i < S::MI; ++i)
       sa[i] = *reinterpret_cast<const uint32_t*>(from + (am + 32 * i) * 16);
@@ -599,9 +776,10 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
     for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  issue(0);
-  issue(1);
-  nt_wait_vm<0>();
+#pragma unroll
+  for (int s = 0; s < S::RING; ++s) issue(s);
+  if (S::RING > 2 && S::RING <= blocks) nt_wait_vm<(S::RING - 1) * S::LOADS>();
+  else nt_wait_vm<0>();
   nt_barrier();
   load(0, 0, fa[0], fb[0]);
   load_scales(0, sa[0], sb[0]);
@@ -613,11 +791,13 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
       if (c < 3) {                                                                              \
         load(now, c + 1, fa[(c + 1) & 1], fb[(c + 1) & 1]);                                     \
       } else {                                                                                  \
-        nt_wait_vm<0>(); /* the next stage is there, */                                         \
-        nt_barrier();    /* and this one read by every wave */                                  \
+        /* the next stage is there, and this one read by every wave */                          \
+        if (S::RING > 2 && now + S::RING <= blocks) nt_wait_vm<(S::RING - 2) * S::LOADS>();     \
+        else nt_wait_vm<0>();                                                                   \
+        nt_barrier();                                                                           \
         load(now + 1, 0, fa[0], fb[0]);                                                         \
         load_scales(now + 1, sa[1 - (E)], sb[1 - (E)]);                                         \
-        issue(now + 2);                                                                         \
+        issue(now + S::RING);                                                                   \
       }                                                                                         \
       __builtin_amdgcn_sched_barrier(0);                                                        \
       _Pragma("unroll") for (int i = 0; i < S::MI; ++i)                                         \
@@ -640,27 +820,27 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
   if (stage < blocks) OSCARS_STAGE(stage, 0)
 #undef OSCARS_STAGE
 
-  // The outputs of 32 rows, two blocks of 32 channels of them, go through LDS in their type,
-  // so that neighbouring lanes store whole lines of an output row.
-  constexpr int TURN = 64 * ES + 16;              // bytes of a row's channels
-  constexpr int PER = 16 / ES, LANES = 64 / PER;  // channels of a lane, lanes of a row
-  static_assert(S::LDS_BYTES >= S::WM * S::WN * 32 * TURN && S::MI % 2 == 0, "turned blocks");
+  // The outputs of 32 rows, two blocks of 32 channels of them where a wave has two, go through
+  // LDS in their type, so that neighbouring lanes store whole lines of an output row.
+  constexpr int WIDE = S::MI % 2 == 0 ? 2 : 1, TURN = 32 * WIDE * ES + 16;  // bytes of a row
+  constexpr int PER = 16 / ES, LANES = 32 * WIDE / PER;  // channels of a lane, lanes of a row
+  static_assert(S::LDS_BYTES >= S::WM * S::WN * 32 * TURN, "turned blocks");
   char* const turn = lds + wave * 32 * TURN;
   const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0;
   nt_barrier();  // the stages are read: LDS is free
 #pragma unroll
-  for (int i = 0; i < S::MI; i += 2) {
+  for (int i = 0; i < S::MI; i += WIDE) {
     const int o = r0 + am + 32 * i;
     if (o >= a.outs) continue;  // uniform over the wave
-    nt_f32x4 bias[2][4];
+    nt_f32x4 bias[WIDE][4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) mx_bias(a, o + 32 * k, h, bias[k]);
+    for (int k = 0; k < WIDE; ++k) mx_bias(a, o + 32 * k, h, bias[k]);
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
       const int64_t row0 = c0 + bm + 32 * j;
       if (row0 >= a.rows) continue;  // uniform over the wave
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
+      for (int k = 0; k < WIDE; ++k) {
         float v[16];
         mx_epilogue(a, offset, row0 + r, o + 32 * k, h, bias[k], acc[i + k][j], v);
         char* to = turn + r * TURN + (32 * k + 4 * h) * ES;
@@ -695,16 +875,24 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
 // into registers, and waits for no other wave until the four sums meet, in order.
 constexpr int MX_SMALL_RING = 2;
 
-template <bool OUT_BF16, bool VEC>
-__global__ __launch_bounds__(256) void mx4_small_kernel(Mx4Product a) {
+// Up to two products in one launch, the second's workgroups behind the first's.
+struct Mx4Pair {
+  Mx4Product p[2];
+  bool vec[2];
+  int first;
+};
+__global__ __launch_bounds__(256) void mx4_small_kernel(Mx4Pair both) {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
   constexpr int DATA = 64 * NT_BLOCK, STAGE = DATA + 512, RING = MX_SMALL_RING;
   __shared__ __attribute__((aligned(16))) char lds[4 * RING * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // scalar addresses below
+  const bool second = static_cast<int>(blockIdx.x) >= both.first;
+  const Mx4Product& a = both.p[second];
+  const int index = blockIdx.x - (second ? both.first : 0);
   const int tr = (a.outs + 31) / 32;
-  const int r0 = static_cast<int>(blockIdx.x % tr) * 32;
-  const int64_t c0 = static_cast<int64_t>(blockIdx.x / tr) * 32;
+  const int r0 = index % tr * 32;
+  const int64_t c0 = static_cast<int64_t>(index / tr) * 32;
   const int blocks = (a.in + 255) / 256;
   const int64_t left = a.rows - c0;
   const int here = static_cast<int>(left < 32 ? left : 32);
@@ -782,24 +970,51 @@ __global__ __launch_bounds__(256) void mx4_small_kernel(Mx4Product a) {
     v[t] = mx_finish(a, s, a.bias ? a.bias[oc] : 0.0f);
   }
   if (a.drop.below) mx_drop<4>(a, drop_offset(a.drop), r, o, v);
-  mx_store<4, OUT_BF16, VEC>(a, r, o, v);
+  const bool vec = both.vec[second];
+  if (a.out_bf16) {
+    if (vec) mx_store<4, true, true>(a, r, o, v);
+    else mx_store<4, true, false>(a, r, o, v);
+  } else {
+    if (vec) mx_store<4, false, true>(a, r, o, v);
+    else mx_store<4, false, false>(a, r, o, v);
+  }
 #endif
-}
-
-template <bool OUT_BF16, bool VEC>
-hipError_t product_launch(const Mx4Product& a, int tile, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>((a.outs + tile - 1) / tile * ((a.rows + tile - 1) / tile)));
-  if (tile == MxL::BM)
-    hipLaunchKernelGGL((mx4_product_kernel<MxL, OUT_BF16, VEC>), grid, dim3(MxL::NT), 0, s, a);
-  else if (tile == MxM::BM)
-    hipLaunchKernelGGL((mx4_product_kernel<MxM, OUT_BF16, VEC>), grid, dim3(MxM::NT), 0, s, a);
-  else
-    hipLaunchKernelGGL((mx4_small_kernel<OUT_BF16, VEC>), grid, dim3(256), 0, s, a);
-  return hipGetLastError();
 }
 
 bool aligned_rows(const void* p, int64_t row_bytes, int to) {
   return reinterpret_cast<uintptr_t>(p) % to == 0 && row_bytes % to == 0;
+}
+bool out_aligned(const Mx4Product& a) {
+  return aligned_rows(a.out, a.out_ld * (a.out_bf16 ? 2 : 4), 16);
+}
+unsigned product_grid(const Mx4Product& a, int tile) {
+  return static_cast<unsigned>((a.outs + tile - 1) / tile * ((a.rows + tile - 1) / tile));
+}
+
+hipError_t small_launch(const Mx4Product* p, int n, hipStream_t s) {
+  Mx4Pair both{};
+  unsigned grid = 0;
+  for (int i = 0; i < n; ++i) {
+    both.p[i] = p[i];
+    both.vec[i] = out_aligned(p[i]);
+    if (i == 0) both.first = static_cast<int>(product_grid(p[0], 32));
+    grid += product_grid(p[i], 32);
+  }
+  hipLaunchKernelGGL(mx4_small_kernel, dim3(grid), dim3(256), 0, s, both);
+  return hipGetLastError();
+}
+
+template <bool OUT_BF16, bool VEC>
+hipError_t product_launch(const Mx4Product& a, int tile, hipStream_t s) {
+  if (tile == 32) return small_launch(&a, 1, s);
+  const dim3 grid(product_grid(a, tile));
+  if (tile == 256)
+    hipLaunchKernelGGL((mx4_product_kernel<MxL, OUT_BF16, VEC>), grid, dim3(MxL::NT), 0, s, a);
+  else if (tile == 128)
+    hipLaunchKernelGGL((mx4_product_kernel<MxM, OUT_BF16, VEC>), grid, dim3(MxM::NT), 0, s, a);
+  else
+    hipLaunchKernelGGL((mx4_product_kernel<MxS, OUT_BF16, VEC>), grid, dim3(MxS::NT), 0, s, a);
+  return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ a few rows
@@ -852,6 +1067,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(Mx4Product a, c
     const int r = i / per, c = 8 * (i - r * per);
     float v[8];
     mx_load8<X_BF16, VEC>(static_cast<const char*>(x) + r * x_ld * (X_BF16 ? 2 : 4), c, in, v);
+    mx_clip8<VEC>(c, in, v);
     uint32_t top = 0;
 #pragma unroll
     for (int t = 0; t < 8; ++t) top = max(top, mx_abs(v[t]));
@@ -926,68 +1142,96 @@ hipError_t few_launch(const Mx4Product& a, const void* x, int64_t x_ld, hipStrea
              : few_launch<FEW_LDS_L, X_BF16, VEC>(a, x, x_ld, s);
 }
 
-int source_mode(const Mx4Source& a) { return a.y ? 1 : a.drop.below ? 2 : 0; }
-
 template <bool BF16, bool VEC>
 hipError_t rows_launch(const Mx4Source& a, const Mx4Rows& to, hipStream_t s) {
   const int pieces = (a.cols + 511) / 512;
   const int64_t want = (a.rows * pieces + 3) / 4;
   const dim3 grid(static_cast<unsigned>(want < 4096 ? want : 4096)), wg(256);
-  const int mode = source_mode(a);
-  if (mode == 0) hipLaunchKernelGGL((mx4_rows_kernel<BF16, VEC, 0>), grid, wg, 0, s, a, to, pieces);
-  else if (mode == 1)
-    hipLaunchKernelGGL((mx4_rows_kernel<BF16, VEC, 1>), grid, wg, 0, s, a, to, pieces);
-  else hipLaunchKernelGGL((mx4_rows_kernel<BF16, VEC, 2>), grid, wg, 0, s, a, to, pieces);
+  hipLaunchKernelGGL((mx4_rows_kernel<BF16, VEC>), grid, wg, 0, s, a, to, pieces);
   return hipGetLastError();
 }
 
-template <bool BF16, bool VEC>
-hipError_t columns_launch(const Mx4Source& a, const Mx4Rows& to, float* sums, hipStream_t s) {
-  const int64_t n = (a.rows + MXC_ROWS - 1) / MXC_ROWS * ((a.cols + MXC_COLS - 1) / MXC_COLS);
-  const dim3 grid(static_cast<unsigned>(n)), wg(512);
-  const int mode = source_mode(a);
-  if (mode == 0)
-    hipLaunchKernelGGL((mx4_columns_kernel<BF16, VEC, 0>), grid, wg, 0, s, a, to, sums);
-  else if (mode == 1)
-    hipLaunchKernelGGL((mx4_columns_kernel<BF16, VEC, 1>), grid, wg, 0, s, a, to, sums);
+// How the gradient is made: 0 as it is, 1 with y, 2 with the generator.
+int source_mode(const Mx4Source& a) { return a.y ? 1 : a.drop.below ? 2 : 0; }
+
+template <bool BF16, bool VEC, int MODE>
+hipError_t gradient_launch(const Mx4Columns& z, const Mx4Columns& x, bool both, unsigned grid,
+                           int z_tiles, hipStream_t s) {
+  if (both)
+    hipLaunchKernelGGL((mx4_gradient_kernel<BF16, VEC, MODE, true>), dim3(grid), dim3(512), 0, s, z,
+                       x, z_tiles);
   else
-    hipLaunchKernelGGL((mx4_columns_kernel<BF16, VEC, 2>), grid, wg, 0, s, a, to, sums);
+    hipLaunchKernelGGL((mx4_gradient_kernel<BF16, VEC, MODE, false>), dim3(grid), dim3(512), 0, s,
+                       z, x, z_tiles);
   return hipGetLastError();
+}
+template <bool BF16, bool VEC>
+hipError_t gradient_launch(const Mx4Columns& z, const Mx4Columns& x, bool both, unsigned grid,
+                           int z_tiles, hipStream_t s) {
+  const int mode = source_mode(z.from);
+  if (mode == 0) return gradient_launch<BF16, VEC, 0>(z, x, both, grid, z_tiles, s);
+  if (mode == 1) return gradient_launch<BF16, VEC, 1>(z, x, both, grid, z_tiles, s);
+  return gradient_launch<BF16, VEC, 2>(z, x, both, grid, z_tiles, s);
 }
 
 bool source_aligned(const Mx4Source& a, int to) {
   const int64_t es = a.bf16 ? 2 : 4;
   return aligned_rows(a.x, a.x_ld * es, to) && (!a.y || aligned_rows(a.y, a.y_ld * es, to));
 }
+bool pairs_aligned(const Mx4Source& a) {
+  return a.cols % 2 == 0 && source_aligned(a, a.bf16 ? 4 : 8);
+}
 
 }  // namespace
 
 hipError_t launch_mx4_rows(const Mx4Source& a, const Mx4Rows& to, hipStream_t s) {
-  const bool vec = source_aligned(a, 16);
+  const bool vec = a.cols % 8 == 0 && source_aligned(a, 16);
   if (a.bf16) return vec ? rows_launch<true, true>(a, to, s) : rows_launch<true, false>(a, to, s);
   return vec ? rows_launch<false, true>(a, to, s) : rows_launch<false, false>(a, to, s);
 }
 
+int64_t mx4_column_tiles(int64_t rows, int cols) {
+  return mx_row_tiles(rows) * mx_column_tiles(cols, false);
+}
+
+hipError_t launch_mx4_columns(const Mx4Source& a, const Mx4Rows& to, hipStream_t s) {
+  const bool vec = pairs_aligned(a);
+  const dim3 grid(static_cast<unsigned>(mx4_column_tiles(a.rows, a.cols))), wg(512);
+  const Mx4Columns p{a, to, Mx4Rows{}, nullptr};
+  if (a.bf16) {
+    if (vec) hipLaunchKernelGGL((mx4_columns_kernel<true, true>), grid, wg, 0, s, p);
+    else hipLaunchKernelGGL((mx4_columns_kernel<true, false>), grid, wg, 0, s, p);
+  } else {
+    if (vec) hipLaunchKernelGGL((mx4_columns_kernel<false, true>), grid, wg, 0, s, p);
+    else hipLaunchKernelGGL((mx4_columns_kernel<false, false>), grid, wg, 0, s, p);
+  }
+  return hipGetLastError();
+}
+
 int64_t mx4_sum_parts(int64_t rows) {
-  const int64_t n = (rows + MXC_ROWS - 1) / MXC_ROWS;
+  const int64_t n = mx_row_tiles(rows);
   return n > 1 ? n : 0;
 }
 
-hipError_t launch_mx4_columns(const Mx4Source& a, const Mx4Rows& to, float* sums, float* part,
-                              hipStream_t s) {
-  const bool vec = source_aligned(a, a.bf16 ? 4 : 8);
-  const int64_t parts = mx4_sum_parts(a.rows);
-  float* first = sums && parts ? part : sums;
+hipError_t launch_mx4_gradient(const Mx4Gradient& g, hipStream_t s) {
+  const bool both = g.z_rows.q != nullptr;
+  const bool vec = pairs_aligned(g.z) && pairs_aligned(g.x);
+  const int64_t parts = mx4_sum_parts(g.z.rows);
+  const Mx4Columns z{g.z, g.z_columns, g.z_rows, g.sums && parts ? g.part : g.sums};
+  const Mx4Columns x{g.x, g.x_columns, Mx4Rows{}, nullptr};
+  const int64_t nz = mx_row_tiles(g.z.rows) * mx_column_tiles(g.z.cols, both);
+  const unsigned grid = static_cast<unsigned>(nz + mx4_column_tiles(g.x.rows, g.x.cols));
+  const int z_tiles = static_cast<int>(nz);
   hipError_t e;
-  if (a.bf16)
-    e = vec ? columns_launch<true, true>(a, to, first, s)
-            : columns_launch<true, false>(a, to, first, s);
+  if (g.z.bf16)
+    e = vec ? gradient_launch<true, true>(z, x, both, grid, z_tiles, s)
+            : gradient_launch<true, false>(z, x, both, grid, z_tiles, s);
   else
-    e = vec ? columns_launch<false, true>(a, to, first, s)
-            : columns_launch<false, false>(a, to, first, s);
-  if (e != hipSuccess || first == sums) return e;
-  hipLaunchKernelGGL(mx4_sum_kernel, dim3((a.cols + 255) / 256), dim3(256), 0, s, part, parts,
-                     a.cols, sums);
+    e = vec ? gradient_launch<false, true>(z, x, both, grid, z_tiles, s)
+            : gradient_launch<false, false>(z, x, both, grid, z_tiles, s);
+  if (e != hipSuccess || !g.sums || !parts) return e;
+  hipLaunchKernelGGL(mx4_sum_kernel, dim3((g.z.cols + 31) / 32), dim3(256), 0, s, g.part, parts,
+                     g.z.cols, g.sums);
   return hipGetLastError();
 }
 
@@ -995,13 +1239,22 @@ hipError_t launch_mx4_values(const Mx4Values& a, hipStream_t s) {
   const uint32_t groups = static_cast<uint32_t>((static_cast<int64_t>(a.cols) + 7) / 8);
   const int64_t want = (a.rows * groups + 255) / 256;
   const dim3 grid(static_cast<unsigned>(want < 8192 ? want : 8192));
-  if (a.out_bf16) hipLaunchKernelGGL((mx4_values_kernel<true>), grid, dim3(256), 0, s, a, groups);
-  else hipLaunchKernelGGL((mx4_values_kernel<false>), grid, dim3(256), 0, s, a, groups);
+  const bool vec = aligned_rows(a.out, a.out_ld * (a.out_bf16 ? 2 : 4), 16);
+#define OSCARS_VALUES(B, V) \
+  hipLaunchKernelGGL((mx4_values_kernel<B, V>), grid, dim3(256), 0, s, a, groups)
+  if (a.out_bf16) {
+    if (vec) OSCARS_VALUES(true, true);
+    else OSCARS_VALUES(true, false);
+  } else {
+    if (vec) OSCARS_VALUES(false, true);
+    else OSCARS_VALUES(false, false);
+  }
+#undef OSCARS_VALUES
   return hipGetLastError();
 }
 
 hipError_t launch_mx4_product(const Mx4Product& args, hipStream_t s) {
-  const bool vec = aligned_rows(args.out, args.out_ld * (args.out_bf16 ? 2 : 4), 16);
+  const bool vec = out_aligned(args);
   hipError_t e = hipSuccess;
   mx4_launches(args.rows, args.in, args.outs, [&](int tile, int64_t at, int64_t rows) {
     Mx4Product a = args;
@@ -1018,6 +1271,23 @@ hipError_t launch_mx4_product(const Mx4Product& args, hipStream_t s) {
   return e;
 }
 
+hipError_t launch_mx4_products(const Mx4Product* p, int n, hipStream_t s) {
+  // in one launch of small tiles, where that is no slower than each as it would go alone
+  double together = 3.0, alone = 0.0;
+  int64_t tiles = 0;
+  for (int i = 0; i < n; ++i) {
+    const Mx4Plan best = mx4_plan(p[i].rows, p[i].in, p[i].outs);
+    together += mx4_small_us(p[i].rows, p[i].in, p[i].outs) - 3.0;
+    alone += best.us;
+    tiles += (p[i].rows + 31) / 32 * ((p[i].outs + 31) / 32);
+  }
+  const bool small = together <= alone && tiles < (1 << 24);
+  if (small) return small_launch(p, n, s);
+  hipError_t e = hipSuccess;
+  for (int i = 0; i < n && e == hipSuccess; ++i) e = launch_mx4_product(p[i], s);
+  return e;
+}
+
 bool mx4_one_launch(int64_t rows, int in) {
   static_assert(FEW_LDS_S >= FEW_ENTRIES * 17 / 32 + FEW_ROWS * (256 + 32) &&
                     FEW_LDS_L >= 65536 / 512 * 272 + 16,
@@ -1027,7 +1297,7 @@ bool mx4_one_launch(int64_t rows, int in) {
 
 hipError_t launch_mx4_few(const Mx4Product& a, const void* x, int64_t x_ld, bool x_bf16,
                           hipStream_t s) {
-  const bool vec = aligned_rows(x, x_ld * (x_bf16 ? 2 : 4), 16);
+  const bool vec = a.in % 8 == 0 && aligned_rows(x, x_ld * (x_bf16 ? 2 : 4), 16);
   if (x_bf16)
     return vec ? few_launch<true, true>(a, x, x_ld, s) : few_launch<true, false>(a, x, x_ld, s);
   return vec ? few_launch<false, true>(a, x, x_ld, s) : few_launch<false, false>(a, x, x_ld, s);

@@ -8,32 +8,48 @@
 
 namespace oscars {
 
-// The first `rows` rows of a product in tiles of `tile`, and its estimated time in us
-// (a K block: 256 inputs).
+// The tile of a product and its estimated time by what the kernels take on this card, in us
+// (a K block: 256 inputs; n tiles):
+//   32    3, and 2250 blocks a us over all CUs, ten more counted for each tile
+//   64    2.9 and a block 0.31 while no CU has two tiles, 0.55 up to two; else 1.5 and a
+//         block 0.58 for 512 at a time
+//   128   3.2 and a block 0.69 up to 128 tiles, 0.86 up to 256; else 4.2 and a block 1.2
+//         for 512 at a time
+//   256   10 and a block 1.1 up to 64 tiles, 1.34 up to 128, 1.87 up to 256; else 8 and a
+//         block 1.9 for 256 at a time
+// Rows x inputs x outputs, measured with 32 / 64 / 128 / 256: 256 x 4096 x 1000: 5.8 / 7.4 /
+// 11.8 / -, 256 x 4096 x 4096: 15.2 / 7.8 / 14.3 / 27.2, 1024 x 2048 x 2048: 20.3 / 7.3 / 8.6
+// / -, 2048 x 4096 x 2048: 49 / 21 / 17 / -, 2048 x 4096 x 4096: 93 / 42 / 24 / 31, 4096 x 4096
+// x 4096: - / - / 47.6 / 39.9, 8192 x 4096 x 4096: - / - / 90 / 77.
 struct Mx4Plan {
   int tile;
-  int64_t rows;
   double us;
 };
+inline double mx4_small_us(int64_t rows, int in, int outs) {
+  return 3.0 + std::ceil(outs / 32.0) * std::ceil(static_cast<double>(rows) / 32.0) *
+                   (std::ceil(in / 256.0) + 10.0) / 2250.0;
+}
 inline Mx4Plan mx4_plan(int64_t rows, int in, int outs) {
   const double k = (in + 255) / 256;
-  Mx4Plan best{0, rows, 0.0};
-  for (int t : {32, 128, 256}) {
-    const double n =
-        static_cast<double>((outs + t - 1) / t) * static_cast<double>((rows + t - 1) / t);
-    const double turns = std::floor(n / 512.0), last = n - 512.0 * turns;
+  Mx4Plan best{0, 0.0};
+  for (int t : {32, 64, 128, 256}) {
+    const double n = std::ceil(static_cast<double>(outs) / t) *
+                     std::ceil(static_cast<double>(rows) / t);
     double us;
     if (t == 32)
-      us = 3.5 + n * k / 2000.0;
+      us = mx4_small_us(rows, in, outs);
+    else if (t == 64)
+      us = n <= 256.0 ? 2.9 + 0.31 * k
+                      : n <= 512.0 ? 2.9 + 0.55 * k : std::ceil(n / 512.0) * (1.5 + 0.58 * k);
     else if (t == 128)
-      us = 8.0 + k * (n <= 256.0 ? 0.55
-                                 : 1.2 * turns + (last > 256.0 ? 1.2 : last > 0.0 ? 0.75 : 0.0));
+      us = n <= 128.0 ? 3.2 + 0.69 * k
+                      : n <= 256.0 ? 3.2 + 0.86 * k : 1.0 + std::ceil(n / 512.0) * (4.2 + 1.2 * k);
     else
-      us = 20.0 + k * (n <= 144.0 ? 1.15 : n <= 256.0 ? 1.55 : 1.75 * std::ceil(n / 256.0));
-    if (best.tile == 0 || us < best.us) {
-      best.tile = t;
-      best.us = us;
-    }
+      us = n <= 64.0 ? 10.0 + 1.1 * k
+                     : n <= 128.0 ? 10.0 + 1.34 * k
+                                  : n <= 256.0 ? 10.0 + 1.87 * k
+                                               : std::ceil(n / 256.0) * (8.0 + 1.9 * k);
+    if (best.tile == 0 || us < best.us) best = {t, us};
   }
   return best;
 }

@@ -2207,7 +2207,9 @@ struct Mx4Grads {
 };
 bool mx4_grad_sizes_ok(int64_t rows, int64_t in, int64_t outs) {
   return rows >= 0 && rows <= MX4_MAX_COLS && in >= 1 && in <= OSCARS_MAX_WIDTH && outs >= 1 &&
-         outs <= OSCARS_MAX_WIDTH;
+         outs <= OSCARS_MAX_WIDTH &&
+         mx4_column_tiles(rows, static_cast<int>(round_up(outs, 512))) +
+                 mx4_column_tiles(rows, static_cast<int>(in)) < (1 << 23);
 }
 
 }  // namespace
@@ -2218,7 +2220,7 @@ oscars_status oscars_quantize_micro(uint8_t* q, int64_t q_ld, uint8_t* scale, in
   if (!is_dtype(dtype) || rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxRows)
     return OSCARS_E_INVALID;
   const int64_t along = transposed ? rows : cols, count = transposed ? cols : rows;
-  if (along > MX4_MAX_COLS || (transposed && rows * cols >= (int64_t{1} << 37)))
+  if (along > MX4_MAX_COLS || (transposed && rows > 0 && mx4_column_tiles(rows, static_cast<int>(cols)) >= (1 << 23)))
     return OSCARS_E_INVALID;
   const int64_t es = dtype_bytes(dtype);
   if (!rows_ok(x, x_ld, cols, es)) return OSCARS_E_INVALID;
@@ -2232,7 +2234,7 @@ oscars_status oscars_quantize_micro(uint8_t* q, int64_t q_ld, uint8_t* scale, in
                     DropArgs{}};
   const Mx4Rows to{q, q_ld, scale, s_ld};
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const hipError_t e = transposed ? launch_mx4_columns(a, to, nullptr, nullptr, s)
+  const hipError_t e = transposed ? launch_mx4_columns(a, to, s)
                                   : launch_mx4_rows(a, to, s);
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
@@ -2384,20 +2386,15 @@ oscars_status oscars_linear_micro_backward(const oscars_micro_gradients* g, void
   const Mx4Rows zr{ws + lay.zq, mx4_bytes(outs), ws + lay.zs, mx4_scales(outs)};
   const Mx4Rows zc{ws + lay.ztq, mx4_bytes(rows), ws + lay.zts, mx4_scales(rows)};
   const Mx4Rows xc{ws + lay.xtq, mx4_bytes(rows), ws + lay.xts, mx4_scales(rows)};
-  e = launch_mx4_columns(z, zc, g->db, reinterpret_cast<float*>(ws + lay.part), s);
-  if (e == hipSuccess) e = launch_mx4_columns(x, xc, nullptr, nullptr, s);
-  if (e == hipSuccess && dx) e = launch_mx4_rows(z, zr, s);
-  if (e == hipSuccess && dx)
-    e = launch_mx4_product(
-        Mx4Product{zr.q, zr.q_ld, zr.scale, zr.s_ld, g->wtq, g->wt_ld, g->wtscale, g->wts_ld,
-                   nullptr, false, rows, outs, in, g->dx, g->dx_ld, g->x_dtype == OSCARS_BF16,
-                   DropArgs{}},
-        s);
-  if (e == hipSuccess)
-    e = launch_mx4_product(
-        Mx4Product{zc.q, zc.q_ld, zc.scale, zc.s_ld, xc.q, xc.q_ld, xc.scale, xc.s_ld, nullptr,
-                   false, outs, static_cast<int>(rows), in, g->dw, g->dw_ld, false, DropArgs{}},
-        s);
+  e = launch_mx4_gradient(Mx4Gradient{z, x, dx ? zr : Mx4Rows{}, zc, xc, g->db,
+                                      reinterpret_cast<float*>(ws + lay.part)},
+                          s);
+  const Mx4Product p[2] = {
+      {zc.q, zc.q_ld, zc.scale, zc.s_ld, xc.q, xc.q_ld, xc.scale, xc.s_ld, nullptr, false, outs,
+       static_cast<int>(rows), in, g->dw, g->dw_ld, false, DropArgs{}},
+      {zr.q, zr.q_ld, zr.scale, zr.s_ld, g->wtq, g->wt_ld, g->wtscale, g->wts_ld, nullptr, false,
+       rows, outs, in, g->dx, g->dx_ld, g->x_dtype == OSCARS_BF16, DropArgs{}}};
+  if (e == hipSuccess) e = launch_mx4_products(p, dx ? 2 : 1, s);
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }
 
