@@ -514,7 +514,7 @@ typedef struct {
  *          out_ld >= outs, aligned to its elements; 1 <= in <= 2^24,
  *          1 <= outs <= 2^24;  dropout  host, or NULL: none.
  * oscars_linear_micro: both, x [rows][x_ld] of `dtype` as for oscars_quantize_micro, in
- *   <= OSCARS_MAX_WIDTH; one row, or up to 16 of together 16384 entries, in one
+ *   <= OSCARS_MAX_WIDTH; one row, or up to 32 of together 16384 entries, in one
  *   launch.  workspace: device, 16-byte aligned, oscars_linear_micro_workspace bytes
  *   (NULL where those are 0), the call's own until the stream has run it. */
 oscars_status oscars_quantize_micro(uint8_t* q, int64_t q_ld, uint8_t* scale, int64_t s_ld,

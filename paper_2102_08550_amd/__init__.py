@@ -166,6 +166,7 @@ def _lib():
 
 
 _lib()  # fail at import time when the library is absent
+import torch  # noqa: E402  (loaded by _lib, in front of the library)
 
 
 def _check(status: int, what: str):
@@ -188,15 +189,17 @@ def _arr(a, dtype):
     return a, a.ctypes.data_as(_P(c))
 
 
-def _stream_handle(stream=None) -> Optional[int]:
-    import torch
+# the handle alone where torch gives it (0.5 us, by way of a Stream object 4)
+_RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_handle(stream=None, device=None) -> Optional[int]:
+    """``stream``'s handle, or the current one's of ``device`` (None: of the current device)."""
     if stream is not None:
         return stream.cuda_stream
-    # the handle alone where torch gives it (0.5 us, by way of a Stream object 4)
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is not None:
-        return raw(torch.cuda.current_device())
-    return torch.cuda.current_stream().cuda_stream
+    if _RAW_STREAM is not None:
+        return _RAW_STREAM(torch.cuda.current_device() if device is None else device.index)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _dev_ptr(t, dtype=None, what="tensor") -> int:
@@ -316,7 +319,6 @@ def broadcast(global_, replicas, K: int, n: int, ld: int, stream=None):
 
 def _on_device(device):
     """The context in which a call's kernels go to ``device``."""
-    import torch
     if torch.cuda.current_device() == device.index:
         return _SAME_DEVICE
     return torch.cuda.device(device)
@@ -325,7 +327,6 @@ def _on_device(device):
 def _workspace(nbytes: int, device, stream=None):
     """Device memory for one call on ``stream`` (None: the current one): torch's
     allocator gives it to later work of that stream only."""
-    import torch
     if stream is None or stream == torch.cuda.current_stream(device):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
     with torch.cuda.stream(stream):
@@ -419,7 +420,6 @@ def orthogonalize(x, out=None, coeffs=NEWTON_SCHULZ, stream=None):
 
 
 def _float_type(dtype, what) -> int:
-    import torch
     if dtype == torch.float32:
         return FP32
     if dtype == torch.bfloat16:
@@ -429,7 +429,6 @@ def _float_type(dtype, what) -> int:
 
 def _rows(t, dtype, device, what):
     """(pointer, rows, row stride, columns) of a 2-D device tensor stored by rows."""
-    import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
         raise TypeError(f"{what} must be a tensor on the input's CUDA (HIP) device")
     if t.dtype != dtype:
@@ -443,7 +442,6 @@ def _rows(t, dtype, device, what):
 
 
 def _vector(t, n, device, what):
-    import torch
     if t is None:
         return None
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
@@ -454,7 +452,6 @@ def _vector(t, n, device, what):
 
 
 def _new(shape, dtype, device, stream):
-    import torch
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
@@ -559,7 +556,6 @@ def _micro_shapes(rows: int, cols: int):
 
 def _micro_rows(q, scale, rows, cols, device, what):
     """(pointer, row stride, scales' pointer, row stride) of quantised rows."""
-    import torch
     if (not isinstance(q, torch.Tensor) or not isinstance(scale, torch.Tensor)
             or q.device != device or scale.device != device or not q.is_cuda):
         raise TypeError(f"{what} and its scales must be tensors on the input's CUDA (HIP) device")
@@ -582,7 +578,6 @@ def _micro_rows(q, scale, rows, cols, device, what):
 
 def _dropout_options(dropout, device):
     """(options, the offset's tensor) of ``(p, seed[, offset])``; Nones for None."""
-    import torch
     if dropout is None:
         return None, None
     p, seed, offset = dropout if len(dropout) == 3 else (*dropout, 0)
@@ -620,7 +615,6 @@ def quantize_mx4(x, transposed: bool = False, out=None, stream=None):
     floating point (oscars_quantize_micro), or with ``transposed`` the rows of its
     transpose: ``(q, scale)``, uint8, two entries a byte and a scale for every 32.
     ``out``: such a pair to write into, row strides multiples of 16."""
-    import torch
     dev = x.device
     xp, n, ld, cols = _rows(x, x.dtype, dev, "x")
     dt = _float_type(x.dtype, "x")
@@ -634,7 +628,7 @@ def quantize_mx4(x, transposed: bool = False, out=None, stream=None):
         return out
     with _on_device(dev):
         _check(_lib().oscars_quantize_micro(qp, qld, sp, sld, xp, ld, dt, n, cols,
-                                            int(bool(transposed)), _stream_handle(stream)),
+                                            int(bool(transposed)), _stream_handle(stream, dev)),
                "oscars_quantize_micro")
     _used_on(stream, x, q, scale)
     return out
@@ -643,7 +637,6 @@ def quantize_mx4(x, transposed: bool = False, out=None, stream=None):
 def dequantize_mx4(q, scale, columns: int, dtype=None, out=None, stream=None):
     """The values of quantised rows of ``columns`` entries (oscars_dequantize_micro), in
     fp32 by default."""
-    import torch
     dev = q.device
     n = q.shape[0]
     qp, qld, sp, sld = _micro_rows(q, scale, n, int(columns), dev, "q")
@@ -652,7 +645,7 @@ def dequantize_mx4(q, scale, columns: int, dtype=None, out=None, stream=None):
         return out
     with _on_device(dev):
         _check(_lib().oscars_dequantize_micro(op, old, odt, qp, qld, sp,
-                                              sld, n, int(columns), _stream_handle(stream)),
+                                              sld, n, int(columns), _stream_handle(stream, dev)),
                "oscars_dequantize_micro")
     _used_on(stream, q, scale, out)
     return out
@@ -664,7 +657,6 @@ def matmul_mx4(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool =
     and weights ``wq`` [outputs][..] as quantize_mx4 gives them, of ``in_features``
     entries each; ``dropout``: ``(p, seed)`` or ``(p, seed, offset)`` as in ``dropout``;
     fp32 by default.  Returns ``out``."""
-    import torch
     dev = xq.device
     n, outs, cols = xq.shape[0], wq.shape[0], int(in_features)
     xp, xld, xsp, xsld = _micro_rows(xq, xscale, n, cols, dev, "xq")
@@ -677,7 +669,7 @@ def matmul_mx4(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool =
         _check(_lib().oscars_matmul_micro(
             op, old, odt, xp, xld, xsp, xsld, wp, wld, wsp, wsld,
             _vector(bias, outs, dev, "bias"), int(bool(relu)), drop, n, cols, outs,
-            _stream_handle(stream)), "oscars_matmul_micro")
+            _stream_handle(stream, dev)), "oscars_matmul_micro")
     _used_on(stream, xq, xscale, wq, wscale, bias, offset, out)
     return out
 
@@ -689,7 +681,6 @@ def linear_mx4(x, wq, wscale, bias=None, relu: bool = False, dropout=None, out_d
     matrix's quantize_mx4.  ``dropout`` (training): ``(p, seed)`` or ``(p, seed,
     offset)`` as in ``dropout``.  The result has ``x``'s type by default.  Returns
     ``out``; linear_mx4_backward has the gradients."""
-    import torch
     dev = x.device
     xp, n, xld, cols = _rows(x, x.dtype, dev, "x")
     dt = _float_type(x.dtype, "x")
@@ -706,7 +697,7 @@ def linear_mx4(x, wq, wscale, bias=None, relu: bool = False, dropout=None, out_d
         _check(lib.oscars_linear_micro(
             op, old, odt, xp, xld, dt, wp, wld, wsp, wsld,
             _vector(bias, outs, dev, "bias"), int(bool(relu)), drop, n, cols, outs,
-            ws.data_ptr() if need else None, need, _stream_handle(stream)),
+            ws.data_ptr() if need else None, need, _stream_handle(stream, dev)),
             "oscars_linear_micro")
     _used_on(stream, x, wq, wscale, bias, offset, out)
     return out
@@ -720,7 +711,6 @@ def linear_mx4_backward(dy, x, wtq=None, wtscale=None, y=None, dropout=None, wan
     output, for a layer with a ReLU.  ``dropout``: as in the forward call.  dx has
     ``x``'s type (None without ``want_dx``, which needs no weights), dw and db are
     fp32.  ``out``: such a triple to write into."""
-    import torch
     dev = dy.device
     dyp, n, dyld, outs = _rows(dy, dy.dtype, dev, "dy")
     xp, xn, xld, cols = _rows(x, x.dtype, dev, "x")
@@ -761,7 +751,7 @@ def linear_mx4_backward(dy, x, wtq=None, wtscale=None, y=None, dropout=None, wan
     ws = _workspace(need, dev, stream) if need else None
     with _on_device(dev):
         _check(lib.oscars_linear_micro_backward(
-            ctypes.byref(g), ws.data_ptr() if need else None, need, _stream_handle(stream)),
+            ctypes.byref(g), ws.data_ptr() if need else None, need, _stream_handle(stream, dev)),
             "oscars_linear_micro_backward")
     _used_on(stream, dy, x, wtq, wtscale, y, offset, dx, dw, db)
     return out
@@ -783,7 +773,7 @@ def dropout(x, p: float, seed: int, offset=0, out=None, stream=None):
         return out
     with _on_device(dev):
         _check(_lib().oscars_dropout(op, old, xp, ld, dt, options, n, cols,
-                                     _stream_handle(stream)), "oscars_dropout")
+                                     _stream_handle(stream, dev)), "oscars_dropout")
     _used_on(stream, x, more, out)
     return out
 

@@ -10,7 +10,7 @@
 //   mx4_values    4 bits back into values;
 //   mx4_product   tiles on 32x32x64 block-scaled matrix instructions: a lane's 16
 //                 bytes of an operand are one block of 32 with one scale;
-//   mx4_few       one row, or up to 16 short ones: a stream of the weights, with the
+//   mx4_few       one row, or up to 32 short ones: a stream of the weights, with the
 //                 rows' quantisation in front of it in every workgroup.
 #include "mx4.h"
 
@@ -1019,27 +1019,30 @@ hipError_t product_launch(const Mx4Product& a, int tile, hipStream_t s) {
 
 // ------------------------------------------------------------------ a few rows
 
-// Up to 16 rows.  A workgroup takes 16 output channels, its eight waves slices of 512
-// of K in turn: four 16x16x128 instructions, lane l channel or row l & 15, block l >> 4
-// of 128 entries.  While the weights are on their way every workgroup quantises all
-// rows into LDS for itself (they come from the L2).  The eight partial sums meet in
-// LDS, in order.
-constexpr int FEW_ROWS = 16;
+// Up to 32 rows.  A workgroup takes 16 output channels, its eight waves slices of 512
+// of K in turn: four 16x16x128 instructions for each 16 rows, lane l channel or row l & 15,
+// block l >> 4 of 128 entries.  While the weights are on their way every workgroup
+// quantises all rows into LDS for itself (they come from the L2).  The eight partial
+// sums meet in LDS, in order.  One row of 4096 by 4096 outputs: 4.8 us.
+constexpr int FEW_ROWS = 32;
 constexpr int FEW_WAVES = 8;
-constexpr int FEW_ENTRIES = 16384;  // of more than one row
+// Every workgroup quantises all rows: up to so many entries that is less than a launch of
+// its own takes.  One row is taken at any length.
+constexpr int FEW_ENTRIES = 16384;
 
 __host__ __device__ __forceinline__ int few_row_bytes(int in) {
   return (in + 511) / 512 * 256 + 16;  // 16 more: consecutive rows start in other banks
 }
 __host__ __device__ __forceinline__ int few_row_scales(int in) { return (in + 511) / 512 * 16; }
-// quantised rows and scales: FEW_ENTRIES of 16 rows, or 65536 of one
-constexpr int FEW_LDS_S = 13 << 10, FEW_LDS_L = 35 << 10;
+// quantised rows and scales: FEW_ENTRIES of FEW_ROWS rows, or 65536 of one
+constexpr int FEW_LDS_S = 18 << 10, FEW_LDS_L = 35 << 10;
 
-template <int LDS, bool X_BF16, bool VEC, bool OUT_BF16>
+template <int LDS, bool X_BF16, bool VEC, bool OUT_BF16, bool TWO>
 __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(Mx4Product a, const void* x,
                                                                  int64_t x_ld) {
+  constexpr int HALVES = TWO ? 2 : 1;  // of 16 rows
   __shared__ __attribute__((aligned(16))) char few_lds[LDS];
-  __shared__ float part[FEW_WAVES][64][4];
+  __shared__ float part[HALVES][FEW_WAVES][64][4];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rows = static_cast<int>(a.rows), in = a.in, ld = few_row_bytes(in);
@@ -1078,39 +1081,48 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(Mx4Product a, c
     if ((lane & 3) == 0) scales[r * sld + c / 32] = static_cast<char>(s.byte);
   }
   __syncthreads();
-  nt_f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  // lanes of rows that are not there read the last one; their sums are not used
-  const int r = (lane & 15) < rows ? (lane & 15) : rows - 1;
-  const char* b = few_lds + r * ld + 16 * g;
-  const char* bs = scales + r * sld;
-  for (int sl = wave; sl < slices; sl += FEW_WAVES) {
-    nt_u32x4 wv[4] = {cur[0], cur[1], cur[2], cur[3]};
-    const nt_u32x4 wsc = cur_s;
-    if (sl + FEW_WAVES < slices) load_w(sl + FEW_WAVES);
-    const nt_u32x4 xsc = *reinterpret_cast<const nt_u32x4*>(bs + sl * 16);
+  nt_f32x4 acc[HALVES];
+  const char *b[HALVES], *bs[HALVES];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const nt_u32x4 xv = *reinterpret_cast<const nt_u32x4*>(b + sl * 256 + 64 * c);
-      const mx_i32x8 p = {static_cast<int>(wv[c][0]), static_cast<int>(wv[c][1]),
-                          static_cast<int>(wv[c][2]), static_cast<int>(wv[c][3]), 0, 0, 0, 0};
-      const mx_i32x8 q = {static_cast<int>(xv[0]), static_cast<int>(xv[1]),
-                          static_cast<int>(xv[2]), static_cast<int>(xv[3]), 0, 0, 0, 0};
-      // the lane's scale to the lowest byte
-      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-          p, q, acc, 4, 4, 0, static_cast<int>(wsc[c] >> (8 * g)), 0,
-          static_cast<int>(xsc[c] >> (8 * g)));
+  for (int n = 0; n < HALVES; ++n) {
+    acc[n] = nt_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // lanes of rows that are not there read the last one; their sums are not used
+    const int r = 16 * n + (lane & 15) < rows ? 16 * n + (lane & 15) : rows - 1;
+    b[n] = few_lds + r * ld + 16 * g;
+    bs[n] = scales + r * sld;
+  }
+  for (int sl = wave; sl < slices; sl += FEW_WAVES) {
+    const nt_u32x4 wv[4] = {cur[0], cur[1], cur[2], cur[3]}, wsc = cur_s;
+    if (sl + FEW_WAVES < slices) load_w(sl + FEW_WAVES);
+#pragma unroll
+    for (int n = 0; n < HALVES; ++n) {
+      const nt_u32x4 xsc = *reinterpret_cast<const nt_u32x4*>(bs[n] + sl * 16);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const nt_u32x4 xv = *reinterpret_cast<const nt_u32x4*>(b[n] + sl * 256 + 64 * c);
+        const mx_i32x8 p = {static_cast<int>(wv[c][0]), static_cast<int>(wv[c][1]),
+                            static_cast<int>(wv[c][2]), static_cast<int>(wv[c][3]), 0, 0, 0, 0};
+        const mx_i32x8 q = {static_cast<int>(xv[0]), static_cast<int>(xv[1]),
+                            static_cast<int>(xv[2]), static_cast<int>(xv[3]), 0, 0, 0, 0};
+        // the lane's scale to the lowest byte
+        acc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+            p, q, acc[n], 4, 4, 0, static_cast<int>(wsc[c] >> (8 * g)), 0,
+            static_cast<int>(xsc[c] >> (8 * g)));
+      }
     }
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) part[wave][lane][e] = acc[e];
+  for (int n = 0; n < HALVES; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[n][wave][lane][e] = acc[n][e];
   __syncthreads();
   // lane l, element e: channel 4 (l >> 4) + e, row l & 15; a thread finishes one output
-  if (tid < 256) {
-    const int e = tid & 3, l = tid >> 2;
+  if (tid < 256 * HALVES) {
+    const int n = tid >> 8, e = tid & 3, l = (tid >> 2) & 63;
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < FEW_WAVES; ++i) sum += part[i][l][e];
-    const int q = l & 15, o = blockIdx.x * 16 + 4 * (l >> 4) + e;
+    for (int i = 0; i < FEW_WAVES; ++i) sum += part[n][i][l][e];
+    const int q = 16 * n + (l & 15), o = blockIdx.x * 16 + 4 * (l >> 4) + e;
     if (q < rows && o < a.outs) {
       float y = mx_finish(a, sum, a.bias ? a.bias[o] : 0.0f);
       if (a.drop.below) {
@@ -1125,21 +1137,22 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(Mx4Product a, c
   }
 }
 
-template <int LDS, bool X_BF16, bool VEC>
+template <int LDS, bool X_BF16, bool VEC, bool TWO>
 hipError_t few_launch(const Mx4Product& a, const void* x, int64_t x_ld, hipStream_t s) {
   const dim3 grid((a.outs + 15) / 16), wg(64 * FEW_WAVES);
   if (a.out_bf16)
-    hipLaunchKernelGGL((mx4_few_kernel<LDS, X_BF16, VEC, true>), grid, wg, 0, s, a, x, x_ld);
+    hipLaunchKernelGGL((mx4_few_kernel<LDS, X_BF16, VEC, true, TWO>), grid, wg, 0, s, a, x, x_ld);
   else
-    hipLaunchKernelGGL((mx4_few_kernel<LDS, X_BF16, VEC, false>), grid, wg, 0, s, a, x, x_ld);
+    hipLaunchKernelGGL((mx4_few_kernel<LDS, X_BF16, VEC, false, TWO>), grid, wg, 0, s, a, x, x_ld);
   return hipGetLastError();
 }
 
 template <bool X_BF16, bool VEC>
 hipError_t few_launch(const Mx4Product& a, const void* x, int64_t x_ld, hipStream_t s) {
+  if (a.rows > 16) return few_launch<FEW_LDS_S, X_BF16, VEC, true>(a, x, x_ld, s);
   return a.rows * (few_row_bytes(a.in) + few_row_scales(a.in)) <= FEW_LDS_S
-             ? few_launch<FEW_LDS_S, X_BF16, VEC>(a, x, x_ld, s)
-             : few_launch<FEW_LDS_L, X_BF16, VEC>(a, x, x_ld, s);
+             ? few_launch<FEW_LDS_S, X_BF16, VEC, false>(a, x, x_ld, s)
+             : few_launch<FEW_LDS_L, X_BF16, VEC, false>(a, x, x_ld, s);
 }
 
 template <bool BF16, bool VEC>

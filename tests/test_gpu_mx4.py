@@ -224,7 +224,7 @@ def test_product_of_strided_rows(P):
 @pytest.mark.parametrize("dtype,out_dtype", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32")])
 @pytest.mark.parametrize("rows,inputs,outs", [
     (1, 8, 2), (1, 1, 1), (1, 4096, 515), (1, 65536, 40), (2, 784, 512), (16, 1024, 37),
-    (16, 1025, 37), (7, 700, 100), (17, 784, 512), (200, 333, 130), (1300, 520, 700)])
+    (16, 1025, 37), (7, 700, 100), (17, 784, 512), (32, 512, 33), (32, 8, 5), (33, 8, 5), (20, 519, 70), (200, 333, 130), (1300, 520, 700)])
 def test_linear(P, rows, inputs, outs, dtype, out_dtype):
     import torch
     rng = np.random.default_rng(rows + inputs + outs)

@@ -89,7 +89,8 @@ def test_workspaces():
     assert lib.oscars_linear_micro_workspace(1, 65536) == 0
     assert lib.oscars_linear_micro_workspace(16, 1024) == 0
     assert lib.oscars_linear_micro_workspace(16, 1025) == 16 * (5 * 128 + 3 * 16)
-    assert lib.oscars_linear_micro_workspace(17, 10) > 0
+    assert lib.oscars_linear_micro_workspace(32, 512) == 0
+    assert lib.oscars_linear_micro_workspace(33, 10) > 0
     assert lib.oscars_linear_micro_workspace(-1, 10) == 0
     assert lib.oscars_linear_micro_backward_workspace(-1, 10, 10, 1) == 0
     assert lib.oscars_linear_micro_backward_workspace(10, 65537, 10, 1) == 0
