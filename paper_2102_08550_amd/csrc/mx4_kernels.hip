@@ -31,9 +31,6 @@ __device__ __forceinline__ uint16_t mx_to_bf16(float v) {
   if ((u & 0x7FFFFFFFu) > 0x7F800000u) return static_cast<uint16_t>(u >> 16) | 0x40;
   return static_cast<uint16_t>((u + 0x7FFF + ((u >> 16) & 1)) >> 16);
 }
-__device__ __forceinline__ uint32_t mx_abs(float v) {
-  return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
-}
 
 // A block's scale from its largest |x| as bits.  Adding a quarter of the significand's
 // range carries into the exponent from 7/4 on: then the largest entry would be
@@ -42,32 +39,61 @@ __device__ __forceinline__ uint32_t mx_abs(float v) {
 // normal entries, 1.04 where channels differ, 2.1 for uniform ones; scales that bring
 // the largest to 6 or below 1.06, 1.10 and 1.00 times.)  Scales end at 2^125: what is
 // left above 6 is cut to 6, where 2^126 would make it 2^128.
-// inv: what an entry is multiplied with, exactly; 0 where the block counts as zeros:
-// with no normal number in it, or with a NaN or an infinity (scale byte 255: NaN).
+// s: what the conversion divides by (its exponent counts, 2^-127 among them).  A block that is
+// not alive has only zeros: one without a normal number (s such that all round to
+// zero), or with a NaN or an infinity (byte 255: NaN).
 struct MxScale {
   uint32_t byte;
-  float inv;
+  float s;
+  bool alive;
 };
 __device__ __forceinline__ MxScale mx_scale(uint32_t top) {
   const uint32_t e = (top + 0x00200000u) >> 23;
   const uint32_t byte = e > 254 ? 252 : e > 2 ? e - 2 : 0;
-  MxScale r{byte, __builtin_bit_cast(float, (254u - byte) << 23)};
-  if (top >= 0x7F800000u) r = MxScale{255u, 0.0f};
-  if (top < 0x00800000u) r = MxScale{0u, 0.0f};
+  MxScale r{byte, __builtin_bit_cast(float, byte << 23),
+            top >= 0x00800000u && top < 0x7F800000u};
+  if (top >= 0x7F800000u) r.byte = 255u;
+  if (top < 0x00800000u) r = MxScale{0u, 1.0f, false};
   return r;
 }
-// Two entries into byte B of w, the first in its low half.  v inv is exact; the conversion
-// rounds to nearest, ties to even.
-template <int B>
-__device__ __forceinline__ uint32_t mx_pack2(uint32_t w, float a, float b, float inv) {
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a * inv, b * inv, 1.0f, B);
+// The larger magnitude; a NaN's bits are above infinity's, and those above every number's.
+__device__ __forceinline__ float mx_larger(float top, float v) {
+  return __builtin_elementwise_maximum(top, __builtin_fabsf(v));  // keeps a NaN
 }
-__device__ __forceinline__ uint32_t mx_pack8(const float* v, float inv) {
-  uint32_t w = mx_pack2<0>(0u, v[0], v[1], inv);
-  w = mx_pack2<1>(w, v[2], v[3], inv);
-  w = mx_pack2<2>(w, v[4], v[5], inv);
-  w = mx_pack2<3>(w, v[6], v[7], inv);
-  return inv > 0.0f ? w : 0u;
+__device__ __forceinline__ uint32_t mx_bits(float top) {
+  return __builtin_bit_cast(uint32_t, top) & 0x7FFFFFFFu;
+}
+// Two entries in units of the scale into byte B of w, the first in its low half: rounded to
+// nearest, ties to even.
+template <int B>
+__device__ __forceinline__ uint32_t mx_pack2(uint32_t w, float a, float b, float s) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, b, s, B);
+}
+template <int B>
+__device__ __forceinline__ uint32_t mx_pack2(uint32_t w, uint32_t pair, float s) {  // of bf16
+  typedef __bf16 two __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(two, pair), s, B);
+}
+__device__ __forceinline__ uint32_t mx_pack8(const float* v, const MxScale& m) {
+  uint32_t w = mx_pack2<0>(0u, v[0], v[1], m.s);
+  w = mx_pack2<1>(w, v[2], v[3], m.s);
+  w = mx_pack2<2>(w, v[4], v[5], m.s);
+  w = mx_pack2<3>(w, v[6], v[7], m.s);
+  return m.alive ? w : 0u;
+}
+__device__ __forceinline__ uint32_t mx_pack8(const uint32_t* pairs, const MxScale& m) {
+  uint32_t w = mx_pack2<0>(0u, pairs[0], m.s);
+  w = mx_pack2<1>(w, pairs[1], m.s);
+  w = mx_pack2<2>(w, pairs[2], m.s);
+  w = mx_pack2<3>(w, pairs[3], m.s);
+  return m.alive ? w : 0u;
+}
+// The larger magnitudes of two pairs in bf16, as bits.
+__device__ __forceinline__ uint32_t mx_larger2(uint32_t top, uint32_t pair) {
+  typedef uint16_t two __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(
+      uint32_t, __builtin_elementwise_max(__builtin_bit_cast(two, top),
+                                          __builtin_bit_cast(two, pair & 0x7FFF7FFFu)));
 }
 
 // Eight consecutive entries from column c (a multiple of 8).  VEC: cols % 8 == 0, 16-byte loads.
@@ -109,10 +135,17 @@ __device__ __forceinline__ void mx_clip8(int c, int cols, float* v) {
   for (int t = 0; t < 8; ++t) v[t] = (VEC ? c : c + t) < cols ? v[t] : 0.0f;
 }
 
-// The gradient behind the layer's epilogue (mx4.h).  A NaN in y passes it on.
-__device__ __forceinline__ float mx_pass(float dy, float y, const DropArgs& d) {
-  const float g = d.below ? dy * d.factor : dy;
-  return y <= 0.0f ? 0.0f : g;
+__device__ __forceinline__ uint32_t mx_top8(const float* v) {
+  float top = 0.0f;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) top = mx_larger(top, v[t]);
+  return mx_bits(top);
+}
+
+// The gradient behind the layer's epilogue (mx4.h), factor 1 without dropout.  A NaN in y passes
+// it on.
+__device__ __forceinline__ float mx_pass(float dy, float y, float factor) {
+  return y <= 0.0f ? 0.0f : dy * factor;
 }
 
 // A wave takes 512 columns of a row, a lane eight of them, four lanes a block; neighbouring
@@ -129,17 +162,33 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(Mx4Source a, Mx4Rows to, 
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * 4 + wave; u < units; u += step) {
     const int64_t row = u / pieces;
     const int c = static_cast<int>(u - row * pieces) * 512 + 8 * lane;
+    const char* from = static_cast<const char*>(a.x) + row * a.x_ld * (BF16 ? 2 : 4);
+    uint32_t top, pairs[4];
     float v[8];
-    mx_load8<BF16, VEC>(static_cast<const char*>(a.x) + row * a.x_ld * (BF16 ? 2 : 4), c, a.cols,
-                        v);
-    mx_clip8<VEC>(c, a.cols, v);
-    uint32_t top = 0;
+    if constexpr (BF16 && VEC) {
+      const nt_u32x4 w = *reinterpret_cast<const nt_u32x4*>(
+          reinterpret_cast<const uint16_t*>(from) + (c < a.cols ? c : a.cols - 8));
+      uint32_t two = 0;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) top = max(top, mx_abs(v[t]));
+      for (int t = 0; t < 4; ++t) {
+        pairs[t] = c < a.cols ? w[t] : 0u;
+        two = mx_larger2(two, pairs[t]);
+      }
+      top = max(two << 16, two & 0xFFFF0000u);
+    } else {
+      mx_load8<BF16, VEC>(from, c, a.cols, v);
+      mx_clip8<VEC>(c, a.cols, v);
+      top = mx_top8(v);
+    }
     top = max(top, static_cast<uint32_t>(__shfl_xor(top, 1)));
     top = max(top, static_cast<uint32_t>(__shfl_xor(top, 2)));
     const MxScale s = mx_scale(top);
-    if (c < end) *reinterpret_cast<uint32_t*>(to.q + row * to.q_ld + c / 2) = mx_pack8(v, s.inv);
+    if (c < end) {
+      uint32_t w;
+      if constexpr (BF16 && VEC) w = mx_pack8(pairs, s);
+      else w = mx_pack8(v, s);
+      *reinterpret_cast<uint32_t*>(to.q + row * to.q_ld + c / 2) = w;
+    }
     if ((lane & 3) == 0) to.scale[row * to.s_ld + c / 32] = static_cast<uint8_t>(s.byte);
   }
 }
@@ -200,64 +249,111 @@ template <bool BF16, bool VEC, int MODE, bool BOTH>
 __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row, int tile_col,
                                            MxColumnsLds<BOTH>& lds) {
   const Mx4Source& a = p.from;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pair = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, pair = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c0 = tile_col * MXC_COLS, c = c0 + 2 * pair;
-  const int64_t r0 = tile_row * MXC_ROWS, mine = r0 + 32 * wave + 16 * h;
+  const int64_t r0 = tile_row * MXC_ROWS, r_wave = r0 + 32 * wave, mine = r_wave + 16 * h;
   constexpr int ES = BF16 ? 2 : 4;
+  typedef MxColumnsLds<BOTH> Lds;
   // Rows and columns behind the last read the last one again, so that no load waits behind
   // a branch, and count as zeros.  VEC: an even number of columns, pairs aligned.
   const int64_t left = a.rows - mine;
   const int seen = static_cast<int>(left < 16 ? left : 16);  // of the lane's rows, may be < 0
   const int c_in = c < a.cols ? c : (VEC ? a.cols - 2 : a.cols - 1);
   const int c_next = c + 1 < a.cols ? 1 : 0;
-  auto load = [&](const void* from, int64_t ld, float(&v)[2][16]) {
-    const char* at = static_cast<const char*>(from) +
-                     ((left > 0 ? mine : a.rows - 1) * ld + c_in) * ES;
+  const bool clip = __any(seen < 16 || c + 1 >= a.cols);
+  // each(i, address of row i's pair)
+  auto rows = [&](const void* from, int64_t ld, auto&& each) {
+    if (r_wave + 32 <= a.rows && ld < (int64_t{1} << 24)) {
+      // the wave's rows from one address, the lane's place in them in 32 bits
+      const char* at = static_cast<const char*>(from) + r_wave * ld * ES;
+      const uint32_t place = (static_cast<uint32_t>(16 * h) * static_cast<uint32_t>(ld) +
+                              static_cast<uint32_t>(c_in)) * ES;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if constexpr (VEC && BF16) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(at);
-        v[0][i] = mx_bf16(w & 0xFFFFu);
-        v[1][i] = mx_bf16(w >> 16);
-      } else if constexpr (VEC) {
-        const mx_f32x2 w = *reinterpret_cast<const mx_f32x2*>(at);
-        v[0][i] = w[0];
-        v[1][i] = w[1];
-      } else if constexpr (BF16) {
-        v[0][i] = mx_bf16(reinterpret_cast<const uint16_t*>(at)[0]);
-        v[1][i] = mx_bf16(reinterpret_cast<const uint16_t*>(at)[c_next]);
-      } else {
-        v[0][i] = reinterpret_cast<const float*>(at)[0];
-        v[1][i] = reinterpret_cast<const float*>(at)[c_next];
+      for (int i = 0; i < 16; ++i) each(i, at + i * ld * ES + place);
+    } else {
+      const char* at = static_cast<const char*>(from) +
+                       ((left > 0 ? mine : a.rows - 1) * ld + c_in) * ES;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        each(i, at);
+        at += i + 1 < seen ? ld * ES : 0;
       }
-      at += i + 1 < seen ? ld * ES : 0;
     }
   };
-  float v[2][16];
-  load(a.x, a.x_ld, v);
-  if constexpr (MODE == 1) {
-    float y[2][16];
-    load(a.y, a.y_ld, y);
+  auto put = [&](int t, const MxScale& s, nt_u32x2 w) {  // of column t of the pair
+    const int col = 2 * pair + t;
+    *reinterpret_cast<nt_u32x2*>(lds.q + col * Lds::LD + 16 * wave + 8 * h) = w;
+    if (h == 0) lds.scale[col][wave] = static_cast<uint8_t>(s.byte);
+  };
+  if constexpr (BF16 && VEC && MODE == 0 && !BOTH) {
+    // as it is: both columns' magnitudes at once, pairs of rows put together for the conversion
+    uint32_t w[16], two = 0;
+    rows(a.x, a.x_ld,
+         [&](int i, const char* at) { w[i] = *reinterpret_cast<const uint32_t*>(at); });
+    if (clip) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      v[0][i] = mx_pass(v[0][i], y[0][i], a.drop);
-      v[1][i] = mx_pass(v[1][i], y[1][i], a.drop);
+      for (int i = 0; i < 16; ++i) w[i] = i < seen && c < a.cols ? w[i] : 0u;
     }
-  }
-  if (__any(seen < 16 || c + 1 >= a.cols)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      v[0][i] = i < seen && c < a.cols ? v[0][i] : 0.0f;
-      v[1][i] = i < seen && c + 1 < a.cols ? v[1][i] : 0.0f;
+    for (int i = 0; i < 16; ++i) two = mx_larger2(two, w[i]);
+    two = mx_larger2(two, __shfl_xor(two, 32));
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const MxScale s = mx_scale(t ? two & 0xFFFF0000u : two << 16);
+      uint32_t rows2[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        rows2[i] =
+            __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], t ? 0x07060302u : 0x05040100u);
+      put(t, s, nt_u32x2{mx_pack8(rows2, s), mx_pack8(rows2 + 4, s)});
     }
-  }
-  if constexpr (MODE == 2) {
-    // four lanes share a call of the generator for a row: each makes one of four rows'
-    const uint64_t offset = drop_offset(a.drop);
-    const int k = lane & 3;
+  } else {
+    auto load = [&](const void* from, int64_t ld, float(&v)[2][16]) {
+      rows(from, ld, [&](int i, const char* at) {
+        if constexpr (VEC && BF16) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(at);
+          v[0][i] = mx_bf16(w & 0xFFFFu);
+          v[1][i] = __builtin_bit_cast(float, w & 0xFFFF0000u);
+        } else if constexpr (VEC) {
+          const mx_f32x2 w = *reinterpret_cast<const mx_f32x2*>(at);
+          v[0][i] = w[0];
+          v[1][i] = w[1];
+        } else if constexpr (BF16) {
+          v[0][i] = mx_bf16(reinterpret_cast<const uint16_t*>(at)[0]);
+          v[1][i] = mx_bf16(reinterpret_cast<const uint16_t*>(at)[c_next]);
+        } else {
+          v[0][i] = reinterpret_cast<const float*>(at)[0];
+          v[1][i] = reinterpret_cast<const float*>(at)[c_next];
+        }
+      });
+    };
+    float v[2][16];
+    load(a.x, a.x_ld, v);
+    if constexpr (MODE == 1) {
+      float y[2][16];
+      load(a.y, a.y_ld, y);
+      const float factor = a.drop.below ? a.drop.factor : 1.0f;
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(mine + i + k), c / 8);
+      for (int i = 0; i < 16; ++i) {
+        v[0][i] = mx_pass(v[0][i], y[0][i], factor);
+        v[1][i] = mx_pass(v[1][i], y[1][i], factor);
+      }
+    }
+    if (clip) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        v[0][i] = i < seen && c < a.cols ? v[0][i] : 0.0f;
+        v[1][i] = i < seen && c + 1 < a.cols ? v[1][i] : 0.0f;
+      }
+    }
+    if constexpr (MODE == 2) {
+      // four lanes share a call of the generator for a row: each makes one of four rows'
+      const uint64_t offset = drop_offset(a.drop);
+      const int k = lane & 3;
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(mine + i + k), c / 8);
 #define OSCARS_KEEP(K)                                                                       \
   {                                                                                          \
     const uint32_t u0 = mx_from_quad<K>(w.w[0]), u1 = mx_from_quad<K>(w.w[1]);               \
@@ -266,74 +362,73 @@ __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row
     v[0][i + K] = (u & 0xFFFFu) >= a.drop.below ? v[0][i + K] * a.drop.factor : 0.0f;        \
     v[1][i + K] = u >> 16 >= a.drop.below ? v[1][i + K] * a.drop.factor : 0.0f;              \
   }
-      OSCARS_KEEP(0)
-      OSCARS_KEEP(1)
-      OSCARS_KEEP(2)
-      OSCARS_KEEP(3)
+        OSCARS_KEEP(0)
+        OSCARS_KEEP(1)
+        OSCARS_KEEP(2)
+        OSCARS_KEEP(3)
 #undef OSCARS_KEEP
+      }
     }
-  }
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    uint32_t top = 0;
+    for (int t = 0; t < 2; ++t) {
+      float most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, mx_abs(v[t][i]));
-    top = max(top, static_cast<uint32_t>(__shfl_xor(top, 32)));
-    const MxScale s = mx_scale(top);
-    const int col = 2 * pair + t;
-    *reinterpret_cast<nt_u32x2*>(lds.q + col * MxColumnsLds<BOTH>::LD + 16 * wave + 8 * h) =
-        nt_u32x2{mx_pack8(v[t], s.inv), mx_pack8(v[t] + 8, s.inv)};
-    if (h == 0) lds.scale[col][wave] = static_cast<uint8_t>(s.byte);
-    if (p.sums) {  // in pairs of pairs: five additions deep
-      float sum[16];
+      for (int i = 0; i < 16; ++i) most = mx_larger(most, v[t][i]);
+      uint32_t top = mx_bits(most);
+      top = max(top, static_cast<uint32_t>(__shfl_xor(top, 32)));
+      const MxScale s = mx_scale(top);
+      put(t, s, nt_u32x2{mx_pack8(v[t], s), mx_pack8(v[t] + 8, s)});
+      if (p.sums) {  // in pairs of pairs: five additions deep
+        float sum[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i] = v[t][i];
+        for (int i = 0; i < 16; ++i) sum[i] = v[t][i];
 #pragma unroll
-      for (int n = 8; n > 0; n /= 2)
+        for (int n = 8; n > 0; n /= 2)
 #pragma unroll
-        for (int i = 0; i < n; ++i) sum[i] += sum[i + n];
-      const float other = __shfl_xor(sum[0], 32);
-      if (h == 0) lds.part[wave][col] = sum[0] + other;
+          for (int i = 0; i < n; ++i) sum[i] += sum[i + n];
+        const float other = __shfl_xor(sum[0], 32);
+        if (h == 0) lds.part[wave][2 * pair + t] = sum[0] + other;
+      }
     }
-  }
-  if constexpr (BOTH) {
-    // 16 lanes have a block of each of 16 rows: lane l comes to hold row l's largest
-    uint32_t m[16];
+    if constexpr (BOTH) {
+      // 16 lanes have a block of each of 16 rows: lane l comes to hold row l's largest
+      uint32_t m[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m[i] = max(mx_abs(v[0][i]), mx_abs(v[1][i]));
-    mx_fold<0x140, 16>(m, lane);  // with lane 15 - l,
-    mx_fold<0x141, 8>(m, lane);   // 7 - l of eight,
-    mx_fold<0x1B, 4>(m, lane);    // 3 - l of four,
-    mx_fold<0xB1, 2>(m, lane);    // 1 - l of two
-    const MxScale s = mx_scale(m[0]);
-    const int row0 = 32 * wave + 16 * h;
-    lds.row_scale[row0 + (lane & 15)][pair >> 4] = static_cast<uint8_t>(s.byte);
-    // bytes of four rows in a lane turn into four lanes' bytes of a row (a block with a NaN may
-    // have codes other than 0: it is its scale that counts)
-    const uint32_t turn1 = lane & 1 ? 0x03070105u : 0x06020400u;
-    const uint32_t turn2 = lane & 2 ? 0x03020706u : 0x05040100u;
+      for (int i = 0; i < 16; ++i) m[i] = mx_bits(mx_larger(__builtin_fabsf(v[0][i]), v[1][i]));
+      mx_fold<0x140, 16>(m, lane);  // with lane 15 - l,
+      mx_fold<0x141, 8>(m, lane);   // 7 - l of eight,
+      mx_fold<0x1B, 4>(m, lane);    // 3 - l of four,
+      mx_fold<0xB1, 2>(m, lane);    // 1 - l of two
+      const MxScale s = mx_scale(m[0]);
+      const int row0 = 32 * wave + 16 * h;
+      lds.row_scale[row0 + (lane & 15)][pair >> 4] = static_cast<uint8_t>(s.byte);
+      // bytes of four rows in a lane turn into four lanes' bytes of a row (a block with a NaN
+      // may have codes other than 0: it is its scale that counts)
+      const uint32_t turn1 = lane & 1 ? 0x03070105u : 0x06020400u;
+      const uint32_t turn2 = lane & 2 ? 0x03020706u : 0x05040100u;
 #define OSCARS_ROWS(I)                                                                           \
   {                                                                                              \
-    uint32_t w = mx_pack2<0>(0u, v[0][I], v[1][I], mx_from_row<I>(s.inv));                       \
-    w = mx_pack2<1>(w, v[0][I + 1], v[1][I + 1], mx_from_row<I + 1>(s.inv));                     \
-    w = mx_pack2<2>(w, v[0][I + 2], v[1][I + 2], mx_from_row<I + 2>(s.inv));                     \
-    w = mx_pack2<3>(w, v[0][I + 3], v[1][I + 3], mx_from_row<I + 3>(s.inv));                     \
+    uint32_t w = mx_pack2<0>(0u, v[0][I], v[1][I], mx_from_row<I>(s.s));                         \
+    w = mx_pack2<1>(w, v[0][I + 1], v[1][I + 1], mx_from_row<I + 1>(s.s));                       \
+    w = mx_pack2<2>(w, v[0][I + 2], v[1][I + 2], mx_from_row<I + 2>(s.s));                       \
+    w = mx_pack2<3>(w, v[0][I + 3], v[1][I + 3], mx_from_row<I + 3>(s.s));                       \
     w = __builtin_amdgcn_perm(mx_dpp<0xB1>(w), w, turn1);                                        \
     w = __builtin_amdgcn_perm(mx_dpp<0x4E>(w), w, turn2);                                        \
     *reinterpret_cast<uint32_t*>(&lds.row_q[row0 + I + (lane & 3)][pair & ~3]) = w;              \
   }
-    OSCARS_ROWS(0)
-    OSCARS_ROWS(4)
-    OSCARS_ROWS(8)
-    OSCARS_ROWS(12)
+      OSCARS_ROWS(0)
+      OSCARS_ROWS(4)
+      OSCARS_ROWS(8)
+      OSCARS_ROWS(12)
 #undef OSCARS_ROWS
+    }
   }
   __syncthreads();
   {
     const int col = tid >> 3, k = tid & 7;
     if (c0 + col < a.cols)
       *reinterpret_cast<nt_u32x4*>(p.to.q + (c0 + col) * p.to.q_ld + tile_row * 128 + 16 * k) =
-          *reinterpret_cast<const nt_u32x4*>(lds.q + col * MxColumnsLds<BOTH>::LD + 16 * k);
+          *reinterpret_cast<const nt_u32x4*>(lds.q + col * Lds::LD + 16 * k);
   }
   if (tid < MXC_COLS && c0 + tid < a.cols) {
     uint8_t* s = p.to.scale + (c0 + tid) * p.to.s_ld + tile_row * 8;
@@ -1071,13 +1166,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(Mx4Product a, c
     float v[8];
     mx_load8<X_BF16, VEC>(static_cast<const char*>(x) + r * x_ld * (X_BF16 ? 2 : 4), c, in, v);
     mx_clip8<VEC>(c, in, v);
-    uint32_t top = 0;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) top = max(top, mx_abs(v[t]));
+    uint32_t top = mx_top8(v);
     top = max(top, static_cast<uint32_t>(__shfl_xor(top, 1)));
     top = max(top, static_cast<uint32_t>(__shfl_xor(top, 2)));
     const MxScale s = mx_scale(top);
-    *reinterpret_cast<uint32_t*>(few_lds + r * ld + c / 2) = mx_pack8(v, s.inv);
+    *reinterpret_cast<uint32_t*>(few_lds + r * ld + c / 2) = mx_pack8(v, s);
     if ((lane & 3) == 0) scales[r * sld + c / 32] = static_cast<char>(s.byte);
   }
   __syncthreads();
