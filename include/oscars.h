@@ -571,6 +571,16 @@ int64_t oscars_linear_micro_backward_workspace(int64_t rows, int64_t in, int64_t
 oscars_status oscars_linear_micro_backward(const oscars_micro_gradients* g, void* workspace,
                                            int64_t workspace_bytes, void* hip_stream);
 
+/* A fully connected model in 4 bits: as oscars_quantized_model_bytes, oscars_quantize_model and
+ * oscars_evaluate_quantized, with the rows of every weight matrix, and the
+ * activations as they come, as oscars_quantize_micro gives them.  Per layer the
+ * rows' bytes, their scales and the biases, each from a multiple of 256 bytes on. */
+int64_t oscars_micro_model_bytes(const oscars_ctx* ctx);
+oscars_status oscars_quantize_model_micro(oscars_ctx* ctx, const float* params, void* model);
+oscars_status oscars_evaluate_micro(oscars_ctx* ctx, const void* model, const void* x,
+                                    const int32_t* y, int64_t n_rows, double* loss_sum,
+                                    int64_t* correct);
+
 /* Dropout by itself: out[r][c] = x[r][c] times the factor, rounded to the type, where
  * kept, else 0 (whatever x holds).  Its gradient is the same call on the output's.
  *   x, out  device [rows][..ld] of dtype, aligned to its elements; out may be x, with

@@ -139,6 +139,9 @@ _SIGS = {
     "oscars_linear_micro_backward_workspace": (_i64, [_i64, _i64, _i64, _i32]),
     "oscars_linear_micro_backward": (_i32, [_P(_Gradients), _vp, _i64, _vp]),
     "oscars_dropout": (_i32, [_vp, _i64, _vp, _i64, _i32, _P(_Dropout), _i64, _i64, _vp]),
+    "oscars_micro_model_bytes": (_i64, [_vp]),
+    "oscars_quantize_model_micro": (_i32, [_vp, _vp, _vp]),
+    "oscars_evaluate_micro": (_i32, [_vp, _vp, _vp, _vp, _i64, _P(ctypes.c_double), _P(_i64)]),
     "oscars_quantized_model_bytes": (_i64, [_vp]),
     "oscars_quantize_model": (_i32, [_vp, _vp, _vp]),
     "oscars_evaluate_quantized": (_i32, [_vp, _vp, _vp, _vp, _i64, _P(ctypes.c_double), _P(_i64)]),
@@ -922,12 +925,7 @@ class Context:
                                      ctypes.byref(loss), ctypes.byref(hits)), name)
         return float(loss.value), int(hits.value)
 
-    def quantize_model(self, params, out=None):
-        """The flat model ``params`` (device tensor [n_pad] fp32) in 8-bit integers,
-        a scale per output channel (oscars_quantize_model): one device tensor
-        for evaluate_i8.  Fully connected models only."""
-        import torch
-        need = int(_lib().oscars_quantized_model_bytes(self._h))
+    def _quantize_model(self, name, need, params, out):
         pp = _dev_ptr(params, torch.float32, "params")
         if params.numel() < self.n_pad:
             raise ValueError("params must hold n_pad floats")
@@ -936,19 +934,16 @@ class Context:
         op = _dev_ptr(out, torch.uint8, "out")
         if out.numel() < need:
             raise ValueError(f"a quantised model takes {need} bytes")
-        _check(_lib().oscars_quantize_model(self._h, pp, op), "oscars_quantize_model")
+        _check(getattr(_lib(), name)(self._h, pp, op), name)
         _used_on(self._stream, params, out)
         return out
 
-    def evaluate_i8(self, model, x, y, n_rows: Optional[int] = None):
-        """``evaluate`` with the products of the quantised ``model``
-        (oscars_evaluate_quantized)."""
-        import torch
+    def _evaluate_quantized(self, name, need, model, x, y, n_rows):
         n = int(x.shape[0] if n_rows is None else n_rows)
         if n > x.shape[0] or n > y.shape[0]:
             raise ValueError("n_rows exceeds the rows of x or y")
         mp = _dev_ptr(model, torch.uint8, "model")
-        if model.numel() < int(_lib().oscars_quantized_model_bytes(self._h)):
+        if model.numel() < need:
             raise ValueError("model is not a quantised model of this context")
         xdt = x.dtype if self.dtype == BF16 and x.dtype in (torch.int16, torch.uint16) else (
             torch.bfloat16 if self.dtype == BF16 else torch.float32)
@@ -956,10 +951,36 @@ class Context:
             raise ValueError("x must be [n_rows][d]")
         loss = ctypes.c_double(0.0)
         hits = _i64(0)
-        _check(_lib().oscars_evaluate_quantized(self._h, mp, _dev_ptr(x, xdt, "x"),
-                                         _dev_ptr(y, torch.int32, "y"), n, ctypes.byref(loss),
-                                         ctypes.byref(hits)), "oscars_evaluate_quantized")
+        _check(getattr(_lib(), name)(self._h, mp, _dev_ptr(x, xdt, "x"),
+                                     _dev_ptr(y, torch.int32, "y"), n, ctypes.byref(loss),
+                                     ctypes.byref(hits)), name)
         return float(loss.value), int(hits.value)
+
+    def quantize_model(self, params, out=None):
+        """The flat model ``params`` (device tensor [n_pad] fp32) in 8-bit integers,
+        a scale per output channel (oscars_quantize_model): one device tensor
+        for evaluate_i8.  Fully connected models only."""
+        return self._quantize_model("oscars_quantize_model",
+                                    int(_lib().oscars_quantized_model_bytes(self._h)), params, out)
+
+    def evaluate_i8(self, model, x, y, n_rows: Optional[int] = None):
+        """``evaluate`` with the products of the quantised ``model``
+        (oscars_evaluate_quantized)."""
+        return self._evaluate_quantized("oscars_evaluate_quantized",
+                                        int(_lib().oscars_quantized_model_bytes(self._h)), model,
+                                        x, y, n_rows)
+
+    def quantize_model_mx4(self, params, out=None):
+        """``quantize_model`` in microscaled 4-bit floating point
+        (oscars_quantize_model_micro), for evaluate_mx4."""
+        return self._quantize_model("oscars_quantize_model_micro",
+                                    int(_lib().oscars_micro_model_bytes(self._h)), params, out)
+
+    def evaluate_mx4(self, model, x, y, n_rows: Optional[int] = None):
+        """``evaluate`` with the products of the 4-bit ``model`` (oscars_evaluate_micro)."""
+        return self._evaluate_quantized("oscars_evaluate_micro",
+                                        int(_lib().oscars_micro_model_bytes(self._h)), model, x,
+                                        y, n_rows)
 
     def server_step(self, global_, replicas, weights: Sequence[float], momentum, lr: float,
                     beta: float = 0.9, nesterov: bool = True, weight_decay: float = 0.0,

@@ -174,26 +174,29 @@ def measure_step_ms(cfg, dataset, init, reps: int = 5) -> float:
     return float(np.median(times))
 
 
-def _check_int8(cfg, int8_eval: bool):
-    if int8_eval and cfg.is_cnn:
-        raise ValueError(f"{cfg.name}: evaluation in 8-bit integers is for fully connected models")
+def _check_quantized(cfg, int8_eval: bool, mx4_eval: bool):
+    if (int8_eval or mx4_eval) and cfg.is_cnn:
+        raise ValueError(f"{cfg.name}: evaluation in 8-bit integers or 4 bits is for fully "
+                         "connected models")
 
 
 def run_paradigm(cfg, dataset, init, eval_set, paradigm: str, schedule: SpeedSchedule,
                  base: float, time_budget: float, local_steps: int = 4, resolution: int = 8,
                  max_rounds: int = 100000, eval_every: int = 1,
                  return_model: bool = False, server: Optional[Dict] = None,
-                 int8_eval: bool = False) -> Dict:
+                 int8_eval: bool = False, mx4_eval: bool = False) -> Dict:
     """Train with one paradigm until the emulated cluster clock reaches
     ``time_budget`` (same unit as ``base``).  Returns per-round records (and
     the final global model as layers when ``return_model``).  ``server``: the
     arguments of OscarsRun.round_server, which then ends every round in the
     place of the average.  ``int8_eval``: every evaluation also with the model
-    in 8-bit integers (eval_loss_i8, eval_acc_i8); of fully connected models only."""
+    in 8-bit integers (eval_loss_i8, eval_acc_i8), ``mx4_eval``: in microscaled
+    4-bit floating point (eval_loss_mx4, eval_acc_mx4); of fully connected models
+    only."""
     import torch
 
     from .rounds import OscarsRun
-    _check_int8(cfg, int8_eval)
+    _check_quantized(cfg, int8_eval, mx4_eval)
     K = cfg.K
     if schedule.K != K:
         raise ValueError("schedule and workload disagree on K")
@@ -210,8 +213,10 @@ def run_paradigm(cfg, dataset, init, eval_set, paradigm: str, schedule: SpeedSch
     gpu_ms = 0.0
 
     def measure(rec):
-        for kind, int8 in (("", False), ("_i8", True))[:1 + int(int8_eval)]:
-            loss, hit = run.evaluate(x_eval, y_eval, int8)
+        kinds = [("", {})] + [("_i8", {"int8": True})] * int8_eval + [
+            ("_mx4", {"mx4": True})] * mx4_eval
+        for kind, how in kinds:
+            loss, hit = run.evaluate(x_eval, y_eval, **how)
             rec["eval_loss" + kind] = loss / n_eval
             rec["eval_acc" + kind] = hit / n_eval
         return rec
@@ -353,12 +358,13 @@ def time_to_loss(result: Dict, target: float) -> Optional[float]:
 
 def compare(cfg, schedule: SpeedSchedule, time_budget_steps: float, local_steps: int = 4,
             resolution: int = 8, n_eval: int = 10000, base: Optional[float] = None,
-            eval_every: int = 1, server: Optional[Dict] = None, int8_eval: bool = False) -> Dict:
+            eval_every: int = 1, server: Optional[Dict] = None, int8_eval: bool = False,
+            mx4_eval: bool = False) -> Dict:
     """The three paradigms on one workload and one emulated cluster.  The
-    budget is in units of the speed-1 step time; ``server`` and ``int8_eval`` as
-    for run_paradigm."""
+    budget is in units of the speed-1 step time; ``server``, ``int8_eval``
+    and ``mx4_eval`` as for run_paradigm."""
     import workload
-    _check_int8(cfg, int8_eval)
+    _check_quantized(cfg, int8_eval, mx4_eval)
     dataset = workload.gen_dataset(cfg)
     init = workload.gen_init(cfg)
     eval_set = workload.gen_eval_set(cfg, n_eval)
@@ -374,7 +380,8 @@ def compare(cfg, schedule: SpeedSchedule, time_budget_steps: float, local_steps:
         t0 = time.perf_counter()
         res = run_paradigm(cfg, dataset, init, eval_set, p, schedule, base_ms, budget,
                            local_steps=local_steps, resolution=resolution,
-                           eval_every=eval_every, server=server, int8_eval=int8_eval)
+                           eval_every=eval_every, server=server, int8_eval=int8_eval,
+                           mx4_eval=mx4_eval)
         res["wall_s"] = time.perf_counter() - t0
         results[p] = res
     # target: the best loss BSP reached within the budget
@@ -396,9 +403,9 @@ def compare(cfg, schedule: SpeedSchedule, time_budget_steps: float, local_steps:
             "curve": [(round(rec["clock"], 4), rec.get("eval_loss"), rec.get("eval_acc"))
                       for rec in recs if "eval_loss" in rec],
         }
-        if int8_eval:
-            out["paradigms"][p]["final_eval_loss_i8"] = last_eval["eval_loss_i8"]
-            out["paradigms"][p]["final_eval_acc_i8"] = last_eval["eval_acc_i8"]
+        for kind in ["_i8"] * int8_eval + ["_mx4"] * mx4_eval:
+            out["paradigms"][p]["final_eval_loss" + kind] = last_eval["eval_loss" + kind]
+            out["paradigms"][p]["final_eval_acc" + kind] = last_eval["eval_acc" + kind]
     out["bsp_best_loss"] = target
     return out
 
@@ -431,6 +438,8 @@ def main(argv=None):
     ap.add_argument("--server-beta", type=float, default=None, help="its momentum (0.9)")
     ap.add_argument("--int8-eval", action="store_true",
                     help="evaluate the global model in 8-bit integers too")
+    ap.add_argument("--mx4-eval", action="store_true",
+                    help="evaluate the global model in microscaled 4-bit floating point too")
     ap.add_argument("--out", default=None, help="also write the JSON here")
     ap.add_argument("--measured", type=int, default=0, metavar="ROUNDS",
                     help="instead: this many rounds with the plan from measured times on the "
@@ -440,9 +449,9 @@ def main(argv=None):
     if args.server_beta is not None and args.server_lr is None:
         ap.error("--server-beta belongs to --server-lr")
     if args.measured > 0:
-        if args.server_lr is not None or args.int8_eval:
+        if args.server_lr is not None or args.int8_eval or args.mx4_eval:
             ap.error("--measured rounds end with the average and evaluate nothing: "
-                     "no --server-lr, no --int8-eval")
+                     "no --server-lr, no --int8-eval, no --mx4-eval")
         cfg = _measured_cfg()
         sched = BatchSchedule(MEASURED_BATCHES,
                               {args.measured // 2: tuple(reversed(MEASURED_BATCHES))})
@@ -463,7 +472,7 @@ def main(argv=None):
                   server=None if args.server_lr is None else {
                       "lr": args.server_lr,
                       "beta": 0.9 if args.server_beta is None else args.server_beta},
-                  int8_eval=args.int8_eval)
+                  int8_eval=args.int8_eval, mx4_eval=args.mx4_eval)
     line = json.dumps(res)
     print(line)
     if args.out:

@@ -1930,34 +1930,40 @@ struct I8Layout {
 
 constexpr int64_t kI8EvalRows = 8192;  // rows of an evaluation's pass
 
-// oscars_evaluate_quantized's temporaries behind EvalLayout's: quantised rows and their
-// scales, two activations, logits.
-struct I8EvalLayout {
+extern "C++" {
+// The temporaries of a quantised evaluation behind EvalLayout's: quantised rows (q_bytes a row at
+// most) and their scales (s_bytes), two activations, logits.
+struct QuantEvalLayout {
   int64_t rows, xq, scale, act[2], logits, end;
-  I8EvalLayout(const oscars_ctx* c, int64_t n_rows) {
+  QuantEvalLayout(const oscars_ctx* c, int64_t n_rows, int64_t q_bytes, int64_t s_bytes) {
     const int64_t passes = (n_rows + kI8EvalRows - 1) / kI8EvalRows;
     rows = (n_rows + passes - 1) / passes;
-    int64_t in = 0, hidden = 0;
-    for (int l = 0; l < c->L; ++l) {
-      in = std::max(in, I8Layout::ld(c->dims[l]));
-      if (l > 0) hidden = std::max<int64_t>(hidden, c->ld[l]);
-    }
+    int64_t hidden = 0;
+    for (int l = 1; l < c->L; ++l) hidden = std::max<int64_t>(hidden, c->ld[l]);
     xq = EvalLayout(n_rows).end;
-    scale = xq + round_up(rows * in, 256);
-    act[0] = scale + round_up(rows * 4, 256);
+    scale = xq + round_up(rows * q_bytes, 256);
+    act[0] = scale + round_up(rows * s_bytes, 256);
     act[1] = act[0] + round_up(rows * hidden * static_cast<int64_t>(c->esize), 256);
     logits = act[1] + round_up(rows * hidden * static_cast<int64_t>(c->esize), 256);
     end = logits + round_up(rows * c->ld[c->L] * 4, 256);
   }
 };
+int64_t widest_input(const oscars_ctx* c) {
+  int64_t in = 0;
+  for (int l = 0; l < c->L; ++l) in = std::max<int64_t>(in, c->dims[l]);
+  return in;
+}
+QuantEvalLayout i8_eval_layout(const oscars_ctx* c, int64_t n_rows) {
+  return QuantEvalLayout(c, n_rows, I8Layout::ld(static_cast<int32_t>(widest_input(c))), 4);
+}
 
-hipError_t run_evaluate_i8(oscars_ctx* c, const void* model, const void* x, const int32_t* y,
-                           int64_t n_rows, void* buf, double* loss_sum, int64_t* correct) {
+// layer(l, in, in_ld, out, n): layer l's outputs of n rows, hidden ones in the model's type.
+template <typename Layer>
+hipError_t run_evaluate_quantized(oscars_ctx* c, const QuantEvalLayout& tmp, const void* x,
+                                  const int32_t* y, int64_t n_rows, void* buf, double* loss_sum,
+                                  int64_t* correct, Layer&& layer) {
   const EvalLayout lay(n_rows);
-  const I8EvalLayout tmp(c, n_rows);
-  const I8Layout m(c);
   char* base = static_cast<char*>(buf);
-  const char* mod = static_cast<const char*>(model);
   struct Results {
     double loss;
     int64_t hits;
@@ -1965,8 +1971,6 @@ hipError_t run_evaluate_i8(oscars_ctx* c, const void* model, const void* x, cons
   Results* d_res = reinterpret_cast<Results*>(base);
   float* d_loss = reinterpret_cast<float*>(base + lay.loss);
   int32_t* d_hit = reinterpret_cast<int32_t*>(base + lay.hit);
-  int8_t* xq = reinterpret_cast<int8_t*>(base + tmp.xq);
-  float* scale = reinterpret_cast<float*>(base + tmp.scale);
   float* logits = reinterpret_cast<float*>(base + tmp.logits);
   const int L = c->L;
   hipError_t e = hipSuccess;
@@ -1975,17 +1979,8 @@ hipError_t run_evaluate_i8(oscars_ctx* c, const void* model, const void* x, cons
     const void* in = static_cast<const char*>(x) + i0 * c->dims[0] * static_cast<int64_t>(c->esize);
     int64_t in_ld = c->dims[0];
     for (int l = 1; l <= L && e == hipSuccess; ++l) {
-      const int64_t q_ld = I8Layout::ld(c->dims[l - 1]);
-      e = launch_quantize_rows(QuantArgs{in, in_ld, c->bf16, n, c->dims[l - 1], xq, q_ld, scale},
-                               c->stream);
-      if (e != hipSuccess) break;
       void* out = l < L ? static_cast<void*>(base + tmp.act[l & 1]) : static_cast<void*>(logits);
-      e = launch_matmul_i8(
-          MatmulI8Args{xq, q_ld, scale, reinterpret_cast<const int8_t*>(mod + m.w[l]), q_ld,
-                       reinterpret_cast<const float*>(mod + m.s[l]),
-                       reinterpret_cast<const float*>(mod + m.b[l]), l < L, n, c->dims[l - 1],
-                       c->dims[l], out, c->ld[l], l < L && c->bf16},
-          c->stream);
+      e = layer(l, in, in_ld, out, n);
       in = out;
       in_ld = c->ld[l];
     }
@@ -2006,6 +2001,56 @@ hipError_t run_evaluate_i8(oscars_ctx* c, const void* model, const void* x, cons
   *correct = h.hits;
   return hipSuccess;
 }
+
+hipError_t run_evaluate_i8(oscars_ctx* c, const void* model, const void* x, const int32_t* y,
+                           int64_t n_rows, void* buf, double* loss_sum, int64_t* correct) {
+  const QuantEvalLayout tmp = i8_eval_layout(c, n_rows);
+  const I8Layout m(c);
+  const char* mod = static_cast<const char*>(model);
+  int8_t* xq = reinterpret_cast<int8_t*>(static_cast<char*>(buf) + tmp.xq);
+  float* scale = reinterpret_cast<float*>(static_cast<char*>(buf) + tmp.scale);
+  return run_evaluate_quantized(
+      c, tmp, x, y, n_rows, buf, loss_sum, correct,
+      [&](int l, const void* in, int64_t in_ld, void* out, int64_t n) {
+        const int64_t q_ld = I8Layout::ld(c->dims[l - 1]);
+        const hipError_t e = launch_quantize_rows(
+            QuantArgs{in, in_ld, c->bf16, n, c->dims[l - 1], xq, q_ld, scale}, c->stream);
+        if (e != hipSuccess) return e;
+        return launch_matmul_i8(
+            MatmulI8Args{xq, q_ld, scale, reinterpret_cast<const int8_t*>(mod + m.w[l]), q_ld,
+                         reinterpret_cast<const float*>(mod + m.s[l]),
+                         reinterpret_cast<const float*>(mod + m.b[l]), l < c->L, n,
+                         c->dims[l - 1], c->dims[l], out, c->ld[l], l < c->L && c->bf16},
+            c->stream);
+      });
+}
+
+// What an evaluation checks, allocates and frees around run(buf).
+template <typename Run>
+oscars_status evaluate_quantized(oscars_ctx* c, const void* model, const void* x, const int32_t* y,
+                                 int64_t n_rows, double* loss_sum, int64_t* correct,
+                                 int64_t (*bytes)(const oscars_ctx*, int64_t), Run&& run) {
+  const oscars_status st =
+      check_evaluate(c, static_cast<const float*>(model), x, y, n_rows, loss_sum, correct);
+  if (st != OSCARS_OK) return st;
+  if (c->cnn) return OSCARS_E_INVALID;
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  hipError_t e = hipStreamIsCapturing(c->stream, &cap);
+  if (e != hipSuccess) return hip_fail(e);
+  if (cap != hipStreamCaptureStatusNone) return OSCARS_E_STATE;
+  void* buf = nullptr;
+  e = hipMalloc(&buf, static_cast<size_t>(bytes(c, n_rows)));
+  if (e != hipSuccess) {
+    if (e != hipErrorOutOfMemory) return hip_fail(e);
+    (void)hipGetLastError();
+    return OSCARS_E_NOMEM;
+  }
+  e = run(buf);
+  const hipError_t f = hipFree(buf);  // waits for the device
+  if (e == hipSuccess) e = f;
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+}  // extern "C++"
 
 }  // namespace
 
@@ -2119,25 +2164,12 @@ oscars_status oscars_quantize_model(oscars_ctx* c, const float* params, void* mo
 oscars_status oscars_evaluate_quantized(oscars_ctx* c, const void* model, const void* x,
                                         const int32_t* y, int64_t n_rows, double* loss_sum,
                                         int64_t* correct) {
-  const oscars_status st =
-      check_evaluate(c, static_cast<const float*>(model), x, y, n_rows, loss_sum, correct);
-  if (st != OSCARS_OK) return st;
-  if (c->cnn) return OSCARS_E_INVALID;
-  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-  hipError_t e = hipStreamIsCapturing(c->stream, &cap);
-  if (e != hipSuccess) return hip_fail(e);
-  if (cap != hipStreamCaptureStatusNone) return OSCARS_E_STATE;
-  void* buf = nullptr;
-  e = hipMalloc(&buf, static_cast<size_t>(I8EvalLayout(c, n_rows).end));
-  if (e != hipSuccess) {
-    if (e != hipErrorOutOfMemory) return hip_fail(e);
-    (void)hipGetLastError();
-    return OSCARS_E_NOMEM;
-  }
-  e = run_evaluate_i8(c, model, x, y, n_rows, buf, loss_sum, correct);
-  const hipError_t f = hipFree(buf);  // waits for the device
-  if (e == hipSuccess) e = f;
-  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+  return evaluate_quantized(
+      c, model, x, y, n_rows, loss_sum, correct,
+      [](const oscars_ctx* k, int64_t n) { return i8_eval_layout(k, n).end; },
+      [&](void* buf) {
+        return run_evaluate_i8(c, model, x, y, n_rows, buf, loss_sum, correct);
+      });
 }
 
 namespace {
@@ -2205,6 +2237,48 @@ struct Mx4Grads {
     end = part + round_up(mx4_sum_parts(rows) * outs * 4, 256);
   }
 };
+// A model in 4 bits: byte offsets of layer l's entries, scales and biases.
+struct Mx4Layout {
+  int64_t w[OSCARS_MAX_LAYERS + 1], s[OSCARS_MAX_LAYERS + 1], b[OSCARS_MAX_LAYERS + 1], end;
+  explicit Mx4Layout(const oscars_ctx* c) {
+    end = 0;
+    for (int l = 1; l <= c->L; ++l) {
+      w[l] = end;
+      s[l] = w[l] + round_up(c->dims[l] * mx4_bytes(c->dims[l - 1]), 256);
+      b[l] = s[l] + round_up(c->dims[l] * mx4_scales(c->dims[l - 1]), 256);
+      end = b[l] + round_up(c->dims[l] * int64_t{4}, 256);
+    }
+  }
+};
+extern "C++" QuantEvalLayout mx4_eval_layout(const oscars_ctx* c, int64_t n_rows) {
+  const int64_t in = widest_input(c);
+  return QuantEvalLayout(c, n_rows, mx4_bytes(in), mx4_scales(in));
+}
+hipError_t run_evaluate_mx4(oscars_ctx* c, const void* model, const void* x, const int32_t* y,
+                            int64_t n_rows, void* buf, double* loss_sum, int64_t* correct) {
+  const QuantEvalLayout tmp = mx4_eval_layout(c, n_rows);
+  const Mx4Layout m(c);
+  const char* mod = static_cast<const char*>(model);
+  uint8_t* xq = static_cast<uint8_t*>(buf) + tmp.xq;
+  uint8_t* scale = static_cast<uint8_t*>(buf) + tmp.scale;
+  return run_evaluate_quantized(
+      c, tmp, x, y, n_rows, buf, loss_sum, correct,
+      [&](int l, const void* in, int64_t in_ld, void* out, int64_t n) {
+        const int width = c->dims[l - 1];
+        const Mx4Rows q{xq, mx4_bytes(width), scale, mx4_scales(width)};
+        const hipError_t e = launch_mx4_rows(
+            Mx4Source{in, in_ld, c->bf16, n, width, nullptr, 0, DropArgs{}}, q, c->stream);
+        if (e != hipSuccess) return e;
+        return launch_mx4_product(
+            Mx4Product{q.q, q.q_ld, q.scale, q.s_ld,
+                       reinterpret_cast<const uint8_t*>(mod + m.w[l]), mx4_bytes(width),
+                       reinterpret_cast<const uint8_t*>(mod + m.s[l]), mx4_scales(width),
+                       reinterpret_cast<const float*>(mod + m.b[l]), l < c->L, n, width,
+                       c->dims[l], out, c->ld[l], l < c->L && c->bf16, DropArgs{}},
+            c->stream);
+      });
+}
+
 bool mx4_grad_sizes_ok(int64_t rows, int64_t in, int64_t outs) {
   return rows >= 0 && rows <= MX4_MAX_COLS && in >= 1 && in <= OSCARS_MAX_WIDTH && outs >= 1 &&
          outs <= OSCARS_MAX_WIDTH &&
@@ -2396,6 +2470,42 @@ oscars_status oscars_linear_micro_backward(const oscars_micro_gradients* g, void
        rows, outs, in, g->dx, g->dx_ld, g->x_dtype == OSCARS_BF16, DropArgs{}}};
   if (e == hipSuccess) e = launch_mx4_products(p, dx ? 2 : 1, s);
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+int64_t oscars_micro_model_bytes(const oscars_ctx* c) {
+  return !c || c->cnn ? 0 : Mx4Layout(c).end;
+}
+
+oscars_status oscars_quantize_model_micro(oscars_ctx* c, const float* params, void* model) {
+  if (!c || c->cnn || !params || !model || !aligned16(params) || !aligned16(model))
+    return OSCARS_E_INVALID;
+  const Mx4Layout m(c);
+  if (overlap(model, m.end, params, c->n_pad * 4)) return OSCARS_E_INVALID;
+  char* base = static_cast<char*>(model);
+  hipError_t e = hipSuccess;
+  for (int l = 1; l <= c->L && e == hipSuccess; ++l) {
+    const int in = c->dims[l - 1], outs = c->dims[l];
+    e = launch_mx4_rows(
+        Mx4Source{params + c->w_off[l], in, false, outs, in, nullptr, 0, DropArgs{}},
+        Mx4Rows{reinterpret_cast<uint8_t*>(base + m.w[l]), mx4_bytes(in),
+                reinterpret_cast<uint8_t*>(base + m.s[l]), mx4_scales(in)},
+        c->stream);
+    if (e == hipSuccess)
+      e = launch_broadcast(params + c->b_off[l], reinterpret_cast<float*>(base + m.b[l]), 1, outs,
+                           round_up(outs, 4), c->stream);
+  }
+  return e == hipSuccess ? OSCARS_OK : hip_fail(e);
+}
+
+oscars_status oscars_evaluate_micro(oscars_ctx* c, const void* model, const void* x,
+                                    const int32_t* y, int64_t n_rows, double* loss_sum,
+                                    int64_t* correct) {
+  return evaluate_quantized(
+      c, model, x, y, n_rows, loss_sum, correct,
+      [](const oscars_ctx* k, int64_t n) { return mx4_eval_layout(k, n).end; },
+      [&](void* buf) {
+        return run_evaluate_mx4(c, model, x, y, n_rows, buf, loss_sum, correct);
+      });
 }
 
 oscars_status oscars_dropout(void* out, int64_t out_ld, const void* x, int64_t x_ld, int32_t dtype,

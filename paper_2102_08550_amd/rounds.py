@@ -57,6 +57,7 @@ class OscarsRun:
         self.weights = paper_weights(cfg.K)
         self.momentum = None   # of round_server
         self.quantized = None  # of evaluate(int8=True)
+        self.quantized_mx4 = None  # of evaluate(mx4=True)
 
     def local_steps(self, tau: Sequence[int]):
         self.ctx.local_steps(self.replicas, self.x, self.y, self.offsets, self.seed, tau,
@@ -96,9 +97,15 @@ class OscarsRun:
                              nesterov=nesterov, weight_decay=weight_decay, plain_lr=plain_lr,
                              plain_layers=plain_layers)
 
-    def evaluate(self, x, y, int8: bool = False):
+    def evaluate(self, x, y, int8: bool = False, mx4: bool = False):
         """Held-out (summed loss, correct count) of the global model; ``int8``:
-        with its weights and activations in 8-bit integers."""
+        with its weights and activations in 8-bit integers; ``mx4``: in
+        microscaled 4-bit floating point."""
+        if int8 and mx4:
+            raise ValueError("one of int8 and mx4")
+        if mx4:
+            self.quantized_mx4 = self.ctx.quantize_model_mx4(self.g, out=self.quantized_mx4)
+            return self.ctx.evaluate_mx4(self.quantized_mx4, x, y)
         if not int8:
             return self.ctx.evaluate(self.g, x, y)
         self.quantized = self.ctx.quantize_model(self.g, out=self.quantized)

@@ -551,3 +551,120 @@ def test_two_graphs_and_another_stream(P):
         assert torch.equal(r, want[0])
     for r in results[2::3]:
         assert torch.equal(r, dropped)
+
+
+# ------------------------------------------------------------------ models
+
+def _losses(z, y):
+    """(summed loss, rows whose label has the largest logit) in float64."""
+    z = z.astype(np.float64)
+    top = z.max(axis=1)
+    mine = z[np.arange(len(z)), y]
+    return float((np.log(np.exp(z - top[:, None]).sum(axis=1)) + top - mine).sum()), \
+        int((mine == top).sum())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dims,n", [((24, 10), 7), ((784, 512, 256, 10), 300),
+                                    ((1000, 520, 136, 40, 3), 257), ((64, 48, 10), 20000)])
+def test_evaluate_mx4(P, dims, n, dtype):
+    """Loss and hits from the logits that the layers give one by one (which the other
+    tests hold to the oracle), and of a single layer from the oracle's."""
+    import torch
+    rng = np.random.default_rng(n)
+    ctx = P.Context(dims, P.FP32 if dtype == "fp32" else P.BF16, 1, 8)
+    try:
+        init = [((2 * rng.random((o, i)) - 1).astype(np.float32) / np.sqrt(i),
+                 (2 * rng.random(o) - 1).astype(np.float32) / np.sqrt(i))
+                for i, o in zip(dims[:-1], dims[1:])]
+        init = [(w.astype(np.float32), b.astype(np.float32)) for w, b in init]
+        params = torch.from_numpy(ctx.pack(init)).cuda()
+        x, y = _rows(rng, n, dims[0], dtype), rng.integers(0, dims[-1], n)
+        model = ctx.quantize_model_mx4(params)
+        passes = -(-n // 8192)
+        rows = -(-n // passes)
+        logits = []
+        for at in range(0, n, rows):
+            a = _dev(x[at:at + rows], dtype)
+            for l, (w, b) in enumerate(init):
+                last = l == len(init) - 1
+                wq = P.quantize_mx4(_dev(w))
+                a = P.matmul_mx4(*P.quantize_mx4(a), *wq, dims[l], bias=_dev(b), relu=not last,
+                                 out_dtype=torch.float32 if last else _type(dtype))
+            logits.append(a.cpu().numpy())
+        z = np.concatenate(logits)
+        want_loss, want_hits = _losses(z, y)
+        dx = _dev(x, dtype)
+        dy = torch.from_numpy(y.astype(np.int32)).cuda()
+        loss, hits = ctx.evaluate_mx4(model, dx, dy)
+        say(f"{dims} {dtype}: 4 bits {loss / n:.5f} {hits}, model {ctx.evaluate(params, dx, dy)}")
+        assert hits == want_hits
+        # a row's loss in fp32: the exponentials' sum and logarithm, and the difference of
+        # logits, some 8 roundings of numbers up to |z| + log C
+        size = np.abs(z).max() + np.log(dims[-1]) + 1
+        assert abs(loss - want_loss) <= n * 8 * 2.0 ** -23 * size
+        if len(dims) == 2:
+            xv, wv = mx4.rounded(x), mx4.rounded(init[0][0])
+            want = mx4.layer(xv, wv, init[0][1])
+            assert (np.abs(z - want) <= _bound(xv, wv, init[0][1], want, "fp32")).all()
+        again = ctx.evaluate_mx4(model, dx, dy, n_rows=max(1, n // 2))
+        assert 0 <= again[1] <= hits
+    finally:
+        ctx.close()
+
+
+def test_evaluate_mx4_refusals(P):
+    import torch
+    cnn = P.Context((8 * 8 * 3, 10), P.FP32, 1, 4, cnn=((8, 8, 3), ((16, 1),)))
+    mlp = P.Context((24, 10), P.FP32, 1, 4)
+    try:
+        with pytest.raises(P.OscarsError):
+            cnn.quantize_model_mx4(torch.zeros(cnn.n_pad, device="cuda"))
+        params = torch.zeros(mlp.n_pad, device="cuda")
+        model = mlp.quantize_model_mx4(params)
+        x, y = torch.zeros(5, 24, device="cuda"), torch.zeros(5, dtype=torch.int32, device="cuda")
+        with pytest.raises(ValueError):
+            mlp.evaluate_mx4(model, x, y, n_rows=6)
+        with pytest.raises(ValueError):
+            mlp.evaluate_mx4(model[:-256], x, y)
+        with pytest.raises(ValueError):
+            mlp.quantize_model_mx4(params[:-64])
+        with pytest.raises(TypeError):
+            mlp.evaluate_mx4(model, x.bfloat16(), y)
+        with pytest.raises(P.OscarsError):
+            cnn.evaluate_mx4(torch.zeros(64, dtype=torch.uint8, device="cuda"),
+                             torch.zeros(5, 192, device="cuda"), y)
+    finally:
+        cnn.close()
+        mlp.close()
+
+
+def test_rounds_and_paradigms_evaluate_in_4_bits(P):
+    """run_paradigm with the 4-bit evaluation beside the ordinary and the 8-bit one:
+    what the rounds by hand give; without it, records as before."""
+    import torch
+    import workload
+    from paper_2102_08550_amd import controller as C
+    from paper_2102_08550_amd import rounds as R
+    cfg = workload.Config("mlp-mx4", (40, 32, 10), workload.FP32, K=2, n_rows=400, batch=16,
+                          tau_rule="given", tau_given=(2, 2))
+    ds, init = workload.gen_dataset(cfg), workload.gen_init(cfg)
+    ev = workload.gen_eval_set(cfg, 100)
+    sched = C.SpeedSchedule([1, 1])
+    res = C.run_paradigm(cfg, ds, init, ev, "local", sched, 1.0, 1e9, local_steps=2, max_rounds=3,
+                         int8_eval=True, mx4_eval=True)
+    run = R.OscarsRun(cfg, ds, init)
+    try:
+        for _ in range(3):
+            run.round([2] * 2)
+        x, y = torch.from_numpy(ev.x).cuda(), torch.from_numpy(ev.y.astype(np.int32)).cuda()
+        loss, hits = run.evaluate(x, y, mx4=True)
+        with pytest.raises(ValueError):
+            run.evaluate(x, y, int8=True, mx4=True)
+    finally:
+        run.close()
+    last = res["records"][-1]
+    assert last["eval_loss_mx4"] == loss / 100 and last["eval_acc_mx4"] == hits / 100
+    assert {"eval_loss", "eval_loss_i8"} <= set(last)
+    plain = C.run_paradigm(cfg, ds, init, ev, "local", sched, 1.0, 1e9, local_steps=2, max_rounds=1)
+    assert not any("mx4" in k or "i8" in k for r in plain["records"] for k in r)
