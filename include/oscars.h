@@ -540,7 +540,7 @@ oscars_status oscars_linear_micro(void* out, int64_t out_ld, int32_t out_dtype, 
 /* The gradients of oscars_linear_micro's layer, straight through the rounding to 4 bits
  * Q:  dz = dy where the layer passed its output on, times dropout's factor (fp32);
  *   dx = Q(dz) Q(w')  along the outputs,  dw = Q(dz') Q(x')  along the rows,
- *   db[o] = sum_r dz[r][o].
+ *   db[o] = sum_r dz[r][o]  (held in 64 bits, rounded once).
  * What the layer passed on is y > 0 (or NaN) where its output y is given, which a layer with
  * a ReLU needs and dropout then asks for nothing else; without y dropout's choice is
  * drawn again from the options of the forward call.

@@ -557,6 +557,12 @@ def _micro_shapes(rows: int, cols: int):
     return (rows, (cols + 255) // 256 * 128), (rows, (cols + 511) // 512 * 16)
 
 
+def _count(q, what) -> int:
+    if not isinstance(q, torch.Tensor) or q.dim() != 2:
+        raise TypeError(f"{what} must be a matrix of quantised rows")
+    return q.shape[0]
+
+
 def _micro_rows(q, scale, rows, cols, device, what):
     """(pointer, row stride, scales' pointer, row stride) of quantised rows."""
     if (not isinstance(q, torch.Tensor) or not isinstance(scale, torch.Tensor)
@@ -640,8 +646,7 @@ def quantize_mx4(x, transposed: bool = False, out=None, stream=None):
 def dequantize_mx4(q, scale, columns: int, dtype=None, out=None, stream=None):
     """The values of quantised rows of ``columns`` entries (oscars_dequantize_micro), in
     fp32 by default."""
-    dev = q.device
-    n = q.shape[0]
+    n, dev = _count(q, "q"), q.device
     qp, qld, sp, sld = _micro_rows(q, scale, n, int(columns), dev, "q")
     out, op, old, odt = _result(out, n, int(columns), torch.float32, dtype, dev, stream)
     if n == 0:
@@ -660,8 +665,7 @@ def matmul_mx4(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool =
     and weights ``wq`` [outputs][..] as quantize_mx4 gives them, of ``in_features``
     entries each; ``dropout``: ``(p, seed)`` or ``(p, seed, offset)`` as in ``dropout``;
     fp32 by default.  Returns ``out``."""
-    dev = xq.device
-    n, outs, cols = xq.shape[0], wq.shape[0], int(in_features)
+    n, outs, cols, dev = _count(xq, "xq"), _count(wq, "wq"), int(in_features), xq.device
     xp, xld, xsp, xsld = _micro_rows(xq, xscale, n, cols, dev, "xq")
     wp, wld, wsp, wsld = _micro_rows(wq, wscale, outs, cols, dev, "wq")
     out, op, old, odt = _result(out, n, outs, torch.float32, out_dtype, dev, stream)
@@ -687,7 +691,7 @@ def linear_mx4(x, wq, wscale, bias=None, relu: bool = False, dropout=None, out_d
     dev = x.device
     xp, n, xld, cols = _rows(x, x.dtype, dev, "x")
     dt = _float_type(x.dtype, "x")
-    outs = wq.shape[0]
+    outs = _count(wq, "wq")
     wp, wld, wsp, wsld = _micro_rows(wq, wscale, outs, cols, dev, "wq")
     out, op, old, odt = _result(out, n, outs, x.dtype, out_dtype, dev, stream)
     drop, offset = _dropout_options(dropout, dev)

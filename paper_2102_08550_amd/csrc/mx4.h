@@ -47,11 +47,12 @@ int64_t mx4_column_tiles(int64_t rows, int cols);
 hipError_t launch_mx4_columns(const Mx4Source& a, const Mx4Rows& to, hipStream_t s);
 
 // What the gradients multiply: dz by columns and, with z_rows.q, by rows; x by columns;
-// and dz's columns' sums, or nullptr; then part holds mx4_sum_parts(rows) x cols floats.
+// and dz's columns' sums, or nullptr; part holds mx4_sum_parts(rows) x cols doubles.
 struct Mx4Gradient {
   Mx4Source z, x;
   Mx4Rows z_rows, z_columns, x_columns;
-  float *sums, *part;
+  float* sums;
+  double* part;
 };
 int64_t mx4_sum_parts(int64_t rows);
 hipError_t launch_mx4_gradient(const Mx4Gradient& g, hipStream_t s);

@@ -206,14 +206,15 @@ struct Mx4Columns {
   Mx4Source from;
   Mx4Rows to;
   Mx4Rows rows;  // BOTH
-  float* sums;   // of the columns, a row of them for each 256 of x; or nullptr
+  float* sums;   // of the columns, held in 64 bits, or nullptr:
+  double* part;  // where they go for each 256 rows, if there are more
 };
 template <bool BOTH>
 struct MxColumnsLds {
   static constexpr int LD = 128 + 16;  // 16 more: neighbouring columns start in other banks
   __attribute__((aligned(16))) uint8_t q[MXC_COLS * LD];
   __attribute__((aligned(16))) uint8_t scale[MXC_COLS][8];
-  float part[8][MXC_COLS];
+  double part[8][MXC_COLS];
   __attribute__((aligned(16))) uint8_t row_q[BOTH ? MXC_ROWS : 1][32];
   __attribute__((aligned(16))) uint8_t row_scale[BOTH ? MXC_ROWS : 1][2];
 };
@@ -378,16 +379,12 @@ __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row
       top = max(top, static_cast<uint32_t>(__shfl_xor(top, 32)));
       const MxScale s = mx_scale(top);
       put(t, s, nt_u32x2{mx_pack8(v[t], s), mx_pack8(v[t] + 8, s)});
-      if (p.sums) {  // in pairs of pairs: five additions deep
-        float sum[16];
+      if (p.sums) {
+        double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum[i] = v[t][i];
-#pragma unroll
-        for (int n = 8; n > 0; n /= 2)
-#pragma unroll
-          for (int i = 0; i < n; ++i) sum[i] += sum[i + n];
-        const float other = __shfl_xor(sum[0], 32);
-        if (h == 0) lds.part[wave][2 * pair + t] = sum[0] + other;
+        for (int i = 0; i < 16; ++i) sum += static_cast<double>(v[t][i]);
+        sum += __shfl_xor(sum, 32);
+        if (h == 0) lds.part[wave][2 * pair + t] = sum;
       }
     }
     if constexpr (BOTH) {
@@ -437,11 +434,11 @@ __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row
     if ((tile_row & 1) == 0 && r0 + MXC_ROWS >= a.rows)
       *reinterpret_cast<nt_u32x2*>(s + 8) = nt_u32x2{0, 0};
     if (p.sums) {
-      float t[8];
+      double sum = 0.0;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) t[w] = lds.part[w][tid];
-      p.sums[tile_row * a.cols + c0 + tid] =
-          ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+      for (int w = 0; w < 8; ++w) sum += lds.part[w][tid];
+      if (p.part) p.part[tile_row * a.cols + c0 + tid] = sum;
+      else p.sums[c0 + tid] = static_cast<float>(sum);
     }
   }
   if constexpr (BOTH) {
@@ -497,19 +494,21 @@ __global__ __launch_bounds__(512) void mx4_gradient_kernel(Mx4Columns z, Mx4Colu
 }
 
 // 32 columns a workgroup, every eighth part a thread.
-__global__ __launch_bounds__(256) void mx4_sum_kernel(const float* part, int64_t parts, int cols,
+__global__ __launch_bounds__(256) void mx4_sum_kernel(const double* part, int64_t parts, int cols,
                                                       float* sums) {
-  __shared__ float some[8][32];
+  __shared__ double some[8][32];
   const int l = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
-  float s = 0.0f;
+  double s = 0.0;
   if (c < cols)
 #pragma unroll 4
     for (int64_t i = k; i < parts; i += 8) s += part[i * cols + c];
   some[k][l] = s;
   __syncthreads();
   if (k == 0 && c < cols) {
-    sums[c] = ((some[0][l] + some[1][l]) + (some[2][l] + some[3][l])) +
-              ((some[4][l] + some[5][l]) + (some[6][l] + some[7][l]));
+    double all = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all += some[i][l];
+    sums[c] = static_cast<float>(all);
   }
 }
 
@@ -683,7 +682,7 @@ static_assert(mx4_threads(256) == MxL::NT && mx4_threads(128) == MxM::NT &&
 // p and bytes are the same for the wave; where the compiler computes them on the vector unit
 // (64-bit comparisons are its), it would loop over the lanes' buffers around every load.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_buffer(const uint8_t* p, int64_t bytes) {
-  const int n = static_cast<int>(bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF);
+  const int n = static_cast<int>(bytes < 0xFFFFFFFFll ? bytes : 0xFFFFFFFFll);
   const uint64_t at = reinterpret_cast<uint64_t>(p);
   const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at));
   const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
@@ -996,27 +995,21 @@ __global__ __launch_bounds__(256) void mx4_small_kernel(Mx4Pair both) {
   ra.init(a.wq, a.w_ld, (a.outs - 1) * a.w_ld + qb, r0, a.outs, lane);
   rb.init(a.xq + c0 * a.x_ld, a.x_ld, (here - 1) * a.x_ld + qb, 0, here, lane);
   // a block's scales: 8 bytes a row, four of them a lane
-  auto scale_rsrc = [](const uint8_t* p, int64_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(p), 0, static_cast<int>(bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF),
-        0x00020000u);
-  };
   const int na = a.outs - r0 < 32 ? a.outs - r0 : 32;
-  const __amdgpu_buffer_rsrc_t rsa = scale_rsrc(a.ws + r0 * a.ws_ld, (na - 1) * a.ws_ld + sb);
-  const __amdgpu_buffer_rsrc_t rsb = scale_rsrc(a.xs + c0 * a.xs_ld, (here - 1) * a.xs_ld + sb);
+  const __amdgpu_buffer_rsrc_t rsa = mx_buffer(a.ws + r0 * a.ws_ld, (na - 1) * a.ws_ld + sb);
+  const __amdgpu_buffer_rsrc_t rsb = mx_buffer(a.xs + c0 * a.xs_ld, (here - 1) * a.xs_ld + sb);
   const int row = lane & 31;
   const int va = static_cast<int>((row < na ? row : na - 1) * a.ws_ld) + 4 * h;
   const int vb = static_cast<int>((row < here ? row : here - 1) * a.xs_ld) + 4 * h;
   char* ring = lds + wave * RING * STAGE;
-  typedef __attribute__((address_space(3))) void* lds_ptr;
   auto issue = [&](int i) {  // the wave's block i
     const int k = wave + 4 * i;
     char* t = ring + (i % RING) * STAGE;
     const int block = k < blocks ? k : blocks - 1;
     ra.issue(t, block * NT_BLOCK, lane);
     rb.issue(t + DATA / 2, block * NT_BLOCK, lane);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (lds_ptr)(t + DATA), 4, va, block * 8, 0, 0);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsb, (lds_ptr)(t + DATA + 256), 4, vb, block * 8, 0,
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (mx_lds)(t + DATA), 4, va, block * 8, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsb, (mx_lds)(t + DATA + 256), 4, vb, block * 8, 0,
                                              0);
   };
   nt_f32x16 acc;
@@ -1303,7 +1296,7 @@ int64_t mx4_column_tiles(int64_t rows, int cols) {
 hipError_t launch_mx4_columns(const Mx4Source& a, const Mx4Rows& to, hipStream_t s) {
   const bool vec = pairs_aligned(a);
   const dim3 grid(static_cast<unsigned>(mx4_column_tiles(a.rows, a.cols))), wg(512);
-  const Mx4Columns p{a, to, Mx4Rows{}, nullptr};
+  const Mx4Columns p{a, to, Mx4Rows{}, nullptr, nullptr};
   if (a.bf16) {
     if (vec) hipLaunchKernelGGL((mx4_columns_kernel<true, true>), grid, wg, 0, s, p);
     else hipLaunchKernelGGL((mx4_columns_kernel<true, false>), grid, wg, 0, s, p);
@@ -1323,8 +1316,8 @@ hipError_t launch_mx4_gradient(const Mx4Gradient& g, hipStream_t s) {
   const bool both = g.z_rows.q != nullptr;
   const bool vec = pairs_aligned(g.z) && pairs_aligned(g.x);
   const int64_t parts = mx4_sum_parts(g.z.rows);
-  const Mx4Columns z{g.z, g.z_columns, g.z_rows, g.sums && parts ? g.part : g.sums};
-  const Mx4Columns x{g.x, g.x_columns, Mx4Rows{}, nullptr};
+  const Mx4Columns z{g.z, g.z_columns, g.z_rows, g.sums, parts ? g.part : nullptr};
+  const Mx4Columns x{g.x, g.x_columns, Mx4Rows{}, nullptr, nullptr};
   const int64_t nz = mx_row_tiles(g.z.rows) * mx_column_tiles(g.z.cols, both);
   const unsigned grid = static_cast<unsigned>(nz + mx4_column_tiles(g.x.rows, g.x.cols));
   const int z_tiles = static_cast<int>(nz);

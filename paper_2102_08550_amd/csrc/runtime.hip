@@ -2234,7 +2234,7 @@ struct Mx4Grads {
     xtq = zts + round_up(outs * mx4_scales(rows), 256);
     xts = xtq + round_up(in * mx4_bytes(rows), 256);
     part = xts + round_up(in * mx4_scales(rows), 256);
-    end = part + round_up(mx4_sum_parts(rows) * outs * 4, 256);
+    end = part + round_up(mx4_sum_parts(rows) * outs * 8, 256);
   }
 };
 // A model in 4 bits: byte offsets of layer l's entries, scales and biases.
@@ -2461,7 +2461,7 @@ oscars_status oscars_linear_micro_backward(const oscars_micro_gradients* g, void
   const Mx4Rows zc{ws + lay.ztq, mx4_bytes(rows), ws + lay.zts, mx4_scales(rows)};
   const Mx4Rows xc{ws + lay.xtq, mx4_bytes(rows), ws + lay.xts, mx4_scales(rows)};
   e = launch_mx4_gradient(Mx4Gradient{z, x, dx ? zr : Mx4Rows{}, zc, xc, g->db,
-                                      reinterpret_cast<float*>(ws + lay.part)},
+                                      reinterpret_cast<double*>(ws + lay.part)},
                           s);
   const Mx4Product p[2] = {
       {zc.q, zc.q_ld, zc.scale, zc.s_ld, xc.q, xc.q_ld, xc.scale, xc.s_ld, nullptr, false, outs,

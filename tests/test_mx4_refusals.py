@@ -154,6 +154,10 @@ def test_python_checks_come_first():
                  lambda: P.linear_mx4_backward(x, x), lambda: P.dropout(x, 0.5, 1)):
         with pytest.raises(TypeError):  # not on a GPU
             call()
+    for call in (lambda: P.linear_mx4(x, None, None), lambda: P.dequantize_mx4(None, None, 5),
+                 lambda: P.matmul_mx4(u, u, u[0], u, 5), lambda: P.quantize_mx4(x.double())):
+        with pytest.raises(TypeError):
+            call()
     for bad in ((1.5, 1), (-0.1, 1), (float("nan"), 1), (0.5, -1), (0.5, 1 << 64), (0.5, 1, -1),
                 (0.5, 1, 1 << 64)):
         with pytest.raises(ValueError):
