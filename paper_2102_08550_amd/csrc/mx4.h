@@ -47,7 +47,8 @@ int64_t mx4_column_tiles(int64_t rows, int cols);
 hipError_t launch_mx4_columns(const Mx4Source& a, const Mx4Rows& to, hipStream_t s);
 
 // What the gradients multiply: dz by columns and, with z_rows.q, by rows; x by columns;
-// and dz's columns' sums, or nullptr; part holds mx4_sum_parts(rows) x cols doubles.
+// and dz's columns' sums, or nullptr: where mx4_sum_parts(rows) is not 0, so many parts of
+// them, for a product to add up.
 struct Mx4Gradient {
   Mx4Source z, x;
   Mx4Rows z_rows, z_columns, x_columns;
@@ -70,6 +71,14 @@ struct Mx4Values {
 };
 hipError_t launch_mx4_values(const Mx4Values& a, hipStream_t s);
 
+// out[c] = sum_i part[i][c], which workgroups behind a product's do.
+struct Mx4Sums {
+  const double* part;  // [parts][cols]; parts 0: nothing
+  int64_t parts;
+  int cols;
+  float* out;
+};
+
 // out[r][o] = drop(relu?(sum_k x[r][k] w[o][k] + bias[o]))
 struct Mx4Product {
   const uint8_t* xq;
@@ -88,6 +97,7 @@ struct Mx4Product {
   int64_t out_ld;
   bool out_bf16;
   DropArgs drop;
+  Mx4Sums sums;
 };
 hipError_t launch_mx4_product(const Mx4Product& a, hipStream_t s);
 // One or two products that wait for nothing of each other, in one launch if they are small.

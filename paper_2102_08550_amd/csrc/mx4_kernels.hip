@@ -493,25 +493,6 @@ __global__ __launch_bounds__(512) void mx4_gradient_kernel(Mx4Columns z, Mx4Colu
   }
 }
 
-// 32 columns a workgroup, every eighth part a thread.
-__global__ __launch_bounds__(256) void mx4_sum_kernel(const double* part, int64_t parts, int cols,
-                                                      float* sums) {
-  __shared__ double some[8][32];
-  const int l = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
-  double s = 0.0;
-  if (c < cols)
-#pragma unroll 4
-    for (int64_t i = k; i < parts; i += 8) s += part[i * cols + c];
-  some[k][l] = s;
-  __syncthreads();
-  if (k == 0 && c < cols) {
-    double all = 0.0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) all += some[i][l];
-    sums[c] = static_cast<float>(all);
-  }
-}
-
 // Values: eight a thread.  A row's scale of 2^-127 is no normal number: entries are
 // converted at scale 1 and multiplied, exactly.
 template <bool OUT_BF16, bool VEC>
@@ -720,6 +701,29 @@ __device__ __forceinline__ nt_u32x4 mx_read(const char* tile, int row, int chunk
   return *reinterpret_cast<const nt_u32x4*>(tile + row * NT_BLOCK + 16 * (chunk ^ mx_turn(row)));
 }
 
+// Sums of parts, workgroup `index` of NT threads: NT / 8 columns, every eighth part a thread.
+template <int NT>
+__device__ __forceinline__ void mx_sums(const Mx4Sums& a, int index, char* lds) {
+  constexpr int COLS = NT / 8;
+  double* some = reinterpret_cast<double*>(lds);
+  const int l = threadIdx.x % COLS, k = threadIdx.x / COLS, c = index * COLS + l;
+  double s = 0.0;
+  if (c < a.cols)
+#pragma unroll 4
+    for (int64_t i = k; i < a.parts; i += 8) s += a.part[i * a.cols + c];
+  some[k * COLS + l] = s;
+  __syncthreads();
+  if (k == 0 && c < a.cols) {
+    double all = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all += some[i * COLS + l];
+    a.out[c] = static_cast<float>(all);
+  }
+}
+unsigned sums_grid(const Mx4Sums& a, int threads) {
+  return a.parts > 0 ? static_cast<unsigned>((a.cols + threads / 8 - 1) / (threads / 8)) : 0u;
+}
+
 // A wave's 32 x 32 block of sums into outputs: acc[4 q + t] is channel o + 8 q + 4 h + t
 // (h: the lane's half of the wave) of row `row`.
 __device__ __forceinline__ void mx_epilogue(const Mx4Product& a, uint64_t offset, int64_t row,
@@ -800,6 +804,10 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
   const int am = (wave / S::WN) * 32 * S::MI, bm = (wave % S::WN) * 32 * S::NJ;
   const int tr = (a.outs + S::BM - 1) / S::BM;
   const int tc = static_cast<int>((a.rows + S::BN - 1) / S::BN);
+  if (static_cast<int>(blockIdx.x) >= tr * tc) {
+    mx_sums<S::NT>(a.sums, blockIdx.x - tr * tc, lds);
+    return;
+  }
   int r0;
   int64_t c0;
   {  // the workgroups of one XCD (index mod 8) take neighbouring tiles
@@ -973,7 +981,7 @@ constexpr int MX_SMALL_RING = 2;
 struct Mx4Pair {
   Mx4Product p[2];
   bool vec[2];
-  int first;
+  int first, all;  // workgroups; p[0]'s sums are behind them
 };
 __global__ __launch_bounds__(256) void mx4_small_kernel(Mx4Pair both) {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer resources: no host form
@@ -981,6 +989,10 @@ __global__ __launch_bounds__(256) void mx4_small_kernel(Mx4Pair both) {
   __shared__ __attribute__((aligned(16))) char lds[4 * RING * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // scalar addresses below
+  if (static_cast<int>(blockIdx.x) >= both.all) {
+    mx_sums<256>(both.p[0].sums, blockIdx.x - both.all, lds);
+    return;
+  }
   const bool second = static_cast<int>(blockIdx.x) >= both.first;
   const Mx4Product& a = both.p[second];
   const int index = blockIdx.x - (second ? both.first : 0);
@@ -1088,14 +1100,16 @@ hipError_t small_launch(const Mx4Product* p, int n, hipStream_t s) {
     if (i == 0) both.first = static_cast<int>(product_grid(p[0], 32));
     grid += product_grid(p[i], 32);
   }
-  hipLaunchKernelGGL(mx4_small_kernel, dim3(grid), dim3(256), 0, s, both);
+  both.all = static_cast<int>(grid);
+  hipLaunchKernelGGL(mx4_small_kernel, dim3(grid + sums_grid(p[0].sums, 256)), dim3(256), 0, s,
+                     both);
   return hipGetLastError();
 }
 
 template <bool OUT_BF16, bool VEC>
 hipError_t product_launch(const Mx4Product& a, int tile, hipStream_t s) {
   if (tile == 32) return small_launch(&a, 1, s);
-  const dim3 grid(product_grid(a, tile));
+  const dim3 grid(product_grid(a, tile) + sums_grid(a.sums, mx4_threads(tile)));
   if (tile == 256)
     hipLaunchKernelGGL((mx4_product_kernel<MxL, OUT_BF16, VEC>), grid, dim3(MxL::NT), 0, s, a);
   else if (tile == 128)
@@ -1321,17 +1335,11 @@ hipError_t launch_mx4_gradient(const Mx4Gradient& g, hipStream_t s) {
   const int64_t nz = mx_row_tiles(g.z.rows) * mx_column_tiles(g.z.cols, both);
   const unsigned grid = static_cast<unsigned>(nz + mx4_column_tiles(g.x.rows, g.x.cols));
   const int z_tiles = static_cast<int>(nz);
-  hipError_t e;
   if (g.z.bf16)
-    e = vec ? gradient_launch<true, true>(z, x, both, grid, z_tiles, s)
-            : gradient_launch<true, false>(z, x, both, grid, z_tiles, s);
-  else
-    e = vec ? gradient_launch<false, true>(z, x, both, grid, z_tiles, s)
-            : gradient_launch<false, false>(z, x, both, grid, z_tiles, s);
-  if (e != hipSuccess || !g.sums || !parts) return e;
-  hipLaunchKernelGGL(mx4_sum_kernel, dim3((g.z.cols + 31) / 32), dim3(256), 0, s, g.part, parts,
-                     g.z.cols, g.sums);
-  return hipGetLastError();
+    return vec ? gradient_launch<true, true>(z, x, both, grid, z_tiles, s)
+               : gradient_launch<true, false>(z, x, both, grid, z_tiles, s);
+  return vec ? gradient_launch<false, true>(z, x, both, grid, z_tiles, s)
+             : gradient_launch<false, false>(z, x, both, grid, z_tiles, s);
 }
 
 hipError_t launch_mx4_values(const Mx4Values& a, hipStream_t s) {
@@ -1361,6 +1369,7 @@ hipError_t launch_mx4_product(const Mx4Product& args, hipStream_t s) {
     a.xq += at * a.x_ld;
     a.xs += at * a.xs_ld;
     a.out = static_cast<char*>(a.out) + at * a.out_ld * (a.out_bf16 ? 2 : 4);
+    if (at > 0) a.sums.parts = 0;
     if (a.out_bf16)
       e = vec ? product_launch<true, true>(a, tile, s) : product_launch<true, false>(a, tile, s);
     else
