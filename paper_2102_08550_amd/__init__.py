@@ -79,7 +79,7 @@ class _Gradients(ctypes.Structure):
                 ("x", _vp), ("dy_ld", _i64), ("y_ld", _i64), ("x_ld", _i64), ("y_dtype", _i32),
                 ("x_dtype", _i32), ("wtq", _vp), ("wtscale", _vp), ("wt_ld", _i64),
                 ("wts_ld", _i64), ("dx", _vp), ("dw", _vp), ("db", _vp), ("dx_ld", _i64),
-                ("dw_ld", _i64), ("dropout", _P(_Dropout))]
+                ("dw_ld", _i64), ("dropout", _vp)]
 
 
 class _Shards(ctypes.Structure):
@@ -590,6 +590,7 @@ def _dropout_options(dropout, device):
     if dropout is None:
         return None, None
     p, seed, offset = dropout if len(dropout) == 3 else (*dropout, 0)
+    p, seed = float(p), int(seed)
     if not 0.0 <= p <= 1.0:
         raise ValueError("dropout's p must be from 0 to 1")
     if not 0 <= seed < 1 << 64:
@@ -600,6 +601,7 @@ def _dropout_options(dropout, device):
         if offset.numel() != 1:
             raise ValueError("dropout's offset must be one number")
         return _Dropout(p, seed, 0, offset.data_ptr()), offset
+    offset = int(offset)
     if not 0 <= offset < 1 << 64:
         raise ValueError("dropout's offset must be of 64 bits, not negative")
     return _Dropout(p, seed, offset, None), None
@@ -723,38 +725,44 @@ def linear_mx4_backward(dy, x, wtq=None, wtscale=None, y=None, dropout=None, wan
     xp, xn, xld, cols = _rows(x, x.dtype, dev, "x")
     if xn != n:
         raise ValueError("dy and x must have as many rows")
-    g = _Gradients(rows=n, inputs=cols, outs=outs, dy=dyp, dy_ld=dyld, x=xp, x_ld=xld,
-                   y_dtype=_float_type(dy.dtype, "dy"), x_dtype=_float_type(x.dtype, "x"))
+    ydt, xdt = _float_type(dy.dtype, "dy"), _float_type(x.dtype, "x")
+    yp, yld = None, 0
     if y is not None:
-        g.y, yn, g.y_ld, yc = _rows(y, dy.dtype, dev, "y")
+        yp, yn, yld, yc = _rows(y, dy.dtype, dev, "y")
         if (yn, yc) != (n, outs):
             raise ValueError("y must have dy's shape")
     if out is None:
-        out = (_new((n, cols), x.dtype, dev, stream) if want_dx else None,
-               _new((outs, cols), torch.float32, dev, stream),
-               _new((outs,), torch.float32, dev, stream))
-    dx, dw, db = out
-    if (dx is not None) != bool(want_dx):
-        raise ValueError("out must hold a dx where it is wanted, and None where it is not")
+        dx = _new((n, cols), x.dtype, dev, stream) if want_dx else None
+        dw, db = _new((outs, cols), torch.float32, dev, stream), \
+            _new((outs,), torch.float32, dev, stream)
+        out = dx, dw, db
+        dxld = dwld = cols
+    else:
+        dx, dw, db = out
+        if (dx is not None) != bool(want_dx):
+            raise ValueError("out must hold a dx where it is wanted, and None where it is not")
+        dxld = 0
+        if want_dx:
+            _, dn, dxld, dc = _rows(dx, x.dtype, dev, "dx")
+            if (dn, dc) != (n, cols):
+                raise ValueError("dx must have x's shape")
+        _, wn, dwld, wc = _rows(dw, torch.float32, dev, "dw")
+        if (wn, wc) != (outs, cols):
+            raise ValueError("dw must be [outputs][inputs]")
+    wtp, wtld, wtsp, wtsld = None, 0, None, 0
     if want_dx:
         if wtq is None or wtscale is None:
             raise ValueError("dx needs the weights' columns in 4 bits")
-        g.wtq, g.wt_ld, g.wtscale, g.wts_ld = _micro_rows(wtq, wtscale, cols, outs, dev, "wtq")
-        g.dx, dn, g.dx_ld, dc = _rows(dx, x.dtype, dev, "dx")
-        if (dn, dc) != (n, cols):
-            raise ValueError("dx must have x's shape")
-    g.dw, wn, g.dw_ld, wc = _rows(dw, torch.float32, dev, "dw")
-    if (wn, wc) != (outs, cols):
-        raise ValueError("dw must be [outputs][inputs]")
-    g.db = _vector(db, outs, dev, "db")
+        wtp, wtld, wtsp, wtsld = _micro_rows(wtq, wtscale, cols, outs, dev, "wtq")
     drop, offset = _dropout_options(dropout, dev)
-    if drop is not None:
-        g.dropout = ctypes.pointer(drop)
+    dxp, dwp, dbp = dx.data_ptr() if want_dx else None, dw.data_ptr(), _vector(db, outs, dev, "db")
     if n == 0:  # what empty tensors point at
-        g.dy = g.x = g.dw
-        g.y, g.dx = None, None
+        dyp = xp = dwp
+        yp = dxp = None
+    g = _Gradients(n, cols, outs, dyp, yp, xp, dyld, yld, xld, ydt, xdt, wtp, wtsp, wtld, wtsld,
+                   dxp, dwp, dbp, dxld, dwld, None if drop is None else ctypes.addressof(drop))
     lib = _lib()
-    need = lib.oscars_linear_micro_backward_workspace(n, cols, outs, int(g.dx is not None))
+    need = lib.oscars_linear_micro_backward_workspace(n, cols, outs, int(dxp is not None))
     ws = _workspace(need, dev, stream) if need else None
     with _on_device(dev):
         _check(lib.oscars_linear_micro_backward(

@@ -98,6 +98,7 @@ struct Mx4Product {
   bool out_bf16;
   DropArgs drop;
   Mx4Sums sums;
+  uint32_t row0;  // of dropout's rows, the first one's number
 };
 hipError_t launch_mx4_product(const Mx4Product& a, hipStream_t s);
 // One or two products that wait for nothing of each other, in one launch if they are small.

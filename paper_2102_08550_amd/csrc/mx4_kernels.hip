@@ -555,7 +555,7 @@ __device__ __forceinline__ float mx_finish(const Mx4Product& a, float acc, float
 template <int N>
 __device__ __forceinline__ void mx_drop(const Mx4Product& a, uint64_t offset, int64_t row, int o,
                                         float* v) {
-  const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(row), o / 8);
+  const Words4 w = drop_words(a.drop, offset, a.row0 + static_cast<uint32_t>(row), o / 8);
 #pragma unroll
   for (int t = 0; t < N; ++t) {
     const bool keep = N == 8 || !(o & 4) ? drop_keeps(a.drop, w, t)
@@ -736,7 +736,7 @@ __device__ __forceinline__ void mx_epilogue(const Mx4Product& a, uint64_t offset
     // each half makes one of two calls, and they swap words
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const Words4 w = drop_words(a.drop, offset, static_cast<uint32_t>(row), o / 8 + 2 * p + h);
+      const Words4 w = drop_words(a.drop, offset, a.row0 + static_cast<uint32_t>(row), o / 8 + 2 * p + h);
       const auto x = __builtin_amdgcn_permlane32_swap(w.w[0], w.w[2], false, false);
       const auto y = __builtin_amdgcn_permlane32_swap(w.w[1], w.w[3], false, false);
 #pragma unroll
@@ -1369,6 +1369,7 @@ hipError_t launch_mx4_product(const Mx4Product& args, hipStream_t s) {
     a.xq += at * a.x_ld;
     a.xs += at * a.xs_ld;
     a.out = static_cast<char*>(a.out) + at * a.out_ld * (a.out_bf16 ? 2 : 4);
+    a.row0 = static_cast<uint32_t>(at);
     if (at > 0) a.sums.parts = 0;
     if (a.out_bf16)
       e = vec ? product_launch<true, true>(a, tile, s) : product_launch<true, false>(a, tile, s);

@@ -2274,7 +2274,7 @@ hipError_t run_evaluate_mx4(oscars_ctx* c, const void* model, const void* x, con
                        reinterpret_cast<const uint8_t*>(mod + m.w[l]), mx4_bytes(width),
                        reinterpret_cast<const uint8_t*>(mod + m.s[l]), mx4_scales(width),
                        reinterpret_cast<const float*>(mod + m.b[l]), l < c->L, n, width,
-                       c->dims[l], out, c->ld[l], l < c->L && c->bf16, DropArgs{}, Mx4Sums{}},
+                       c->dims[l], out, c->ld[l], l < c->L && c->bf16, DropArgs{}, Mx4Sums{}, 0},
             c->stream);
       });
 }
@@ -2343,7 +2343,7 @@ oscars_status oscars_matmul_micro(void* out, int64_t out_ld, int32_t out_dtype, 
   if (!is_dtype(out_dtype) || !drop_args(dropout, &drop)) return OSCARS_E_INVALID;
   const Mx4Product a{xq,    x_ld, xscale, xs_ld, wq, w_ld, wscale, ws_ld, bias, relu != 0,
                      rows,  static_cast<int>(in), static_cast<int>(outs), out, out_ld,
-                     out_dtype == OSCARS_BF16, drop, Mx4Sums{}};
+                     out_dtype == OSCARS_BF16, drop, Mx4Sums{}, 0};
   if (!mx4_product_ok(a, in, outs) || !mx4_rows_ok(xq, x_ld, xscale, xs_ld, in))
     return OSCARS_E_INVALID;
   const Range r[] = {{out, rows_span(rows, out_ld, outs, dtype_bytes(out_dtype))},
@@ -2377,7 +2377,7 @@ oscars_status oscars_linear_micro(void* out, int64_t out_ld, int32_t out_dtype, 
     return OSCARS_E_INVALID;
   Mx4Product a{nullptr, 0, nullptr, 0, wq, w_ld, wscale, ws_ld, bias, relu != 0,
                rows, static_cast<int>(in), static_cast<int>(outs), out, out_ld,
-               out_dtype == OSCARS_BF16, drop, Mx4Sums{}};
+               out_dtype == OSCARS_BF16, drop, Mx4Sums{}, 0};
   const int64_t es = dtype_bytes(dtype);
   if (!mx4_product_ok(a, in, outs) || in > OSCARS_MAX_WIDTH || !rows_ok(x, x_ld, in, es))
     return OSCARS_E_INVALID;
@@ -2467,9 +2467,10 @@ oscars_status oscars_linear_micro_backward(const oscars_micro_gradients* g, void
       {zc.q, zc.q_ld, zc.scale, zc.s_ld, xc.q, xc.q_ld, xc.scale, xc.s_ld, nullptr, false, outs,
        static_cast<int>(rows), in, g->dw, g->dw_ld, false, DropArgs{},
        Mx4Sums{reinterpret_cast<const double*>(ws + lay.part), g->db ? mx4_sum_parts(rows) : 0,
-               outs, g->db}},
+               outs, g->db},
+       0},
       {zr.q, zr.q_ld, zr.scale, zr.s_ld, g->wtq, g->wt_ld, g->wtscale, g->wts_ld, nullptr, false,
-       rows, outs, in, g->dx, g->dx_ld, g->x_dtype == OSCARS_BF16, DropArgs{}, Mx4Sums{}}};
+       rows, outs, in, g->dx, g->dx_ld, g->x_dtype == OSCARS_BF16, DropArgs{}, Mx4Sums{}, 0}};
   if (e == hipSuccess) e = launch_mx4_products(p, dx ? 2 : 1, s);
   return e == hipSuccess ? OSCARS_OK : hip_fail(e);
 }

@@ -290,6 +290,23 @@ def test_rows_do_not_depend_on_others(P):
     assert P.quantize_mx4(x[:0], transposed=True)[0].shape == (900, 0)
 
 
+def test_dropout_of_a_product_in_two_launches(P):
+    """Rows past 2^29, which go to a second launch: dropout counts them on."""
+    import torch
+    rows = 2 ** 29 + 70
+    q = torch.zeros(rows, 128, dtype=torch.uint8, device="cuda")
+    s = torch.zeros(rows, 16, dtype=torch.uint8, device="cuda")
+    wq, ws = P.quantize_mx4(torch.ones(2, 1, device="cuda"))
+    ones = torch.ones(2, device="cuda")
+    y = P.matmul_mx4(q, s, wq, ws, 1, bias=ones, dropout=(0.5, 21, 4), out_dtype=torch.bfloat16)
+    del q, s
+    want = P.dropout(torch.ones(rows, 2, dtype=torch.bfloat16, device="cuda"), 0.5, 21, 4)
+    same = torch.equal(y, want)
+    del y, want
+    torch.cuda.empty_cache()
+    assert same
+
+
 # ------------------------------------------------------------------ dropout
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])

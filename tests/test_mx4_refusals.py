@@ -110,7 +110,7 @@ def _gradients(**change):
     drop = change.pop("dropout", None)
     g = P._Gradients(**dict(f, **change))
     if drop is not None:
-        g.dropout = ctypes.pointer(drop)
+        g.dropout = ctypes.addressof(drop)
     return lib.oscars_linear_micro_backward(ctypes.byref(g), ws, n, None)
 
 
