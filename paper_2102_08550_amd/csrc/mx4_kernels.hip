@@ -880,7 +880,7 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 #pragma unroll
   for (int s = 0; s < S::RING; ++s) issue(s);
-  if (S::RING > 2 && S::RING <= blocks) nt_wait_vm<(S::RING - 1) * S::LOADS>();
+  if (S::RING <= blocks) nt_wait_vm<(S::RING - 1) * S::LOADS>();
   else nt_wait_vm<0>();
   nt_barrier();
   load(0, 0, fa[0], fb[0]);
