@@ -473,7 +473,8 @@ oscars_status oscars_evaluate_quantized(oscars_ctx* ctx, const void* model, cons
 /* The linear layer in microscaled 4-bit floating point, for answers and for
  * training.  Rows in 4 bits: 32 consecutive entries share a scale, the least power
  * of two s from 2^-127 on with max |x| < 7 s, or 2^125 (so that no finite entry
- * becomes infinite); an entry is x / s rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, ties to the even code.
+ * becomes infinite); an entry is x / s rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3,
+ * 4, 6 and their negatives, ties to the even code.
  * An entry's code is its magnitude's place in that list, plus 8 where it is
  * negative; two codes a byte, the first entry's in the low half.  A scale is the byte
  * log2(s) + 127.  A block whose largest magnitude is below 2^-126 counts as zeros
@@ -551,7 +552,8 @@ oscars_status oscars_linear_micro(void* out, int64_t out_ld, int32_t out_dtype, 
  *   dx       device [rows][dx_ld], x_dtype, or NULL: not wanted (wtq, wtscale unused);
  *   dw       device [outs][dw_ld] fp32;  db  device [outs] fp32, or NULL;
  *   0 <= rows <= 2^24 (0: dw and db are 0), 1 <= in, outs <= OSCARS_MAX_WIDTH, x and dy
- *            together fewer than 2^37 entries, counted as for oscars_quantize_micro;
+ *            together fewer than 2^37 entries, counted as for oscars_quantize_micro, but
+ *            dy's columns to a whole 512;
  *   workspace  device, 16-byte aligned, oscars_linear_micro_backward_workspace bytes,
  *            the call's own until the stream has run it. */
 typedef struct {

@@ -674,7 +674,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_buffer(const uint8_t* p, in
 typedef __attribute__((address_space(3))) void* mx_lds;
 
 // Rows and scales of a tile's operands as buffers that end behind the last row: what
-// lies behind it reads as zeros.
+// lies behind it reads as zeros.  A row's place is in the vector offset, which is checked
+// against the buffer's end; the scalar offset, the place in the row, need not be.
 struct MxTile {
   __amdgpu_buffer_rsrc_t a, b, scales;
 };
@@ -841,12 +842,12 @@ __global__ __launch_bounds__(S::NT, S::EU) void mx4_product_kernel(Mx4Product a)
     const int k = s * NT_BLOCK;
 #pragma unroll
     for (int p = 0; p < MxPlace<S>::PA; ++p)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(t.a, (mx_lds)(to + S::NT * 16 * p), 16, at.a,
-                                               k + p * at.a_step, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(t.a, (mx_lds)(to + S::NT * 16 * p), 16,
+                                               at.a + p * at.a_step, k, 0, 0);
 #pragma unroll
     for (int p = 0; p < MxPlace<S>::PB; ++p)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(t.b, (mx_lds)(to + ABYTES + S::NT * 16 * p), 16,
-                                               at.b, k + p * at.b_step, 0, 0);
+                                               at.b + p * at.b_step, k, 0, 0);
     if ((s & 1) == 0 && 64 * wave < S::BM + S::BN)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           t.scales, (mx_lds)(scales + (s >> 1) % S::PARTS * S::SCALES + wave * 1024), 16,
