@@ -246,7 +246,8 @@ __device__ __forceinline__ float mx_from_row(float v) {
   return __builtin_bit_cast(float, mx_dpp<0x150 + K>(__builtin_bit_cast(uint32_t, v)));
 }
 
-template <bool BF16, bool VEC, int MODE, bool BOTH>
+// SUMS: the columns' sums too, if p.sums is there.
+template <bool BF16, bool VEC, int MODE, bool BOTH, bool SUMS>
 __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row, int tile_col,
                                            MxColumnsLds<BOTH>& lds) {
   const Mx4Source& a = p.from;
@@ -287,6 +288,17 @@ __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row
     *reinterpret_cast<nt_u32x2*>(lds.q + col * Lds::LD + 16 * wave + 8 * h) = w;
     if (h == 0) lds.scale[col][wave] = static_cast<uint8_t>(s.byte);
   };
+  auto add = [&](int t, auto&& value) {  // value(i), i < 16: of column t of the pair
+    if constexpr (SUMS) {
+      if (p.sums) {
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += static_cast<double>(value(i));
+        sum += __shfl_xor(sum, 32);
+        if (h == 0) lds.part[wave][2 * pair + t] = sum;
+      }
+    }
+  };
   if constexpr (BF16 && VEC && MODE == 0 && !BOTH) {
     // as it is: both columns' magnitudes at once, pairs of rows put together for the conversion
     uint32_t w[16], two = 0;
@@ -308,6 +320,7 @@ __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row
         rows2[i] =
             __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], t ? 0x07060302u : 0x05040100u);
       put(t, s, nt_u32x2{mx_pack8(rows2, s), mx_pack8(rows2 + 4, s)});
+      add(t, [&](int i) { return mx_bf16(t ? w[i] >> 16 : w[i] & 0xFFFFu); });
     }
   } else {
     auto load = [&](const void* from, int64_t ld, float(&v)[2][16]) {
@@ -379,13 +392,7 @@ __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row
       top = max(top, static_cast<uint32_t>(__shfl_xor(top, 32)));
       const MxScale s = mx_scale(top);
       put(t, s, nt_u32x2{mx_pack8(v[t], s), mx_pack8(v[t] + 8, s)});
-      if (p.sums) {
-        double sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum += static_cast<double>(v[t][i]);
-        sum += __shfl_xor(sum, 32);
-        if (h == 0) lds.part[wave][2 * pair + t] = sum;
-      }
+      add(t, [&](int i) { return v[t][i]; });
     }
     if constexpr (BOTH) {
       // 16 lanes have a block of each of 16 rows: lane l comes to hold row l's largest
@@ -433,12 +440,14 @@ __device__ __forceinline__ void mx_columns(const Mx4Columns& p, int64_t tile_row
     // the last tile fills the scales to a whole 16
     if ((tile_row & 1) == 0 && r0 + MXC_ROWS >= a.rows)
       *reinterpret_cast<nt_u32x2*>(s + 8) = nt_u32x2{0, 0};
-    if (p.sums) {
-      double sum = 0.0;
+    if constexpr (SUMS) {
+      if (p.sums) {
+        double sum = 0.0;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) sum += lds.part[w][tid];
-      if (p.part) p.part[tile_row * a.cols + c0 + tid] = sum;
-      else p.sums[c0 + tid] = static_cast<float>(sum);
+        for (int w = 0; w < 8; ++w) sum += lds.part[w][tid];
+        if (p.part) p.part[tile_row * a.cols + c0 + tid] = sum;
+        else p.sums[c0 + tid] = static_cast<float>(sum);
+      }
     }
   }
   if constexpr (BOTH) {
@@ -467,8 +476,8 @@ template <bool BF16, bool VEC>
 __global__ __launch_bounds__(512) void mx4_columns_kernel(Mx4Columns p) {
   __shared__ __attribute__((aligned(16))) MxColumnsLds<false> lds;
   const int across = mx_column_tiles(p.from.cols, false);
-  mx_columns<BF16, VEC, 0, false>(p, blockIdx.x / across, static_cast<int>(blockIdx.x % across),
-                                  lds);
+  mx_columns<BF16, VEC, 0, false, false>(p, blockIdx.x / across,
+                                         static_cast<int>(blockIdx.x % across), lds);
 }
 
 // What the gradients quantise in one launch: dz by columns, and for dx by rows, and x by
@@ -483,13 +492,13 @@ __global__ __launch_bounds__(512) void mx4_gradient_kernel(Mx4Columns z, Mx4Colu
   int id = n * per + (n < rem ? n : rem) + q;
   if (id < z_tiles) {
     const int across = mx_column_tiles(z.from.cols, BOTH);
-    mx_columns<BF16, VEC, MODE, BOTH>(z, id / across, id % across, lds);
+    mx_columns<BF16, VEC, MODE, BOTH, true>(z, id / across, id % across, lds);
   } else {
     id -= z_tiles;
     const int across = mx_column_tiles(x.from.cols, false);
     auto& own = reinterpret_cast<MxColumnsLds<false>&>(lds);
-    if (x.from.bf16) mx_columns<true, VEC, 0, false>(x, id / across, id % across, own);
-    else mx_columns<false, VEC, 0, false>(x, id / across, id % across, own);
+    if (x.from.bf16) mx_columns<true, VEC, 0, false, false>(x, id / across, id % across, own);
+    else mx_columns<false, VEC, 0, false, false>(x, id / across, id % across, own);
   }
 }
 

@@ -400,6 +400,42 @@ def test_gradients(P, rows, inputs, outs, x_dtype, y_dtype, p, relu):
     assert torch.equal(dw, got[1]) and torch.equal(db, got[2])
 
 
+@pytest.mark.parametrize("relu", [True, False])
+@pytest.mark.parametrize("p", [0.0, 0.25])
+@pytest.mark.parametrize("x_dtype,y_dtype", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32"),
+                                             ("fp32", "bf16")])
+@pytest.mark.parametrize("rows,inputs,outs", [(1, 2, 2), (64, 512, 256), (256, 30, 66),
+                                              (257, 32, 130), (600, 260, 300)])
+def test_gradients_without_dx(P, rows, inputs, outs, x_dtype, y_dtype, p, relu):
+    """Of aligned tensors, up to 256 rows and more: dw and db are what they should be and
+    what they are beside dx, whatever ran on the card before."""
+    import torch
+    rng = np.random.default_rng(rows + inputs + outs)
+    x = _rows(rng, rows, inputs, x_dtype, relu=True)
+    w = (rng.standard_normal((outs, inputs)) / np.sqrt(inputs)).astype(np.float32)
+    dy = _rows(rng, rows, outs, y_dtype) * np.float32(2.0 ** -10)
+    drop = (p, 77, 3) if p else None
+    y = _rows(rng, rows, outs, y_dtype, relu=True) if relu else None
+    if relu and p:
+        y = np.where(oracle_dropout.kept(rows, outs, *drop), y, 0)
+    dyd, xd = _dev(dy, y_dtype), _dev(x, x_dtype)
+    yd = None if y is None else _dev(y, y_dtype)
+    # gradients of other numbers first, on every CU
+    P.linear_mx4_backward(torch.full((512, 32768), 3.0e5, device="cuda"),
+                          torch.ones(512, 32, device="cuda"), want_dx=False)
+    got = P.linear_mx4_backward(dyd, xd, y=yd, dropout=drop, want_dx=False)
+    assert got[0] is None
+    _assert_gradients(P, got, dy, x, w, y, drop, x_dtype)
+    both = P.linear_mx4_backward(dyd, xd, *P.quantize_mx4(_dev(w), transposed=True), y=yd,
+                                 dropout=drop)
+    _assert_gradients(P, both, dy, x, w, y, drop, x_dtype)
+    assert torch.equal(got[2], both[2])  # sums in one order; dw's tiles may be others
+    # without db too
+    lone = torch.empty_like(got[1])
+    P.linear_mx4_backward(dyd, xd, y=yd, dropout=drop, want_dx=False, out=(None, lone, None))
+    assert torch.equal(lone, got[1])
+
+
 def test_gradients_of_no_rows(P):
     import torch
     wt, wts = P.quantize_mx4(torch.ones(5, 9, device="cuda"), transposed=True)
