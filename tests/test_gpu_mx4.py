@@ -307,6 +307,38 @@ def test_dropout_of_a_product_in_two_launches(P):
     assert same
 
 
+# rows, inputs, outputs that one launch does not hold (test_mx4_plan.py asks the plan)
+TWO_LAUNCHES = (2 ** 30 + 70, 1, 2)
+
+
+def test_product_of_more_rows_than_a_launch_holds(P):
+    """The second launch's rows: dropout counts them on from the first's, operands and
+    outputs are theirs.  160 GB."""
+    import torch
+    rows, inputs, outs = TWO_LAUNCHES
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 190 * 10 ** 9:
+        pytest.skip("needs 190 GB of free device memory")
+    x = torch.arange(300, device="cuda") % 7  # codes of the last rows' entries
+    value = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4], device="cuda")[x].bfloat16()
+    q = torch.zeros(rows, 128, dtype=torch.uint8, device="cuda")
+    s = torch.zeros(rows, 16, dtype=torch.uint8, device="cuda")
+    q[-300:, 0] = x.to(torch.uint8)
+    s[-300:, 0] = 127
+    wq, ws = P.quantize_mx4(torch.ones(outs, inputs, device="cuda"))
+    ones = torch.ones(outs, device="cuda")
+    y = P.matmul_mx4(q, s, wq, ws, inputs, bias=ones, dropout=(0.5, 21, 4),
+                     out_dtype=torch.bfloat16)
+    del q, s
+    want = torch.ones(rows, outs, dtype=torch.bfloat16, device="cuda")
+    want[-300:] += value[:, None]
+    P.dropout(want, 0.5, 21, 4, out=want)  # times 2: exact
+    same = torch.equal(y, want)
+    del y, want
+    torch.cuda.empty_cache()
+    assert same
+
+
 # ------------------------------------------------------------------ dropout
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])

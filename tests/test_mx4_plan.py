@@ -75,3 +75,12 @@ def test_the_gpu_tests_reach_every_tile(plan):
     import test_gpu_mx4
     tiles = {plan(rows, inputs, outs)[0] for outs, inputs, rows in test_gpu_mx4.PRODUCTS}
     assert tiles == {32, 64, 128, 256}
+
+
+def test_the_gpu_test_of_two_launches_makes_two(plan):
+    sys.path.insert(0, os.path.join(ROOT, "tests"))
+    import test_gpu_mx4
+    rows, inputs, outs = test_gpu_mx4.TWO_LAUNCHES
+    launches = plan(rows, inputs, outs)[3]
+    assert len(launches) == 2 and launches[1][1] > 0
+    assert rows - launches[1][1] < 300  # the rows that it gives values reach into the first
