@@ -594,6 +594,37 @@ def test_training_step_together_and_captured(P):
     assert int(offset) == 4
 
 
+def test_captured_training_stays_finite(P):
+    """Captured and replayed with a step that lets the weights settle: every replay is what
+    the eager step gives, of finite numbers, and moves the weights."""
+    import torch
+    rng = np.random.default_rng(9)
+    x = _dev(_rows(rng, 96, 200, "fp32"))
+    target = _dev(rng.standard_normal((96, 40)))
+    w0 = [_dev(rng.standard_normal((144, 200)) / 14), _dev(rng.standard_normal((40, 144)) / 12)]
+    b0 = [_dev(rng.standard_normal(144)), _dev(rng.standard_normal(40))]
+    eager_w, eager_b = [w.clone() for w in w0], [b.clone() for b in b0]
+    ws, bs = [w.clone() for w in w0], [b.clone() for b in b0]
+    offset = torch.zeros(1, dtype=torch.int64, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = _step(P, x, target, ws, bs, 5, offset, 2.0 ** -7)
+        offset.add_(1)
+    offset.zero_()
+    before = w0
+    for step in range(4):
+        graph.replay()
+        want = _step(P, x, target, eager_w, eager_b, 5, step, 2.0 ** -7)
+        torch.cuda.synchronize()
+        assert all(torch.isfinite(t).all() for t in (*out, *ws, *bs)), step
+        assert all(_same(a, c) for a, c in zip(out, want)), step
+        assert all(_same(a, c) for a, c in zip(ws + bs, eager_w + eager_b)), step
+        assert not any(torch.equal(a, b) for a, b in zip(ws, before)), step
+        before = [w.clone() for w in ws]
+    assert int(offset) == 4
+
+
 def test_two_graphs_and_another_stream(P):
     """Two captured calls with workspaces of their own, replayed in turns, and calls on a
     stream that is named, whose inputs the caller drops at once."""
