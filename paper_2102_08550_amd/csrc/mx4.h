@@ -110,7 +110,7 @@ bool mx4_one_launch(int64_t rows, int in);
 hipError_t launch_mx4_few(const Mx4Product& a, const void* x, int64_t x_ld, bool x_bf16,
                           hipStream_t s);
 
-// p[0 .. n) = 0
+// `rows` rows of `cols` floats, ld apart: zeros.
 hipError_t launch_mx4_zero(float* p, int64_t ld, int64_t rows, int cols, hipStream_t s);
 
 }  // namespace oscars

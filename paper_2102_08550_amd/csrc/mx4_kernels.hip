@@ -560,47 +560,40 @@ __device__ __forceinline__ float mx_finish(const Mx4Product& a, float acc, float
   const float y = acc + b;
   return a.relu ? __builtin_elementwise_maximum(y, 0.0f) : y;  // keeps a NaN
 }
-// N (4 or 8) outputs of a row from o (a multiple of N) on.
-template <int N>
-__device__ __forceinline__ void mx_drop(const Mx4Product& a, uint64_t offset, int64_t row, int o,
-                                        float* v) {
+// Four outputs of a row from o (a multiple of 4) on.
+__device__ __forceinline__ void mx_drop4(const Mx4Product& a, uint64_t offset, int64_t row, int o,
+                                         float* v) {
   const Words4 w = drop_words(a.drop, offset, a.row0 + static_cast<uint32_t>(row), o / 8);
 #pragma unroll
-  for (int t = 0; t < N; ++t) {
-    const bool keep = N == 8 || !(o & 4) ? drop_keeps(a.drop, w, t)
-                                         : drop_keeps(a.drop, w, (t + 4) & 7);
+  for (int t = 0; t < 4; ++t) {
+    const bool keep = o & 4 ? drop_keeps(a.drop, w, t + 4) : drop_keeps(a.drop, w, t);
     v[t] = keep ? v[t] * a.drop.factor : 0.0f;
   }
 }
 
-// N channels from o on of an output row.
-template <int N, bool OUT_BF16, bool VEC>
-__device__ __forceinline__ void mx_store(const Mx4Product& a, int64_t row, int o, const float* v) {
+// Four channels from o on of an output row.
+template <bool OUT_BF16, bool VEC>
+__device__ __forceinline__ void mx_store4(const Mx4Product& a, int64_t row, int o, const float* v) {
   if constexpr (OUT_BF16) {
     uint16_t* p = static_cast<uint16_t*>(a.out) + row * a.out_ld + o;
-    if (VEC && o + N <= a.outs) {
-      uint32_t w[N / 2];
+    if (VEC && o + 4 <= a.outs) {
+      uint32_t w[2];
 #pragma unroll
-      for (int e = 0; e < N / 2; ++e)
+      for (int e = 0; e < 2; ++e)
         w[e] = mx_to_bf16(v[2 * e]) | static_cast<uint32_t>(mx_to_bf16(v[2 * e + 1])) << 16;
-      if constexpr (N == 8)
-        *reinterpret_cast<nt_u32x4*>(p) = nt_u32x4{w[0], w[1], w[2], w[3]};
-      else
-        *reinterpret_cast<nt_u32x2*>(p) = nt_u32x2{w[0], w[1]};
+      *reinterpret_cast<nt_u32x2*>(p) = nt_u32x2{w[0], w[1]};
     } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e)
+      for (int e = 0; e < 4; ++e)
         if (o + e < a.outs) p[e] = mx_to_bf16(v[e]);
     }
   } else {
     float* p = static_cast<float*>(a.out) + row * a.out_ld + o;
-    if (VEC && o + N <= a.outs) {
-#pragma unroll
-      for (int e = 0; e < N; e += 4)
-        *reinterpret_cast<nt_f32x4*>(p + e) = nt_f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    if (VEC && o + 4 <= a.outs) {
+      *reinterpret_cast<nt_f32x4*>(p) = nt_f32x4{v[0], v[1], v[2], v[3]};
     } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e)
+      for (int e = 0; e < 4; ++e)
         if (o + e < a.outs) p[e] = v[e];
     }
   }
@@ -1079,14 +1072,14 @@ __global__ __launch_bounds__(256) void mx4_small_kernel(Mx4Pair both) {
     const int oc = o + t < a.outs ? o + t : a.outs - 1;
     v[t] = mx_finish(a, s, a.bias ? a.bias[oc] : 0.0f);
   }
-  if (a.drop.below) mx_drop<4>(a, drop_offset(a.drop), r, o, v);
+  if (a.drop.below) mx_drop4(a, drop_offset(a.drop), r, o, v);
   const bool vec = both.vec[second];
   if (a.out_bf16) {
-    if (vec) mx_store<4, true, true>(a, r, o, v);
-    else mx_store<4, true, false>(a, r, o, v);
+    if (vec) mx_store4<true, true>(a, r, o, v);
+    else mx_store4<true, false>(a, r, o, v);
   } else {
-    if (vec) mx_store<4, false, true>(a, r, o, v);
-    else mx_store<4, false, false>(a, r, o, v);
+    if (vec) mx_store4<false, true>(a, r, o, v);
+    else mx_store4<false, false>(a, r, o, v);
   }
 #endif
 }

@@ -13,8 +13,8 @@ namespace oscars {
 //   32    3, and 2250 blocks a us over all CUs, ten more counted for each tile
 //   64    2.9 and a block 0.31 while no CU has two tiles, 0.55 up to two; else 1.5 and a
 //         block 0.58 for 512 at a time
-//   128   3.2 and a block 0.69 up to 128 tiles, 0.86 up to 256; else 4.2 and a block 1.2
-//         for 512 at a time
+//   128   3.2 and a block 0.69 up to 128 tiles, 0.86 up to 256; else 1.0, and 4.2 and a block
+//         1.2 for 512 at a time
 //   256   10 and a block 1.1 up to 64 tiles, 1.34 up to 128, 1.87 up to 256; else 8 and a
 //         block 1.9 for 256 at a time
 // Rows x inputs x outputs, measured with 32 / 64 / 128 / 256: 256 x 4096 x 1000: 5.8 / 7.4 /
