@@ -666,7 +666,7 @@ def matmul_mx4(xq, xscale, wq, wscale, in_features: int, bias=None, relu: bool =
     """drop(relu(x w' + bias)) (oscars_matmul_micro) of quantised rows ``xq`` [rows][..]
     and weights ``wq`` [outputs][..] as quantize_mx4 gives them, of ``in_features``
     entries each; ``dropout``: ``(p, seed)`` or ``(p, seed, offset)`` as in ``dropout``;
-    fp32 by default.  Returns ``out``."""
+    fp32 by default.  Returns ``out``, which autograd does not follow."""
     n, outs, cols, dev = _count(xq, "xq"), _count(wq, "wq"), int(in_features), xq.device
     xp, xld, xsp, xsld = _micro_rows(xq, xscale, n, cols, dev, "xq")
     wp, wld, wsp, wsld = _micro_rows(wq, wscale, outs, cols, dev, "wq")
@@ -689,7 +689,8 @@ def linear_mx4(x, wq, wscale, bias=None, relu: bool = False, dropout=None, out_d
     ``x`` (fp32 or bf16) are quantised on the way, ``wq`` and ``wscale`` are a weight
     matrix's quantize_mx4.  ``dropout`` (training): ``(p, seed)`` or ``(p, seed,
     offset)`` as in ``dropout``.  The result has ``x``'s type by default.  Returns
-    ``out``; linear_mx4_backward has the gradients."""
+    ``out``.  Autograd does not follow the call, whatever requires a gradient: a
+    program's training step calls linear_mx4_backward."""
     dev = x.device
     xp, n, xld, cols = _rows(x, x.dtype, dev, "x")
     dt = _float_type(x.dtype, "x")
@@ -778,7 +779,8 @@ def dropout(x, p: float, seed: int, offset=0, out=None, stream=None):
     multiplied by 1 / (1 - p) otherwise.  The mask is a function of ``seed``,
     ``offset`` (the call's number in a training run; an int64 tensor of one element
     on the device is read when the call runs) and the place, so the gradient is
-    ``dropout(dy, p, seed, offset)``.  ``out``: ``x`` itself is allowed."""
+    ``dropout(dy, p, seed, offset)``, which the program calls itself: autograd does not
+    follow.  ``out``: ``x`` itself is allowed."""
     dev = x.device
     xp, n, ld, cols = _rows(x, x.dtype, dev, "x")
     dt = _float_type(x.dtype, "x")
