@@ -168,6 +168,29 @@ def test_quantize_rows_beyond_32_bits(P):
     assert torch.equal(d, x[-3:])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_columns_of_rows_far_apart(P, dtype):
+    """Rows 2^24 entries apart and more: by columns, and in gradients by rows too."""
+    import torch
+    rng = np.random.default_rng(3)
+    n, c = 70, 66
+    x = _rows(rng, n, c, dtype)
+    base = torch.full((n, (1 << 24) + 8), float("nan"), dtype=_type(dtype), device="cuda")
+    base[:, :c] = _dev(x, dtype)
+    far = base[:, :c]
+    near = far.contiguous()
+    q, s = P.quantize_mx4(far, transposed=True)
+    wq, ws = mx4.packed(*mx4.quantize_rows(x.T))
+    assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), ws)
+    wt = P.quantize_mx4(_dev(rng.standard_normal((c, c))), transposed=True)
+    for y in (None, near):
+        got = P.linear_mx4_backward(far, far, *wt, y=None if y is None else far)
+        want = P.linear_mx4_backward(near, near, *wt, y=y)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    del base, far
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------ products
 
 # outputs x inputs x rows over tiles of every size, their edges, one entry
