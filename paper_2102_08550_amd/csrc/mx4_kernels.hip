@@ -149,10 +149,11 @@ __device__ __forceinline__ float mx_pass(float dy, float y, float factor) {
 }
 
 // A wave takes 512 columns of a row, a lane eight of them, four lanes a block; neighbouring
-// waves have neighbouring pieces.  4096 x 4096 in fp32 12.5 us, 6.1 TB/s; 8191 x 4096 in
-// bf16 16.3.  Four pieces a wave with all loads on their way: 13.9 and 17.2; 16 rows of
-// the same columns a workgroup, which in rows a power of two apart meet in the same
-// channels: 17 and 17.4.
+// waves have neighbouring pieces.  4096 x 4096 in fp32 12.9 us, 8191 x 4096 in bf16 14.3:
+// 5.9 TB/s; 10000 x 784 in bf16, two pieces a row, 6.5 to 7.9.  Tried against an earlier
+// form (12.5 and 16.3 us): four pieces a wave with all loads on their way 13.9 and 17.2; 16
+// rows of the same columns a workgroup, which in rows a power of two apart meet in the
+// same channels, 17 and 17.4.
 template <bool BF16, bool VEC>
 __global__ __launch_bounds__(256) void mx4_rows_kernel(Mx4Source a, Mx4Rows to, int pieces) {
   const int lane = threadIdx.x & 63;
@@ -198,8 +199,8 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(Mx4Source a, Mx4Rows to, 
 // bytes are turned by LDS so that eight neighbouring lanes store a column's 128.
 // BOTH: by rows as well, a block of 32 columns 16 lanes', for which the gradient is
 // read once.  4096 x 4096 in fp32 12.7 us, 6.0 TB/s; dz of 8191 x 2048 both ways, from dy and
-// y in bf16, with x of 8191 x 4096 42 us, 4.0 TB/s (98 with loads behind branches and
-// every lane reducing every row).
+// y in bf16, with x of 8191 x 4096 41 us, 4.3 TB/s (98 in an early form with loads behind
+// branches and every lane reducing every row).
 constexpr int MXC_ROWS = 256, MXC_COLS = 64;
 
 struct Mx4Columns {
@@ -785,12 +786,14 @@ __device__ __forceinline__ void mx_bias(const Mx4Product& a, int o, int h, nt_f3
 // free go out, a whole stage ahead.  The empty asm keeps each group's products where
 // they are written: without it they sink below the loads of the groups behind
 // them, whose operands then do not fit the registers (8192 x 4096 x 4096: 139 us instead
-// of 78).  A 256 x 256 tile's stage takes 3250 cycles at 1.7 GHz, where 32 products a
-// wave are 2048: instructions from registers alone run at 6.5 PFLOP/s, 1.55 GHz, so it
-// is power that bounds both.  Stages of 64 bytes, four of them in LDS: 88 us; four waves
-// of 128 x 128 outputs: 87 us; workgroups that take one tile after the other, the next
-// one's loads ahead of the stores: 76 us, but 55 instead of 51 where there is one tile a
-// CU (2048 x 8192 x 4096).
+// of 78).  A 256 x 256 tile's stage takes 2900 cycles, where two waves' 32 products are
+// 2048, and a tile 2.4 us until its first stage is there and 4.6 for its outputs.  The
+// clock goes by the operands' bits: 1.6 to 1.7 GHz on random ones, 2.37 on zeros, which
+// take as many cycles (77 and 59 us; instructions from registers alone 6.4 and 9.6 PFLOP/s
+// at the same clocks); 70.5 us where half of x is zeros.  Tried when the kernel took 78:
+// stages of 64 bytes, four of them in LDS, 88 us; four waves of 128 x 128 outputs 87;
+// workgroups that take one tile after the other, the next one's loads ahead of the stores,
+// 76, but 55 instead of 51 where there is one tile a CU.
 // Of a stage's eight chunks a lane takes 4 h + c in group c (h: its half of the wave), so
 // that its four scales are neighbouring bytes and the instruction picks byte c.  The order
 // of K within a stage is free, both operands have the same.  Scales come in parts of

@@ -17,10 +17,14 @@ namespace oscars {
 //         1.2 for 512 at a time
 //   256   10 and a block 1.1 up to 64 tiles, 1.34 up to 128, 1.87 up to 256; else 8 and a
 //         block 1.9 for 256 at a time
-// Rows x inputs x outputs, measured with 32 / 64 / 128 / 256: 256 x 4096 x 1000: 5.8 / 7.4 /
-// 11.8 / -, 256 x 4096 x 4096: 15.2 / 7.8 / 14.3 / 27.2, 1024 x 2048 x 2048: 20.3 / 7.3 / 8.6
-// / -, 2048 x 4096 x 2048: 49 / 21 / 17 / -, 2048 x 4096 x 4096: 93 / 42 / 24 / 31, 4096 x 4096
-// x 4096: - / - / 47.6 / 39.9, 8192 x 4096 x 4096: - / - / 90 / 77.
+// Rows x inputs x outputs, measured with 32 / 64 / 128 / 256 (half of x zeros, bf16 outputs):
+// 256 x 4096 x 1000: 6.2 / 7.4 / 11.8 / 26, 256 x 4096 x 4096: 15.2 / 7.9 / 14.2 / 27, 1024 x
+// 2048 x 2048: 20 / 7.4 / 8.3 / 16.5, 2048 x 4096 x 2048: 49 / 20 / 16.5 / 27, 2048 x 4096 x
+// 4096: 93 / 36 / 22.9 / 29, 4096 x 8191 x 2048: 151 / 68 / 39 / 51, 4096 x 4096 x 4096: 184 /
+// 72 / 43 / 36.5, 8192 x 2048 x 4096: 275 / 80 / 48 / 43, 8192 x 4096 x 4096: 362 / 143 / 84 /
+// 70.5.  The estimates of the large tiles, from an earlier form of the kernel, are up to 10%
+// above these; of these shapes and 4096 x 256 x 4096 only the last gets another than its
+// fastest tile (94 / 18 / 11.8 / 10.9: it takes 128).
 struct Mx4Plan {
   int tile;
   double us;
