@@ -788,9 +788,9 @@ __device__ __forceinline__ void mx_bias(const Mx4Product& a, int o, int h, nt_f3
 // them, whose operands then do not fit the registers (8192 x 4096 x 4096: 139 us instead
 // of 78).  A 256 x 256 tile's stage takes 2900 cycles, where two waves' 32 products are
 // 2048, and a tile 2.4 us until its first stage is there and 4.6 for its outputs.  The
-// clock goes by the operands' bits: 1.6 to 1.7 GHz on random ones, 2.37 on zeros, which
-// take as many cycles (77 and 59 us; instructions from registers alone 6.4 and 9.6 PFLOP/s
-// at the same clocks); 70.5 us where half of x is zeros.  Tried when the kernel took 78:
+// clock goes by the operands' bits: 1.6 to 1.8 GHz on random ones, 2.37 on zeros, which
+// take as many cycles (76 and 58 us; instructions from registers alone 6.5 and 9.7 PFLOP/s
+// at 1.63 and 2.38 GHz); 70.5 us where half of x is zeros.  Tried when the kernel took 78:
 // stages of 64 bytes, four of them in LDS, 88 us; four waves of 128 x 128 outputs 87;
 // workgroups that take one tile after the other, the next one's loads ahead of the stores,
 // 76, but 55 instead of 51 where there is one tile a CU.
