@@ -491,6 +491,47 @@ def test_gradients_without_dx(P, rows, inputs, outs, x_dtype, y_dtype, p, relu):
     assert torch.equal(lone, got[1])
 
 
+# rows, inputs, outputs whose dw takes tiles of 64, 128 and 256 (test_mx4_plan.py asks the plan)
+LARGE_GRADIENTS = [(300, 1100, 1024), (600, 2048, 2048), (600, 4096, 4096)]
+
+
+@pytest.mark.parametrize("want_dx", [True, False])
+@pytest.mark.parametrize("relu", [True, False])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,inputs,outs", LARGE_GRADIENTS)
+def test_gradients_in_large_tiles(P, rows, inputs, outs, dtype, relu, want_dx):
+    """dw's tiles with the workgroups behind them that add up db's parts: against products
+    in 64 bits of what quantize_mx4 makes of dz, x and w."""
+    import torch
+    rng = np.random.default_rng(rows + inputs + outs)
+    x = _dev(_rows(rng, rows, inputs, dtype, relu=True), dtype)
+    w = _dev(rng.standard_normal((outs, inputs)) / np.sqrt(inputs))
+    dy = _dev(_rows(rng, rows, outs, dtype) * np.float32(2.0 ** -10), dtype)
+    y = _dev(_rows(rng, rows, outs, dtype, relu=True), dtype) if relu else None
+    wt = P.quantize_mx4(w, transposed=True)
+    got = P.linear_mx4_backward(dy, x, *wt, y=y, want_dx=want_dx)
+    dz = dy.float() if y is None else torch.where(y > 0, dy.float(), 0.0)
+
+    def values(t, transposed, along):
+        return P.dequantize_mx4(*P.quantize_mx4(t, transposed=transposed), along).double()
+
+    zr, zc, xc = values(dz, False, outs), values(dz, True, rows), values(x, True, rows)
+    wc = P.dequantize_mx4(*wt, outs).double()
+    for what, g, a, b, k in (("dx", got[0], zr, wc, outs), ("dw", got[1], zc, xc, rows)):
+        if g is None:
+            assert what == "dx" and not want_dx
+            continue
+        b = b.t().contiguous()
+        want, size = a @ b, a.abs() @ b.abs()
+        half = HALF[dtype if what == "dx" else "fp32"]
+        bound = (128 + k / 64 + 8) * 2.0 ** -23 * size + half * want.abs() + 2.0 ** -126
+        assert ((g.double() - want).abs() <= bound).all(), what
+    want, size = dz.double().sum(0), dz.double().abs().sum(0)
+    # both sums in 64 bits, in orders of their own; one rounding
+    assert ((got[2].double() - want).abs()
+            <= 2 * rows * 2.0 ** -52 * size + HALF["fp32"] * want.abs()).all()
+
+
 def test_gradients_of_no_rows(P):
     import torch
     wt, wts = P.quantize_mx4(torch.ones(5, 9, device="cuda"), transposed=True)

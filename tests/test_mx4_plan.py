@@ -84,3 +84,15 @@ def test_the_gpu_test_of_two_launches_makes_two(plan):
     launches = plan(rows, inputs, outs)[3]
     assert len(launches) == 2 and launches[1][1] > 0
     assert rows - launches[1][1] < 300  # the rows that it gives values reach into the first
+
+
+def test_the_gpu_tests_of_gradients_reach_the_large_tiles(plan):
+    """dw's product alone; beside dx's it goes by itself too, not as small tiles."""
+    sys.path.insert(0, os.path.join(ROOT, "tests"))
+    import test_gpu_mx4
+    tiles = []
+    for rows, inputs, outs in test_gpu_mx4.LARGE_GRADIENTS:
+        dw, dx = plan(outs, rows, inputs), plan(rows, outs, inputs)
+        assert rows > 256 and dw[2] + dx[2] - 3.0 > dw[1] + dx[1]
+        tiles.append(dw[0])
+    assert tiles == [64, 128, 256]
